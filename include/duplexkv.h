@@ -50,7 +50,7 @@ extern "C" {
 #define KV_EUNSUP   (-7)  /* the chosen path cannot serve this shape or request */
 #define KV_ENOSPC   (-8)  /* block table: not enough free HBM blocks or host slots */
 #define KV_EBUSY    (-9)  /* a block or slot is still used the other way round by an un-waited call on the other stream */
-#define KV_E2BIG    (-10) /* kv_rotate_static: more blocks than its scratch array holds */
+#define KV_E2BIG    (-10) /* kv_rotate_static: more blocks than its scratch array holds; a decoder: more requests than it was made for */
 
 /* ---- host pool layouts ---- */
 #define KV_HOST_BLOCK_FIRST 0
@@ -398,6 +398,17 @@ int kv_table_rotate_eager(kv_table *table, const int32_t *preempt, int32_t n_pre
  * close the interval kv_last_stats() reports. */
 int kv_table_finish(kv_table *table, int32_t req);
 
+/*
+ * Blocks of a resident request leave it for good (kv_evict() says which): at[] holds
+ * their places in the request, ascending, each once.  Their HBM blocks and host slots are
+ * free again, the blocks behind close up, the request's length falls by block_size per
+ * block.  The last block of a request can leave only if it is full.  KV_EINVAL for a
+ * request that is not resident and for places that do not fit, with nothing changed.  If a
+ * transfer that names HBM blocks of this request may still be in flight, the call first
+ * waits for the engine's transfers, as kv_table_finish() does.
+ */
+int kv_table_drop(kv_table *table, int32_t req, const int32_t *at, int32_t n);
+
 /* Mapping of a request: per block HBM id (-1 if none), host slot (-1 if
  * none), state; arrays may be NULL, else hold `cap` entries.  info[0] =
  * tokens, info[1] = 1 if resident. */
@@ -447,6 +458,165 @@ double kv_sched_vlt(const kv_sched_params *params, const kv_sched_req *req, doub
 int kv_sched_lvf(const kv_sched_params *params, const kv_sched_req *reqs, int32_t n, double t_now,
                  int32_t b_xfer, int32_t b_hbm, int32_t *preempt, int32_t *n_preempt, int32_t *prioritize,
                  int32_t *n_prioritize, int32_t *fcfs);
+
+/* ------------------------------------------------------------------------
+ * The operators of a decode step over the paged cache: what writes it, what
+ * reads it and what says which of its blocks are worth keeping.
+ *   kv_put     new tokens: q and k get their rotary positions, k and v go into
+ *              their pages, rounded to the cache's type
+ *   kv_attend  attention of one new token per request over the pages it holds
+ *   kv_evict   the blocks that attention has weighed least leave a request
+ * A decoder is the handle they are called through: a cache (kv_config gives its
+ * shape and layout; host pool, path and launch fields are not looked at), the
+ * model's query heads, the element types, and device memory for intermediate
+ * results, allocated once.  A call allocates nothing, enqueues kernels on the
+ * stream it is given (NULL: the default stream) on the decoder's device,
+ * whichever device is current, and returns; it may be recorded into a HIP graph.
+ *
+ * Tables, lengths and everything else a call names are device memory and are
+ * read when the kernels run, so a recorded step goes on with whatever they hold
+ * then.  A request's table row names, block after block, the pages that its
+ * tokens lie in: token t of request s in row t % block_size of block
+ * table[s][t / block_size].  An id outside [0, n_hbm_blocks) is no page: such
+ * a block is skipped, neither read nor written (kv_table_blocks() gives -1 for
+ * a block that is in DRAM).  lens[s] below 0 counts as 0, above max_blocks *
+ * block_size as that.  Rows of a page behind a request's last token may hold
+ * anything, NaN too.
+ *
+ * Calls through one decoder have to be ordered one after the other (the same
+ * stream, or streams the caller orders), replays of recorded ones included:
+ * kv_attend's calls share the decoder's memory.  Steps that overlap in time
+ * take a decoder each; any number may exist over one cache.  The caller orders
+ * them against transfers, too: a block that a swap-in fills is read after
+ * kv_wait() or kv_stream_wait_layer().
+ * ------------------------------------------------------------------------ */
+#define KV_BF16 0
+#define KV_FP16 1
+#define KV_FP8  2   /* e4m3: 448 is the largest, there is no infinity */
+
+typedef struct kv_decoder kv_decoder; /* opaque, owned by the library */
+
+typedef struct {
+    int32_t n_heads;     /* query heads, a multiple of n_kv_heads: query head i reads KV head i / (n_heads / n_kv_heads) */
+    int32_t x_type;      /* of q, k, v and the outputs: KV_BF16 or KV_FP16 */
+    int32_t kv_type;     /* of the cache: x_type (elem_bytes 2), or KV_FP8 (elem_bytes 1) */
+    int32_t max_seqs;    /* most requests of a call */
+    int32_t max_blocks;  /* most blocks of a request: entries of a table row */
+    float k_scale;       /* what a stored 1 of K stands for (KV_FP8; else it has to be 1) */
+    float v_scale;
+} kv_decoder_config;
+
+/*
+ * hbm_cache: device pointer, kv_cache_bytes(cfg) bytes, owned by the caller; it
+ * must outlive the decoder.  KV_EINVAL: bad configuration, types that do not fit
+ * elem_bytes, scales that are not finite and above 0.  KV_EUNSUP: head_dim above
+ * 256 or no multiple of 8, more than 1024 query heads, a cache that is not
+ * aligned to 16 bytes or of 2^32 and more token rows per KV plane.  KV_ENOMEM, KV_EHIP.
+ */
+int kv_decoder_create(kv_decoder **decoder, const kv_config *cfg, const kv_decoder_config *dc, void *hbm_cache);
+
+/* Waits for the device's work, then frees the decoder's memory. */
+int kv_decoder_destroy(kv_decoder *decoder);
+
+/*
+ * Strides are in elements; the last dimension is contiguous.  Rows of q, k, v and
+ * the outputs have to begin on multiples of 16 bytes (KV_EUNSUP otherwise).
+ */
+typedef struct {
+    const void *data;
+    int64_t row;   /* from one token to the next */
+    int64_t head;  /* from one head to the next */
+} kv_rows;
+
+typedef struct {
+    int32_t layer;
+    int32_t n_seqs;
+    int32_t n_rows;        /* rows of k and v (and q); those at and behind starts[n_seqs] are padding: not read, not written */
+    int32_t table_stride;  /* entries from one request's row to the next's; max_blocks of them are looked at */
+    const int32_t *table;
+    const int32_t *lens;   /* tokens of each request, the new ones included */
+    const int32_t *starts; /* n_seqs + 1: request s has rows starts[s] .. starts[s + 1] - 1, its last tokens; they must not
+                              fall.  NULL: one row each (n_rows == n_seqs) */
+    kv_rows k, v;
+    kv_rows q;             /* NULL data: no q */
+    kv_rows q_out;         /* where rotated q goes; may be q itself */
+    const float *inv_freq; /* rot_dim / 2 angles per position; NULL: nothing rotates (k as it is, q is copied) */
+    int32_t rot_dim;       /* the first rot_dim dimensions of a head rotate: a multiple of 8 */
+    int32_t interleaved;   /* pairs are (2i, 2i + 1); else (i, i + rot_dim / 2) */
+    int32_t n_axes;        /* 1 to 3 */
+    int32_t sections[3];   /* pairs of each axis, one axis after the other: sum rot_dim / 2 */
+    const int32_t *positions; /* [n_axes][position_stride]: of each row; NULL (1 axis): its place in the request */
+    int64_t position_stride;
+} kv_put_args;
+
+/*
+ * New tokens go into the cache, layer by layer.  With a = position[axis of pair i] *
+ * inv_freq[i] (the product, its cosine and its sine as exact as float holds them, at far
+ * positions too) a pair (x, y) of q and k becomes (x cos a - y sin a, y cos a + x sin a),
+ * in 32 bits, rounded once.  An 8-bit cache holds the nearest of value / scale, at most
+ * 448 either way; NaN stays NaN.  Tokens whose block is no page, or that lie beyond
+ * max_blocks, are left out of the cache (their q is rotated all the same).  Two tokens
+ * that name one row of one page leave either's values there.
+ * KV_EINVAL: NULL or negative, a layer, axis or section that does not fit.  KV_E2BIG:
+ * more requests than the decoder's.
+ */
+int kv_put(kv_decoder *decoder, const kv_put_args *args, void *stream);
+
+typedef struct {
+    int32_t layer;
+    int32_t n_seqs;
+    int32_t table_stride;
+    float scale;           /* of the products of q and k (1 / sqrt(head_dim) as a rule) */
+    const int32_t *table;
+    const int32_t *lens;   /* tokens to attend over: the new one too, if it has been put */
+    kv_rows q, out;        /* one row per request; out is written */
+    float *lse;            /* NULL, or [n_seqs][n_heads]: log of the sum of exp(score), -inf where nothing is attended to */
+    const float *mass;     /* [n_seqs][mass_stride]: weight that each block has received so far; NULL: none */
+    float *mass_out;       /* NULL, or the same with this call's weights added (may be mass itself), max_blocks entries a row */
+    int64_t mass_stride;
+} kv_attend_args;
+
+/*
+ * out = softmax(scale * q K^T) V of each request and query head over the request's
+ * tokens in present pages; 0 where there are none.  Products and sums in 32 bits; the
+ * weights are rounded to x_type before they meet V.  mass_out[s][j] = mass[s][j] + the
+ * weights that the tokens of block j got, summed over the query heads (n_heads in all,
+ * per request), j below the request's blocks; behind these it is mass[s][j].  The result
+ * is the same, bit for bit, whenever the same call runs with the same lens.
+ * KV_EINVAL, KV_EUNSUP, KV_E2BIG as for kv_put.
+ */
+int kv_attend(kv_decoder *decoder, const kv_attend_args *args, void *stream);
+
+typedef struct {
+    int32_t n_seqs;
+    int32_t budget;        /* blocks that a request may keep */
+    int32_t n_first;       /* its first blocks that stay whatever they weigh, */
+    int32_t n_last;        /* and its last ones: at least 1, the block being filled */
+    int32_t max_evict;     /* most blocks to leave a request in one call: entries of a row of evicted_* */
+    int32_t table_stride;  /* of table and table_out */
+    int64_t mass_stride;   /* of mass and mass_out */
+    const int32_t *table;
+    int32_t *table_out;    /* may be table itself, as the next two */
+    const int32_t *lens;
+    int32_t *lens_out;
+    const float *mass;
+    float *mass_out;
+    int32_t *evicted_ids;  /* [n_seqs][max_evict]: the blocks that left, in the order of the table, then -1 */
+    int32_t *evicted_at;   /* the same for their entries in the table before the call (kv_table_drop() takes these) */
+    int32_t *n_evicted;    /* [n_seqs] */
+} kv_evict_args;
+
+/*
+ * A request of more than `budget` blocks gives up the lightest of those that may go, as
+ * many as it is over (at most max_evict, and at most all that may go): lowest mass first,
+ * of equal ones the lower entry; NaN weighs most.  Its table and mass rows close up in
+ * their order, its length falls by block_size per block.  Rows have max_blocks entries;
+ * behind the blocks that stay, table_out holds -1 and mass_out 0.  Keys keep the rotary
+ * positions that they were put with.  Only tables change: the caller copies the blocks out
+ * (kv_swap_out) if they are to be had again, and gives them back (kv_table_drop).
+ * KV_EINVAL, KV_E2BIG as for kv_put.
+ */
+int kv_evict(kv_decoder *decoder, const kv_evict_args *args, void *stream);
 
 const char *kv_strerror(int code);
 

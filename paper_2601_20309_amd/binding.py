@@ -30,9 +30,10 @@ EXPORTS = ["kv_seg_bytes", "kv_block_bytes", "kv_cache_bytes", "kv_pool_bytes", 
            "kv_create", "kv_destroy", "kv_swap_out", "kv_swap_in", "kv_rotate", "kv_rotate_static", "kv_wait", "kv_query", "kv_stream_wait_layer", "kv_wait_layer",
            "kv_host_pool", "kv_last_stats", "kv_probe_link", "kv_reader_start", "kv_reader_wait",
            "kv_table_create", "kv_table_destroy", "kv_table_append", "kv_table_eager", "kv_table_rotate", "kv_table_rotate_eager",
-           "kv_table_finish", "kv_table_blocks", "kv_table_get_counts", "kv_sched_vlt", "kv_sched_lvf",
-           "kv_strerror"]
+           "kv_table_finish", "kv_table_drop", "kv_table_blocks", "kv_table_get_counts", "kv_sched_vlt", "kv_sched_lvf",
+           "kv_decoder_create", "kv_decoder_destroy", "kv_put", "kv_attend", "kv_evict", "kv_strerror"]
 KV_REQ_RUNNING, KV_REQ_WAITING, KV_REQ_ROTARY = 0, 1, 2
+KV_BF16, KV_FP16, KV_FP8 = 0, 1, 2
 
 
 class kv_config(C.Structure):
@@ -60,6 +61,34 @@ class kv_sched_params(C.Structure):
 class kv_sched_req(C.Structure):
     _fields_ = [("id", C.c_int32), ("state", C.c_int32), ("blocks", C.c_int32), ("pad", C.c_int32),
                 ("t_ref", C.c_double)]
+
+
+class kv_decoder_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_heads", "x_type", "kv_type", "max_seqs", "max_blocks")] + \
+        [("k_scale", C.c_float), ("v_scale", C.c_float)]
+
+
+class kv_rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row", C.c_int64), ("head", C.c_int64)]
+
+
+class kv_put_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("layer", "n_seqs", "n_rows", "table_stride")] + \
+        [(n, C.c_void_p) for n in ("table", "lens", "starts")] + [(n, kv_rows) for n in ("k", "v", "q", "q_out")] + \
+        [("inv_freq", C.c_void_p)] + [(n, C.c_int32) for n in ("rot_dim", "interleaved", "n_axes")] + \
+        [("sections", C.c_int32 * 3), ("positions", C.c_void_p), ("position_stride", C.c_int64)]
+
+
+class kv_attend_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("layer", "n_seqs", "table_stride")] + [("scale", C.c_float)] + \
+        [(n, C.c_void_p) for n in ("table", "lens")] + [(n, kv_rows) for n in ("q", "out")] + \
+        [(n, C.c_void_p) for n in ("lse", "mass", "mass_out")] + [("mass_stride", C.c_int64)]
+
+
+class kv_evict_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_seqs", "budget", "n_first", "n_last", "max_evict", "table_stride")] + \
+        [("mass_stride", C.c_int64)] + [(n, C.c_void_p) for n in (
+            "table", "table_out", "lens", "lens_out", "mass", "mass_out", "evicted_ids", "evicted_at", "n_evicted")]
 
 
 class KVError(RuntimeError):
@@ -124,6 +153,8 @@ def _load() -> C.CDLL:
     L.kv_table_rotate_eager.argtypes = [C.c_void_p, pids, C.c_int32, pids, C.c_int32, C.c_int32, p32]
     L.kv_table_finish.restype = C.c_int
     L.kv_table_finish.argtypes = [C.c_void_p, C.c_int32]
+    L.kv_table_drop.restype = C.c_int
+    L.kv_table_drop.argtypes = [C.c_void_p, C.c_int32, pids, C.c_int32]
     L.kv_table_blocks.restype = C.c_int
     L.kv_table_blocks.argtypes = [C.c_void_p, C.c_int32, p32, p32, p32, C.c_int32, p32, p32]
     L.kv_table_get_counts.restype = C.c_int
@@ -133,6 +164,13 @@ def _load() -> C.CDLL:
     L.kv_sched_lvf.restype = C.c_int
     L.kv_sched_lvf.argtypes = [C.POINTER(kv_sched_params), C.POINTER(kv_sched_req), C.c_int32, C.c_double,
                                C.c_int32, C.c_int32, p32, p32, p32, p32, p32]
+    L.kv_decoder_create.restype = C.c_int
+    L.kv_decoder_create.argtypes = [C.POINTER(C.c_void_p), pcfg, C.POINTER(kv_decoder_config), C.c_void_p]
+    L.kv_decoder_destroy.restype = C.c_int
+    L.kv_decoder_destroy.argtypes = [C.c_void_p]
+    for n, args in (("kv_put", kv_put_args), ("kv_attend", kv_attend_args), ("kv_evict", kv_evict_args)):
+        getattr(L, n).restype = C.c_int
+        getattr(L, n).argtypes = [C.c_void_p, C.POINTER(args), C.c_void_p]
     L.kv_strerror.restype = C.c_char_p
     L.kv_strerror.argtypes = [C.c_int]
     return L
@@ -361,6 +399,11 @@ class Table:
 
     def kv_table_finish(self, req: int) -> int:
         return lib.kv_table_finish(self._h, req)
+
+    def kv_table_drop(self, req: int, at) -> int:
+        """The blocks at these places of the request leave it (ascending: kv_evict's evicted_at)."""
+        pa, n = _ids(at)
+        return lib.kv_table_drop(self._h, req, pa, n)
 
     def kv_table_blocks(self, req: int):
         """None if the request does not exist, else dict(ids, slots, states, len, resident)."""

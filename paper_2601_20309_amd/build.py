@@ -8,8 +8,9 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
-SRCS = [os.path.join(CSRC, n) for n in ("duplexkv.hip", "kv_table.cpp", "kv_sched.cpp")]
+SRCS = [os.path.join(CSRC, n) for n in ("duplexkv.hip", "kv_decode.hip", "kv_table.cpp", "kv_sched.cpp")]
 DEPS = SRCS + [os.path.join(CSRC, "kv_kernels.hpp"), os.path.join(CSRC, "kv_engine.hpp"),
+               os.path.join(CSRC, "kv_decode_kernels.hpp"),
                os.path.join(ROOT, "include", "duplexkv.h")]
 LIB = os.path.join(HERE, "libduplexkv.so")
 

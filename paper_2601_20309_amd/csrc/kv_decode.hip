@@ -1,0 +1,369 @@
+// Host side of the decode step's operators (see include/duplexkv.h): checks,
+// launch shapes, and the handle that holds their device memory.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdio>
+#include <new>
+#include <numeric>
+
+#include "../../include/duplexkv.h"
+#include "kv_decode_kernels.hpp"
+
+struct kv_decoder {
+    kv_config cfg;
+    kv_decoder_config dc;
+    int device = 0, n_cus = 0;
+    uint8_t *hbm = nullptr;
+    uint32_t token_bytes = 0, cells_per_block = 0;
+    uint64_t plane_bytes = 0;  // from K to V of a layer, and half the way to the next layer
+    // kv_attend: how the KV heads' units and their waves make up workgroups
+    uint32_t units = 0, head_tiles = 0, units_per_wg = 0, subs = 0, wgs_per_group = 0, max_groups = 0;
+    uint32_t granule = 0, max_granules = 0;
+    // one allocation, in this order
+    float *part = nullptr;
+    dkv::f32x4 *part_ml = nullptr;
+    float *lse2 = nullptr, *granules = nullptr;
+};
+
+namespace {
+
+#define DECTRY(call)                                                                                            \
+    do {                                                                                                        \
+        hipError_t err_ = (call);                                                                               \
+        if (err_ != hipSuccess) {                                                                               \
+            fprintf(stderr, "duplexkv: %s failed: %s (%s:%d)\n", #call, hipGetErrorString(err_), __FILE__, __LINE__); \
+            return KV_EHIP;                                                                                     \
+        }                                                                                                       \
+    } while (0)
+
+// The decoder's device is the current one for as long as this lives.
+class OnDevice {
+  public:
+    explicit OnDevice(int device)
+    {
+        if (hipGetDevice(&before_) != hipSuccess) return;
+        ok_ = before_ == device || hipSetDevice(device) == hipSuccess;
+        moved_ = ok_ && before_ != device;
+    }
+    ~OnDevice()
+    {
+        if (moved_) (void)hipSetDevice(before_);
+    }
+    bool ok() const { return ok_; }
+
+  private:
+    int before_ = 0;
+    bool ok_ = false, moved_ = false;
+};
+
+constexpr uint32_t kAttendWaves = 8;  // most waves of a workgroup
+
+bool rows_ok(const kv_rows &r) { return r.row >= 0 && r.head >= 0; }
+// 16-bit elements: rows begin on multiples of 16 bytes
+bool rows_aligned(const kv_rows &r) { return (uintptr_t)r.data % 16 == 0 && r.row % 8 == 0 && r.head % 8 == 0; }
+
+uint8_t *plane(const kv_decoder *d, int32_t layer, int which)
+{
+    return d->hbm + (2ull * (uint64_t)layer + (uint64_t)which) * d->plane_bytes;
+}
+
+int kinds(const kv_decoder *d, int &dp)
+{
+    dp = d->cfg.head_dim <= 64 ? 64 : d->cfg.head_dim <= 128 ? 128 : 256;
+    return (d->dc.x_type == KV_FP16 ? 1 : 0) + (d->dc.kv_type == KV_FP8 ? 2 : 0);
+}
+
+template <typename X, bool FP8>
+void launch_attend(int dp, dim3 g, dim3 b, hipStream_t s, const dkv::AttendParams &p)
+{
+    if (dp == 64) hipLaunchKernelGGL((dkv::kv_attend_kernel<X, FP8, 64>), g, b, 0, s, p);
+    else if (dp == 128) hipLaunchKernelGGL((dkv::kv_attend_kernel<X, FP8, 128>), g, b, 0, s, p);
+    else hipLaunchKernelGGL((dkv::kv_attend_kernel<X, FP8, 256>), g, b, 0, s, p);
+}
+
+}  // namespace
+
+extern "C" {
+
+int kv_decoder_create(kv_decoder **out, const kv_config *cfg, const kv_decoder_config *dc, void *hbm_cache)
+{
+    if (!out) return KV_EINVAL;
+    *out = nullptr;
+    const uint64_t cache_bytes = cfg ? kv_cache_bytes(cfg) : 0;
+    if (!cache_bytes || !dc || !hbm_cache) return KV_EINVAL;
+    if (dc->n_heads <= 0 || dc->n_heads % cfg->n_kv_heads != 0 || dc->max_seqs <= 0 || dc->max_blocks <= 0) return KV_EINVAL;
+    if (dc->x_type != KV_BF16 && dc->x_type != KV_FP16) return KV_EINVAL;
+    if (dc->kv_type == KV_FP8 ? cfg->elem_bytes != 1 : dc->kv_type != dc->x_type || cfg->elem_bytes != 2) return KV_EINVAL;
+    for (float scale : {dc->k_scale, dc->v_scale})
+        if (!(scale > 0.f) || !std::isfinite(scale) || !std::isfinite(1.f / scale) || (dc->kv_type != KV_FP8 && scale != 1.f))
+            return KV_EINVAL;
+    if (cfg->head_dim > 256 || cfg->head_dim % 8 != 0 || dc->n_heads > 1024 || (uintptr_t)hbm_cache % 16 != 0) return KV_EUNSUP;
+    if ((int64_t)dc->max_blocks * cfg->block_size > 0x7FFFFFC0) return KV_EUNSUP;
+    const uint64_t token_bytes = (uint64_t)cfg->n_kv_heads * (uint64_t)cfg->head_dim * (uint64_t)cfg->elem_bytes;
+    const uint64_t cells = (uint64_t)cfg->block_size * (cfg->hbm_layout == KV_HBM_BLOCK_FIRST ? 2ull * cfg->n_layers : 1ull);
+    if (token_bytes >> 31 || cells >> 31 || cells * (uint64_t)cfg->n_hbm_blocks >= 0xFFFFFFFFull) return KV_EUNSUP;
+    int ndev = 0;
+    if (hipGetDeviceCount(&ndev) != hipSuccess || ndev <= 0) {
+        (void)hipGetLastError();
+        fprintf(stderr, "duplexkv: no HIP device is visible\n");
+        return KV_EHIP;
+    }
+    hipPointerAttribute_t at;
+    hipDeviceptr_t base = nullptr;
+    size_t span = 0;
+    if (hipPointerGetAttributes(&at, hbm_cache) != hipSuccess || at.type != hipMemoryTypeDevice ||
+        hipMemGetAddressRange(&base, &span, (hipDeviceptr_t)hbm_cache) != hipSuccess ||
+        (uintptr_t)hbm_cache + cache_bytes > (uintptr_t)base + span) {
+        (void)hipGetLastError();
+        fprintf(stderr, "duplexkv: hbm_cache is not a device allocation of the configured size\n");
+        return KV_EINVAL;
+    }
+    kv_decoder *d = new (std::nothrow) kv_decoder;
+    if (!d) return KV_ENOMEM;
+    d->cfg = *cfg;
+    d->dc = *dc;
+    d->device = at.device;
+    d->hbm = (uint8_t *)hbm_cache;
+    d->token_bytes = (uint32_t)token_bytes;
+    d->cells_per_block = (uint32_t)cells;
+    d->plane_bytes = kv_seg_bytes(cfg) * (cfg->hbm_layout == KV_HBM_BLOCK_FIRST ? 1ull : (uint64_t)cfg->n_hbm_blocks);
+    const uint32_t group = (uint32_t)(dc->n_heads / cfg->n_kv_heads);
+    d->head_tiles = (group + 15) / 16;
+    d->units = (uint32_t)cfg->n_kv_heads * d->head_tiles;
+    d->wgs_per_group = (d->units + kAttendWaves - 1) / kAttendWaves;
+    d->units_per_wg = (d->units + d->wgs_per_group - 1) / d->wgs_per_group;
+    d->subs = 1;
+    while (2 * d->subs * d->units_per_wg <= kAttendWaves) d->subs *= 2;
+    d->granule = std::gcd((uint32_t)cfg->block_size, 16u);
+    d->max_granules = (uint32_t)dc->max_blocks * ((uint32_t)cfg->block_size / d->granule);
+    OnDevice on(d->device);
+    auto fail = [&](int code) {
+        delete d;
+        return code;
+    };
+    if (!on.ok() || hipDeviceGetAttribute(&d->n_cus, hipDeviceAttributeMultiprocessorCount, d->device) != hipSuccess)
+        return fail(KV_EHIP);
+    // ranges: as many workgroups as the chip holds at once, no more than there can be turns
+    const uint64_t most_tiles = (uint64_t)dc->max_seqs * (((uint64_t)dc->max_blocks * cfg->block_size + dkv::kTile - 1) / dkv::kTile);
+    d->max_groups = (uint32_t)std::min<uint64_t>(std::max(1u, 2u * (uint32_t)d->n_cus / d->wgs_per_group),
+                                                 (most_tiles + d->subs - 1) / d->subs);
+    const uint64_t slots = 2ull * d->max_groups * (uint64_t)dc->n_heads;
+    const uint64_t n_part = slots * (uint64_t)cfg->head_dim * 4, n_ml = slots * sizeof(dkv::f32x4),
+                   n_lse = ((uint64_t)dc->max_seqs * (uint64_t)dc->n_heads * 4 + 255) / 256 * 256,
+                   n_gran = (uint64_t)dc->max_seqs * d->max_granules * (uint64_t)dc->n_heads * 4;
+    uint8_t *mem = nullptr;
+    if (hipMalloc((void **)&mem, n_part + n_ml + n_lse + n_gran) != hipSuccess) {
+        (void)hipGetLastError();
+        return fail(KV_ENOMEM);
+    }
+    d->part = (float *)mem;
+    d->part_ml = (dkv::f32x4 *)(mem + n_part);
+    d->lse2 = (float *)(mem + n_part + n_ml);
+    d->granules = (float *)(mem + n_part + n_ml + n_lse);
+    *out = d;
+    return KV_OK;
+}
+
+int kv_decoder_destroy(kv_decoder *d)
+{
+    if (!d) return KV_EINVAL;
+    OnDevice on(d->device);
+    (void)hipDeviceSynchronize();
+    (void)hipFree(d->part);
+    delete d;
+    return KV_OK;
+}
+
+int kv_put(kv_decoder *d, const kv_put_args *a, void *stream)
+{
+    if (!d || !a || a->layer < 0 || a->layer >= d->cfg.n_layers || a->n_seqs < 0 || a->n_rows < 0) return KV_EINVAL;
+    if (a->n_seqs > d->dc.max_seqs) return KV_E2BIG;
+    const bool rows_here = a->n_seqs > 0 && a->n_rows > 0;
+    if (!a->starts && a->n_rows != a->n_seqs) return KV_EINVAL;
+    if (rows_here && (!a->table || !a->lens || !a->k.data || !a->v.data)) return KV_EINVAL;
+    if (a->table_stride < d->dc.max_blocks && a->n_seqs > 1) return KV_EINVAL;
+    if (!rows_ok(a->k) || !rows_ok(a->v) || !rows_ok(a->q) || !rows_ok(a->q_out)) return KV_EINVAL;
+    if ((a->q.data == nullptr) != (a->q_out.data == nullptr)) return KV_EINVAL;
+    int32_t pairs = 0;
+    if (a->inv_freq) {
+        if (a->rot_dim <= 0 || a->rot_dim > d->cfg.head_dim || a->n_axes < 1 || a->n_axes > 3) return KV_EINVAL;
+        if (!a->positions && a->n_axes != 1) return KV_EINVAL;
+        for (int i = 0; i < a->n_axes; i++) {
+            if (a->sections[i] < 0 || a->sections[i] > a->rot_dim) return KV_EINVAL;
+            pairs += a->sections[i];
+        }
+        if (2 * pairs != a->rot_dim) return KV_EINVAL;
+        if (a->positions && a->n_axes > 1 && a->position_stride < a->n_rows) return KV_EINVAL;
+        if (a->rot_dim % 8 != 0) return KV_EUNSUP;
+    }
+    if (!rows_aligned(a->k) || !rows_aligned(a->v) || !rows_aligned(a->q) || !rows_aligned(a->q_out)) return KV_EUNSUP;
+    if (!rows_here) return KV_OK;
+    OnDevice on(d->device);
+    if (!on.ok()) return KV_EHIP;
+    dkv::PutParams p{};
+    p.k = plane(d, a->layer, 0);
+    p.v = plane(d, a->layer, 1);
+    p.table = a->table;
+    p.lens = a->lens;
+    p.starts = a->starts;
+    p.ks = (const uint8_t *)a->k.data;
+    p.vs = (const uint8_t *)a->v.data;
+    p.qs = (const uint8_t *)a->q.data;
+    p.qd = (uint8_t *)const_cast<void *>(a->q_out.data);
+    p.inv_freq = a->inv_freq;
+    p.positions = a->positions;
+    p.k_row = 2ull * (uint64_t)a->k.row;
+    p.k_head = 2ull * (uint64_t)a->k.head;
+    p.v_row = 2ull * (uint64_t)a->v.row;
+    p.v_head = 2ull * (uint64_t)a->v.head;
+    p.q_row = 2ull * (uint64_t)a->q.row;
+    p.q_head = 2ull * (uint64_t)a->q.head;
+    p.qd_row = 2ull * (uint64_t)a->q_out.row;
+    p.qd_head = 2ull * (uint64_t)a->q_out.head;
+    p.table_stride = a->table_stride;
+    p.position_stride = a->position_stride;
+    p.n_seqs = (uint32_t)a->n_seqs;
+    p.n_rows = (uint32_t)a->n_rows;
+    p.n_heads = (uint32_t)d->dc.n_heads;
+    p.n_kv_heads = (uint32_t)d->cfg.n_kv_heads;
+    p.max_blocks = (uint32_t)d->dc.max_blocks;
+    p.dim = (uint32_t)d->cfg.head_dim;
+    p.token_bytes = d->token_bytes;
+    p.head_bytes = p.dim * (uint32_t)d->cfg.elem_bytes;
+    p.block_size = (uint32_t)d->cfg.block_size;
+    p.cells_per_block = d->cells_per_block;
+    p.n_blocks = (uint32_t)d->cfg.n_hbm_blocks;
+    p.rot = a->inv_freq ? (uint32_t)a->rot_dim : 0u;
+    p.interleaved = a->interleaved ? 1u : 0u;
+    p.section0 = a->inv_freq ? (uint32_t)a->sections[0] : 0u;
+    p.section01 = p.section0 + (a->inv_freq && a->n_axes > 1 ? (uint32_t)a->sections[1] : 0u);
+    p.k_inv = 1.f / d->dc.k_scale;
+    p.v_inv = 1.f / d->dc.v_scale;
+    hipStream_t s = (hipStream_t)stream;
+    const dim3 g(p.n_rows), b(256);
+    int dp;
+    switch (kinds(d, dp)) {
+    case 0: hipLaunchKernelGGL((dkv::kv_put_kernel<dkv::Bf16, false>), g, b, 0, s, p); break;
+    case 1: hipLaunchKernelGGL((dkv::kv_put_kernel<dkv::Fp16, false>), g, b, 0, s, p); break;
+    case 2: hipLaunchKernelGGL((dkv::kv_put_kernel<dkv::Bf16, true>), g, b, 0, s, p); break;
+    default: hipLaunchKernelGGL((dkv::kv_put_kernel<dkv::Fp16, true>), g, b, 0, s, p); break;
+    }
+    DECTRY(hipGetLastError());
+    return KV_OK;
+}
+
+int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
+{
+    if (!d || !a || a->layer < 0 || a->layer >= d->cfg.n_layers || a->n_seqs < 0 || !std::isfinite(a->scale)) return KV_EINVAL;
+    if (a->n_seqs > d->dc.max_seqs) return KV_E2BIG;
+    if (a->n_seqs > 0 && (!a->table || !a->lens || !a->q.data || !a->out.data)) return KV_EINVAL;
+    if (!rows_ok(a->q) || !rows_ok(a->out)) return KV_EINVAL;
+    if (a->n_seqs > 1 && (a->table_stride < d->dc.max_blocks || (a->mass_out && a->mass_stride < d->dc.max_blocks))) return KV_EINVAL;
+    if (a->mass && !a->mass_out) return KV_EINVAL;
+    if (!rows_aligned(a->q) || !rows_aligned(a->out)) return KV_EUNSUP;
+    if (a->n_seqs == 0) return KV_OK;
+    OnDevice on(d->device);
+    if (!on.ok()) return KV_EHIP;
+    dkv::AttendParams p{};
+    p.k = plane(d, a->layer, 0);
+    p.v = plane(d, a->layer, 1);
+    p.table = a->table;
+    p.lens = a->lens;
+    p.q = (const uint8_t *)a->q.data;
+    p.out = (uint8_t *)const_cast<void *>(a->out.data);
+    p.lse = a->lse;
+    p.part = d->part;
+    p.part_ml = d->part_ml;
+    p.lse2 = d->lse2;
+    p.granules = a->mass_out ? d->granules : nullptr;
+    p.mass = a->mass;
+    p.mass_out = a->mass_out;
+    p.mass_stride = a->mass_stride;
+    p.q_row = 2ull * (uint64_t)a->q.row;
+    p.q_head = 2ull * (uint64_t)a->q.head;
+    p.out_row = 2ull * (uint64_t)a->out.row;
+    p.out_head = 2ull * (uint64_t)a->out.head;
+    p.table_stride = a->table_stride;
+    p.n_seqs = (uint32_t)a->n_seqs;
+    p.n_heads = (uint32_t)d->dc.n_heads;
+    p.max_blocks = (uint32_t)d->dc.max_blocks;
+    p.max_tokens = p.max_blocks * (uint32_t)d->cfg.block_size;
+    p.dim = (uint32_t)d->cfg.head_dim;
+    p.token_bytes = d->token_bytes;
+    p.head_bytes = p.dim * (uint32_t)d->cfg.elem_bytes;
+    p.block_size = (uint32_t)d->cfg.block_size;
+    p.cells_per_block = d->cells_per_block;
+    p.n_blocks = (uint32_t)d->cfg.n_hbm_blocks;
+    p.groups = d->max_groups;
+    p.wgs_per_group = d->wgs_per_group;
+    p.units = d->units;
+    p.units_per_wg = d->units_per_wg;
+    p.subs = d->subs;
+    p.group_heads = (uint32_t)(d->dc.n_heads / d->cfg.n_kv_heads);
+    p.head_tiles = d->head_tiles;
+    p.granule = d->granule;
+    p.max_granules = d->max_granules;
+    p.qk_scale = (float)((double)a->scale * 1.4426950408889634074 * (double)d->dc.k_scale);
+    p.v_scale = d->dc.v_scale;
+    // no more ranges than there can be turns in this call
+    const uint64_t most = (uint64_t)p.n_seqs * ((p.max_tokens + dkv::kTile - 1) / dkv::kTile);
+    p.groups = (uint32_t)std::min<uint64_t>(p.groups, (most + p.subs - 1) / p.subs);
+    hipStream_t s = (hipStream_t)stream;
+    const dim3 g(p.groups * p.wgs_per_group), b(64 * p.units_per_wg * p.subs);
+    int dp;
+    const int kind = kinds(d, dp);
+    switch (kind) {
+    case 0: launch_attend<dkv::Bf16, false>(dp, g, b, s, p); break;
+    case 1: launch_attend<dkv::Fp16, false>(dp, g, b, s, p); break;
+    case 2: launch_attend<dkv::Bf16, true>(dp, g, b, s, p); break;
+    default: launch_attend<dkv::Fp16, true>(dp, g, b, s, p); break;
+    }
+    DECTRY(hipGetLastError());
+    const dim3 gj(p.n_heads, p.n_seqs);
+    if (d->dc.x_type == KV_FP16) hipLaunchKernelGGL(dkv::kv_join_kernel<dkv::Fp16>, gj, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL(dkv::kv_join_kernel<dkv::Bf16>, gj, dim3(256), 0, s, p);
+    DECTRY(hipGetLastError());
+    if (p.granules) {
+        hipLaunchKernelGGL(dkv::kv_mass_kernel, dim3((p.max_blocks + 15u) / 16u, p.n_seqs), dim3(256), 0, s, p);
+        DECTRY(hipGetLastError());
+    }
+    return KV_OK;
+}
+
+int kv_evict(kv_decoder *d, const kv_evict_args *a, void *stream)
+{
+    if (!d || !a || a->n_seqs < 0 || a->budget < 0 || a->n_first < 0 || a->n_last < 1 || a->max_evict < 0) return KV_EINVAL;
+    if (a->n_seqs > d->dc.max_seqs) return KV_E2BIG;
+    if (a->n_seqs > 1 && (a->table_stride < d->dc.max_blocks || a->mass_stride < d->dc.max_blocks)) return KV_EINVAL;
+    if (a->n_seqs == 0) return KV_OK;
+    if (!a->table || !a->table_out || !a->lens || !a->lens_out || !a->mass || !a->mass_out || !a->n_evicted ||
+        (a->max_evict > 0 && (!a->evicted_ids || !a->evicted_at)))
+        return KV_EINVAL;
+    OnDevice on(d->device);
+    if (!on.ok()) return KV_EHIP;
+    dkv::EvictParams p{};
+    p.table = a->table;
+    p.lens = a->lens;
+    p.table_out = a->table_out;
+    p.lens_out = a->lens_out;
+    p.mass = a->mass;
+    p.mass_out = a->mass_out;
+    p.ids = a->evicted_ids;
+    p.at = a->evicted_at;
+    p.count = a->n_evicted;
+    p.table_stride = a->table_stride;
+    p.mass_stride = a->mass_stride;
+    p.max_blocks = (uint32_t)d->dc.max_blocks;
+    p.block_size = (uint32_t)d->cfg.block_size;
+    p.budget = (uint32_t)a->budget;
+    p.n_first = (uint32_t)a->n_first;
+    p.n_last = (uint32_t)a->n_last;
+    p.max_evict = (uint32_t)a->max_evict;
+    hipLaunchKernelGGL(dkv::kv_evict_kernel, dim3((uint32_t)a->n_seqs), dim3(dkv::kEvictThreads), 0, (hipStream_t)stream, p);
+    DECTRY(hipGetLastError());
+    return KV_OK;
+}
+
+}  // extern "C"

@@ -449,6 +449,45 @@ int kv_table_finish(kv_table *t, int32_t rq)
     return KV_OK;
 }
 
+int kv_table_drop(kv_table *t, int32_t rq, const int32_t *at, int32_t n)
+{
+    if (!t || rq < 0 || rq >= t->max_req || !t->req[(size_t)rq].used || list_bad(at, n)) return KV_EINVAL;
+    TableReq &r = t->req[(size_t)rq];
+    if (!r.resident) return KV_EINVAL;
+    const int32_t P = t->e->cfg.block_size, held = (int32_t)r.hbm.size(), full = r.len / P;
+    for (int32_t i = 0; i < n; i++)  // only full blocks: every one but a last one that is being filled
+        if (at[i] < 0 || at[i] >= std::min(held, full) || (i > 0 && at[i] <= at[i - 1])) return KV_EINVAL;
+    if (n == 0) return KV_OK;
+    // the blocks go to new owners, as in kv_table_finish()
+    if (r.named_at == (int64_t)t->e->idle_epoch) {
+        const int rc = dkv::drain(t->e);
+        if (rc != KV_OK) return rc;
+    } else if (t->e->sticky != KV_OK) {
+        return t->e->sticky;
+    }
+    size_t to = 0;
+    int32_t next = 0;
+    for (size_t b = 0; b < r.hbm.size(); b++) {
+        if (next < n && at[next] == (int32_t)b) {
+            next++;
+            t->free_hbm.push(r.hbm[b]);
+            if (r.slot[b] >= 0) t->free_slot.push(r.slot[b]);
+            if (r.state[b] == KV_BLOCK_FULL) r.n_full--;
+            continue;
+        }
+        r.hbm[to] = r.hbm[b];
+        r.slot[to] = r.slot[b];
+        r.state[to] = r.state[b];
+        to++;
+    }
+    r.hbm.resize(to);
+    r.slot.resize(to);
+    r.state.resize(to);
+    r.len -= n * P;
+    if (r.n_full == 0) t->with_full.remove(rq);
+    return KV_OK;
+}
+
 int kv_table_blocks(kv_table *t, int32_t rq, int32_t *ids, int32_t *slots, int32_t *states, int32_t cap,
                     int32_t *n, int32_t *info)
 {
