@@ -7,6 +7,7 @@
 #include <cstdio>
 #include <new>
 #include <numeric>
+#include <type_traits>
 
 #include "../../include/duplexkv.h"
 #include "kv_decode_kernels.hpp"
@@ -20,9 +21,10 @@ struct kv_decoder {
     uint64_t plane_bytes = 0;  // from K to V of a layer, and half the way to the next layer
     // kv_attend: how the KV heads' units and their waves make up workgroups
     uint32_t units = 0, head_tiles = 0, units_per_wg = 0, subs = 0, wgs_per_group = 0, max_groups = 0;
+    uint32_t part_rows = 0, part_vecs = 0;
     uint32_t granule = 0, max_granules = 0;
     // one allocation, in this order
-    float *part = nullptr;
+    dkv::f32x4 *part = nullptr;
     dkv::f32x4 *part_ml = nullptr;
     float *lse2 = nullptr, *granules = nullptr;
 };
@@ -59,6 +61,7 @@ class OnDevice {
 };
 
 constexpr uint32_t kAttendWaves = 8;  // most waves of a workgroup
+constexpr uint32_t kJoinWgs = 1024;   // workgroups that join, over all requests
 
 bool rows_ok(const kv_rows &r) { return r.row >= 0 && r.head >= 0; }
 // 16-bit elements: rows begin on multiples of 16 bytes
@@ -78,9 +81,14 @@ int kinds(const kv_decoder *d, int &dp)
 template <typename X, bool FP8>
 void launch_attend(int dp, dim3 g, dim3 b, hipStream_t s, const dkv::AttendParams &p)
 {
-    if (dp == 64) hipLaunchKernelGGL((dkv::kv_attend_kernel<X, FP8, 64>), g, b, 0, s, p);
-    else if (dp == 128) hipLaunchKernelGGL((dkv::kv_attend_kernel<X, FP8, 128>), g, b, 0, s, p);
-    else hipLaunchKernelGGL((dkv::kv_attend_kernel<X, FP8, 256>), g, b, 0, s, p);
+    auto go = [&](auto dims) {
+        constexpr int DP = decltype(dims)::value;
+        if ((int)p.dim == DP) hipLaunchKernelGGL((dkv::kv_attend_kernel<X, FP8, DP, true>), g, b, 0, s, p);
+        else hipLaunchKernelGGL((dkv::kv_attend_kernel<X, FP8, DP, false>), g, b, 0, s, p);
+    };
+    if (dp == 64) go(std::integral_constant<int, 64>{});
+    else if (dp == 128) go(std::integral_constant<int, 128>{});
+    else go(std::integral_constant<int, 256>{});
 }
 
 }  // namespace
@@ -136,7 +144,9 @@ int kv_decoder_create(kv_decoder **out, const kv_config *cfg, const kv_decoder_c
     d->units_per_wg = (d->units + d->wgs_per_group - 1) / d->wgs_per_group;
     d->subs = 1;
     while (2 * d->subs * d->units_per_wg <= kAttendWaves) d->subs *= 2;
-    d->granule = std::gcd((uint32_t)cfg->block_size, 16u);
+    d->part_rows = std::min(group, 16u);
+    d->part_vecs = (cfg->head_dim <= 64 ? 4u : cfg->head_dim <= 128 ? 8u : 16u) * 4u * d->part_rows;
+    d->granule = cfg->block_size % 4 ? 1u : std::gcd((uint32_t)cfg->block_size, 16u);
     d->max_granules = (uint32_t)dc->max_blocks * ((uint32_t)cfg->block_size / d->granule);
     OnDevice on(d->device);
     auto fail = [&](int code) {
@@ -147,10 +157,10 @@ int kv_decoder_create(kv_decoder **out, const kv_config *cfg, const kv_decoder_c
         return fail(KV_EHIP);
     // ranges: as many workgroups as the chip holds at once, no more than there can be turns
     const uint64_t most_tiles = (uint64_t)dc->max_seqs * (((uint64_t)dc->max_blocks * cfg->block_size + dkv::kTile - 1) / dkv::kTile);
-    d->max_groups = (uint32_t)std::min<uint64_t>(std::max(1u, 2u * (uint32_t)d->n_cus / d->wgs_per_group),
+    d->max_groups = (uint32_t)std::min<uint64_t>(std::max(1u, std::min(dkv::kMaxGroups, (uint32_t)d->n_cus / d->wgs_per_group)),
                                                  (most_tiles + d->subs - 1) / d->subs);
-    const uint64_t slots = 2ull * d->max_groups * (uint64_t)dc->n_heads;
-    const uint64_t n_part = slots * (uint64_t)cfg->head_dim * 4, n_ml = slots * sizeof(dkv::f32x4),
+    const uint64_t slots = 2ull * d->max_groups;
+    const uint64_t n_part = slots * d->units * d->part_vecs * sizeof(dkv::f32x4), n_ml = slots * (uint64_t)dc->n_heads * sizeof(dkv::f32x4),
                    n_lse = ((uint64_t)dc->max_seqs * (uint64_t)dc->n_heads * 4 + 255) / 256 * 256,
                    n_gran = (uint64_t)dc->max_seqs * d->max_granules * (uint64_t)dc->n_heads * 4;
     uint8_t *mem = nullptr;
@@ -158,7 +168,7 @@ int kv_decoder_create(kv_decoder **out, const kv_config *cfg, const kv_decoder_c
         (void)hipGetLastError();
         return fail(KV_ENOMEM);
     }
-    d->part = (float *)mem;
+    d->part = (dkv::f32x4 *)mem;
     d->part_ml = (dkv::f32x4 *)(mem + n_part);
     d->lse2 = (float *)(mem + n_part + n_ml);
     d->granules = (float *)(mem + n_part + n_ml + n_lse);
@@ -303,7 +313,14 @@ int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
     p.subs = d->subs;
     p.group_heads = (uint32_t)(d->dc.n_heads / d->cfg.n_kv_heads);
     p.head_tiles = d->head_tiles;
+    p.part_rows = d->part_rows;
+    p.part_vecs = d->part_vecs;
+    p.by_items = dkv::Divide::by(p.part_vecs / 4u);
+    p.by_rows = dkv::Divide::by(p.part_rows);
+    p.by_head_tiles = dkv::Divide::by(p.head_tiles);
     p.granule = d->granule;
+    p.granule_bits = (uint32_t)__builtin_ctz(d->granule);
+    p.by_block = dkv::Divide::by(p.block_size);
     p.max_granules = d->max_granules;
     p.qk_scale = (float)((double)a->scale * 1.4426950408889634074 * (double)d->dc.k_scale);
     p.v_scale = d->dc.v_scale;
@@ -321,14 +338,12 @@ int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
     default: launch_attend<dkv::Fp16, true>(dp, g, b, s, p); break;
     }
     DECTRY(hipGetLastError());
-    const dim3 gj(p.n_heads, p.n_seqs);
+    const uint32_t lines = (p.units * p.part_vecs / 4u + 7u) / 8u;
+    p.joins = std::min(lines, std::max(1u, kJoinWgs / p.n_seqs));
+    const dim3 gj(p.joins + (p.granules ? (p.max_blocks + dkv::kMassBlocks - 1u) / dkv::kMassBlocks : 0u), p.n_seqs);
     if (d->dc.x_type == KV_FP16) hipLaunchKernelGGL(dkv::kv_join_kernel<dkv::Fp16>, gj, dim3(256), 0, s, p);
     else hipLaunchKernelGGL(dkv::kv_join_kernel<dkv::Bf16>, gj, dim3(256), 0, s, p);
     DECTRY(hipGetLastError());
-    if (p.granules) {
-        hipLaunchKernelGGL(dkv::kv_mass_kernel, dim3((p.max_blocks + 15u) / 16u, p.n_seqs), dim3(256), 0, s, p);
-        DECTRY(hipGetLastError());
-    }
     return KV_OK;
 }
 

@@ -82,14 +82,33 @@ struct Fp16 {
 // brought in the same order (the order of a contraction is free).  For the values it loads
 // 8 dimensions of each of those eight tokens, 16 lanes a row, whole rows of 256 bytes, and puts
 // the pairs of tokens that a dimension's operand is made of together with byte permutes.
+// Quotients of whole numbers below 2^31 by a divisor that the host knows: with 2^(bits - 1) < divisor <= 2^bits and
+// magic = ceil(2^(31 + bits) / divisor), x / divisor = x * magic >> (31 + bits).
+struct Divide {
+    uint32_t magic, shift;  // 0: the divisor is 1
+    static Divide by(uint32_t divisor)
+    {
+        uint32_t bits = 0;
+        while ((1ull << bits) < divisor) bits++;
+        if (bits == 0) return Divide{0u, 0u};
+        return Divide{(uint32_t)(((1ull << (31 + bits)) + divisor - 1) / divisor), bits - 1u};
+    }
+    __host__ __device__ __forceinline__ uint32_t quotient(uint32_t x) const
+    {
+        return magic ? (uint32_t)((uint64_t)x * magic >> 32) >> shift : x;
+    }
+};
+
 struct AttendParams {
     const uint8_t *k, *v;      // the layer's planes
     const int32_t *table, *lens;
     const uint8_t *q;
     uint8_t *out;
     float *lse;                // nullptr: not wanted
-    float *part;               // [groups * 2][n_heads][dim], unnormalised
-    f32x4 *part_ml;            // [groups * 2][n_heads]: reference, sum of rounded weights, sum of weights, -
+    // What ranges leave of requests that go on in others, unnormalised and as it lies in a wave's registers:
+    // [groups * 2][units][sum i][kq][part_rows], a vector of the dimensions i + (kq * 4 + r) * (8, or 4 up to 64 dimensions)
+    f32x4 *part;
+    f32x4 *part_ml;            // [groups * 2][n_heads]: reference, sum of rounded weights, sum of weights, its log2 + reference
     float *lse2;               // [n_seqs][n_heads], base 2; written where granules is
     float *granules;           // nullptr, or [n_seqs][max_granules][n_heads]: log2 of the weight of `granule` tokens
     const float *mass;
@@ -100,8 +119,12 @@ struct AttendParams {
     uint32_t n_seqs, n_heads, max_blocks, max_tokens;
     uint32_t dim, token_bytes, head_bytes;
     uint32_t block_size, cells_per_block, n_blocks;  // a block begins cells_per_block rows of token_bytes behind the one before it
+    Divide by_block;
     uint32_t groups, wgs_per_group, units, units_per_wg, subs, group_heads, head_tiles;
-    uint32_t granule, max_granules;
+    uint32_t part_rows, part_vecs;  // heads of a unit, and vectors: sums * 4 * part_rows
+    Divide by_items, by_rows, by_head_tiles;  // by part_vecs / 4, part_rows, head_tiles
+    uint32_t granule, granule_bits, max_granules;
+    uint32_t joins;            // workgroups that join, per request
     float qk_scale;            // to base 2
     float v_scale;
 };
@@ -116,50 +139,67 @@ __device__ __forceinline__ uint32_t seq_tokens(const int32_t *lens, uint32_t s, 
 
 __device__ __forceinline__ uint32_t tiles_of(uint32_t tokens) { return (tokens + kTile - 1u) / kTile; }
 
-__device__ __forceinline__ uint32_t wave_scan(uint32_t v, uint32_t lane)  // inclusive
+// Inclusive sum over the wave's lanes, in steps of 1, 2, 4, 8 within rows of 16 lanes, then from row to row.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v)
 {
-#pragma unroll
-    for (uint32_t d = 1; d < 64; d <<= 1) {
-        const uint32_t o = (uint32_t)__shfl_up((int)v, d, 64);
-        v += lane >= d ? o : 0u;
-    }
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);
     return v;
 }
 
 // Where the tiles of all requests go.  Every wave finds out for itself.
 struct Deal {
     uint32_t total, per;  // tiles, and tiles of a range
-    __device__ __forceinline__ Deal(const AttendParams &p, uint32_t lane)
+    // Of request (n_seqs - 1) / 64 * 64 + lane: its tokens, its tiles, and those of its 64 up to and with it.
+    uint32_t tokens, mine, upto;
+    uint32_t before;  // tiles of the requests before the one asked for
+    __device__ __forceinline__ Deal(const AttendParams &p, uint32_t lane, uint32_t asked) : total(0), before(0)
     {
-        uint32_t sum = 0;
         for (uint32_t base = 0; base < p.n_seqs; base += 64) {
-            const uint32_t s = base + lane;
-            sum += s < p.n_seqs ? tiles_of(seq_tokens(p.lens, s, p.max_tokens)) : 0u;
+            tokens = base + lane < p.n_seqs ? seq_tokens(p.lens, base + lane, p.max_tokens) : 0u;
+            mine = tiles_of(tokens);
+            upto = wave_scan(mine);
+            if (asked >= base && asked - base < 64u) before = total + (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), (int)(asked - base));
+            total += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
         }
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) sum += (uint32_t)__shfl_xor((int)sum, d, 64);
-        total = __builtin_amdgcn_readfirstlane(sum);
-        per = max((total + p.groups - 1u) / p.groups, 1u);
-        per = (per + p.subs - 1u) / p.subs * p.subs;
+        per = max((total + p.groups - 1u) / p.groups, p.subs);  // at least a tile for each wave
+    }
+    __device__ __forceinline__ uint32_t tokens_of(uint32_t s) const { return (uint32_t)__builtin_amdgcn_readlane((int)tokens, (int)s); }
+    // The request that tile `at` is one of, and which of its tiles.
+    __device__ __forceinline__ void find(const AttendParams &p, uint32_t lane, uint32_t at, uint32_t &s, uint32_t &t) const
+    {
+        uint32_t m = mine, u = upto, before = 0;
+        for (uint32_t base = 0; base < p.n_seqs; base += 64) {
+            if (p.n_seqs > 64u) {
+                m = base + lane < p.n_seqs ? tiles_of(seq_tokens(p.lens, base + lane, p.max_tokens)) : 0u;
+                u = wave_scan(m);
+            }
+            const uint64_t beyond = __ballot(before + u > at);
+            if (beyond) {
+                const uint32_t first = (uint32_t)__builtin_ctzll(beyond);
+                s = base + first;
+                t = at - before - (uint32_t)__builtin_amdgcn_readlane((int)(u - m), (int)first);
+                return;
+            }
+            before += (uint32_t)__builtin_amdgcn_readlane((int)u, 63);
+        }
+        s = t = 0;  // not reached: `at` is below total
     }
 };
 
-// Tiles of the requests before `s`.
-__device__ __forceinline__ uint32_t tiles_before(const AttendParams &p, uint32_t s, uint32_t lane)
-{
-    uint32_t sum = 0;
-    for (uint32_t at = lane; at < s; at += 64) sum += tiles_of(seq_tokens(p.lens, at, p.max_tokens));
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) sum += (uint32_t)__shfl_xor((int)sum, d, 64);
-    return __builtin_amdgcn_readfirstlane(sum);
-}
-
-template <typename X, bool FP8, int DP>
-struct Tile {
+template <bool FP8, int DP>
+struct Step {
     static constexpr int KJ = DP / 32;              // steps of 32 dimensions of q.k
     static constexpr int VW = DP == 64 ? 4 : 8;     // dimensions of a row that a lane loads at once,
     static constexpr int NV = DP == 64 ? 1 : DP / 128;  // and how often
     static constexpr int ACC = VW * NV;
+    // Tiles that a wave takes at a time.  Rows of 128 bytes and less: two, so that as many bytes are in
+    // flight as with rows of 256.
+    static constexpr int NT = DP * (FP8 ? 1 : 2) <= 128 ? 2 : 1;
 };
 
 template <int BYTES>
@@ -171,14 +211,26 @@ struct Raw<8> { typedef w32x2 type; };
 template <>
 struct Raw<4> { typedef uint32_t type; };
 
-template <typename X, bool FP8, int DP>
+__device__ __forceinline__ void clear(w32x4 &v) { v = w32x4{0u, 0u, 0u, 0u}; }
+__device__ __forceinline__ void clear(w32x2 &v) { v = w32x2{0u, 0u}; }
+__device__ __forceinline__ void clear(uint32_t &v) { v = 0u; }
+
+// WHOLE: heads have exactly DP dimensions.  Otherwise lanes whose dimensions are not there read the row's
+// first ones, in vain.
+template <typename X, bool FP8, int DP, bool WHOLE>
 __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
 {
-    using T = Tile<X, FP8, DP>;
-    constexpr int KJ = T::KJ, VW = T::VW, NV = T::NV, ACC = T::ACC;
-    typedef typename Raw<FP8 ? 8 : 16>::type kraw;
+    using T = Step<FP8, DP>;
+    constexpr int KJ = T::KJ, VW = T::VW, NV = T::NV, ACC = T::ACC, NT = T::NT;
+    // Of a key a lane takes 8 dimensions for each step of 32: in 16 bits dimensions 32 j + 8 kq on, 64 bytes
+    // of a row at once; in 8 bits, where rows are whole, those of its quarter of the row, 16 at once (q is
+    // brought in the same order).
+    constexpr bool RUNS = FP8 && WHOLE;
+    constexpr int KL = RUNS ? KJ / 2 : KJ;
+    typedef typename Raw<FP8 && !RUNS ? 8 : 16>::type kraw;
+    auto k_dim = [](int j, uint32_t kq) { return RUNS ? kq * (DP / 4) + (uint32_t)j * 8u : (uint32_t)j * 32u + kq * 8u; };
     typedef typename Raw<(FP8 ? 1 : 2) * VW>::type vraw;
-    __shared__ float joined[4][ACC * 4][64];
+    __shared__ f32x4 joined[4][ACC][64];
     __shared__ f32x4 ml[8][16];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t n = lane & 15u, kq = lane >> 4;
@@ -186,359 +238,501 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
     const uint32_t unit = (blockIdx.x - group * p.wgs_per_group) * p.units_per_wg + wave % p.units_per_wg;
     const uint32_t sub = wave / p.units_per_wg;
     const bool active = unit < p.units;
-    const Deal deal(p, lane);
+    const Deal deal(p, lane, 0u);
     uint32_t at = group * deal.per;
     const uint32_t end = min(at + deal.per, deal.total);
     if (at >= end) return;
-    // the request that tile `at` is one of, and which of its tiles
-    uint32_t s = 0, t = 0;
-    {
-        uint32_t before = 0;
-        for (uint32_t base = 0; base < p.n_seqs; base += 64) {
-            const uint32_t mine = base + lane < p.n_seqs ? tiles_of(seq_tokens(p.lens, base + lane, p.max_tokens)) : 0u;
-            const uint32_t upto = wave_scan(mine, lane);
-            const uint64_t beyond = __ballot(before + upto > at);
-            if (beyond) {
-                const uint32_t first = (uint32_t)__builtin_ctzll(beyond);
-                s = base + first;
-                t = at - before - (uint32_t)__shfl((int)(upto - mine), (int)first, 64);
-                break;
-            }
-            before += (uint32_t)__shfl((int)upto, 63, 64);
-        }
-        s = __builtin_amdgcn_readfirstlane(s);
-        t = __builtin_amdgcn_readfirstlane(t);
-    }
+    uint32_t s, t;
+    deal.find(p, lane, at, s, t);
     const uint32_t kv_head = active ? unit / p.head_tiles : 0u, ht = active ? unit - kv_head * p.head_tiles : 0u;
     const uint32_t rows = min(16u, p.group_heads - ht * 16u);      // query heads of this wave
     const uint32_t head = kv_head * p.group_heads + ht * 16u + n;  // this lane's
     const bool has_row = active && n < rows;
-    const uint8_t *const kb = p.k + (uint64_t)kv_head * p.head_bytes;
-    const uint8_t *const vb = p.v + (uint64_t)kv_head * p.head_bytes;
     constexpr uint32_t elem = FP8 ? 1u : 2u;
+    const uint8_t *const kb = p.k + (uint64_t)kv_head * p.head_bytes + (WHOLE ? k_dim(0, kq) * elem : 0u);
+    const uint8_t *const vb = p.v + (uint64_t)kv_head * p.head_bytes + (WHOLE ? n * VW * elem : 0u);
+    auto k_off = [&](int l) {
+        const uint32_t d = (uint32_t)l * 32u + kq * 8u;
+        return RUNS ? (uint32_t)l * 16u : WHOLE ? (uint32_t)l * 32u * elem : (d < p.dim ? d : 0u) * elem;
+    };
+    auto v_off = [&](int c) {
+        const uint32_t d = (uint32_t)c * 128u + n * VW;
+        return WHOLE ? (uint32_t)c * 128u * elem : (d < p.dim ? d : 0u) * elem;
+    };
 
-    while (at < end && s < p.n_seqs) {
-        const uint32_t tokens = seq_tokens(p.lens, s, p.max_tokens), n_tiles = tiles_of(tokens);
-        if (n_tiles == 0) {
-            s++;
-            t = 0;
-            continue;
+    // What a step needs is asked for a step (its pages two steps) ahead, across the ends of requests,
+    // too: a range goes on in the next request with its first keys under way.
+    struct Part {
+        uint32_t s, first, here;  // request, its tiles in this range
+        uint32_t tokens, upto;    // its tokens, and those that lie in its tiles up to here
+    };
+    auto tokens_of = [&](uint32_t i) { return p.n_seqs > 64u ? seq_tokens(p.lens, i, p.max_tokens) : deal.tokens_of(i); };
+    // The part that begins with tile `flat` of all, in request `i` or the first one behind it that has tiles.
+    auto part_at = [&](uint32_t i, uint32_t first, uint32_t flat) {
+        Part part = {i, first, 0u, 0u, 0u};
+        for (; flat < end && part.s < p.n_seqs; part.s++, part.first = 0u) {
+            part.tokens = tokens_of(part.s);
+            const uint32_t n_tiles = tiles_of(part.tokens);
+            if (n_tiles > part.first) {
+                part.here = min(n_tiles - part.first, end - flat);
+                part.upto = min(part.tokens, (part.first + part.here) * kTile);
+                break;
+            }
         }
-        const uint32_t here = min(n_tiles - t, end - at);
-        const int32_t *const row = p.table + (int64_t)s * p.table_stride;
-        w32x4 qf[KJ];
+        return part;
+    };
+    // The page of this lane's token of half tile h from `tile` on, and the row of the cache that makes it.
+    auto page_of = [&](const Part &part, uint32_t tile, int h) {
+        const uint32_t token = tile * kTile + (uint32_t)h * 16u + n;
+        return token < part.upto ? (uint32_t)p.table[(int64_t)part.s * p.table_stride + p.by_block.quotient(token)] : kNoCell;
+    };
+    auto cell_of = [&](uint32_t tile, int h, uint32_t page) {
+        const uint32_t token = tile * kTile + (uint32_t)h * 16u + n;
+        return page < p.n_blocks ? page * p.cells_per_block + (token - p.by_block.quotient(token) * p.block_size) : kNoCell;
+    };
+    Part now = {s, t, 0u, 0u, 0u}, next = part_at(s, t, at);
+    w32x4 qf[KJ];
+    kraw kr[2 * NT][KL];
+    uint32_t cell[2 * NT], page[2 * NT];
+    for (;;) {
+        uint32_t next_page[2 * NT];
+        const uint32_t next_first = next.first + sub * NT, next_stop = active ? next.first + next.here : 0u;
 #pragma unroll
-        for (int j = 0; j < KJ; j++) {
-            const uint32_t d = (uint32_t)j * 32u + kq * 8u;
-            qf[j] = w32x4{0u, 0u, 0u, 0u};
-            if (has_row && d < p.dim)
-                qf[j] = *reinterpret_cast<const w32x4 *>(p.q + (uint64_t)s * p.q_row + (uint64_t)head * p.q_head + d * 2u);
-        }
+        for (int h = 0; h < 2 * NT; h++) next_page[h] = next_first < next_stop ? page_of(next, next_first, h) : kNoCell;
         f32x4 acc[ACC], sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < ACC; i++) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
         float ref = -1e30f;  // finite, so that a score of -inf has weight 0 from the start
         float own = 0.f;     // this lane's part of the sum of weights as they are, before they are rounded
-
-        // The row of the cache that token (half, n) of tile `tt` lies in.
-        auto cell_of = [&](uint32_t tt, uint32_t half) {
-            const uint32_t token = tt * kTile + half * 16u + n;
-            uint32_t cell = kNoCell;
-            if (token < tokens) {
-                const uint32_t entry = token / p.block_size;
-                const uint32_t id = (uint32_t)row[entry];
-                if (id < p.n_blocks) cell = id * p.cells_per_block + (token - entry * p.block_size);
-            }
-            return cell;
-        };
-        for (uint32_t tt = t + sub; tt < t + here && active; tt += p.subs) {
-            uint32_t cell[2];
-            cell[0] = cell_of(tt, 0);
-            cell[1] = cell_of(tt, 1);
-            kraw kr[2][KJ];
-            vraw vr[8][NV];
-            uint32_t vcell[8];
+        const uint32_t stop = active ? now.first + now.here : 0u;
+        // at least once: a wave without a tile here still asks for what comes next
+        uint32_t tt = now.first + sub * NT;
+        do {
+            const bool have = tt < stop, last = tt + p.subs * NT >= stop;
+            vraw vr[8 * NT][NV];
+            uint32_t present = 0;  // bit r: token r of the lane's 8 NT is there
+            f32x4 sc[2 * NT];
+            if (have) {
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                const uint64_t off = (uint64_t)(cell[h] == kNoCell ? 0u : cell[h]) * p.token_bytes;
+                for (int r = 0; r < 8 * NT; r++) {
+                    const uint32_t c = (uint32_t)__shfl((int)cell[r / 4], (int)(kq * 4u + (r & 3)), 64);
+                    present |= c == kNoCell ? 0u : 1u << r;
+                    const uint64_t off = (uint64_t)(c == kNoCell ? 0u : c) * p.token_bytes;
 #pragma unroll
-                for (int j = 0; j < KJ; j++) {
-                    const uint32_t d = (uint32_t)j * 32u + kq * 8u;
-                    kr[h][j] = *reinterpret_cast<const kraw *>(kb + off + (d < p.dim ? d : 0u) * elem);
+                    for (int c = 0; c < NV; c++)
+                        vr[r][c] = __builtin_nontemporal_load(reinterpret_cast<const vraw *>(vb + off + v_off(c)));
                 }
-            }
-#pragma unroll
-            for (int r = 0; r < 8; r++) {
-                vcell[r] = (uint32_t)__shfl((int)cell[r / 4], (int)(kq * 4u + (r & 3)), 64);
-                const uint64_t off = (uint64_t)(vcell[r] == kNoCell ? 0u : vcell[r]) * p.token_bytes;
-#pragma unroll
-                for (int c = 0; c < NV; c++) {
-                    const uint32_t d = (uint32_t)c * 128u + n * VW;
-                    vr[r][c] = *reinterpret_cast<const vraw *>(vb + off + (d < p.dim ? d : 0u) * elem);
-                }
-            }
-            // scores: token x head
-            f32x4 sc[2];
-#pragma unroll
-            for (int h = 0; h < 2; h++) {
-                sc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int j = 0; j < KJ; j++) {
-                    w32x4 a;
-                    if constexpr (FP8) a = w32x4{X::template from_fp8<false>(kr[h][j].x), X::template from_fp8<true>(kr[h][j].x),
-                                                 X::template from_fp8<false>(kr[h][j].y), X::template from_fp8<true>(kr[h][j].y)};
-                    else a = kr[h][j];
+                if constexpr (!WHOLE) {
                     // dimensions that are not there meet zeros of q: they must not be NaN
-                    if ((uint32_t)j * 32u + 32u > p.dim && (uint32_t)j * 32u + kq * 8u >= p.dim) a = w32x4{0u, 0u, 0u, 0u};
-                    sc[h] = X::mma(a, qf[j], sc[h]);
+#pragma unroll
+                    for (int j = 0; j < KJ; j++) {
+                        if ((uint32_t)j * 32u + kq * 8u < p.dim) continue;
+#pragma unroll
+                        for (int h = 0; h < 2 * NT; h++) clear(kr[h][j]);
+                    }
+                }
+                // scores: token x head
+#pragma unroll
+                for (int h = 0; h < 2 * NT; h++) {
+                    sc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int j = 0; j < KJ; j++) {
+                        w32x4 a;
+                        if constexpr (FP8) {
+                            const uint32_t lo = RUNS ? kr[h][j / 2][2 * (j & 1)] : kr[h][j][0], hi = RUNS ? kr[h][j / 2][2 * (j & 1) + 1] : kr[h][j][1];
+                            a = w32x4{X::template from_fp8<false>(lo), X::template from_fp8<true>(lo), X::template from_fp8<false>(hi),
+                                      X::template from_fp8<true>(hi)};
+                        } else {
+                            a = kr[h][j];
+                        }
+                        sc[h] = X::mma(a, qf[j], sc[h]);
+                    }
                 }
             }
-            float w[8], top = -__builtin_inff();
+            // the next step's keys, while this one's values arrive
+            const uint32_t tile = last ? next_first : tt + p.subs * NT;
+            if (tile < (last ? next_stop : stop)) {
+                Part part = now;
+                if (last) part = next;
 #pragma unroll
-            for (int r = 0; r < 8; r++) {
-                w[r] = vcell[r] == kNoCell ? -__builtin_inff() : sc[r / 4][r & 3] * p.qk_scale;
-                top = fmaxf(top, w[r]);
+                for (int h = 0; h < 2 * NT; h++) cell[h] = cell_of(tile, h, last ? next_page[h] : page[h]);
+                if (last) {
+#pragma unroll
+                    for (int j = 0; j < KJ; j++) {
+                        const uint32_t d = k_dim(j, kq);
+                        qf[j] = w32x4{0u, 0u, 0u, 0u};
+                        if (has_row && (WHOLE || d < p.dim))
+                            qf[j] = *reinterpret_cast<const w32x4 *>(p.q + (uint64_t)part.s * p.q_row + (uint64_t)head * p.q_head + d * 2u);
+                    }
+                }
+#pragma unroll
+                for (int h = 0; h < 2 * NT; h++) {
+                    const uint64_t off = (uint64_t)(cell[h] == kNoCell ? 0u : cell[h]) * p.token_bytes;
+#pragma unroll
+                    for (int l = 0; l < KL; l++) kr[h][l] = *reinterpret_cast<const kraw *>(kb + off + k_off(l));
+                }
+#pragma unroll
+                for (int h = 0; h < 2 * NT; h++) page[h] = page_of(part, tile + p.subs * NT, h);
             }
+            if (!have) break;
+            float w[8 * NT], top = -__builtin_inff();
+#pragma unroll
+            for (int r = 0; r < 8 * NT; r++) w[r] = sc[r / 4][r & 3] * p.qk_scale;
+            const bool gaps = __any(present != (NT == 2 ? 0xFFFFu : 0xFFu));
+            if (gaps) {
+#pragma unroll
+                for (int r = 0; r < 8 * NT; r++) w[r] = present >> r & 1u ? w[r] : -__builtin_inff();
+            }
+#pragma unroll
+            for (int r = 0; r < 8 * NT; r++) top = fmaxf(top, w[r]);
             if (__any(top > ref + X::kBias + X::kSlack)) {
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const float next = fmaxf(ref, top - X::kBias), shrink = __builtin_amdgcn_exp2f(ref - next);
-                ref = next;
+                const float higher = fmaxf(ref, top - X::kBias), shrink = __builtin_amdgcn_exp2f(ref - higher);
+                ref = higher;
 #pragma unroll
                 for (int i = 0; i < ACC; i++) acc[i] *= shrink;
                 sum *= shrink;
                 own *= shrink;
             }
+            w32x4 pw[NT];
 #pragma unroll
-            for (int r = 0; r < 8; r++) {
+            for (int r = 0; r < 8 * NT; r++) {
                 w[r] = __builtin_amdgcn_exp2f(w[r] - ref);
                 own += w[r];
             }
-            const w32x4 pw = {X::pack(w[0], w[1]), X::pack(w[2], w[3]), X::pack(w[4], w[5]), X::pack(w[6], w[7])};
-            // out is divided by the sum of the weights that it is made of, the rounded ones (rows of
-            // ones beside the values); lse and the blocks' weights go by the sum of those that they were.
-            sum = X::mma(w32x4{X::kOnes, X::kOnes, X::kOnes, X::kOnes}, pw, sum);
+#pragma unroll
+            for (int i = 0; i < NT; i++) {
+#pragma unroll
+                for (int k = 0; k < 4; k++) pw[i][k] = X::pack(w[8 * i + 2 * k], w[8 * i + 2 * k + 1]);
+                // out is divided by the sum of the weights that it is made of, the rounded ones (rows of
+                // ones beside the values); lse and the blocks' weights go by the sum of those that they were.
+                sum = X::mma(w32x4{X::kOnes, X::kOnes, X::kOnes, X::kOnes}, pw[i], sum);
+            }
+            if (gaps) {  // a weight of 0 does not make up for NaN
+#pragma unroll
+                for (int r = 0; r < 8 * NT; r++) {
+                    if (present >> r & 1u) continue;
+#pragma unroll
+                    for (int c = 0; c < NV; c++) clear(vr[r][c]);
+                }
+            }
 #pragma unroll
             for (int c = 0; c < NV; c++) {
-                uint32_t pair[8][VW / 2];  // of each token: dimensions 2i and 2i + 1
 #pragma unroll
-                for (int r = 0; r < 8; r++) {
+                for (int m = 0; m < NT; m++) {
+                    // of token r: dimensions 2i and 2i + 1
+                    auto pair = [&](int r, int i) {
+                        const vraw &v = vr[8 * m + r][c];
+                        if constexpr (FP8 && VW == 8) return i & 1 ? X::template from_fp8<true>(v[i / 2]) : X::template from_fp8<false>(v[i / 2]);
+                        else if constexpr (FP8) return i & 1 ? X::template from_fp8<true>(v) : X::template from_fp8<false>(v);
+                        else return v[i];
+                    };
 #pragma unroll
                     for (int i = 0; i < VW / 2; i++) {
-                        if constexpr (FP8 && VW == 8)
-                            pair[r][i] = i & 1 ? X::template from_fp8<true>(vr[r][c][i / 2]) : X::template from_fp8<false>(vr[r][c][i / 2]);
-                        else if constexpr (FP8)
-                            pair[r][i] = i & 1 ? X::template from_fp8<true>(vr[r][c]) : X::template from_fp8<false>(vr[r][c]);
-                        else
-                            pair[r][i] = vr[r][c][i];
-                        // a weight of 0 does not make up for NaN
-                        if (vcell[r] == kNoCell) pair[r][i] = 0u;
-                    }
-                }
+                        w32x4 even, odd;
 #pragma unroll
-                for (int i = 0; i < VW / 2; i++) {
-                    w32x4 even, odd;
-#pragma unroll
-                    for (int k = 0; k < 4; k++) {
-                        even[k] = __builtin_amdgcn_perm(pair[2 * k + 1][i], pair[2 * k][i], 0x05040100u);
-                        odd[k] = __builtin_amdgcn_perm(pair[2 * k + 1][i], pair[2 * k][i], 0x07060302u);
+                        for (int k = 0; k < 4; k++) {
+                            const uint32_t a = pair(2 * k, i), b = pair(2 * k + 1, i);
+                            even[k] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+                            odd[k] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+                        }
+                        acc[c * VW + 2 * i] = X::mma(even, pw[m], acc[c * VW + 2 * i]);
+                        acc[c * VW + 2 * i + 1] = X::mma(odd, pw[m], acc[c * VW + 2 * i + 1]);
                     }
-                    acc[c * VW + 2 * i] = X::mma(even, pw, acc[c * VW + 2 * i]);
-                    acc[c * VW + 2 * i + 1] = X::mma(odd, pw, acc[c * VW + 2 * i + 1]);
                 }
             }
             if (p.granules) {
-                // weights of runs of `granule` tokens (1, 2, 4, 8 or 16: it divides a block and a half tile)
-                float *const g = p.granules + (uint64_t)s * p.max_granules * p.n_heads;
-                const uint32_t n_gran = (tokens + p.granule - 1u) / p.granule;
+                // weights of runs of `granule` tokens (1, 4, 8 or 16: it divides a block)
+                float *const g = p.granules + (uint64_t)now.s * p.max_granules * p.n_heads;
+                auto put = [&](uint32_t token, float weight) {
+                    if (has_row && token < now.upto) g[(uint64_t)(token >> p.granule_bits) * p.n_heads + head] = ref + __builtin_amdgcn_logf(weight);
+                };
 #pragma unroll
-                for (int h = 0; h < 2; h++) {
+                for (int h = 0; h < 2 * NT; h++) {
                     const uint32_t first = tt * kTile + (uint32_t)h * 16u + kq * 4u;
-                    auto put = [&](uint32_t token, float weight) {
-                        const uint32_t i = token / p.granule;
-                        if (has_row && i < n_gran) g[(uint64_t)i * p.n_heads + head] = ref + __builtin_amdgcn_logf(weight);
-                    };
-                    const float *x = w + 4 * h;
                     if (p.granule == 1u) {
-                        for (uint32_t r = 0; r < 4; r++) put(first + r, x[r]);
-                    } else if (p.granule == 2u) {
-                        put(first, x[0] + x[1]);
-                        put(first + 2u, x[2] + x[3]);
+#pragma unroll
+                        for (uint32_t r = 0; r < 4; r++) put(first + r, w[4 * h + r]);
                     } else {
-                        float y = (x[0] + x[1]) + (x[2] + x[3]);
-                        if (p.granule >= 8u) y += __shfl_xor(y, 16, 64);
-                        if (p.granule == 16u) y += __shfl_xor(y, 32, 64);
-                        if ((kq * 4u) % p.granule == 0u) put(first, y);
+                        float y = (w[4 * h] + w[4 * h + 1]) + (w[4 * h + 2] + w[4 * h + 3]);
+                        const float y8 = y + __shfl_xor(y, 16, 64), y16 = y8 + __shfl_xor(y8, 32, 64);
+                        y = p.granule == 16u ? y16 : p.granule == 8u ? y8 : y;
+                        if (((kq * 4u) & (p.granule - 1u)) == 0u) put(first, y);
                     }
                 }
             }
-        }
-        own += __shfl_xor(own, 16, 64);
-        own += __shfl_xor(own, 32, 64);
-        // waves that took turns at the tiles join
-        if (p.subs > 1u) {
-            if (kq == 0) ml[wave][n] = f32x4{ref, sum[0], own, 0.f};
-            __syncthreads();
-            float top = -1e30f, all = 0.f, all_own = 0.f;
-            for (uint32_t o = 0; o < p.subs; o++) top = fmaxf(top, ml[o * p.units_per_wg + wave % p.units_per_wg][n].x);
-            for (uint32_t o = 0; o < p.subs; o++) {
-                const f32x4 x = ml[o * p.units_per_wg + wave % p.units_per_wg][n];
-                const float f = __builtin_amdgcn_exp2f(x.x - top);
-                all += x.y * f;
-                all_own += x.z * f;
-            }
-            const float shrink = __builtin_amdgcn_exp2f(ref - top);
-            ref = top;
-            sum[0] = all;
-            own = all_own;
-#pragma unroll
-            for (int i = 0; i < ACC; i++) acc[i] *= shrink;
-            for (uint32_t half = p.subs / 2u; half > 0; half >>= 1) {
-                const uint32_t slot = wave - half * p.units_per_wg;
-                if (sub >= half && sub < 2u * half) {
-#pragma unroll
-                    for (int i = 0; i < ACC * 4; i++) joined[slot][i][lane] = acc[i / 4][i & 3];
-                }
+            tt += p.subs * NT;
+        } while (tt < stop);
+        if (now.here) {
+            own += __shfl_xor(own, 16, 64);
+            own += __shfl_xor(own, 32, 64);
+            // waves that took turns at the tiles join
+            if (p.subs > 1u) {
+                if (kq == 0) ml[wave][n] = f32x4{ref, sum[0], own, 0.f};
                 __syncthreads();
-                if (sub < half) {
-#pragma unroll
-                    for (int i = 0; i < ACC * 4; i++) acc[i / 4][i & 3] += joined[wave][i][lane];
+                float top = -1e30f, all = 0.f, all_own = 0.f;
+                for (uint32_t o = 0; o < p.subs; o++) top = fmaxf(top, ml[o * p.units_per_wg + wave % p.units_per_wg][n].x);
+                for (uint32_t o = 0; o < p.subs; o++) {
+                    const f32x4 x = ml[o * p.units_per_wg + wave % p.units_per_wg][n];
+                    const float f = __builtin_amdgcn_exp2f(x.x - top);
+                    all += x.y * f;
+                    all_own += x.z * f;
                 }
-                __syncthreads();
+                const float shrink = __builtin_amdgcn_exp2f(ref - top);
+                ref = top;
+                sum[0] = all;
+                own = all_own;
+#pragma unroll
+                for (int i = 0; i < ACC; i++) acc[i] *= shrink;
+                for (uint32_t half = p.subs / 2u; half > 0; half >>= 1) {
+                    const uint32_t slot = wave - half * p.units_per_wg;
+                    if (sub >= half && sub < 2u * half) {
+#pragma unroll
+                        for (int i = 0; i < ACC; i++) joined[slot][i][lane] = acc[i];
+                    }
+                    __syncthreads();
+                    if (sub < half) {
+#pragma unroll
+                        for (int i = 0; i < ACC; i++) acc[i] += joined[wave][i][lane];
+                    }
+                    __syncthreads();
+                }
             }
-        }
-        if (has_row && sub == 0u) {
-            const bool whole = here == n_tiles;
-            const float total = sum[0];
-            const uint32_t slot = group * 2u + (t > 0u ? 0u : 1u);
-            const float inv = total == 0.f ? 0.f : p.v_scale / total;
-            if (whole && kq == 0u) {
+            if (has_row && sub == 0u) {
+                const bool whole = now.here == tiles_of(now.tokens);
+                const float total = sum[0];
+                const uint32_t slot = group * 2u + (now.first > 0u ? 0u : 1u);
                 const float l2 = own == 0.f ? -__builtin_inff() : ref + __builtin_amdgcn_logf(own);
-                if (p.lse) p.lse[(uint64_t)s * p.n_heads + head] = l2 * 0.693147180559945309f;
-                if (p.granules) p.lse2[(uint64_t)s * p.n_heads + head] = l2;
-            }
-            if (!whole && kq == 0u) p.part_ml[(uint64_t)slot * p.n_heads + head] = f32x4{ref, total, own, 0.f};
+                const float inv = total == 0.f ? 0.f : p.v_scale / total;
+                if (whole && kq == 0u) {
+                    if (p.lse) p.lse[(uint64_t)now.s * p.n_heads + head] = l2 * 0.693147180559945309f;
+                    if (p.granules) p.lse2[(uint64_t)now.s * p.n_heads + head] = l2;
+                }
+                if (!whole && kq == 0u) p.part_ml[(uint64_t)slot * p.n_heads + head] = f32x4{ref, total, own, l2};
+                if (whole) {
+                    uint8_t *const to = p.out + (uint64_t)now.s * p.out_row + (uint64_t)head * p.out_head;
 #pragma unroll
-            for (int c = 0; c < NV; c++) {
+                    for (int c = 0; c < NV; c++) {
 #pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    const uint32_t d = (uint32_t)c * 128u + (kq * 4u + (uint32_t)r) * VW;
-                    if (d >= p.dim) continue;
-                    if (whole) {
-                        uint8_t *const to = p.out + (uint64_t)s * p.out_row + (uint64_t)head * p.out_head + d * 2u;
+                        for (int r = 0; r < 4; r++) {
+                            const uint32_t d = (uint32_t)c * 128u + (kq * 4u + (uint32_t)r) * VW;
+                            const f32x4 *a = acc + c * VW;
+                            uint32_t w[VW / 2];
 #pragma unroll
-                        for (int i = 0; i < VW / 4; i++) {
-                            const f32x4 *a = acc + c * VW + 4 * i;
-                            *reinterpret_cast<w32x2 *>(to + 8 * i) =
-                                w32x2{X::pack(a[0][r] * inv, a[1][r] * inv), X::pack(a[2][r] * inv, a[3][r] * inv)};
-                        }
-                    } else {
-                        float *const to = p.part + ((uint64_t)slot * p.n_heads + head) * p.dim + d;
-#pragma unroll
-                        for (int i = 0; i < VW / 4; i++) {
-                            const f32x4 *a = acc + c * VW + 4 * i;
-                            *reinterpret_cast<f32x4 *>(to + 4 * i) = f32x4{a[0][r], a[1][r], a[2][r], a[3][r]};
+                            for (int i = 0; i < VW / 2; i++) w[i] = X::pack(a[2 * i][r] * inv, a[2 * i + 1][r] * inv);
+                            if (WHOLE || d < p.dim) *reinterpret_cast<typename Raw<2 * VW>::type *>(to + d * 2u) = __builtin_bit_cast(typename Raw<2 * VW>::type, w);
                         }
                     }
+                } else {
+                    f32x4 *const to = p.part + ((uint64_t)slot * p.units + unit) * p.part_vecs + kq * p.part_rows + n;
+#pragma unroll
+                    for (int i = 0; i < ACC; i++) to[4u * (uint32_t)i * p.part_rows] = acc[i];
                 }
             }
         }
-        at += here;
-        t = 0;
-        s++;
+        if (!next.here) break;
+        at += next.here;
+        now = next;
+        next = part_at(now.s + 1u, 0u, at);
     }
 }
 
-// Joins what several ranges left of one request, a workgroup per request and query head:
-// out = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i.
-template <typename X>
-__global__ __launch_bounds__(256) void kv_join_kernel(const AttendParams p)
-{
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, head = blockIdx.x, s = blockIdx.y;
-    const uint32_t n_tiles = tiles_of(seq_tokens(p.lens, s, p.max_tokens));
-    const Deal deal(p, lane);
-    const uint32_t first = tiles_before(p, s, lane);
-    uint8_t *const to = p.out + (uint64_t)s * p.out_row + (uint64_t)head * p.out_head;
-    const uint32_t g0 = first / deal.per, g1 = n_tiles ? (first + n_tiles - 1u) / deal.per : g0;
-    if (n_tiles && g0 == g1) return;  // finished where it was computed
-    __shared__ f32x4 part[4];
-    __shared__ float rest[3][256];
-    auto slot_of = [&](uint32_t g) { return (uint64_t)(g * 2u + (g == g0 ? 1u : 0u)) * p.n_heads + head; };
-    float top = -1e30f, sum = 0.f, own = 0.f;
-    if (n_tiles) {
-        for (uint32_t g = g0 + threadIdx.x; g <= g1; g += 256) {
-            const f32x4 x = p.part_ml[slot_of(g)];
-            const float m = fmaxf(top, x.x), f = __builtin_amdgcn_exp2f(top - m), fx = __builtin_amdgcn_exp2f(x.x - m);
-            sum = sum * f + x.y * fx;
-            own = own * f + x.z * fx;
-            top = m;
-        }
-    }
+constexpr uint32_t kMaxGroups = 256;    // ranges of a call
+constexpr uint32_t kMassBlocks = 32;    // blocks of a workgroup that adds up weights
+
+// Joins what several ranges left of one request: out = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i.
+struct Joined {
+    float top, sum, own;  // reference, sum of rounded weights, sum of weights
+    f32x4 all[4];
+    __device__ __forceinline__ void none()
+    {
+        top = -1e30f;
+        sum = own = 0.f;
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        const float m2 = __shfl_xor(top, d, 64), l2 = __shfl_xor(sum, d, 64), o2 = __shfl_xor(own, d, 64), m = fmaxf(top, m2);
-        const float f = __builtin_amdgcn_exp2f(top - m), f2 = __builtin_amdgcn_exp2f(m2 - m);
-        sum = sum * f + l2 * f2;
-        own = own * f + o2 * f2;
-        top = m;
+        for (int i = 0; i < 4; i++) all[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    if (lane == 0) part[wave] = f32x4{top, sum, own, 0.f};
-    __syncthreads();
-    top = fmaxf(fmaxf(part[0].x, part[1].x), fmaxf(part[2].x, part[3].x));
-    sum = own = 0.f;
-    for (int w = 0; w < 4; w++) {
-        const float f = __builtin_amdgcn_exp2f(part[w].x - top);
-        sum += part[w].y * f;
-        own += part[w].z * f;
+    __device__ __forceinline__ void add(const f32x4 &x, const f32x4 (&o)[4])
+    {
+        const float next = fmaxf(top, x.x), f = __builtin_amdgcn_exp2f(top - next), g = __builtin_amdgcn_exp2f(x.x - next);
+        top = next;
+        sum = sum * f + x.y * g;
+        own = own * f + x.z * g;
+#pragma unroll
+        for (int i = 0; i < 4; i++) all[i] = all[i] * f + o[i] * g;
     }
-    const float inv = sum == 0.f ? 0.f : p.v_scale / sum;
-    if (threadIdx.x == 0) {
-        const float l2 = own == 0.f ? -__builtin_inff() : top + __builtin_amdgcn_logf(own);
-        if (p.lse) p.lse[(uint64_t)s * p.n_heads + head] = l2 * 0.693147180559945309f;
-        if (p.granules) p.lse2[(uint64_t)s * p.n_heads + head] = l2;
+    // with what the lanes `step` away hold
+    __device__ __forceinline__ void add_lanes(int step)
+    {
+        const f32x4 x = {__shfl_xor(top, step, 64), __shfl_xor(sum, step, 64), __shfl_xor(own, step, 64), 0.f};
+        f32x4 o[4];
+#pragma unroll
+        for (int i = 0; i < 16; i++) o[i / 4][i & 3] = __shfl_xor(all[i / 4][i & 3], step, 64);
+        add(x, o);
     }
-    // a lane has 4 dimensions, a wave every fourth range
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    const uint32_t d = lane * 4u;
-    if (n_tiles && d < p.dim) {
-#pragma unroll 4
-        for (uint32_t g = g0 + wave; g <= g1; g += 4) {
-            const uint64_t at = slot_of(g);
-            const float f = __builtin_amdgcn_exp2f(p.part_ml[at].x - top);
-            o += *reinterpret_cast<const f32x4 *>(p.part + at * p.dim + d) * f;
+};
+
+// A lane has four vectors of a range's part that follow one another along i, 4 x 4 dimensions, so
+// that it has 4 dimensions to store at a time.  8 lanes take a range; a wave takes up to 8 ranges
+// at once, or, of a request in fewer, as many more places; of a request in more, where that
+// takes fewer turns, the four waves of a workgroup take a quarter of the ranges each.
+template <typename X>
+__device__ __forceinline__ void join(const AttendParams &p, uint32_t s, uint32_t wg, uint32_t wgs, uint32_t n_parts, uint32_t g0)
+{
+    __shared__ f32x4 ml[4][8];
+    __shared__ f32x4 rest[4][4][8];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, u = lane & 7u, q = lane >> 3;
+    const uint32_t vecs = p.units * p.part_vecs, items = vecs / 4u, lines = (items + 7u) / 8u;
+    const uint32_t bits = n_parts <= 1u ? 0u : n_parts <= 2u ? 1u : n_parts <= 4u ? 2u : 3u;
+    auto turns = [](uint32_t n, uint32_t each) { return (n + each - 1u) / each; };
+    const bool wide = n_parts > 8u && turns(lines, wgs) * turns(n_parts, 64u) < turns(lines, wgs * 4u) * turns(n_parts, 16u);
+    const uint32_t at_once = wide ? 32u : 1u << bits, c = wide ? wave * 8u + q : q & (at_once - 1u);  // ranges
+    const uint32_t first = wide ? wg : (wg * 4u + wave) << (3u - bits), step = wide ? wgs : wgs * 4u << (3u - bits);
+    for (uint32_t line0 = first; line0 < lines; line0 += step) {
+        const uint32_t item = (line0 + (wide ? 0u : q >> bits)) * 8u + u;
+        const uint32_t unit = p.by_items.quotient(item), in_unit = item - unit * (p.part_vecs / 4u);
+        const uint32_t row_of_i4 = p.by_rows.quotient(in_unit), i4 = row_of_i4 >> 2, kq = row_of_i4 & 3u;
+        const uint32_t kv_head = p.by_head_tiles.quotient(unit);
+        const uint32_t in_group = (unit - kv_head * p.head_tiles) * 16u + in_unit - row_of_i4 * p.part_rows;
+        const uint32_t head = kv_head * p.group_heads + in_group;
+        const bool here = item < items && in_group < p.group_heads;
+        const uint32_t vec = unit * p.part_vecs + (i4 * 16u + kq) * p.part_rows + in_unit - row_of_i4 * p.part_rows;
+        Joined j;
+        j.none();
+        for (uint32_t base = 0; base < n_parts; base += 2u * at_once) {
+            f32x4 x[2], o[2][4];
+#pragma unroll
+            for (uint32_t k = 0; k < 2; k++) {
+                const uint32_t i = base + c + at_once * k;
+                const uint64_t slot = (g0 + i) * 2u + (i == 0u ? 1u : 0u);
+                x[k] = f32x4{-1e30f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (uint32_t m = 0; m < 4; m++) o[k][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (i < n_parts && here) {
+                    x[k] = p.part_ml[slot * p.n_heads + head];
+#pragma unroll
+                    for (uint32_t m = 0; m < 4; m++) o[k][m] = p.part[slot * vecs + vec + m * 4u * p.part_rows];
+                }
+            }
+#pragma unroll
+            for (uint32_t k = 0; k < 2; k++) j.add(x[k], o[k]);
         }
-    }
-    if (wave > 0) *reinterpret_cast<f32x4 *>(&rest[wave - 1][d]) = o;
-    __syncthreads();
-    if (wave == 0 && d < p.dim) {
-        for (int w = 0; w < 3; w++) o += *reinterpret_cast<const f32x4 *>(&rest[w][d]);
-        o *= inv;
-        *reinterpret_cast<w32x2 *>(to + d * 2u) = w32x2{X::pack(o[0], o[1]), X::pack(o[2], o[3])};
+        for (uint32_t m = 8; m < 8u * min(at_once, 8u); m <<= 1) j.add_lanes((int)m);
+        if (wide) {
+            __syncthreads();
+            if (q == 0u) {
+                ml[wave][u] = f32x4{j.top, j.sum, j.own, 0.f};
+#pragma unroll
+                for (int i = 0; i < 4; i++) rest[wave][i][u] = j.all[i];
+            }
+            __syncthreads();
+            if (threadIdx.x < 8u) {
+                for (int w = 1; w < 4; w++) {
+                    const f32x4 o[4] = {rest[w][0][u], rest[w][1][u], rest[w][2][u], rest[w][3][u]};
+                    j.add(ml[w][u], o);
+                }
+            }
+        }
+        if (!here || c != 0u) continue;
+        const float inv = j.sum == 0.f ? 0.f : p.v_scale / j.sum;
+        const uint32_t vw = p.dim <= 64u ? 4u : 8u;
+        uint8_t *const to = p.out + (uint64_t)s * p.out_row + (uint64_t)head * p.out_head;
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+            const uint32_t d = i4 / 2u * 128u + (kq * 4u + (uint32_t)r) * vw + (i4 & 1u) * 4u;
+            if (d < p.dim)
+                *reinterpret_cast<w32x2 *>(to + d * 2u) = w32x2{X::pack(j.all[0][r] * inv, j.all[1][r] * inv),
+                                                                X::pack(j.all[2][r] * inv, j.all[3][r] * inv)};
+        }
+        if (p.lse && row_of_i4 == 0u)
+            p.lse[(uint64_t)s * p.n_heads + head] =
+                j.own == 0.f ? -__builtin_inff() : (j.top + __builtin_amdgcn_logf(j.own)) * 0.693147180559945309f;
     }
 }
 
 // What each block received: 16 lanes a block add up 2^(granule - lse) over its granules and
-// all query heads, in a fixed order.
-static __global__ __launch_bounds__(256) void kv_mass_kernel(const AttendParams p)
+// all query heads, in a fixed order.  The heads' lse are joined once more here, for 32 blocks
+// at a time, so that this need not wait for the workgroups that join.
+__device__ __forceinline__ void add_mass(const AttendParams &p, uint32_t s, uint32_t first_block, uint32_t tokens, uint32_t g0, uint32_t g1)
 {
-    const uint32_t s = blockIdx.y, part = threadIdx.x & 15u, j = blockIdx.x * 16u + (threadIdx.x >> 4);
-    const uint32_t tokens = seq_tokens(p.lens, s, p.max_tokens);
-    const uint32_t per_block = p.block_size / p.granule, n_gran = (tokens + p.granule - 1u) / p.granule;
-    const uint32_t g0 = min(j * per_block, n_gran), g1 = min(g0 + per_block, n_gran);
-    const float *const g = p.granules + ((uint64_t)s * p.max_granules + g0) * p.n_heads;
-    float sum = 0.f;
-    for (uint32_t i = part, h = part % p.n_heads; i < (g1 - g0) * p.n_heads; i += 16u) {
-        const float l2 = p.lse2[(uint64_t)s * p.n_heads + h];
-        sum += l2 == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(g[i] - l2);
-        h += 16u;
-        while (h >= p.n_heads) h -= p.n_heads;
-    }
+    __shared__ float lse[1024];
+    __shared__ float2 some[256];
+    const uint32_t tid = threadIdx.x, part = tid & 15u;
+    // the first granules of a lane are under way while the heads' lse are found
+    constexpr uint32_t kAhead = 4;
+    const uint32_t per_block = p.block_size >> p.granule_bits, n_gran = (tokens + p.granule - 1u) >> p.granule_bits;
+    const float *from[2];
+    uint32_t n[2];
+    float ahead[2][kAhead];
 #pragma unroll
-    for (int d = 8; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
-    if (part == 0u && j < p.max_blocks) {
-        const int64_t at = (int64_t)s * p.mass_stride + j;
-        p.mass_out[at] = (p.mass ? p.mass[at] : 0.f) + sum;
+    for (int k = 0; k < 2; k++) {
+        const uint32_t j = first_block + 16u * (uint32_t)k + (tid >> 4), f = min(j * per_block, n_gran), l = min(f + per_block, n_gran);
+        from[k] = p.granules + ((uint64_t)s * p.max_granules + f) * p.n_heads;
+        n[k] = (l - f) * p.n_heads;
+#pragma unroll
+        for (uint32_t i = 0; i < kAhead; i++) ahead[k][i] = part + 16u * i < n[k] ? from[k][part + 16u * i] : 0.f;
     }
+    if (g0 == g1) {
+        for (uint32_t h = tid; h < p.n_heads; h += 256u) lse[h] = tokens ? p.lse2[(uint64_t)s * p.n_heads + h] : 0.f;
+    } else {
+        const uint32_t across = min(p.n_heads, 256u), parts = 256u / across, h0 = tid % across, from = tid / across;
+        for (uint32_t h = h0; h - h0 < p.n_heads; h += across) {
+            float top = -1e30f, sum = 0.f;
+            if (h < p.n_heads && from < parts) {
+#pragma unroll 8
+                for (uint32_t g = g0 + from; g <= g1; g += parts) {
+                    const float l2 = p.part_ml[(uint64_t)(g * 2u + (g == g0 ? 1u : 0u)) * p.n_heads + h].w, m = fmaxf(top, l2);
+                    sum = sum * __builtin_amdgcn_exp2f(top - m) + __builtin_amdgcn_exp2f(l2 - m);
+                    top = m;
+                }
+            }
+            __syncthreads();
+            some[tid] = float2{top, sum};
+            __syncthreads();
+            if (tid < across && h < p.n_heads) {
+                for (uint32_t i = 1; i < parts; i++) top = fmaxf(top, some[i * across + tid].x);
+                sum = 0.f;
+                for (uint32_t i = 0; i < parts; i++) sum += some[i * across + tid].y * __builtin_amdgcn_exp2f(some[i * across + tid].x - top);
+                lse[h] = sum == 0.f ? -__builtin_inff() : top + __builtin_amdgcn_logf(sum);
+            }
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; k++) {
+        const uint32_t j = first_block + 16u * (uint32_t)k + (tid >> 4);
+        float sum = 0.f;
+        uint32_t h = part % p.n_heads;
+        auto add = [&](float granule) {
+            sum += lse[h] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(granule - lse[h]);
+            h = (h + 16u) % p.n_heads;
+        };
+#pragma unroll
+        for (uint32_t i = 0; i < kAhead; i++)
+            if (part + 16u * i < n[k]) add(ahead[k][i]);
+#pragma unroll 4
+        for (uint32_t i = part + 16u * kAhead; i < n[k]; i += 16u) add(from[k][i]);
+#pragma unroll
+        for (int d = 8; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+        if (part == 0u && j < p.max_blocks) {
+            const int64_t at = (int64_t)s * p.mass_stride + j;
+            p.mass_out[at] = (p.mass ? p.mass[at] : 0.f) + sum;
+        }
+    }
+}
+
+// What is left when all ranges are done: a row of workgroups per request, first those that join, then
+// those that add up the blocks' weights.
+template <typename X>
+__global__ __launch_bounds__(256) void kv_join_kernel(const AttendParams p)
+{
+    const uint32_t s = blockIdx.y, lane = threadIdx.x & 63u;
+    const uint32_t tokens = seq_tokens(p.lens, s, p.max_tokens), n_tiles = tiles_of(tokens);
+    const Deal deal(p, lane, s);
+    const uint32_t first = deal.before;
+    const uint32_t g0 = first / deal.per, g1 = n_tiles ? (first + n_tiles - 1u) / deal.per : g0;
+    if (blockIdx.x >= p.joins) add_mass(p, s, (blockIdx.x - p.joins) * kMassBlocks, tokens, g0, g1);
+    else if (!n_tiles || g0 != g1) join<X>(p, s, blockIdx.x, p.joins, n_tiles ? g1 - g0 + 1u : 0u, g0);
 }
 
 // ---- new tokens into the cache ---------------------------------------------------------------
@@ -727,7 +921,7 @@ static __global__ __launch_bounds__(kEvictThreads) void kv_evict_kernel(const Ev
         if (wave == 0) {
             uint32_t mine[4], sum = 0;
             for (int i = 0; i < 4; i++) sum += mine[i] = bins[lane * 4u + i];
-            uint32_t before = wave_scan(sum, lane) - sum;
+            uint32_t before = wave_scan(sum) - sum;
             for (int i = 0; i < 4; i++) {
                 if (before < left && left <= before + mine[i]) {
                     chosen[0] = lane * 4u + i;

@@ -91,7 +91,8 @@ def evict(table, lens, mass, p, budget, first, last, cap):
         may = [j for j in range(held) if first <= j < held - last]
         weight = lambda j: (math.inf, 1, j) if math.isnan(mass[s, j]) else (float(mass[s, j]), 0, j)  # noqa: E731
         go = sorted(sorted(may, key=weight)[:max(0, min(held - budget, len(may), cap))])
-        stay = [j for j in range(held) if j not in set(go)]
+        gone = set(go)
+        stay = [j for j in range(held) if j not in gone]
         row, m = table[s].clone(), mass[s].clone()
         table[s], mass[s] = -1, 0
         table[s, :len(stay)], mass[s, :len(stay)] = row[stay], m[stay]
