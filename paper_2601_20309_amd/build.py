@@ -50,6 +50,29 @@ def build(force: bool = True, verbose: bool = False) -> str:
     return LIB
 
 
+TENSORS_SRC = os.path.join(CSRC, "decode_tensors.cpp")
+TENSORS_LIB = os.path.join(HERE, "_decode_tensors.so")
+
+
+def build_tensors(out: str = TENSORS_LIB) -> str:
+    """The Python module that takes the decoder's tensors apart, against torch's headers and the built library."""
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    inc = [os.path.join(root, "include"), sysconfig.get_paths()["include"], os.path.join(ROOT, "include"),
+           os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include")]
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}", TENSORS_SRC, "-o", out]
+    cmd += [x for d in inc for x in ("-isystem", d)]
+    cmd += ["-L", os.path.join(root, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python", "-L", HERE, "-lduplexkv",
+            "-Wl,-rpath,$ORIGIN"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("building _decode_tensors failed:\n" + r.stderr)
+    return out
+
+
 PROBE_SRC = os.path.join(CSRC, "pack_probe.hip")
 PROBE_BIN = os.path.join(HERE, "pack_probe")
 
@@ -86,3 +109,4 @@ def build_example(out: str = EXAMPLE_BIN) -> str:
 
 if __name__ == "__main__":
     print(build(force=True, verbose=True))
+    print(build_tensors())
