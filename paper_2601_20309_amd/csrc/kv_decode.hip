@@ -79,6 +79,13 @@ int kinds(const kv_decoder *d, int &dp)
 }
 
 template <typename X, bool FP8>
+void launch_put(bool eights, uint32_t threads, hipStream_t s, const dkv::PutParams &p)
+{
+    if (eights) hipLaunchKernelGGL((dkv::kv_put_kernel<X, FP8, 8>), dim3(p.n_rows), dim3(threads), 0, s, p);
+    else hipLaunchKernelGGL((dkv::kv_put_kernel<X, FP8, 4>), dim3(p.n_rows), dim3(threads), 0, s, p);
+}
+
+template <typename X, bool FP8>
 void launch_attend(int dp, dim3 g, dim3 b, hipStream_t s, const dkv::AttendParams &p)
 {
     auto go = [&](auto dims) {
@@ -251,14 +258,26 @@ int kv_put(kv_decoder *d, const kv_put_args *a, void *stream)
     p.section01 = p.section0 + (a->inv_freq && a->n_axes > 1 ? (uint32_t)a->sections[1] : 0u);
     p.k_inv = 1.f / d->dc.k_scale;
     p.v_inv = 1.f / d->dc.v_scale;
+    // 8 dimensions a step, or 4 where the halves of pairs are no multiple of 8 apart
+    const bool eights = p.interleaved || p.rot % 16u == 0;
+    const uint32_t n = eights ? 8u : 4u;
+    p.by_vecs = dkv::Divide::by(p.dim / n);
+    const uint32_t steps = p.dim / n - (p.interleaved ? 0u : p.rot / (2u * n));
+    p.by_steps = dkv::Divide::by(steps);
+    // Few rows: a thread for each place of a row, up to 512.  More rows than the chip has room for at
+    // once: workgroups of up to 256, so that more of them are under way, and of equal turns.  us, 448 places a
+    // row, by 512 / 128 lanes: 64 rows 3.7 / 5.1, 1000 7.6 / 9.5, 1500 11.2 / 11.3, 8192 38.1 / 32.5; 88 places,
+    // 6200 rows 27.6 / 11.0.
+    const uint32_t places = (p.n_heads * (p.qs ? 1u : 0u) + p.n_kv_heads) * steps + p.n_kv_heads * (p.dim / n);
+    const uint32_t most = p.n_rows <= 1024u ? 512u : 256u, turns = (places + most - 1u) / most;
+    const uint32_t threads = ((places + turns - 1u) / turns + 63u) / 64u * 64u;
     hipStream_t s = (hipStream_t)stream;
-    const dim3 g(p.n_rows), b(256);
     int dp;
     switch (kinds(d, dp)) {
-    case 0: hipLaunchKernelGGL((dkv::kv_put_kernel<dkv::Bf16, false>), g, b, 0, s, p); break;
-    case 1: hipLaunchKernelGGL((dkv::kv_put_kernel<dkv::Fp16, false>), g, b, 0, s, p); break;
-    case 2: hipLaunchKernelGGL((dkv::kv_put_kernel<dkv::Bf16, true>), g, b, 0, s, p); break;
-    default: hipLaunchKernelGGL((dkv::kv_put_kernel<dkv::Fp16, true>), g, b, 0, s, p); break;
+    case 0: launch_put<dkv::Bf16, false>(eights, threads, s, p); break;
+    case 1: launch_put<dkv::Fp16, false>(eights, threads, s, p); break;
+    case 2: launch_put<dkv::Bf16, true>(eights, threads, s, p); break;
+    default: launch_put<dkv::Fp16, true>(eights, threads, s, p); break;
     }
     DECTRY(hipGetLastError());
     return KV_OK;
@@ -376,7 +395,11 @@ int kv_evict(kv_decoder *d, const kv_evict_args *a, void *stream)
     p.n_first = (uint32_t)a->n_first;
     p.n_last = (uint32_t)a->n_last;
     p.max_evict = (uint32_t)a->max_evict;
-    hipLaunchKernelGGL(dkv::kv_evict_kernel, dim3((uint32_t)a->n_seqs), dim3(dkv::kEvictThreads), 0, (hipStream_t)stream, p);
+    const dim3 g((uint32_t)a->n_seqs);
+    hipStream_t s = (hipStream_t)stream;
+    if (p.max_blocks <= 512u) hipLaunchKernelGGL((dkv::kv_evict_kernel<512, 1, 11>), g, dim3(512), 0, s, p);
+    else if (p.max_blocks <= 2048u) hipLaunchKernelGGL((dkv::kv_evict_kernel<1024, 2, 11>), g, dim3(1024), 0, s, p);
+    else hipLaunchKernelGGL((dkv::kv_evict_kernel<1024, 8, 11>), g, dim3(1024), 0, s, p);
     DECTRY(hipGetLastError());
     return KV_OK;
 }

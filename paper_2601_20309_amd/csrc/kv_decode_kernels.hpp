@@ -748,6 +748,7 @@ struct PutParams {
     uint32_t n_seqs, n_rows, n_heads, n_kv_heads, max_blocks;
     uint32_t dim, token_bytes, head_bytes, block_size, cells_per_block, n_blocks;
     uint32_t rot, interleaved, section0, section01;  // pairs of the first axis, of the first two
+    Divide by_steps, by_vecs;  // by a rotated head's steps, and by a head's vectors
     float k_inv, v_inv;
 };
 
@@ -763,107 +764,129 @@ __device__ __forceinline__ uint32_t to_fp8(float a, float b, float c, float d, f
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(bound(c), bound(d), w, true);
 }
 
-// A workgroup takes a row at a time: its angles into LDS, then q, k and v in steps of 4
-// dimensions (two of them where the pairs' halves lie apart).
-template <typename X, bool FP8>
-__global__ __launch_bounds__(256) void kv_put_kernel(const PutParams p)
+// The nearest 16-bit or 8-bit values of N numbers.
+template <typename X, bool FP8, int N>
+__device__ __forceinline__ void store_row(uint8_t *to, uint32_t d, const float (&x)[N], float inv)
 {
+    if constexpr (FP8) {
+        uint32_t w[N / 4];
+#pragma unroll
+        for (int i = 0; i < N / 4; i++) w[i] = to_fp8(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3], inv);
+        __builtin_nontemporal_store(__builtin_bit_cast(typename Raw<N>::type, w), reinterpret_cast<typename Raw<N>::type *>(to + d));
+    } else {
+        uint32_t w[N / 2];
+#pragma unroll
+        for (int i = 0; i < N / 2; i++) w[i] = X::pack(x[2 * i], x[2 * i + 1]);
+        __builtin_nontemporal_store(__builtin_bit_cast(typename Raw<2 * N>::type, w), reinterpret_cast<typename Raw<2 * N>::type *>(to + d * 2u));
+    }
+}
+
+// A workgroup has a row.  A thread's first place (N dimensions, or where the halves of pairs lie apart N of each half)
+// is asked for first; while it arrives, the angles are found, one pair a thread, and left in LDS for all
+// heads, and the row's page is looked up.  Rows are short: what counts is how many of them a CU has under way, so
+// a thread holds one place at a time (8192 rows of 32 + 8 + 8 heads of 128, us: four places in flight 41.8, two
+// 35.7, one 33.0; loads that stay in the caches 39.1 with two; stores that do not 32.5 with one.  168 MB in
+// 32.5 us are 5.2 TB/s in and out, what a large copy reaches is 5.0).
+template <typename X, bool FP8, int N>
+__global__ __launch_bounds__(512) void kv_put_kernel(const PutParams p)
+{
+    typedef typename Raw<2 * N>::type raw;
     __shared__ float2 turn[128];
-    const uint32_t row = blockIdx.x, tid = threadIdx.x;
-    // the request whose row this is
+    const uint32_t row = blockIdx.x, tid = threadIdx.x, lane = tid & 63u;
+    // the request whose row this is: as many as begin behind the first, up to it
     uint32_t s = row, start = row, next = row + 1u;
     if (p.starts) {
-        uint32_t lo = 0, hi = p.n_seqs;  // starts[lo] <= row, starts[hi] > row
-        if (row >= (uint32_t)p.starts[p.n_seqs] || row < (uint32_t)p.starts[0]) return;
-        while (hi - lo > 1u) {
-            const uint32_t mid = (lo + hi) / 2u;
-            if ((uint32_t)p.starts[mid] <= row) lo = mid;
-            else hi = mid;
-        }
-        s = lo;
+        s = 0;
+        for (uint32_t base = 1; base <= p.n_seqs; base += 64u)
+            s += (uint32_t)__popcll(__ballot(base + lane <= p.n_seqs && p.starts[base + lane] <= (int32_t)row));
+        if (s >= p.n_seqs || (int32_t)row < p.starts[0]) return;
         start = (uint32_t)p.starts[s];
         next = (uint32_t)p.starts[s + 1u];
     }
-    const int64_t cell_token = (int64_t)p.lens[s] - (int64_t)(next - start) + (int64_t)(row - start);
-    bool page = cell_token >= 0 && cell_token < (int64_t)p.max_blocks * p.block_size;
-    uint64_t cell = 0;
-    if (page) {
-        const uint32_t entry = (uint32_t)cell_token / p.block_size;
-        const uint32_t id = (uint32_t)p.table[(int64_t)s * p.table_stride + entry];
-        page = id < p.n_blocks;
-        cell = (uint64_t)id * p.cells_per_block + ((uint32_t)cell_token - entry * p.block_size);
-    }
+    const uint32_t vecs = p.dim / N, apart = p.interleaved ? 0u : p.rot / (2u * N);  // steps of the lower halves
+    const uint32_t steps = vecs - apart;                                             // steps of a rotated head
+    const uint32_t n_q = p.qs ? p.n_heads * steps : 0u, n_k = n_q + p.n_kv_heads * steps, n_all = n_k + p.n_kv_heads * vecs;
     const uint32_t pairs = p.rot / 2u;
-    for (uint32_t i = tid; i < pairs; i += 256u) {
-        const uint32_t axis = i < p.section0 ? 0u : i < p.section01 ? 1u : 2u;
-        const double pos = p.positions ? (double)p.positions[(int64_t)axis * p.position_stride + row] : (double)cell_token;
-        // in 64 bits: half turns, and of those what is left of whole turns
-        const double turns = pos * (double)p.inv_freq[i] * 0.15915494309189533577;
-        const float half = 2.0f * (float)(turns - rint(turns));
-        float sn, cs;
-        sincospif(half, &sn, &cs);
-        turn[i] = float2{cs, sn};
-    }
-    __syncthreads();
-    const uint32_t v4 = p.dim / 4u, r4 = p.rot / 4u;
-    const uint32_t apart = p.interleaved ? 0u : r4 / 2u;   // steps of the lower halves
-    const uint32_t steps = v4 - apart;                     // steps of a rotated head
-    const uint32_t n_q = p.qs ? p.n_heads * steps : 0u, n_k = p.n_kv_heads * steps, n_v = p.n_kv_heads * v4;
-    uint8_t *const kc = p.k + cell * p.token_bytes, *const vc = p.v + cell * p.token_bytes;
-    auto rotated = [&](uint32_t step, const uint8_t *src, auto &&store) {
-        if (step < apart) {
-            const uint32_t d = step * 4u, d2 = d + p.rot / 2u;
-            const w32x2 a = *reinterpret_cast<const w32x2 *>(src + d * 2u), b = *reinterpret_cast<const w32x2 *>(src + d2 * 2u);
-            const float x[4] = {X::lo(a.x), X::hi(a.x), X::lo(a.y), X::hi(a.y)};
-            const float y[4] = {X::lo(b.x), X::hi(b.x), X::lo(b.y), X::hi(b.y)};
-            float u[4], w[4];
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const float2 c = turn[d + i];
-                u[i] = x[i] * c.x - y[i] * c.y;
-                w[i] = y[i] * c.x + x[i] * c.y;
-            }
-            store(d, u);
-            store(d2, w);
-            return;
+    bool page = false;
+    uint8_t *kc = nullptr, *vc = nullptr;
+    for (uint32_t first = 0; first < n_all; first += blockDim.x) {
+        raw a, b;
+        clear(a);
+        clear(b);
+        const uint32_t i = first + tid;
+        uint32_t head = 0, d = 0;
+        bool two = false;
+        if (i < n_all) {
+            const uint32_t in = i < n_q ? i : i < n_k ? i - n_q : i - n_k;
+            head = i < n_k ? p.by_steps.quotient(in) : p.by_vecs.quotient(in);
+            const uint32_t step = in - head * (i < n_k ? steps : vecs);
+            const uint8_t *const src = i < n_q ? p.qs + row * p.q_row + head * p.q_head
+                                       : i < n_k ? p.ks + row * p.k_row + head * p.k_head
+                                                 : p.vs + row * p.v_row + head * p.v_head;
+            two = i < n_k && step < apart;
+            d = (i < n_k && !two ? step + apart : step) * N;
+            a = __builtin_nontemporal_load(reinterpret_cast<const raw *>(src + d * 2u));
+            if (two) b = __builtin_nontemporal_load(reinterpret_cast<const raw *>(src + (d + pairs) * 2u));
         }
-        const uint32_t d = (step + apart) * 4u;
-        const w32x2 a = *reinterpret_cast<const w32x2 *>(src + d * 2u);
-        float x[4] = {X::lo(a.x), X::hi(a.x), X::lo(a.y), X::hi(a.y)};
-        if (d < p.rot) {
+        if (first == 0u) {
+            const int64_t token = (int64_t)p.lens[s] - (int64_t)(next - start) + (int64_t)(row - start);
+            for (uint32_t i = tid; i < pairs; i += blockDim.x) {
+                const uint32_t axis = i < p.section0 ? 0u : i < p.section01 ? 1u : 2u;
+                const double pos = p.positions ? (double)p.positions[(int64_t)axis * p.position_stride + row] : (double)token;
+                // in 64 bits: whole turns, and what is left of them; the rest as half turns
+                const double turns = pos * (double)p.inv_freq[i] * 0.15915494309189533577;
+                float sn, cs;
+                sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
+                turn[i] = float2{cs, sn};
+            }
+            page = token >= 0 && token < (int64_t)p.max_blocks * p.block_size;
+            uint64_t cell = 0;
+            if (page) {
+                const uint32_t entry = (uint32_t)token / p.block_size;
+                const uint32_t id = (uint32_t)p.table[(int64_t)s * p.table_stride + entry];
+                page = id < p.n_blocks;
+                cell = (uint64_t)id * p.cells_per_block + ((uint32_t)token - entry * p.block_size);
+            }
+            kc = p.k + cell * p.token_bytes;
+            vc = p.v + cell * p.token_bytes;
+            __syncthreads();
+        }
+        if (i >= n_all || (i >= n_q && !page)) continue;
+        const uint32_t *const wa = reinterpret_cast<const uint32_t *>(&a), *const wb = reinterpret_cast<const uint32_t *>(&b);
+        float x[N], y[N];
 #pragma unroll
-            for (int i = 0; i < 4; i += 2) {
-                const float2 c = turn[(d + i) / 2u];
-                const float u = x[i] * c.x - x[i + 1] * c.y, w = x[i + 1] * c.x + x[i] * c.y;
-                x[i] = u;
-                x[i + 1] = w;
+        for (int e = 0; e < N / 2; e++) {
+            x[2 * e] = X::lo(wa[e]);
+            x[2 * e + 1] = X::hi(wa[e]);
+            y[2 * e] = X::lo(wb[e]);
+            y[2 * e + 1] = X::hi(wb[e]);
+        }
+        if (two) {
+#pragma unroll
+            for (int e = 0; e < N; e++) {
+                const float2 c = turn[d + e];
+                const float u = x[e] * c.x - y[e] * c.y, w = y[e] * c.x + x[e] * c.y;
+                x[e] = u;
+                y[e] = w;
+            }
+        } else if (i < n_k && d < p.rot) {
+#pragma unroll
+            for (int e = 0; e < N; e += 2) {
+                const float2 c = turn[(d + e) / 2u];
+                const float u = x[e] * c.x - x[e + 1] * c.y, w = x[e + 1] * c.x + x[e] * c.y;
+                x[e] = u;
+                x[e + 1] = w;
             }
         }
-        store(d, x);
-    };
-    auto into_cache = [&](uint8_t *to, float inv) {
-        return [=](uint32_t d, const float(&x)[4]) {
-            if constexpr (FP8) *reinterpret_cast<uint32_t *>(to + d) = to_fp8(x[0], x[1], x[2], x[3], inv);
-            else *reinterpret_cast<w32x2 *>(to + d * 2u) = w32x2{X::pack(x[0], x[1]), X::pack(x[2], x[3])};
-        };
-    };
-    for (uint32_t i = tid; i < n_q + n_k + n_v; i += 256u) {
         if (i < n_q) {
-            const uint32_t h = i / steps, step = i - h * steps;
-            uint8_t *const to = p.qd + row * p.qd_row + h * p.qd_head;
-            rotated(step, p.qs + row * p.q_row + h * p.q_head, [=](uint32_t d, const float(&x)[4]) {
-                *reinterpret_cast<w32x2 *>(to + d * 2u) = w32x2{X::pack(x[0], x[1]), X::pack(x[2], x[3])};
-            });
-        } else if (!page) {
-            break;
-        } else if (i < n_q + n_k) {
-            const uint32_t h = (i - n_q) / steps, step = i - n_q - h * steps;
-            rotated(step, p.ks + row * p.k_row + h * p.k_head, into_cache(kc + h * p.head_bytes, p.k_inv));
+            uint8_t *const to = p.qd + row * p.qd_row + head * p.qd_head;
+            store_row<X, false>(to, d, x, 1.f);
+            if (two) store_row<X, false>(to, d + pairs, y, 1.f);
         } else {
-            const uint32_t j = i - n_q - n_k, h = j / v4, d = (j - h * v4) * 4u;
-            const w32x2 a = *reinterpret_cast<const w32x2 *>(p.vs + row * p.v_row + h * p.v_head + d * 2u);
-            const float x[4] = {X::lo(a.x), X::hi(a.x), X::lo(a.y), X::hi(a.y)};
-            into_cache(vc + h * p.head_bytes, p.v_inv)(d, x);
+            uint8_t *const to = (i < n_k ? kc : vc) + head * p.head_bytes;
+            const float inv = i < n_k ? p.k_inv : p.v_inv;
+            store_row<X, FP8>(to, d, x, inv);
+            if (two) store_row<X, FP8>(to, d + pairs, y, inv);
         }
     }
 }
@@ -879,8 +902,6 @@ struct EvictParams {
     uint32_t max_blocks, block_size, budget, n_first, n_last, max_evict;
 };
 
-constexpr int kEvictThreads = 1024;
-
 // Weights as whole numbers of the same order: lightest first, NaN last, -0 as 0.
 __device__ __forceinline__ uint32_t weight_key(float x)
 {
@@ -889,16 +910,20 @@ __device__ __forceinline__ uint32_t weight_key(float x)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// One workgroup per request.  The key of the last block to go is found digit by digit (8 bits at a
-// time, counted in LDS); then the row is closed up, 1024 entries at a time: what
-// is read of a stretch is read before anything is written, and nothing is written behind what has
-// been read, so a row may be its own output.
-static __global__ __launch_bounds__(kEvictThreads) void kv_evict_kernel(const EvictParams p)
+// One workgroup per request.  A thread holds 8 entries, THREADS apart, of those that are looked at together; a
+// row of no more than 8 THREADS is read once.  The key of the last block to go is found digit by digit, counted
+// in LDS, by four of 8 bits or three of 11 and less: with 11 the first has 8 steps per power of two, so that few
+// lanes of many meet in one count.  Then the row is closed up: a block moves down by the number of those before it that went.  All that
+// is written lies before all that is read later, so a row may be its own output.
+template <uint32_t THREADS, uint32_t EACH, uint32_t DIGIT>
+__global__ __launch_bounds__(THREADS) void kv_evict_kernel(const EvictParams p)
 {
+    constexpr uint32_t kWaves = THREADS / 64, kEach = EACH, kAtOnce = kEach * THREADS, kBins = 1u << DIGIT, kOwn = kBins / THREADS;
     const uint32_t s = blockIdx.x, tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
-    __shared__ uint32_t bins[256];
-    __shared__ uint32_t chosen[2];
-    __shared__ uint2 waves[kEvictThreads / 64];
+    __shared__ uint32_t bins[kBins];
+    __shared__ uint32_t sums[kWaves];
+    __shared__ uint32_t chosen[3];
+    __shared__ uint2 counts[kEach * kWaves];
     const uint32_t tokens = seq_tokens(p.lens, s, p.max_blocks * p.block_size);
     const uint32_t held = (tokens + p.block_size - 1u) / p.block_size;
     const int32_t *const table = p.table + (int64_t)s * p.table_stride;
@@ -908,81 +933,128 @@ static __global__ __launch_bounds__(kEvictThreads) void kv_evict_kernel(const Ev
     int32_t *const ids = p.ids + (int64_t)s * p.max_evict, *const ats = p.at + (int64_t)s * p.max_evict;
     const uint32_t from = min(p.n_first, held), to = held > p.n_last ? max(held - p.n_last, from) : from;  // may go
     const uint32_t go = min(min(held > p.budget ? held - p.budget : 0u, to - from), p.max_evict);
-    // key of the go-th lightest, and how many of that key go
-    uint32_t prefix = 0, left = go;
-    for (int shift = 24; shift >= 0 && go; shift -= 8) {
-        if (tid < 256u) bins[tid] = 0u;
+    const bool resident = held <= kAtOnce;
+    float m[kEach];
+    int32_t id[kEach];
+    auto load = [&](uint32_t base, bool with_ids) {
+#pragma unroll
+        for (uint32_t e = 0; e < kEach; e++) {
+            const uint32_t j = base + e * THREADS + tid;
+            m[e] = j < held ? mass[j] : 0.f;
+            if (with_ids) id[e] = j < held ? table[j] : -1;
+        }
+    };
+    if (resident) load(0u, true);
+    // the largest key that goes, and how many of that key do
+    uint32_t prefix = 0, known = 0, left = go;
+#pragma unroll 1
+    for (uint32_t low = 32; low > 0u && go;) {
+        const uint32_t bits = min(DIGIT, low), shift = low - bits, digit = (1u << bits) - 1u;
+        low = shift;
+#pragma unroll
+        for (uint32_t i = 0; i < kOwn; i++) bins[kOwn * tid + i] = 0u;
         __syncthreads();
-        for (uint32_t j = from + tid; j < to; j += kEvictThreads) {
-            const uint32_t key = weight_key(mass[j]);
-            if (shift == 24 || (key >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&bins[key >> shift & 255u], 1u);
+        for (uint32_t base = 0; base < to; base += kAtOnce) {
+            if (!resident) load(base, false);
+#pragma unroll
+            for (uint32_t e = 0; e < kEach; e++) {
+                const uint32_t j = base + e * THREADS + tid, key = weight_key(m[e]);
+                if (j >= from && j < to && (key & known) == prefix) atomicAdd(&bins[key >> shift & digit], 1u);
+            }
         }
         __syncthreads();
-        if (wave == 0) {
-            uint32_t mine[4], sum = 0;
-            for (int i = 0; i < 4; i++) sum += mine[i] = bins[lane * 4u + i];
-            uint32_t before = wave_scan(sum) - sum;
-            for (int i = 0; i < 4; i++) {
-                if (before < left && left <= before + mine[i]) {
-                    chosen[0] = lane * 4u + i;
-                    chosen[1] = left - before;
-                }
-                before += mine[i];
+        uint32_t own[kOwn], all = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kOwn; i++) all += own[i] = bins[kOwn * tid + i];
+        const uint32_t upto = wave_scan(all);
+        if (lane == 63u) sums[wave] = upto;
+        __syncthreads();
+        uint32_t before = upto - all;
+#pragma unroll
+        for (uint32_t w = 0; w < kWaves; w++) before += w < wave ? sums[w] : 0u;
+#pragma unroll
+        for (uint32_t i = 0; i < kOwn; i++) {
+            if (before < left && left <= before + own[i]) {
+                chosen[0] = kOwn * tid + i;
+                chosen[1] = left - before;
+                chosen[2] = own[i];
             }
+            before += own[i];
         }
         __syncthreads();
         prefix |= chosen[0] << shift;
+        known |= digit << shift;
         left = chosen[1];
+        if (left == chosen[2]) {  // all that begin so go
+            prefix |= ~known;
+            known = ~0u;
+            break;
+        }
     }
-    uint32_t gone = 0, ties = 0;  // in the stretches before
-    for (uint32_t base = 0; base < held; base += kEvictThreads) {
-        const uint32_t j = base + tid;
-        int32_t id = -1;
-        float m = 0.f;
-        uint32_t key = 0;
-        bool less = false, tie = false;
-        if (j < held) {
-            id = table[j];
-            m = mass[j];
-            key = weight_key(m);
+    const uint64_t below = (1ull << lane) - 1u;
+    uint32_t less_base = 0, tie_base = 0;  // of the entries looked at before
+    for (uint32_t base = 0; base < held; base += kAtOnce) {
+        if (!resident) load(base, true);
+        uint32_t less = 0, tie = 0;  // bit e
+        uint64_t bl[kEach], bt[kEach];
+#pragma unroll
+        for (uint32_t e = 0; e < kEach; e++) {
+            const uint32_t j = base + e * THREADS + tid, key = weight_key(m[e]);
             const bool may = go && j >= from && j < to;
-            less = may && key < prefix;
-            tie = may && key == prefix;
+            less |= may && key < prefix ? 1u << e : 0u;
+            tie |= may && key == prefix ? 1u << e : 0u;
+            bl[e] = __ballot(less >> e & 1u);
+            bt[e] = __ballot(tie >> e & 1u);
+            if (lane == 0u) counts[e * kWaves + wave] = uint2{(uint32_t)__popcll(bl[e]), (uint32_t)__popcll(bt[e])};
         }
-        const uint64_t below = (1ull << lane) - 1u, bl = __ballot(less), bt = __ballot(tie);
-        if (lane == 0) waves[wave] = uint2{(uint32_t)__popcll(bl), (uint32_t)__popcll(bt)};
         __syncthreads();
-        uint32_t less_before = 0, tie_before = ties, less_all = 0, tie_all = 0;
-        for (uint32_t w = 0; w < kEvictThreads / 64; w++) {
-            const uint2 x = waves[w];
-            less_before += w < wave ? x.x : 0u;
-            tie_before += w < wave ? x.y : 0u;
-            less_all += x.x;
-            tie_all += x.y;
-        }
-        less_before += (uint32_t)__popcll(bl & below);
-        tie_before += (uint32_t)__popcll(bt & below);
-        const bool goes = less || (tie && tie_before < left);
-        // those that went before j: the lighter ones, and of the ties the first `left`
-        const uint32_t left_before = gone + less_before + (min(tie_before, left) - min(ties, left));
-        if (j < held) {
-            if (goes) {
-                ids[left_before] = id;
-                ats[left_before] = (int32_t)j;
-            } else {
-                table_out[j - left_before] = id;
-                mass_out[j - left_before] = m;
+        if (wave == 0u) {  // sums of those before each, in the order of the entries
+            constexpr uint32_t kPer = (kEach * kWaves + 63u) / 64u;
+            uint2 c[kPer], sum = {0u, 0u};
+#pragma unroll
+            for (uint32_t i = 0; i < kPer; i++) {
+                c[i] = kPer * lane + i < kEach * kWaves ? counts[kPer * lane + i] : uint2{0u, 0u};
+                sum.x += c[i].x;
+                sum.y += c[i].y;
+            }
+            const uint32_t l = wave_scan(sum.x), t = wave_scan(sum.y);
+            uint2 first = {l - sum.x, t - sum.y};
+#pragma unroll
+            for (uint32_t i = 0; i < kPer; i++) {
+                if (kPer * lane + i < kEach * kWaves) counts[kPer * lane + i] = first;
+                first.x += c[i].x;
+                first.y += c[i].y;
+            }
+            if (lane == 63u) {
+                chosen[0] = l;
+                chosen[1] = t;
             }
         }
-        gone += less_all + (min(ties + tie_all, left) - min(ties, left));
-        ties += tie_all;
-        __syncthreads();  // the next stretch's counts, and reads of rows that are their own output
+        __syncthreads();
+#pragma unroll
+        for (uint32_t e = 0; e < kEach; e++) {
+            const uint32_t j = base + e * THREADS + tid;
+            if (j >= held) continue;
+            const uint2 c = counts[e * kWaves + wave];
+            const uint32_t tie_before = tie_base + c.y + (uint32_t)__popcll(bt[e] & below);
+            const uint32_t gone = less_base + c.x + (uint32_t)__popcll(bl[e] & below) + min(tie_before, left);
+            if (less >> e & 1u || (tie >> e & 1u && tie_before < left)) {
+                ids[gone] = id[e];
+                ats[gone] = (int32_t)j;
+            } else {
+                table_out[j - gone] = id[e];
+                mass_out[j - gone] = m[e];
+            }
+        }
+        less_base += chosen[0];
+        tie_base += chosen[1];
+        __syncthreads();
     }
-    for (uint32_t j = held - go + tid; j < p.max_blocks; j += kEvictThreads) {
+    for (uint32_t j = held - go + tid; j < p.max_blocks; j += THREADS) {
         table_out[j] = -1;
         mass_out[j] = 0.f;
     }
-    for (uint32_t j = go + tid; j < p.max_evict; j += kEvictThreads) ids[j] = ats[j] = -1;
+    for (uint32_t j = go + tid; j < p.max_evict; j += THREADS) ids[j] = ats[j] = -1;
     if (tid == 0) {
         p.count[s] = (int32_t)go;
         p.lens_out[s] = (int32_t)(tokens - go * p.block_size);
