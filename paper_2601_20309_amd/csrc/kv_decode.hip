@@ -344,8 +344,10 @@ int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
     p.qk_scale = (float)((double)a->scale * 1.4426950408889634074 * (double)d->dc.k_scale);
     p.v_scale = d->dc.v_scale;
     // no more ranges than there can be turns in this call
-    const uint64_t most = (uint64_t)p.n_seqs * ((p.max_tokens + dkv::kTile - 1) / dkv::kTile);
-    p.groups = (uint32_t)std::min<uint64_t>(p.groups, (most + p.subs - 1) / p.subs);
+    const uint32_t tiles = (p.max_tokens + dkv::kTile - 1) / dkv::kTile;
+    p.groups = (uint32_t)std::min<uint64_t>(p.groups, ((uint64_t)p.n_seqs * tiles + p.subs - 1) / p.subs);
+    p.by_request = tiles <= 2u * p.subs ? 1u : 0u;
+    if (p.by_request) p.groups = p.n_seqs;
     hipStream_t s = (hipStream_t)stream;
     const dim3 g(p.groups * p.wgs_per_group), b(64 * p.units_per_wg * p.subs);
     int dp;
@@ -358,8 +360,9 @@ int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
     }
     DECTRY(hipGetLastError());
     const uint32_t lines = (p.units * p.part_vecs / 4u + 7u) / 8u;
-    p.joins = std::min(lines, std::max(1u, kJoinWgs / p.n_seqs));
+    if (!p.by_request) p.joins = std::min(lines, std::max(1u, kJoinWgs / p.n_seqs));
     const dim3 gj(p.joins + (p.granules ? (p.max_blocks + dkv::kMassBlocks - 1u) / dkv::kMassBlocks : 0u), p.n_seqs);
+    if (gj.x == 0u) return KV_OK;
     if (d->dc.x_type == KV_FP16) hipLaunchKernelGGL(dkv::kv_join_kernel<dkv::Fp16>, gj, dim3(256), 0, s, p);
     else hipLaunchKernelGGL(dkv::kv_join_kernel<dkv::Bf16>, gj, dim3(256), 0, s, p);
     DECTRY(hipGetLastError());

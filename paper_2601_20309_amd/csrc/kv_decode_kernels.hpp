@@ -69,7 +69,8 @@ struct Fp16 {
 //
 // Work is cut into tiles of 32 tokens of one request.  The tiles of all requests, one behind
 // the other, are dealt to `groups` equal ranges, whatever the requests' lengths; a range
-// belongs to one workgroup (or several that share the KV heads).  A wave has one KV head and up
+// belongs to one workgroup (or several that share the KV heads).  (Where no request can be longer than a few
+// steps of a workgroup's waves, a range is a request, by_request: a second launch would take longer than they do.)  A wave has one KV head and up
 // to 16 of its query heads (a unit); where there are fewer units than waves, several
 // waves take turns at the tiles of a range and join in LDS.  A request that lies in one
 // range is finished there; others leave sum, reference and unnormalised output per range, and
@@ -125,6 +126,7 @@ struct AttendParams {
     Divide by_items, by_rows, by_head_tiles;  // by part_vecs / 4, part_rows, head_tiles
     uint32_t granule, granule_bits, max_granules;
     uint32_t joins;            // workgroups that join, per request
+    uint32_t by_request;       // a range is a request: nothing to join
     float qk_scale;            // to base 2
     float v_scale;
 };
@@ -159,6 +161,7 @@ struct Deal {
     uint32_t before;  // tiles of the requests before the one asked for
     __device__ __forceinline__ Deal(const AttendParams &p, uint32_t lane, uint32_t asked) : total(0), before(0)
     {
+        if (p.by_request) return;
         for (uint32_t base = 0; base < p.n_seqs; base += 64) {
             tokens = base + lane < p.n_seqs ? seq_tokens(p.lens, base + lane, p.max_tokens) : 0u;
             mine = tiles_of(tokens);
@@ -191,15 +194,12 @@ struct Deal {
     }
 };
 
-template <bool FP8, int DP>
+template <int DP>
 struct Step {
     static constexpr int KJ = DP / 32;              // steps of 32 dimensions of q.k
     static constexpr int VW = DP == 64 ? 4 : 8;     // dimensions of a row that a lane loads at once,
     static constexpr int NV = DP == 64 ? 1 : DP / 128;  // and how often
     static constexpr int ACC = VW * NV;
-    // Tiles that a wave takes at a time.  Rows of 128 bytes and less: two, so that as many bytes are in
-    // flight as with rows of 256.
-    static constexpr int NT = DP * (FP8 ? 1 : 2) <= 128 ? 2 : 1;
 };
 
 template <int BYTES>
@@ -220,17 +220,22 @@ __device__ __forceinline__ void clear(uint32_t &v) { v = 0u; }
 template <typename X, bool FP8, int DP, bool WHOLE>
 __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
 {
-    using T = Step<FP8, DP>;
-    constexpr int KJ = T::KJ, VW = T::VW, NV = T::NV, ACC = T::ACC, NT = T::NT;
+    using T = Step<DP>;
+    constexpr int KJ = T::KJ, VW = T::VW, NV = T::NV, ACC = T::ACC;
     // Of a key a lane takes 8 dimensions for each step of 32: in 16 bits dimensions 32 j + 8 kq on, 64 bytes
     // of a row at once; in 8 bits, where rows are whole, those of its quarter of the row, 16 at once (q is
     // brought in the same order).
     constexpr bool RUNS = FP8 && WHOLE;
     constexpr int KL = RUNS ? KJ / 2 : KJ;
+    // Rows of 512 bytes: half a tile of keys, and half of the values' dimensions, are what registers hold at a
+    // time, and nothing is asked for ahead.
+    constexpr bool LATE = NV > 1 && !FP8;
+    // Rows of 128 bytes and less in 8 bits leave room for two tiles of values: they are asked for ahead, too.
+    constexpr bool AHEAD = FP8 && DP <= 128;
     typedef typename Raw<FP8 && !RUNS ? 8 : 16>::type kraw;
     auto k_dim = [](int j, uint32_t kq) { return RUNS ? kq * (DP / 4) + (uint32_t)j * 8u : (uint32_t)j * 32u + kq * 8u; };
     typedef typename Raw<(FP8 ? 1 : 2) * VW>::type vraw;
-    __shared__ f32x4 joined[4][ACC][64];
+    __shared__ f32x4 joined[8][ACC][64];
     __shared__ f32x4 ml[8][16];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t n = lane & 15u, kq = lane >> 4;
@@ -239,16 +244,22 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
     const uint32_t sub = wave / p.units_per_wg;
     const bool active = unit < p.units;
     const Deal deal(p, lane, 0u);
-    uint32_t at = group * deal.per;
-    const uint32_t end = min(at + deal.per, deal.total);
-    if (at >= end) return;
-    uint32_t s, t;
-    deal.find(p, lane, at, s, t);
+    uint32_t at = p.by_request ? 0u : group * deal.per;
+    const uint32_t end = p.by_request ? tiles_of(seq_tokens(p.lens, group, p.max_tokens)) : min(at + deal.per, deal.total);
+    if (at >= end && !p.by_request) return;
+    uint32_t s = group, t = 0;
+    if (!p.by_request) deal.find(p, lane, at, s, t);
     const uint32_t kv_head = active ? unit / p.head_tiles : 0u, ht = active ? unit - kv_head * p.head_tiles : 0u;
     const uint32_t rows = min(16u, p.group_heads - ht * 16u);      // query heads of this wave
     const uint32_t head = kv_head * p.group_heads + ht * 16u + n;  // this lane's
     const bool has_row = active && n < rows;
     constexpr uint32_t elem = FP8 ? 1u : 2u;
+    if (at >= end) {  // a request of its own range, without a token
+        for (uint32_t d = kq * 4u; has_row && sub == 0u && d < p.dim; d += 16u)
+            *reinterpret_cast<w32x2 *>(p.out + (uint64_t)s * p.out_row + (uint64_t)head * p.out_head + d * 2u) = w32x2{0u, 0u};
+        if (p.lse && has_row && sub == 0u && kq == 0u) p.lse[(uint64_t)s * p.n_heads + head] = -__builtin_inff();
+        return;
+    }
     const uint8_t *const kb = p.k + (uint64_t)kv_head * p.head_bytes + (WHOLE ? k_dim(0, kq) * elem : 0u);
     const uint8_t *const vb = p.v + (uint64_t)kv_head * p.head_bytes + (WHOLE ? n * VW * elem : 0u);
     auto k_off = [&](int l) {
@@ -266,7 +277,7 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
         uint32_t s, first, here;  // request, its tiles in this range
         uint32_t tokens, upto;    // its tokens, and those that lie in its tiles up to here
     };
-    auto tokens_of = [&](uint32_t i) { return p.n_seqs > 64u ? seq_tokens(p.lens, i, p.max_tokens) : deal.tokens_of(i); };
+    auto tokens_of = [&](uint32_t i) { return p.n_seqs > 64u || p.by_request ? seq_tokens(p.lens, i, p.max_tokens) : deal.tokens_of(i); };
     // The part that begins with tile `flat` of all, in request `i` or the first one behind it that has tiles.
     auto part_at = [&](uint32_t i, uint32_t first, uint32_t flat) {
         Part part = {i, first, 0u, 0u, 0u};
@@ -292,13 +303,37 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
     };
     Part now = {s, t, 0u, 0u, 0u}, next = part_at(s, t, at);
     w32x4 qf[KJ];
-    kraw kr[2 * NT][KL];
-    uint32_t cell[2 * NT], page[2 * NT];
-    for (;;) {
-        uint32_t next_page[2 * NT];
-        const uint32_t next_first = next.first + sub * NT, next_stop = active ? next.first + next.here : 0u;
+    kraw kr[LATE ? 1 : 2][KL];
+    auto load_keys = [&](kraw(&to)[KL], uint32_t cell) {
+        const uint64_t off = (uint64_t)(cell == kNoCell ? 0u : cell) * p.token_bytes;
 #pragma unroll
-        for (int h = 0; h < 2 * NT; h++) next_page[h] = next_first < next_stop ? page_of(next, next_first, h) : kNoCell;
+        for (int l = 0; l < KL; l++) to[l] = *reinterpret_cast<const kraw *>(kb + off + k_off(l));
+    };
+    uint32_t cell[2], page[2];
+    // The lane's 8 tokens of the step whose cells are `cell`, and their values.
+    uint32_t vcell[8];
+    auto find_values = [&](uint32_t &present) {
+        present = 0;
+#pragma unroll
+        for (int r = 0; r < 8; r++) {
+            const uint32_t c = (uint32_t)__shfl((int)cell[r / 4], (int)(kq * 4u + (r & 3)), 64);
+            present |= c == kNoCell ? 0u : 1u << r;
+            vcell[r] = c == kNoCell ? 0u : c;
+        }
+    };
+    auto load_values = [&](vraw(&to)[8][LATE ? 1 : NV], int c) {
+#pragma unroll
+        for (int r = 0; r < 8; r++)
+            to[r][LATE ? 0 : c] = __builtin_nontemporal_load(
+                reinterpret_cast<const vraw *>(vb + (uint64_t)vcell[r] * p.token_bytes + v_off(c)));
+    };
+    vraw next_vr[8][LATE ? 1 : NV];
+    uint32_t next_present = 0;
+    for (;;) {
+        uint32_t next_page[2];
+        const uint32_t next_first = next.first + sub, next_stop = active ? next.first + next.here : 0u;
+#pragma unroll
+        for (int h = 0; h < 2; h++) next_page[h] = next_first < next_stop ? page_of(next, next_first, h) : kNoCell;
         f32x4 acc[ACC], sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < ACC; i++) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -306,56 +341,58 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
         float own = 0.f;     // this lane's part of the sum of weights as they are, before they are rounded
         const uint32_t stop = active ? now.first + now.here : 0u;
         // at least once: a wave without a tile here still asks for what comes next
-        uint32_t tt = now.first + sub * NT;
+        uint32_t tt = now.first + sub;
         do {
-            const bool have = tt < stop, last = tt + p.subs * NT >= stop;
-            vraw vr[8 * NT][NV];
-            uint32_t present = 0;  // bit r: token r of the lane's 8 NT is there
-            f32x4 sc[2 * NT];
+            const bool have = tt < stop, last = tt + p.subs >= stop;
+            vraw vr[8][LATE ? 1 : NV];
+            uint32_t present = 0;  // bit r: token r of the lane's 8 is there
+            f32x4 sc[2];
             if (have) {
+                if constexpr (AHEAD) {
+                    present = next_present;
 #pragma unroll
-                for (int r = 0; r < 8 * NT; r++) {
-                    const uint32_t c = (uint32_t)__shfl((int)cell[r / 4], (int)(kq * 4u + (r & 3)), 64);
-                    present |= c == kNoCell ? 0u : 1u << r;
-                    const uint64_t off = (uint64_t)(c == kNoCell ? 0u : c) * p.token_bytes;
+                    for (int r = 0; r < 8; r++) {
 #pragma unroll
-                    for (int c = 0; c < NV; c++)
-                        vr[r][c] = __builtin_nontemporal_load(reinterpret_cast<const vraw *>(vb + off + v_off(c)));
-                }
-                if constexpr (!WHOLE) {
-                    // dimensions that are not there meet zeros of q: they must not be NaN
-#pragma unroll
-                    for (int j = 0; j < KJ; j++) {
-                        if ((uint32_t)j * 32u + kq * 8u < p.dim) continue;
-#pragma unroll
-                        for (int h = 0; h < 2 * NT; h++) clear(kr[h][j]);
+                        for (int c = 0; c < NV; c++) vr[r][c] = next_vr[r][c];
                     }
+                } else {
+                    find_values(present);
+#pragma unroll
+                    for (int c = 0; c < (LATE ? 1 : NV); c++) load_values(vr, c);
                 }
                 // scores: token x head
 #pragma unroll
-                for (int h = 0; h < 2 * NT; h++) {
+                for (int h = 0; h < 2; h++) {
+                    kraw(&key)[KL] = kr[LATE ? 0 : h];
+                    if constexpr (LATE) load_keys(key, cell[h]);
+                    if constexpr (!WHOLE) {
+                        // dimensions that are not there meet zeros of q: they must not be NaN
+#pragma unroll
+                        for (int j = 0; j < KJ; j++)
+                            if ((uint32_t)j * 32u + kq * 8u >= p.dim) clear(key[j]);
+                    }
                     sc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int j = 0; j < KJ; j++) {
                         w32x4 a;
                         if constexpr (FP8) {
-                            const uint32_t lo = RUNS ? kr[h][j / 2][2 * (j & 1)] : kr[h][j][0], hi = RUNS ? kr[h][j / 2][2 * (j & 1) + 1] : kr[h][j][1];
+                            const uint32_t lo = RUNS ? key[j / 2][2 * (j & 1)] : key[j][0], hi = RUNS ? key[j / 2][2 * (j & 1) + 1] : key[j][1];
                             a = w32x4{X::template from_fp8<false>(lo), X::template from_fp8<true>(lo), X::template from_fp8<false>(hi),
                                       X::template from_fp8<true>(hi)};
                         } else {
-                            a = kr[h][j];
+                            a = key[j];
                         }
                         sc[h] = X::mma(a, qf[j], sc[h]);
                     }
                 }
             }
             // the next step's keys, while this one's values arrive
-            const uint32_t tile = last ? next_first : tt + p.subs * NT;
+            const uint32_t tile = last ? next_first : tt + p.subs;
             if (tile < (last ? next_stop : stop)) {
                 Part part = now;
                 if (last) part = next;
 #pragma unroll
-                for (int h = 0; h < 2 * NT; h++) cell[h] = cell_of(tile, h, last ? next_page[h] : page[h]);
+                for (int h = 0; h < 2; h++) cell[h] = cell_of(tile, h, last ? next_page[h] : page[h]);
                 if (last) {
 #pragma unroll
                     for (int j = 0; j < KJ; j++) {
@@ -365,26 +402,29 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
                             qf[j] = *reinterpret_cast<const w32x4 *>(p.q + (uint64_t)part.s * p.q_row + (uint64_t)head * p.q_head + d * 2u);
                     }
                 }
+                if constexpr (!LATE) {
 #pragma unroll
-                for (int h = 0; h < 2 * NT; h++) {
-                    const uint64_t off = (uint64_t)(cell[h] == kNoCell ? 0u : cell[h]) * p.token_bytes;
+                    for (int h = 0; h < 2; h++) load_keys(kr[h], cell[h]);
+                }
+                if constexpr (AHEAD) {
+                    find_values(next_present);
 #pragma unroll
-                    for (int l = 0; l < KL; l++) kr[h][l] = *reinterpret_cast<const kraw *>(kb + off + k_off(l));
+                    for (int c = 0; c < NV; c++) load_values(next_vr, c);
                 }
 #pragma unroll
-                for (int h = 0; h < 2 * NT; h++) page[h] = page_of(part, tile + p.subs * NT, h);
+                for (int h = 0; h < 2; h++) page[h] = page_of(part, tile + p.subs, h);
             }
             if (!have) break;
-            float w[8 * NT], top = -__builtin_inff();
+            float w[8], top = -__builtin_inff();
 #pragma unroll
-            for (int r = 0; r < 8 * NT; r++) w[r] = sc[r / 4][r & 3] * p.qk_scale;
-            const bool gaps = __any(present != (NT == 2 ? 0xFFFFu : 0xFFu));
+            for (int r = 0; r < 8; r++) w[r] = sc[r / 4][r & 3] * p.qk_scale;
+            const bool gaps = __any(present != 0xFFu);
             if (gaps) {
 #pragma unroll
-                for (int r = 0; r < 8 * NT; r++) w[r] = present >> r & 1u ? w[r] : -__builtin_inff();
+                for (int r = 0; r < 8; r++) w[r] = present >> r & 1u ? w[r] : -__builtin_inff();
             }
 #pragma unroll
-            for (int r = 0; r < 8 * NT; r++) top = fmaxf(top, w[r]);
+            for (int r = 0; r < 8; r++) top = fmaxf(top, w[r]);
             if (__any(top > ref + X::kBias + X::kSlack)) {
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
@@ -395,51 +435,41 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
                 sum *= shrink;
                 own *= shrink;
             }
-            w32x4 pw[NT];
 #pragma unroll
-            for (int r = 0; r < 8 * NT; r++) {
+            for (int r = 0; r < 8; r++) {
                 w[r] = __builtin_amdgcn_exp2f(w[r] - ref);
                 own += w[r];
             }
-#pragma unroll
-            for (int i = 0; i < NT; i++) {
-#pragma unroll
-                for (int k = 0; k < 4; k++) pw[i][k] = X::pack(w[8 * i + 2 * k], w[8 * i + 2 * k + 1]);
-                // out is divided by the sum of the weights that it is made of, the rounded ones (rows of
-                // ones beside the values); lse and the blocks' weights go by the sum of those that they were.
-                sum = X::mma(w32x4{X::kOnes, X::kOnes, X::kOnes, X::kOnes}, pw[i], sum);
-            }
-            if (gaps) {  // a weight of 0 does not make up for NaN
-#pragma unroll
-                for (int r = 0; r < 8 * NT; r++) {
-                    if (present >> r & 1u) continue;
-#pragma unroll
-                    for (int c = 0; c < NV; c++) clear(vr[r][c]);
-                }
-            }
+            const w32x4 pw = {X::pack(w[0], w[1]), X::pack(w[2], w[3]), X::pack(w[4], w[5]), X::pack(w[6], w[7])};
+            // out is divided by the sum of the weights that it is made of, the rounded ones (rows of
+            // ones beside the values); lse and the blocks' weights go by the sum of those that they were.
+            sum = X::mma(w32x4{X::kOnes, X::kOnes, X::kOnes, X::kOnes}, pw, sum);
 #pragma unroll
             for (int c = 0; c < NV; c++) {
+                if (LATE && c > 0) load_values(vr, c);
+                if (gaps) {  // a weight of 0 does not make up for NaN
 #pragma unroll
-                for (int m = 0; m < NT; m++) {
-                    // of token r: dimensions 2i and 2i + 1
-                    auto pair = [&](int r, int i) {
-                        const vraw &v = vr[8 * m + r][c];
-                        if constexpr (FP8 && VW == 8) return i & 1 ? X::template from_fp8<true>(v[i / 2]) : X::template from_fp8<false>(v[i / 2]);
-                        else if constexpr (FP8) return i & 1 ? X::template from_fp8<true>(v) : X::template from_fp8<false>(v);
-                        else return v[i];
-                    };
+                    for (int r = 0; r < 8; r++)
+                        if (!(present >> r & 1u)) clear(vr[r][LATE ? 0 : c]);
+                }
+                // of token r: dimensions 2i and 2i + 1
+                auto pair = [&](int r, int i) {
+                    const vraw &v = vr[r][LATE ? 0 : c];
+                    if constexpr (FP8 && VW == 8) return i & 1 ? X::template from_fp8<true>(v[i / 2]) : X::template from_fp8<false>(v[i / 2]);
+                    else if constexpr (FP8) return i & 1 ? X::template from_fp8<true>(v) : X::template from_fp8<false>(v);
+                    else return v[i];
+                };
 #pragma unroll
-                    for (int i = 0; i < VW / 2; i++) {
-                        w32x4 even, odd;
+                for (int i = 0; i < VW / 2; i++) {
+                    w32x4 even, odd;
 #pragma unroll
-                        for (int k = 0; k < 4; k++) {
-                            const uint32_t a = pair(2 * k, i), b = pair(2 * k + 1, i);
-                            even[k] = __builtin_amdgcn_perm(b, a, 0x05040100u);
-                            odd[k] = __builtin_amdgcn_perm(b, a, 0x07060302u);
-                        }
-                        acc[c * VW + 2 * i] = X::mma(even, pw[m], acc[c * VW + 2 * i]);
-                        acc[c * VW + 2 * i + 1] = X::mma(odd, pw[m], acc[c * VW + 2 * i + 1]);
+                    for (int k = 0; k < 4; k++) {
+                        const uint32_t a = pair(2 * k, i), b = pair(2 * k + 1, i);
+                        even[k] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+                        odd[k] = __builtin_amdgcn_perm(b, a, 0x07060302u);
                     }
+                    acc[c * VW + 2 * i] = X::mma(even, pw, acc[c * VW + 2 * i]);
+                    acc[c * VW + 2 * i + 1] = X::mma(odd, pw, acc[c * VW + 2 * i + 1]);
                 }
             }
             if (p.granules) {
@@ -449,7 +479,7 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
                     if (has_row && token < now.upto) g[(uint64_t)(token >> p.granule_bits) * p.n_heads + head] = ref + __builtin_amdgcn_logf(weight);
                 };
 #pragma unroll
-                for (int h = 0; h < 2 * NT; h++) {
+                for (int h = 0; h < 2; h++) {
                     const uint32_t first = tt * kTile + (uint32_t)h * 16u + kq * 4u;
                     if (p.granule == 1u) {
 #pragma unroll
@@ -462,56 +492,46 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
                     }
                 }
             }
-            tt += p.subs * NT;
+            tt += p.subs;
         } while (tt < stop);
         if (now.here) {
             own += __shfl_xor(own, 16, 64);
             own += __shfl_xor(own, 32, 64);
-            // waves that took turns at the tiles join
+            const bool whole = now.here == tiles_of(now.tokens);
+            const uint32_t slot = group * 2u + (now.first > 0u ? 0u : 1u);
+            f32x4 *const part = p.part + ((uint64_t)slot * p.units + unit) * p.part_vecs;
+            uint8_t *const out = p.out + (uint64_t)now.s * p.out_row;
+            // Waves that took turns at the tiles leave what they have in LDS, and share the sums out among them.
+            float scale[8];  // of each one's: 2^(its reference - the largest)
             if (p.subs > 1u) {
-                if (kq == 0) ml[wave][n] = f32x4{ref, sum[0], own, 0.f};
+                const uint32_t u = wave % p.units_per_wg;
+                if (kq == 0u) ml[wave][n] = f32x4{ref, sum[0], own, 0.f};
+#pragma unroll
+                for (int i = 0; i < ACC; i++) joined[wave][i][lane] = acc[i];
                 __syncthreads();
-                float top = -1e30f, all = 0.f, all_own = 0.f;
-                for (uint32_t o = 0; o < p.subs; o++) top = fmaxf(top, ml[o * p.units_per_wg + wave % p.units_per_wg][n].x);
-                for (uint32_t o = 0; o < p.subs; o++) {
-                    const f32x4 x = ml[o * p.units_per_wg + wave % p.units_per_wg][n];
-                    const float f = __builtin_amdgcn_exp2f(x.x - top);
-                    all += x.y * f;
-                    all_own += x.z * f;
+                f32x4 x[8];
+#pragma unroll
+                for (uint32_t o = 0; o < 8; o++) {
+                    x[o] = o < p.subs ? ml[o * p.units_per_wg + u][n] : f32x4{-1e30f, 0.f, 0.f, 0.f};
+                    ref = fmaxf(ref, x[o].x);
                 }
-                const float shrink = __builtin_amdgcn_exp2f(ref - top);
-                ref = top;
-                sum[0] = all;
-                own = all_own;
+                sum[0] = own = 0.f;
 #pragma unroll
-                for (int i = 0; i < ACC; i++) acc[i] *= shrink;
-                for (uint32_t half = p.subs / 2u; half > 0; half >>= 1) {
-                    const uint32_t slot = wave - half * p.units_per_wg;
-                    if (sub >= half && sub < 2u * half) {
-#pragma unroll
-                        for (int i = 0; i < ACC; i++) joined[slot][i][lane] = acc[i];
-                    }
-                    __syncthreads();
-                    if (sub < half) {
-#pragma unroll
-                        for (int i = 0; i < ACC; i++) acc[i] += joined[wave][i][lane];
-                    }
-                    __syncthreads();
+                for (uint32_t o = 0; o < 8; o++) {
+                    scale[o] = __builtin_amdgcn_exp2f(x[o].x - ref);
+                    sum[0] += x[o].y * scale[o];
+                    own += x[o].z * scale[o];
                 }
             }
-            if (has_row && sub == 0u) {
-                const bool whole = now.here == tiles_of(now.tokens);
-                const float total = sum[0];
-                const uint32_t slot = group * 2u + (now.first > 0u ? 0u : 1u);
+            const float total = sum[0], inv = total == 0.f ? 0.f : p.v_scale / total;
+            if (has_row && sub == 0u && kq == 0u) {
                 const float l2 = own == 0.f ? -__builtin_inff() : ref + __builtin_amdgcn_logf(own);
-                const float inv = total == 0.f ? 0.f : p.v_scale / total;
-                if (whole && kq == 0u) {
-                    if (p.lse) p.lse[(uint64_t)now.s * p.n_heads + head] = l2 * 0.693147180559945309f;
-                    if (p.granules) p.lse2[(uint64_t)now.s * p.n_heads + head] = l2;
-                }
-                if (!whole && kq == 0u) p.part_ml[(uint64_t)slot * p.n_heads + head] = f32x4{ref, total, own, l2};
-                if (whole) {
-                    uint8_t *const to = p.out + (uint64_t)now.s * p.out_row + (uint64_t)head * p.out_head;
+                if (!whole) p.part_ml[(uint64_t)slot * p.n_heads + head] = f32x4{ref, total, own, l2};
+                if (whole && p.lse) p.lse[(uint64_t)now.s * p.n_heads + head] = l2 * 0.693147180559945309f;
+                if (whole && p.granules) p.lse2[(uint64_t)now.s * p.n_heads + head] = l2;
+            }
+            if (p.subs == 1u) {
+                if (has_row && whole) {
 #pragma unroll
                     for (int c = 0; c < NV; c++) {
 #pragma unroll
@@ -521,14 +541,39 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
                             uint32_t w[VW / 2];
 #pragma unroll
                             for (int i = 0; i < VW / 2; i++) w[i] = X::pack(a[2 * i][r] * inv, a[2 * i + 1][r] * inv);
-                            if (WHOLE || d < p.dim) *reinterpret_cast<typename Raw<2 * VW>::type *>(to + d * 2u) = __builtin_bit_cast(typename Raw<2 * VW>::type, w);
+                            if (WHOLE || d < p.dim)
+                                *reinterpret_cast<typename Raw<2 * VW>::type *>(out + (uint64_t)head * p.out_head + d * 2u) =
+                                    __builtin_bit_cast(typename Raw<2 * VW>::type, w);
                         }
                     }
-                } else {
-                    f32x4 *const to = p.part + ((uint64_t)slot * p.units + unit) * p.part_vecs + kq * p.part_rows + n;
+                } else if (has_row) {
 #pragma unroll
-                    for (int i = 0; i < ACC; i++) to[4u * (uint32_t)i * p.part_rows] = acc[i];
+                    for (int i = 0; i < ACC; i++) part[((uint32_t)i * 4u + kq) * p.part_rows + n] = acc[i];
                 }
+            } else {
+                const uint32_t u = wave % p.units_per_wg;
+                for (uint32_t i0 = sub * 2u; i0 < ACC; i0 += p.subs * 2u) {
+                    f32x4 a[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+                    for (uint32_t o = 0; o < 8; o++) {
+                        if (o >= p.subs) break;
+                        a[0] += joined[o * p.units_per_wg + u][i0][lane] * scale[o];
+                        a[1] += joined[o * p.units_per_wg + u][i0 + 1u][lane] * scale[o];
+                    }
+                    if (has_row && whole) {
+                        // two dimensions at a time
+#pragma unroll
+                        for (int r = 0; r < 4; r++) {
+                            const uint32_t d = i0 / 8u * 128u + (kq * 4u + (uint32_t)r) * VW + i0 % 8u;
+                            if (WHOLE || d < p.dim)
+                                *reinterpret_cast<uint32_t *>(out + (uint64_t)head * p.out_head + d * 2u) = X::pack(a[0][r] * inv, a[1][r] * inv);
+                        }
+                    } else if (has_row) {
+                        part[(i0 * 4u + kq) * p.part_rows + n] = a[0];
+                        part[((i0 + 1u) * 4u + kq) * p.part_rows + n] = a[1];
+                    }
+                }
+                if (next.here) __syncthreads();
             }
         }
         if (!next.here) break;
@@ -730,7 +775,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(const AttendParams p)
     const uint32_t tokens = seq_tokens(p.lens, s, p.max_tokens), n_tiles = tiles_of(tokens);
     const Deal deal(p, lane, s);
     const uint32_t first = deal.before;
-    const uint32_t g0 = first / deal.per, g1 = n_tiles ? (first + n_tiles - 1u) / deal.per : g0;
+    const uint32_t g0 = p.by_request ? 0u : first / deal.per, g1 = p.by_request ? 0u : n_tiles ? (first + n_tiles - 1u) / deal.per : g0;
     if (blockIdx.x >= p.joins) add_mass(p, s, (blockIdx.x - p.joins) * kMassBlocks, tokens, g0, g1);
     else if (!n_tiles || g0 != g1) join<X>(p, s, blockIdx.x, p.joins, n_tiles ? g1 - g0 + 1u : 0u, g0);
 }
