@@ -504,6 +504,8 @@ typedef struct {
     int32_t max_blocks;  /* most blocks of a request: entries of a table row */
     float k_scale;       /* what a stored 1 of K stands for (KV_FP8; else it has to be 1) */
     float v_scale;
+    int32_t weigh;       /* 1: kv_attend may be asked for mass_out, which takes max_seqs * max_blocks * n_heads floats of
+                            memory (as many times that as an odd block has tokens, or 4, 8 or 16 go into one) */
 } kv_decoder_config;
 
 /*
@@ -511,7 +513,8 @@ typedef struct {
  * must outlive the decoder.  KV_EINVAL: bad configuration, types that do not fit
  * elem_bytes, scales that are not finite and above 0.  KV_EUNSUP: head_dim above
  * 256 or no multiple of 8, more than 1024 query heads, a cache that is not
- * aligned to 16 bytes or of 2^32 and more token rows per KV plane.  KV_ENOMEM, KV_EHIP.
+ * aligned to 16 bytes or of 2^32 and more token rows per KV plane, more than 65535
+ * requests, 2^31 and more tokens in a table row or tiles of 32 tokens in all.  KV_ENOMEM, KV_EHIP.
  */
 int kv_decoder_create(kv_decoder **decoder, const kv_config *cfg, const kv_decoder_config *dc, void *hbm_cache);
 
@@ -583,7 +586,8 @@ typedef struct {
  * weights that the tokens of block j got, summed over the query heads (n_heads in all,
  * per request), j below the request's blocks; behind these it is mass[s][j].  The result
  * is the same, bit for bit, whenever the same call runs with the same lens.
- * KV_EINVAL, KV_EUNSUP, KV_E2BIG as for kv_put.
+ * out may be q itself.  KV_EINVAL, KV_EUNSUP, KV_E2BIG as for kv_put; KV_EUNSUP for mass_out
+ * without `weigh`.
  */
 int kv_attend(kv_decoder *decoder, const kv_attend_args *args, void *stream);
 

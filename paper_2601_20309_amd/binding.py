@@ -65,7 +65,7 @@ class kv_sched_req(C.Structure):
 
 class kv_decoder_config(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_heads", "x_type", "kv_type", "max_seqs", "max_blocks")] + \
-        [("k_scale", C.c_float), ("v_scale", C.c_float)]
+        [("k_scale", C.c_float), ("v_scale", C.c_float), ("weigh", C.c_int32)]
 
 
 class kv_rows(C.Structure):

@@ -5,6 +5,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <c10/hip/HIPStream.h>
+#include <hip/hip_runtime_api.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
@@ -20,12 +21,14 @@ struct Spec {
     int64_t n_heads, n_kv_heads, dim, max_blocks;
     at::ScalarType x;
     float scale;
+    int device;
 };
 
 // One call's arguments.  ok falls when something does not fit.
 struct Call {
     bool ok = true;
-    int device = -1;
+    int device;  // the decoder's: tensors lie there
+    explicit Call(const Spec *d) : device(d->device) {}
 
     const at::Tensor *tensor(PyObject *o)
     {
@@ -35,11 +38,10 @@ struct Call {
             return nullptr;
         }
         const at::Tensor *t = &THPVariable_Unpack(o);
-        if (!t->defined() || !t->is_cuda() || t->layout() != at::kStrided || (device >= 0 && t->device().index() != device)) {
+        if (!t->defined() || !t->is_cuda() || t->layout() != at::kStrided || t->device().index() != device) {
             ok = false;
             return nullptr;
         }
-        device = t->device().index();
         return t;
     }
 
@@ -105,7 +107,7 @@ struct Call {
         return v;
     }
 
-    // None: the current stream of the tensors' device
+    // None: the current stream of the decoder's device
     void *stream(PyObject *o)
     {
         if (o == Py_None) return (void *)c10::hip::getCurrentHIPStream((c10::DeviceIndex)device).stream();
@@ -138,17 +140,24 @@ bool count_is(Py_ssize_t n, Py_ssize_t want)
 
 void free_spec(PyObject *o) { delete spec_of(o); }
 
-// spec(handle, n_heads, n_kv_heads, head_dim, max_blocks, x_type, scale)
+// spec(handle, cache address, n_heads, n_kv_heads, head_dim, max_blocks, x_type, scale)
 PyObject *spec(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    if (!count_is(n, 7)) return nullptr;
+    if (!count_is(n, 8)) return nullptr;
     void *handle = PyLong_AsVoidPtr(a[0]);
-    const int64_t v[5] = {PyLong_AsLongLong(a[1]), PyLong_AsLongLong(a[2]), PyLong_AsLongLong(a[3]), PyLong_AsLongLong(a[4]),
-                          PyLong_AsLongLong(a[5])};
-    const double scale = PyFloat_AsDouble(a[6]);
+    void *cache = PyLong_AsVoidPtr(a[1]);
+    const int64_t v[5] = {PyLong_AsLongLong(a[2]), PyLong_AsLongLong(a[3]), PyLong_AsLongLong(a[4]), PyLong_AsLongLong(a[5]),
+                          PyLong_AsLongLong(a[6])};
+    const double scale = PyFloat_AsDouble(a[7]);
     if (PyErr_Occurred()) return nullptr;
+    hipPointerAttribute_t at;
+    if (hipPointerGetAttributes(&at, cache) != hipSuccess) {
+        PyErr_SetString(PyExc_RuntimeError, "the cache's device is not known");
+        return nullptr;
+    }
     Spec *s = new (std::nothrow)
-        Spec{(kv_decoder *)handle, v[0], v[1], v[2], v[3], v[4] == KV_FP16 ? at::kHalf : at::kBFloat16, (float)scale};
+        Spec{(kv_decoder *)handle, v[0], v[1], v[2], v[3], v[4] == KV_FP16 ? at::kHalf : at::kBFloat16, (float)scale,
+             at.device};
     if (!s) return PyErr_NoMemory();
     PyObject *capsule = PyCapsule_New(s, "duplexkv.decoder", free_spec);
     if (!capsule) delete s;
@@ -162,7 +171,7 @@ PyObject *put(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     const Spec *d = spec_of(a[0]);
     if (!d) return nullptr;
     return result([&] {
-        Call c;
+        Call c(d);
         kv_put_args p;
         memset(&p, 0, sizeof p);
         p.layer = (int32_t)c.number(a[1], INT32_MIN, INT32_MAX);
@@ -207,7 +216,7 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     const Spec *d = spec_of(a[0]);
     if (!d) return nullptr;
     return result([&] {
-        Call c;
+        Call c(d);
         kv_attend_args p;
         memset(&p, 0, sizeof p);
         p.layer = (int32_t)c.number(a[1], INT32_MIN, INT32_MAX);
@@ -234,7 +243,7 @@ PyObject *evict(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     const Spec *d = spec_of(a[0]);
     if (!d) return nullptr;
     return result([&] {
-        Call c;
+        Call c(d);
         kv_evict_args p;
         memset(&p, 0, sizeof p);
         const int64_t n = c.length(a[2], 1);

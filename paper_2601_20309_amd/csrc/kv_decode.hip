@@ -67,6 +67,9 @@ bool rows_ok(const kv_rows &r) { return r.row >= 0 && r.head >= 0; }
 // 16-bit elements: rows begin on multiples of 16 bytes
 bool rows_aligned(const kv_rows &r) { return (uintptr_t)r.data % 16 == 0 && r.row % 8 == 0 && r.head % 8 == 0; }
 
+// rows that are written must not be one and the same
+bool apart(const kv_rows &r, int32_t n, int32_t heads) { return (n < 2 || r.row > 0) && (heads < 2 || r.head > 0); }
+
 uint8_t *plane(const kv_decoder *d, int32_t layer, int which)
 {
     return d->hbm + (2ull * (uint64_t)layer + (uint64_t)which) * d->plane_bytes;
@@ -115,7 +118,9 @@ int kv_decoder_create(kv_decoder **out, const kv_config *cfg, const kv_decoder_c
         if (!(scale > 0.f) || !std::isfinite(scale) || !std::isfinite(1.f / scale) || (dc->kv_type != KV_FP8 && scale != 1.f))
             return KV_EINVAL;
     if (cfg->head_dim > 256 || cfg->head_dim % 8 != 0 || dc->n_heads > 1024 || (uintptr_t)hbm_cache % 16 != 0) return KV_EUNSUP;
-    if ((int64_t)dc->max_blocks * cfg->block_size > 0x7FFFFFC0) return KV_EUNSUP;
+    // tokens of a request, tiles of a call and the requests of a launch are counted in 31, 31 and 16 bits
+    const int64_t tokens = (int64_t)dc->max_blocks * cfg->block_size;
+    if (tokens > 0x7FFFFFC0 || dc->max_seqs > 65535 || (tokens / dkv::kTile + 1) * dc->max_seqs > 0x7FFFFFFF) return KV_EUNSUP;
     const uint64_t token_bytes = (uint64_t)cfg->n_kv_heads * (uint64_t)cfg->head_dim * (uint64_t)cfg->elem_bytes;
     const uint64_t cells = (uint64_t)cfg->block_size * (cfg->hbm_layout == KV_HBM_BLOCK_FIRST ? 2ull * cfg->n_layers : 1ull);
     if (token_bytes >> 31 || cells >> 31 || cells * (uint64_t)cfg->n_hbm_blocks >= 0xFFFFFFFFull) return KV_EUNSUP;
@@ -169,7 +174,7 @@ int kv_decoder_create(kv_decoder **out, const kv_config *cfg, const kv_decoder_c
     const uint64_t slots = 2ull * d->max_groups;
     const uint64_t n_part = slots * d->units * d->part_vecs * sizeof(dkv::f32x4), n_ml = slots * (uint64_t)dc->n_heads * sizeof(dkv::f32x4),
                    n_lse = ((uint64_t)dc->max_seqs * (uint64_t)dc->n_heads * 4 + 255) / 256 * 256,
-                   n_gran = (uint64_t)dc->max_seqs * d->max_granules * (uint64_t)dc->n_heads * 4;
+                   n_gran = dc->weigh ? (uint64_t)dc->max_seqs * d->max_granules * (uint64_t)dc->n_heads * 4 : 0;
     uint8_t *mem = nullptr;
     if (hipMalloc((void **)&mem, n_part + n_ml + n_lse + n_gran) != hipSuccess) {
         (void)hipGetLastError();
@@ -203,6 +208,7 @@ int kv_put(kv_decoder *d, const kv_put_args *a, void *stream)
     if (a->table_stride < d->dc.max_blocks && a->n_seqs > 1) return KV_EINVAL;
     if (!rows_ok(a->k) || !rows_ok(a->v) || !rows_ok(a->q) || !rows_ok(a->q_out)) return KV_EINVAL;
     if ((a->q.data == nullptr) != (a->q_out.data == nullptr)) return KV_EINVAL;
+    if (a->q_out.data && !apart(a->q_out, a->n_rows, d->dc.n_heads)) return KV_EINVAL;
     int32_t pairs = 0;
     if (a->inv_freq) {
         if (a->rot_dim <= 0 || a->rot_dim > d->cfg.head_dim || a->n_axes < 1 || a->n_axes > 3) return KV_EINVAL;
@@ -291,6 +297,8 @@ int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
     if (!rows_ok(a->q) || !rows_ok(a->out)) return KV_EINVAL;
     if (a->n_seqs > 1 && (a->table_stride < d->dc.max_blocks || (a->mass_out && a->mass_stride < d->dc.max_blocks))) return KV_EINVAL;
     if (a->mass && !a->mass_out) return KV_EINVAL;
+    if (!apart(a->out, a->n_seqs, d->dc.n_heads)) return KV_EINVAL;
+    if (a->mass_out && !d->dc.weigh) return KV_EUNSUP;
     if (!rows_aligned(a->q) || !rows_aligned(a->out)) return KV_EUNSUP;
     if (a->n_seqs == 0) return KV_OK;
     OnDevice on(d->device);

@@ -133,6 +133,13 @@ struct AttendParams {
 
 constexpr uint32_t kTile = 32;
 constexpr uint32_t kNoCell = ~0u;
+constexpr float kLowest = -3.402823466e38f;  // a reference below every score, and finite: a score of -inf has weight 0 beside it
+
+// The row of the cache, in rows of one token, that row `row` of page `page` is; kNoCell for an id that is no page.
+__host__ __device__ __forceinline__ uint32_t cell_in(uint32_t page, uint32_t n_blocks, uint32_t cells_per_block, uint32_t row)
+{
+    return page < n_blocks ? page * cells_per_block + row : kNoCell;
+}
 
 __device__ __forceinline__ uint32_t seq_tokens(const int32_t *lens, uint32_t s, uint32_t most)
 {
@@ -299,7 +306,7 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
     };
     auto cell_of = [&](uint32_t tile, int h, uint32_t page) {
         const uint32_t token = tile * kTile + (uint32_t)h * 16u + n;
-        return page < p.n_blocks ? page * p.cells_per_block + (token - p.by_block.quotient(token) * p.block_size) : kNoCell;
+        return cell_in(page, p.n_blocks, p.cells_per_block, token - p.by_block.quotient(token) * p.block_size);
     };
     Part now = {s, t, 0u, 0u, 0u}, next = part_at(s, t, at);
     w32x4 qf[KJ];
@@ -337,7 +344,7 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
         f32x4 acc[ACC], sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < ACC; i++) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        float ref = -1e30f;  // finite, so that a score of -inf has weight 0 from the start
+        float ref = kLowest;
         float own = 0.f;     // this lane's part of the sum of weights as they are, before they are rounded
         const uint32_t stop = active ? now.first + now.here : 0u;
         // at least once: a wave without a tile here still asks for what comes next
@@ -512,7 +519,7 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
                 f32x4 x[8];
 #pragma unroll
                 for (uint32_t o = 0; o < 8; o++) {
-                    x[o] = o < p.subs ? ml[o * p.units_per_wg + u][n] : f32x4{-1e30f, 0.f, 0.f, 0.f};
+                    x[o] = o < p.subs ? ml[o * p.units_per_wg + u][n] : f32x4{kLowest, 0.f, 0.f, 0.f};
                     ref = fmaxf(ref, x[o].x);
                 }
                 sum[0] = own = 0.f;
@@ -592,7 +599,7 @@ struct Joined {
     f32x4 all[4];
     __device__ __forceinline__ void none()
     {
-        top = -1e30f;
+        top = kLowest;
         sum = own = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; i++) all[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -650,7 +657,7 @@ __device__ __forceinline__ void join(const AttendParams &p, uint32_t s, uint32_t
             for (uint32_t k = 0; k < 2; k++) {
                 const uint32_t i = base + c + at_once * k;
                 const uint64_t slot = (g0 + i) * 2u + (i == 0u ? 1u : 0u);
-                x[k] = f32x4{-1e30f, 0.f, 0.f, 0.f};
+                x[k] = f32x4{kLowest, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (uint32_t m = 0; m < 4; m++) o[k][m] = f32x4{0.f, 0.f, 0.f, 0.f};
                 if (i < n_parts && here) {
@@ -722,7 +729,7 @@ __device__ __forceinline__ void add_mass(const AttendParams &p, uint32_t s, uint
     } else {
         const uint32_t across = min(p.n_heads, 256u), parts = 256u / across, h0 = tid % across, from = tid / across;
         for (uint32_t h = h0; h - h0 < p.n_heads; h += across) {
-            float top = -1e30f, sum = 0.f;
+            float top = kLowest, sum = 0.f;
             if (h < p.n_heads && from < parts) {
 #pragma unroll 8
                 for (uint32_t g = g0 + from; g <= g1; g += parts) {
@@ -885,15 +892,15 @@ __global__ __launch_bounds__(512) void kv_put_kernel(const PutParams p)
                 turn[i] = float2{cs, sn};
             }
             page = token >= 0 && token < (int64_t)p.max_blocks * p.block_size;
-            uint64_t cell = 0;
+            uint32_t cell = kNoCell;
             if (page) {
                 const uint32_t entry = (uint32_t)token / p.block_size;
-                const uint32_t id = (uint32_t)p.table[(int64_t)s * p.table_stride + entry];
-                page = id < p.n_blocks;
-                cell = (uint64_t)id * p.cells_per_block + ((uint32_t)token - entry * p.block_size);
+                cell = cell_in((uint32_t)p.table[(int64_t)s * p.table_stride + entry], p.n_blocks, p.cells_per_block,
+                               (uint32_t)token - entry * p.block_size);
+                page = cell != kNoCell;
             }
-            kc = p.k + cell * p.token_bytes;
-            vc = p.v + cell * p.token_bytes;
+            kc = p.k + (uint64_t)cell * p.token_bytes;  // not looked at without a page
+            vc = p.v + (uint64_t)cell * p.token_bytes;
             __syncthreads();
         }
         if (i >= n_all || (i >= n_q && !page)) continue;
@@ -948,7 +955,7 @@ struct EvictParams {
 };
 
 // Weights as whole numbers of the same order: lightest first, NaN last, -0 as 0.
-__device__ __forceinline__ uint32_t weight_key(float x)
+__host__ __device__ __forceinline__ uint32_t weight_key(float x)
 {
     if (x != x) return ~0u;
     const uint32_t b = __builtin_bit_cast(uint32_t, x + 0.0f);

@@ -38,18 +38,22 @@ class Rope:
 class Decoder:
     """Owns one kv_decoder handle.  `cfg` and `cache_ptr` are the Engine's; the cache must
     outlive the decoder.  Calls have to be ordered one after the other (one stream, or
-    streams that the caller orders): steps that overlap in time take a decoder each."""
+    streams that the caller orders) and come from one host thread at a time: steps that overlap
+    in time take a decoder each.  weigh=False: without the memory that kv_attend's mass takes.
+    There are no gradients."""
 
     def __init__(self, cfg: B.kv_config, cache_ptr: int, n_heads: int, max_seqs: int, max_blocks: int,
-                 x_type: int = B.KV_BF16, kv_type: Optional[int] = None, k_scale: float = 1.0, v_scale: float = 1.0):
+                 x_type: int = B.KV_BF16, kv_type: Optional[int] = None, k_scale: float = 1.0, v_scale: float = 1.0,
+                 weigh: bool = True):
         self.cfg = cfg
         self._h = C.c_void_p()
-        dc = B.kv_decoder_config(n_heads, x_type, x_type if kv_type is None else kv_type, max_seqs, max_blocks, k_scale, v_scale)
+        dc = B.kv_decoder_config(n_heads, x_type, x_type if kv_type is None else kv_type, max_seqs, max_blocks,
+                                 k_scale, v_scale, int(weigh))
         rc = B.lib.kv_decoder_create(C.byref(self._h), C.byref(cfg), C.byref(dc), C.c_void_p(cache_ptr or None))
         if rc != B.KV_OK:
             self._h = C.c_void_p()
             raise B.KVError(rc, "kv_decoder_create")
-        self._spec = _T.spec(self._h.value, n_heads, int(cfg.n_kv_heads), int(cfg.head_dim), max_blocks, x_type,
+        self._spec = _T.spec(self._h.value, cache_ptr, n_heads, int(cfg.n_kv_heads), int(cfg.head_dim), max_blocks, x_type,
                              1.0 / math.sqrt(cfg.head_dim))
 
     def kv_put(self, layer: int, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, *,

@@ -4,6 +4,7 @@
   python -m paper_2601_20309_amd.experiments configs       # the headline, batch and long-context rotations, default path
   python -m paper_2601_20309_amd.experiments interference  # the interference workload: rotation beside a decode reader
   python -m paper_2601_20309_amd.experiments reader        # the decode reader alone (profiling target)
+  python -m paper_2601_20309_amd.experiments decode        # attention of decode steps, recorded, beside rotations, with eviction
   python -m paper_2601_20309_amd.experiments eager         # a preemption with and without eager block rotation
   python -m paper_2601_20309_amd.experiments layouts       # layer-first against block-first cache layout
   python -m paper_2601_20309_amd.experiments linksweep     # bandwidth against segment size, copies and kernels
@@ -32,6 +33,7 @@ import numpy as np
 import torch
 
 from . import binding as B
+from . import decode as D
 from . import workloads as W
 
 
@@ -779,6 +781,138 @@ def reader():
     eng.kv_destroy()
 
 
+def decode(name="llama3_8b", n_heads=32, n_run=32, n_rotate=8, rotate_tokens=2048, budget=64, steps=10, seed=0, longest=8192):
+    """Decode steps with real attention over the block table's blocks: per layer the new tokens' keys and
+    values go into their pages and one token of every running request attends over what it holds.  Eager,
+    recorded into a HIP graph, recorded beside rotations of other requests, and once more after the requests
+    have given up their lightest blocks (kv_evict, kv_table_drop) down to `budget` each."""
+    base = W.SHAPES[name]
+    shape = W.KVShape(base.n_layers, base.n_kv_heads, base.head_dim, base.block_size, base.n_hbm_blocks, base.n_host_slots)
+    cache = _cache(shape)
+    eng = B.Engine(B.make_config(shape), cache.data_ptr())
+    tab = B.Table(eng, n_run + 2 * n_rotate)
+    lens = W.lognormal_lengths(n_run, seed, hi=longest)
+    max_blocks = W.blocks_for_tokens(int(lens.max()) + 4 * steps + 8, shape.block_size)
+    dec = D.Decoder(eng.cfg, cache.data_ptr(), n_heads, max_seqs=n_run, max_blocks=max_blocks)
+    for r in range(n_run):
+        assert tab.kv_table_append(r, int(lens[r]))[0] == 0
+    # two groups of requests take turns in HBM
+    groups = [list(range(n_run, n_run + n_rotate)), list(range(n_run + n_rotate, n_run + 2 * n_rotate))]
+    for g, group in enumerate(groups):
+        for r in group:
+            assert tab.kv_table_append(r, rotate_tokens)[0] == 0
+        if g == 0:
+            assert tab.kv_table_rotate(group, []) == 0 and eng.kv_wait() == 0
+    L, H, dim, dev = shape.n_layers, shape.n_kv_heads, shape.head_dim, "cuda"
+    gen = torch.Generator(device=dev).manual_seed(seed)
+    qkv = torch.empty((L, n_run, n_heads + 2 * H, dim), dtype=torch.bfloat16, device=dev).normal_(generator=gen)
+    q = torch.empty((n_run, n_heads, dim), dtype=torch.bfloat16, device=dev)
+    out = torch.zeros((L, n_run, n_heads, dim), dtype=torch.bfloat16, device=dev)
+    table = torch.full((n_run, max_blocks), -1, dtype=torch.int32, device=dev)
+    length, count = (torch.zeros(n_run, dtype=torch.int32, device=dev) for _ in range(2))
+    position = torch.from_numpy(lens.astype(np.int32))[None].to(dev)      # of the next token; eviction does not change it
+    mass = torch.zeros((n_run, max_blocks), device=dev)
+    rope = D.Rope((500000.0 ** -(torch.arange(dim // 2, dtype=torch.float64) * 2 / dim)).float().to(dev))
+
+    def tables():
+        """The running requests' blocks and lengths as the block table has them."""
+        t, n = torch.full((n_run, max_blocks), -1, dtype=torch.int32), torch.zeros(n_run, dtype=torch.int32)
+        for r in range(n_run):
+            b = tab.kv_table_blocks(r)
+            t[r, :len(b["ids"])], n[r] = torch.tensor(b["ids"], dtype=torch.int32), b["len"]
+        table.copy_(t), length.copy_(n)
+
+    def one_more_token():
+        for r in range(n_run):
+            assert tab.kv_table_append(r, 1)[0] == 0
+        tables()
+        position.add_(1)
+
+    def step():
+        for layer in range(L):
+            x = qkv[layer]
+            assert dec.kv_put(layer, x[:, n_heads:n_heads + H], x[:, n_heads + H:], table, length, q=x[:, :n_heads], q_out=q,
+                              rope=rope, positions=position) == 0
+            assert dec.kv_attend(layer, q, table, length, out[layer], mass=mass) == 0
+
+    def timed(fn, before=None):
+        ms = []
+        for _ in range(steps):
+            one_more_token()
+            if before:
+                before()
+            torch.cuda.synchronize()
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            fn()
+            b.record()
+            b.synchronize()
+            ms.append(a.elapsed_time(b))
+        return statistics.median(ms)
+
+    one_more_token()
+    step()
+    want = out.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    out.zero_()
+    graph.replay()
+    assert torch.equal(out, want)                 # the same step, recorded
+    rows, link = [], {}
+    kv_bytes = lambda: int(length.sum()) * 2 * H * dim * 2 * L  # noqa: E731
+
+    def row(label, ms, extra=""):
+        rows.append(dict(label=label, ms=ms, gib=kv_bytes() / 2**30, tbs=kv_bytes() / ms / 1e9))
+        print(f"| {label} | {int(length.sum())} | {kv_bytes() / 2**30:.2f} | {ms:.3f} | {kv_bytes() / ms / 1e9:.2f} | {extra} |", flush=True)
+
+    print(f"\n{L} layers, {n_heads} query heads over {H} of {dim}, {n_run} requests of {int(lens.min())} to {int(lens.max())} tokens\n")
+    print("| step | tokens attended to | GiB of keys and values | ms | TB/s | rotation beside it |")
+    print("|---|---|---|---|---|---|")
+    row("eager", timed(step))
+    row("recorded", timed(graph.replay))
+    turn = [0]
+
+    def rotate():
+        # (a block is copied out only when its tokens are there: the step before has been waited for)
+        away, back = groups[1 - turn[0]], groups[turn[0]]
+        turn[0] = 1 - turn[0]
+        assert tab.kv_table_rotate(away, back) == 0
+
+    def beside():
+        rotate()
+        graph.replay()
+
+    def waited():
+        if link:
+            assert eng.kv_wait() == 0
+            st = eng.kv_last_stats()
+            link["gbs"] = (st["bytes_out"] + st["bytes_in"]) / max(st["ms_out"], st["ms_in"]) / 1e6
+            link["ms"] = max(st["ms_out"], st["ms_in"])
+        link["on"] = True
+
+    ms = timed(beside, waited)
+    waited()
+    row("recorded, beside a rotation", ms, f"{link['gbs']:.1f} GB/s for {link['ms']:.2f} ms")
+    # the lightest blocks leave; what stays is attended to as before
+    most = int(max_blocks)
+    ids, at = (torch.zeros((n_run, most), dtype=torch.int32, device=dev) for _ in range(2))
+    free = tab.kv_table_get_counts()["free_hbm_blocks"]
+    assert dec.kv_evict(table, length, mass, budget=budget, n_first=1, n_last=4, evicted_ids=ids, evicted_at=at, n_evicted=count) == 0
+    gone, places = count.tolist(), at.cpu().numpy()
+    for r in range(n_run):
+        assert tab.kv_table_drop(r, places[r, :gone[r]]) == 0
+    assert tab.kv_table_get_counts()["free_hbm_blocks"] == free + sum(gone)
+    kept_table, kept_length = table.clone(), length.clone()
+    tables()
+    assert torch.equal(kept_table, table) and torch.equal(kept_length, length)   # both have closed up alike
+    row(f"recorded, at most {budget} blocks each", timed(graph.replay), f"{sum(gone)} blocks given back")
+    finite = bool(torch.isfinite(out).all())
+    tab.kv_table_destroy()
+    eng.kv_destroy()
+    return dict(rows=rows, evicted=sum(gone), finite=finite, rotated=link)
+
+
 def eager():
     """What eager block rotation buys at a preemption (Section 4.3.2): 8 requests
     of 4096 tokens leave while 8 others come back, Llama-3-8B shape, with and
@@ -1011,7 +1145,7 @@ if __name__ == "__main__":
               exec_passes=int(sys.argv[4]) if len(sys.argv) > 4 else 1)
         sys.exit(0)
     {"ladder": ladder, "configs": configs, "interference": interference, "reader": reader,
-     "eager": eager, "layouts": layouts,
+     "decode": decode, "eager": eager, "layouts": layouts,
      "linksweep": linksweep, "serve": serve,
      "sizes": sizes, "ratio": ratio, "chunks": chunks, "layers": layers, "poolkinds": poolkinds, "splitcalls": splitcalls, "packalone": packalone,
      "packshapes": packshapes}[what]()

@@ -700,6 +700,54 @@ def test_attend_beside_rotation_and_eviction_through_the_table():
     tab.kv_table_destroy(), eng.kv_destroy()
 
 
+def test_decode_command_runs_on_a_small_cache():
+    """The command's own checks (recorded step equals eager, tables close up alike, blocks given back), then its rows."""
+    from paper_2601_20309_amd import experiments as X
+    got = X.decode("small8b", n_heads=32, n_run=6, n_rotate=2, rotate_tokens=160, budget=6, steps=3, longest=300)
+    assert got["finite"] and got["evicted"] > 0 and len(got["rows"]) == 4 and got["rotated"]["gbs"] > 0
+    assert got["rows"][3]["gib"] < got["rows"][0]["gib"]
+
+
+def test_q_is_its_own_output_and_broadcast_queries():
+    c = Case(4, 3, 128, lens=(700, 33, 0, 5), seed=31)
+    q = c.queries()
+    want, _, _ = c.check_attend(q)
+    mine = q.cuda()
+    assert c.dec.kv_attend(c.layer, mine, c.table.cuda(), c.lens.cuda(), mine) == 0
+    assert torch.equal(mine, want)
+    one = q[:1, :1].cuda().expand(4, 12, 128)            # one query for all requests and heads
+    same = one.contiguous()
+    a, b = torch.empty_like(same), torch.empty_like(same)
+    for x, o in ((one, a), (same, b)):
+        assert c.dec.kv_attend(c.layer, x, c.table.cuda(), c.lens.cuda(), o) == 0
+    assert torch.equal(a, b)
+    assert c.dec.kv_attend(c.layer, same, c.table.cuda(), c.lens.cuda(), a[:1].expand(4, 12, 128)) == B.KV_EINVAL
+
+
+def test_scores_near_the_lowest_float():
+    """All scores of a row far below zero: the softmax is that of their differences."""
+    c = Case(1, 1, 64, lens=(70,), seed=32, types=("bf16", "bf16"))
+    c.plane(0).fill_(-1.0)
+    q = torch.full((1, 1, 64), 3e36, dtype=torch.bfloat16)
+    out = torch.empty((1, 1, 64), dtype=torch.bfloat16, device="cuda")
+    assert c.dec.kv_attend(c.layer, q.cuda(), c.table.cuda(), c.lens.cuda(), out, scale=1.0) == 0
+    v = c.values(1)
+    mean = torch.stack([v[c.table[0, t // 16], t % 16, 0] for t in range(70)]).mean(0)
+    size = torch.stack([v[c.table[0, t // 16], t % 16, 0] for t in range(70)]).abs().mean(0)
+    assert ((out.cpu()[0, 0].double() - mean).abs() <= 2 ** -8 * (mean.abs() + 2 * size)).all()
+
+
+def test_without_memory_for_weights():
+    c = Case(2, 2, 64, lens=(50, 20), seed=33)
+    light = D.Decoder(c.cfg, c.cache.data_ptr(), 4, max_seqs=2, max_blocks=c.max_blocks, weigh=False)
+    q = c.queries()
+    want, _, _ = c.check_attend(q)
+    out, mass = torch.empty_like(want), torch.zeros((2, c.max_blocks), device="cuda")
+    assert light.kv_attend(c.layer, q.cuda(), c.table.cuda(), c.lens.cuda(), out, mass=mass) == B.KV_EUNSUP
+    assert light.kv_attend(c.layer, q.cuda(), c.table.cuda(), c.lens.cuda(), out) == 0
+    assert torch.equal(out, want)
+
+
 def test_two_decoders_on_two_streams():
     """Steps that overlap in time, each with its own decoder over one cache."""
     c = Case(4, 4, 128, lens=(5000, 300, 17), seed=30)
