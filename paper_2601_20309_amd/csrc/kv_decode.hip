@@ -19,8 +19,8 @@ struct kv_decoder {
     uint8_t *hbm = nullptr;
     uint32_t token_bytes = 0, cells_per_block = 0;
     uint64_t plane_bytes = 0;  // from K to V of a layer, and half the way to the next layer
-    // kv_attend: how the KV heads' units and their waves make up workgroups
-    uint32_t units = 0, head_tiles = 0, units_per_wg = 0, subs = 0, wgs_per_group = 0, max_groups = 0;
+    // kv_attend: units (up to 16 query heads of a KV head), and the most ranges that there is memory for
+    uint32_t units = 0, head_tiles = 0, max_groups = 0;
     uint32_t part_rows = 0, part_vecs = 0;
     uint32_t granule = 0, max_granules = 0;
     // one allocation, in this order
@@ -61,7 +61,26 @@ class OnDevice {
 };
 
 constexpr uint32_t kAttendWaves = 8;  // most waves of a workgroup
-constexpr uint32_t kJoinWgs = 1024;   // workgroups that join, over all requests
+constexpr uint32_t kFewRequests = 16;
+// Workgroups that join, over all requests.  us of the joins, with 512 / 1024 / 2048: 32 requests around 1024 tokens 7.0 /
+// 6.4 / 6.3, 128 around 500 9.2 / 8.1 / 9.2.
+constexpr uint32_t kJoinWgs = 1024;
+
+// How units and waves make up workgroups: up to `most` units each, evenly, and as many waves per unit as then fit.
+struct Workgroup {
+    uint32_t per_range, units, subs;  // workgroups of a range, units of one, waves of a unit
+    Workgroup(uint32_t all, uint32_t most)
+        : per_range((all + most - 1) / most), units((all + per_range - 1) / per_range), subs(1)
+    {
+        while (2 * subs * units <= kAttendWaves) subs *= 2;
+    }
+};
+
+// ranges: as many workgroups as the chip holds at once
+uint32_t ranges(const kv_decoder *d, const Workgroup &w)
+{
+    return std::max(1u, std::min(dkv::kMaxGroups, (uint32_t)d->n_cus / w.per_range));
+}
 
 bool rows_ok(const kv_rows &r) { return r.row >= 0 && r.head >= 0; }
 // 16-bit elements: rows begin on multiples of 16 bytes
@@ -152,10 +171,6 @@ int kv_decoder_create(kv_decoder **out, const kv_config *cfg, const kv_decoder_c
     const uint32_t group = (uint32_t)(dc->n_heads / cfg->n_kv_heads);
     d->head_tiles = (group + 15) / 16;
     d->units = (uint32_t)cfg->n_kv_heads * d->head_tiles;
-    d->wgs_per_group = (d->units + kAttendWaves - 1) / kAttendWaves;
-    d->units_per_wg = (d->units + d->wgs_per_group - 1) / d->wgs_per_group;
-    d->subs = 1;
-    while (2 * d->subs * d->units_per_wg <= kAttendWaves) d->subs *= 2;
     d->part_rows = std::min(group, 16u);
     d->part_vecs = (cfg->head_dim <= 64 ? 4u : cfg->head_dim <= 128 ? 8u : 16u) * 4u * d->part_rows;
     d->granule = cfg->block_size % 4 ? 1u : std::gcd((uint32_t)cfg->block_size, 16u);
@@ -169,8 +184,7 @@ int kv_decoder_create(kv_decoder **out, const kv_config *cfg, const kv_decoder_c
         return fail(KV_EHIP);
     // ranges: as many workgroups as the chip holds at once, no more than there can be turns
     const uint64_t most_tiles = (uint64_t)dc->max_seqs * (((uint64_t)dc->max_blocks * cfg->block_size + dkv::kTile - 1) / dkv::kTile);
-    d->max_groups = (uint32_t)std::min<uint64_t>(std::max(1u, std::min(dkv::kMaxGroups, (uint32_t)d->n_cus / d->wgs_per_group)),
-                                                 (most_tiles + d->subs - 1) / d->subs);
+    d->max_groups = (uint32_t)std::min<uint64_t>(ranges(d, Workgroup(d->units, kAttendWaves)), most_tiles);
     const uint64_t slots = 2ull * d->max_groups;
     const uint64_t n_part = slots * d->units * d->part_vecs * sizeof(dkv::f32x4), n_ml = slots * (uint64_t)dc->n_heads * sizeof(dkv::f32x4),
                    n_lse = ((uint64_t)dc->max_seqs * (uint64_t)dc->n_heads * 4 + 255) / 256 * 256,
@@ -333,11 +347,7 @@ int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
     p.block_size = (uint32_t)d->cfg.block_size;
     p.cells_per_block = d->cells_per_block;
     p.n_blocks = (uint32_t)d->cfg.n_hbm_blocks;
-    p.groups = d->max_groups;
-    p.wgs_per_group = d->wgs_per_group;
     p.units = d->units;
-    p.units_per_wg = d->units_per_wg;
-    p.subs = d->subs;
     p.group_heads = (uint32_t)(d->dc.n_heads / d->cfg.n_kv_heads);
     p.head_tiles = d->head_tiles;
     p.part_rows = d->part_rows;
@@ -351,11 +361,29 @@ int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
     p.max_granules = d->max_granules;
     p.qk_scale = (float)((double)a->scale * 1.4426950408889634074 * (double)d->dc.k_scale);
     p.v_scale = d->dc.v_scale;
-    // no more ranges than there can be turns in this call
     const uint32_t tiles = (p.max_tokens + dkv::kTile - 1) / dkv::kTile;
-    p.groups = (uint32_t)std::min<uint64_t>(p.groups, ((uint64_t)p.n_seqs * tiles + p.subs - 1) / p.subs);
-    p.by_request = tiles <= 2u * p.subs ? 1u : 0u;
-    if (p.by_request) p.groups = p.n_seqs;
+    // Up to 16 requests: four units and two waves each to a workgroup, so that ranges are longer and leave half as many
+    // parts.  More requests: eight and one, so that ranges meet fewer of their ends.  us, by eight / by four: 4 requests of
+    // 32768 tokens (64 query heads) 93.2 / 90.7, one of 8192 17.7 / 16.7; 32 around 1024 43.4 / 45.6.
+    Workgroup w(d->units, p.n_seqs <= kFewRequests ? kAttendWaves / 2 : kAttendWaves);
+    // Where no request can be longer than two steps of its waves, each is a range, and nothing is left to join: with
+    // fewer units, and so more waves for each, to a workgroup, as long as two workgroups per compute unit take all requests,
+    // and no second launch is needed for block weights anyway.  us, split and joined / a range each: 3 requests of up to
+    // 100 tokens 9.6 / 5.9; 32 of 192 15.2 / 10.6, of 512 21.1 / 15.7; 128 of 256 31.0 / 27.6; with weights 16 of up to
+    // 512 13.0 / 15.2.
+    for (uint32_t most = kAttendWaves; most > 0 && !p.by_request; most /= 2) {
+        const Workgroup x(d->units, most);
+        if (tiles > 2u * x.subs) continue;
+        if (most < kAttendWaves && (p.n_seqs * x.per_range > 2u * (uint32_t)d->n_cus || p.granules)) continue;
+        w = x;
+        p.by_request = 1u;
+    }
+    p.wgs_per_group = w.per_range;
+    p.units_per_wg = w.units;
+    p.subs = w.subs;
+    // no more ranges than there is memory for, and than there can be turns in this call
+    p.groups = p.by_request ? p.n_seqs
+                            : (uint32_t)std::min<uint64_t>(std::min(d->max_groups, ranges(d, w)), ((uint64_t)p.n_seqs * tiles + w.subs - 1) / w.subs);
     hipStream_t s = (hipStream_t)stream;
     const dim3 g(p.groups * p.wgs_per_group), b(64 * p.units_per_wg * p.subs);
     int dp;
