@@ -19,8 +19,8 @@ struct kv_decoder {
     uint8_t *hbm = nullptr;
     uint32_t token_bytes = 0, cells_per_block = 0;
     uint64_t plane_bytes = 0;  // from K to V of a layer, and half the way to the next layer
-    // kv_attend: units (up to 16 query heads of a KV head), and the most ranges that there is memory for
-    uint32_t units = 0, head_tiles = 0, max_groups = 0;
+    // kv_attend: most waves of a workgroup, units (up to 16 query heads of a KV head), and the most ranges that there is memory for
+    uint32_t waves = 0, units = 0, head_tiles = 0, max_groups = 0;
     uint32_t part_rows = 0, part_vecs = 0;
     uint32_t granule = 0, max_granules = 0;
     // one allocation, in this order
@@ -60,7 +60,6 @@ class OnDevice {
     bool ok_ = false, moved_ = false;
 };
 
-constexpr uint32_t kAttendWaves = 8;  // most waves of a workgroup
 constexpr uint32_t kFewRequests = 16;
 // Workgroups that join, over all requests.  us of the joins, with 512 / 1024 / 2048: 32 requests around 1024 tokens 7.0 /
 // 6.4 / 6.3, 128 around 500 9.2 / 8.1 / 9.2.
@@ -69,10 +68,10 @@ constexpr uint32_t kJoinWgs = 1024;
 // How units and waves make up workgroups: up to `most` units each, evenly, and as many waves per unit as then fit.
 struct Workgroup {
     uint32_t per_range, units, subs;  // workgroups of a range, units of one, waves of a unit
-    Workgroup(uint32_t all, uint32_t most)
+    Workgroup(uint32_t all, uint32_t most, uint32_t waves)
         : per_range((all + most - 1) / most), units((all + per_range - 1) / per_range), subs(1)
     {
-        while (2 * subs * units <= kAttendWaves) subs *= 2;
+        while (2 * subs * units <= waves) subs *= 2;
     }
 };
 
@@ -169,6 +168,7 @@ int kv_decoder_create(kv_decoder **out, const kv_config *cfg, const kv_decoder_c
     d->cells_per_block = (uint32_t)cells;
     d->plane_bytes = kv_seg_bytes(cfg) * (cfg->hbm_layout == KV_HBM_BLOCK_FIRST ? 1ull : (uint64_t)cfg->n_hbm_blocks);
     const uint32_t group = (uint32_t)(dc->n_heads / cfg->n_kv_heads);
+    d->waves = cfg->head_dim <= 64 ? dkv::Step<64>::WAVES : cfg->head_dim <= 128 ? dkv::Step<128>::WAVES : dkv::Step<256>::WAVES;
     d->head_tiles = (group + 15) / 16;
     d->units = (uint32_t)cfg->n_kv_heads * d->head_tiles;
     d->part_rows = std::min(group, 16u);
@@ -184,7 +184,7 @@ int kv_decoder_create(kv_decoder **out, const kv_config *cfg, const kv_decoder_c
         return fail(KV_EHIP);
     // ranges: as many workgroups as the chip holds at once, no more than there can be turns
     const uint64_t most_tiles = (uint64_t)dc->max_seqs * (((uint64_t)dc->max_blocks * cfg->block_size + dkv::kTile - 1) / dkv::kTile);
-    d->max_groups = (uint32_t)std::min<uint64_t>(ranges(d, Workgroup(d->units, kAttendWaves)), most_tiles);
+    d->max_groups = (uint32_t)std::min<uint64_t>(ranges(d, Workgroup(d->units, d->waves, d->waves)), most_tiles);
     const uint64_t slots = 2ull * d->max_groups;
     const uint64_t n_part = slots * d->units * d->part_vecs * sizeof(dkv::f32x4), n_ml = slots * (uint64_t)dc->n_heads * sizeof(dkv::f32x4),
                    n_lse = ((uint64_t)dc->max_seqs * (uint64_t)dc->n_heads * 4 + 255) / 256 * 256,
@@ -362,19 +362,19 @@ int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
     p.qk_scale = (float)((double)a->scale * 1.4426950408889634074 * (double)d->dc.k_scale);
     p.v_scale = d->dc.v_scale;
     const uint32_t tiles = (p.max_tokens + dkv::kTile - 1) / dkv::kTile;
-    // Up to 16 requests: four units and two waves each to a workgroup, so that ranges are longer and leave half as many
-    // parts.  More requests: eight and one, so that ranges meet fewer of their ends.  us, by eight / by four: 4 requests of
+    // Up to 16 requests: half as many units, and two waves each, to a workgroup, so that ranges are longer and leave half as many
+    // parts.  More requests: a wave each, so that ranges meet fewer of their ends.  us, by eight / by four: 4 requests of
     // 32768 tokens (64 query heads) 93.2 / 90.7, one of 8192 17.7 / 16.7; 32 around 1024 43.4 / 45.6.
-    Workgroup w(d->units, p.n_seqs <= kFewRequests ? kAttendWaves / 2 : kAttendWaves);
+    Workgroup w(d->units, p.n_seqs <= kFewRequests ? d->waves / 2 : d->waves, d->waves);
     // Where no request can be longer than two steps of its waves, each is a range, and nothing is left to join: with
     // fewer units, and so more waves for each, to a workgroup, as long as two workgroups per compute unit take all requests,
     // and no second launch is needed for block weights anyway.  us, split and joined / a range each: 3 requests of up to
     // 100 tokens 9.6 / 5.9; 32 of 192 15.2 / 10.6, of 512 21.1 / 15.7; 128 of 256 31.0 / 27.6; with weights 16 of up to
     // 512 13.0 / 15.2.
-    for (uint32_t most = kAttendWaves; most > 0 && !p.by_request; most /= 2) {
-        const Workgroup x(d->units, most);
+    for (uint32_t most = d->waves; most > 0 && !p.by_request; most /= 2) {
+        const Workgroup x(d->units, most, d->waves);
         if (tiles > 2u * x.subs) continue;
-        if (most < kAttendWaves && (p.n_seqs * x.per_range > 2u * (uint32_t)d->n_cus || p.granules)) continue;
+        if (most < d->waves && (p.n_seqs * x.per_range > 2u * (uint32_t)d->n_cus || p.granules)) continue;
         w = x;
         p.by_request = 1u;
     }

@@ -207,6 +207,8 @@ struct Step {
     static constexpr int VW = DP == 64 ? 4 : 8;     // dimensions of a row that a lane loads at once,
     static constexpr int NV = DP == 64 ? 1 : DP / 128;  // and how often
     static constexpr int ACC = VW * NV;
+    // Waves of a workgroup, one or two per SIMD: rows of 256 dimensions need more than half of its registers.
+    static constexpr uint32_t WAVES = DP == 256 ? 4 : 8;
 };
 
 template <int BYTES>
@@ -225,25 +227,23 @@ __device__ __forceinline__ void clear(uint32_t &v) { v = 0u; }
 // WHOLE: heads have exactly DP dimensions.  Otherwise lanes whose dimensions are not there read the row's
 // first ones, in vain.
 template <typename X, bool FP8, int DP, bool WHOLE>
-__global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
+__global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const AttendParams p)
 {
     using T = Step<DP>;
     constexpr int KJ = T::KJ, VW = T::VW, NV = T::NV, ACC = T::ACC;
+    constexpr uint32_t WAVES = T::WAVES;
     // Of a key a lane takes 8 dimensions for each step of 32: in 16 bits dimensions 32 j + 8 kq on, 64 bytes
     // of a row at once; in 8 bits, where rows are whole, those of its quarter of the row, 16 at once (q is
     // brought in the same order).
     constexpr bool RUNS = FP8 && WHOLE;
     constexpr int KL = RUNS ? KJ / 2 : KJ;
-    // Rows of 512 bytes: half a tile of keys, and half of the values' dimensions, are what registers hold at a
-    // time, and nothing is asked for ahead.
-    constexpr bool LATE = NV > 1 && !FP8;
     // Rows of 128 bytes and less in 8 bits leave room for two tiles of values: they are asked for ahead, too.
     constexpr bool AHEAD = FP8 && DP <= 128;
     typedef typename Raw<FP8 && !RUNS ? 8 : 16>::type kraw;
     auto k_dim = [](int j, uint32_t kq) { return RUNS ? kq * (DP / 4) + (uint32_t)j * 8u : (uint32_t)j * 32u + kq * 8u; };
     typedef typename Raw<(FP8 ? 1 : 2) * VW>::type vraw;
-    __shared__ f32x4 joined[8][ACC][64];
-    __shared__ f32x4 ml[8][16];
+    __shared__ f32x4 joined[WAVES][ACC][64];
+    __shared__ f32x4 ml[WAVES][16];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t n = lane & 15u, kq = lane >> 4;
     const uint32_t group = blockIdx.x / p.wgs_per_group;
@@ -269,13 +269,14 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
     }
     const uint8_t *const kb = p.k + (uint64_t)kv_head * p.head_bytes + (WHOLE ? k_dim(0, kq) * elem : 0u);
     const uint8_t *const vb = p.v + (uint64_t)kv_head * p.head_bytes + (WHOLE ? n * VW * elem : 0u);
-    auto k_off = [&](int l) {
+    // (Where rows are not whole, found anew for every row: kept, they are what does not fit the registers.)
+    auto k_off = [&](int l, uint32_t kq) {
         const uint32_t d = (uint32_t)l * 32u + kq * 8u;
-        return RUNS ? (uint32_t)l * 16u : WHOLE ? (uint32_t)l * 32u * elem : (d < p.dim ? d : 0u) * elem;
+        return RUNS ? (uint32_t)l * 16u : WHOLE ? (uint32_t)l * 32u * elem : min(d, p.dim - 8u) * elem;
     };
-    auto v_off = [&](int c) {
+    auto v_off = [&](int c, uint32_t n) {
         const uint32_t d = (uint32_t)c * 128u + n * VW;
-        return WHOLE ? (uint32_t)c * 128u * elem : (d < p.dim ? d : 0u) * elem;
+        return WHOLE ? (uint32_t)c * 128u * elem : min(d, p.dim - VW) * elem;
     };
 
     // What a step needs is asked for a step (its pages two steps) ahead, across the ends of requests,
@@ -310,11 +311,13 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
     };
     Part now = {s, t, 0u, 0u, 0u}, next = part_at(s, t, at);
     w32x4 qf[KJ];
-    kraw kr[LATE ? 1 : 2][KL];
+    kraw kr[2][KL];
     auto load_keys = [&](kraw(&to)[KL], uint32_t cell) {
         const uint64_t off = (uint64_t)(cell == kNoCell ? 0u : cell) * p.token_bytes;
+        uint32_t k = kq;
+        if constexpr (!WHOLE) asm volatile("" : "+v"(k));
 #pragma unroll
-        for (int l = 0; l < KL; l++) to[l] = *reinterpret_cast<const kraw *>(kb + off + k_off(l));
+        for (int l = 0; l < KL; l++) to[l] = *reinterpret_cast<const kraw *>(kb + off + k_off(l, k));
     };
     uint32_t cell[2], page[2];
     // The lane's 8 tokens of the step whose cells are `cell`, and their values.
@@ -328,13 +331,14 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
             vcell[r] = c == kNoCell ? 0u : c;
         }
     };
-    auto load_values = [&](vraw(&to)[8][LATE ? 1 : NV], int c) {
+    auto load_values = [&](vraw(&to)[8][NV], int c) {
+        uint32_t v = n;
+        if constexpr (!WHOLE) asm volatile("" : "+v"(v));
 #pragma unroll
         for (int r = 0; r < 8; r++)
-            to[r][LATE ? 0 : c] = __builtin_nontemporal_load(
-                reinterpret_cast<const vraw *>(vb + (uint64_t)vcell[r] * p.token_bytes + v_off(c)));
+            to[r][c] = __builtin_nontemporal_load(reinterpret_cast<const vraw *>(vb + (uint64_t)vcell[r] * p.token_bytes + v_off(c, v)));
     };
-    vraw next_vr[8][LATE ? 1 : NV];
+    vraw next_vr[8][NV];
     uint32_t next_present = 0;
     for (;;) {
         uint32_t next_page[2];
@@ -351,7 +355,7 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
         uint32_t tt = now.first + sub;
         do {
             const bool have = tt < stop, last = tt + p.subs >= stop;
-            vraw vr[8][LATE ? 1 : NV];
+            vraw vr[8][NV];
             uint32_t present = 0;  // bit r: token r of the lane's 8 is there
             f32x4 sc[2];
             if (have) {
@@ -365,13 +369,12 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
                 } else {
                     find_values(present);
 #pragma unroll
-                    for (int c = 0; c < (LATE ? 1 : NV); c++) load_values(vr, c);
+                    for (int c = 0; c < NV; c++) load_values(vr, c);
                 }
                 // scores: token x head
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
-                    kraw(&key)[KL] = kr[LATE ? 0 : h];
-                    if constexpr (LATE) load_keys(key, cell[h]);
+                    kraw(&key)[KL] = kr[h];
                     if constexpr (!WHOLE) {
                         // dimensions that are not there meet zeros of q: they must not be NaN
 #pragma unroll
@@ -409,10 +412,8 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
                             qf[j] = *reinterpret_cast<const w32x4 *>(p.q + (uint64_t)part.s * p.q_row + (uint64_t)head * p.q_head + d * 2u);
                     }
                 }
-                if constexpr (!LATE) {
 #pragma unroll
-                    for (int h = 0; h < 2; h++) load_keys(kr[h], cell[h]);
-                }
+                for (int h = 0; h < 2; h++) load_keys(kr[h], cell[h]);
                 if constexpr (AHEAD) {
                     find_values(next_present);
 #pragma unroll
@@ -453,15 +454,14 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
             sum = X::mma(w32x4{X::kOnes, X::kOnes, X::kOnes, X::kOnes}, pw, sum);
 #pragma unroll
             for (int c = 0; c < NV; c++) {
-                if (LATE && c > 0) load_values(vr, c);
                 if (gaps) {  // a weight of 0 does not make up for NaN
 #pragma unroll
                     for (int r = 0; r < 8; r++)
-                        if (!(present >> r & 1u)) clear(vr[r][LATE ? 0 : c]);
+                        if (!(present >> r & 1u)) clear(vr[r][c]);
                 }
                 // of token r: dimensions 2i and 2i + 1
                 auto pair = [&](int r, int i) {
-                    const vraw &v = vr[r][LATE ? 0 : c];
+                    const vraw &v = vr[r][c];
                     if constexpr (FP8 && VW == 8) return i & 1 ? X::template from_fp8<true>(v[i / 2]) : X::template from_fp8<false>(v[i / 2]);
                     else if constexpr (FP8) return i & 1 ? X::template from_fp8<true>(v) : X::template from_fp8<false>(v);
                     else return v[i];
@@ -509,22 +509,22 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
             f32x4 *const part = p.part + ((uint64_t)slot * p.units + unit) * p.part_vecs;
             uint8_t *const out = p.out + (uint64_t)now.s * p.out_row;
             // Waves that took turns at the tiles leave what they have in LDS, and share the sums out among them.
-            float scale[8];  // of each one's: 2^(its reference - the largest)
+            float scale[WAVES];  // of each one's: 2^(its reference - the largest)
             if (p.subs > 1u) {
                 const uint32_t u = wave % p.units_per_wg;
                 if (kq == 0u) ml[wave][n] = f32x4{ref, sum[0], own, 0.f};
 #pragma unroll
                 for (int i = 0; i < ACC; i++) joined[wave][i][lane] = acc[i];
                 __syncthreads();
-                f32x4 x[8];
+                f32x4 x[WAVES];
 #pragma unroll
-                for (uint32_t o = 0; o < 8; o++) {
+                for (uint32_t o = 0; o < WAVES; o++) {
                     x[o] = o < p.subs ? ml[o * p.units_per_wg + u][n] : f32x4{kLowest, 0.f, 0.f, 0.f};
                     ref = fmaxf(ref, x[o].x);
                 }
                 sum[0] = own = 0.f;
 #pragma unroll
-                for (uint32_t o = 0; o < 8; o++) {
+                for (uint32_t o = 0; o < WAVES; o++) {
                     scale[o] = __builtin_amdgcn_exp2f(x[o].x - ref);
                     sum[0] += x[o].y * scale[o];
                     own += x[o].z * scale[o];
@@ -562,7 +562,7 @@ __global__ __launch_bounds__(512) void kv_attend_kernel(const AttendParams p)
                 for (uint32_t i0 = sub * 2u; i0 < ACC; i0 += p.subs * 2u) {
                     f32x4 a[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-                    for (uint32_t o = 0; o < 8; o++) {
+                    for (uint32_t o = 0; o < WAVES; o++) {
                         if (o >= p.subs) break;
                         a[0] += joined[o * p.units_per_wg + u][i0][lane] * scale[o];
                         a[1] += joined[o * p.units_per_wg + u][i0 + 1u][lane] * scale[o];
