@@ -479,9 +479,10 @@ int kv_sched_lvf(const kv_sched_params *params, const kv_sched_req *reqs, int32_
  * tokens lie in: token t of request s in row t % block_size of block
  * table[s][t / block_size].  An id outside [0, n_hbm_blocks) is no page: such
  * a block is skipped, neither read nor written (kv_table_blocks() gives -1 for
- * a block that is in DRAM).  lens[s] below 0 counts as 0, above max_blocks *
- * block_size as that.  Rows of a page behind a request's last token may hold
- * anything, NaN too.
+ * a block that is in DRAM).  Several entries may name one page: it is read as
+ * often.  lens[s] below 0 counts as 0, above max_blocks * block_size as that
+ * (kv_put leaves out the tokens that lie there).  Rows of a page behind a
+ * request's last token may hold anything, NaN too.
  *
  * Calls through one decoder have to be ordered one after the other (the same
  * stream, or streams the caller orders), replays of recorded ones included:
@@ -514,7 +515,8 @@ typedef struct {
  * elem_bytes, scales that are not finite and above 0.  KV_EUNSUP: head_dim above
  * 256 or no multiple of 8, more than 1024 query heads, a cache that is not
  * aligned to 16 bytes or of 2^32 and more token rows per KV plane, more than 65535
- * requests, 2^31 and more tokens in a table row or tiles of 32 tokens in all.  KV_ENOMEM, KV_EHIP.
+ * requests, 2^31 and more tokens in a table row, tiles of 32 tokens in all or, with
+ * `weigh`, tokens of a block times query heads.  KV_ENOMEM, KV_EHIP.
  */
 int kv_decoder_create(kv_decoder **decoder, const kv_config *cfg, const kv_decoder_config *dc, void *hbm_cache);
 
@@ -523,7 +525,9 @@ int kv_decoder_destroy(kv_decoder *decoder);
 
 /*
  * Strides are in elements; the last dimension is contiguous.  Rows of q, k, v and
- * the outputs have to begin on multiples of 16 bytes (KV_EUNSUP otherwise).
+ * the outputs have to begin on multiples of 16 bytes (KV_EUNSUP otherwise).  Strides of
+ * what is read may be 0; what is written lies token by token or head by head, no row
+ * in another's memory (KV_EINVAL otherwise).
  */
 typedef struct {
     const void *data;
@@ -549,7 +553,7 @@ typedef struct {
     int32_t n_axes;        /* 1 to 3 */
     int32_t sections[3];   /* pairs of each axis, one axis after the other: sum rot_dim / 2 */
     const int32_t *positions; /* [n_axes][position_stride]: of each row; NULL (1 axis): its place in the request */
-    int64_t position_stride;
+    int64_t position_stride;  /* n_rows and more, or 0: all axes have the first one's */
 } kv_put_args;
 
 /*
@@ -561,7 +565,7 @@ typedef struct {
  * max_blocks, are left out of the cache (their q is rotated all the same).  Two tokens
  * that name one row of one page leave either's values there.
  * KV_EINVAL: NULL or negative, a layer, axis or section that does not fit.  KV_E2BIG:
- * more requests than the decoder's.
+ * more requests than the decoder's.  KV_EUNSUP: 2^24 rows and more.
  */
 int kv_put(kv_decoder *decoder, const kv_put_args *args, void *stream);
 

@@ -4,12 +4,15 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/core/grad_mode.h>
 #include <c10/hip/HIPStream.h>
 #include <hip/hip_runtime_api.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cstring>
 #include <exception>
+#include <new>
 
 #include "../../include/duplexkv.h"
 
@@ -38,7 +41,8 @@ struct Call {
             return nullptr;
         }
         const at::Tensor *t = &THPVariable_Unpack(o);
-        if (!t->defined() || !t->is_cuda() || t->layout() != at::kStrided || t->device().index() != device) {
+        if (!t->defined() || !t->is_cuda() || t->layout() != at::kStrided || t->device().index() != device || t->is_neg() ||
+            (t->requires_grad() && at::GradMode::is_enabled())) {
             ok = false;
             return nullptr;
         }
@@ -187,10 +191,9 @@ PyObject *put(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         if ((a[6] == Py_None) != (a[7] == Py_None) || a[3] == Py_None) return KV_EINVAL;
         p.starts = c.plain<int32_t>(a[8], at::kInt, n + 1);
         if (a[9] != Py_None) {
-            const at::Tensor *f = c.tensor(a[9]);
-            if (!f) return KV_EINVAL;
-            p.inv_freq = (const float *)f->data_ptr();
-            p.rot_dim = (int32_t)(2 * f->numel());
+            const int64_t pairs = c.length(a[9], 1);
+            p.inv_freq = c.plain<float>(a[9], at::kFloat, pairs);
+            p.rot_dim = (int32_t)std::min<int64_t>(2 * pairs, INT32_MAX);
             p.interleaved = PyObject_IsTrue(a[10]);
             p.n_axes = (int32_t)PyTuple_Size(a[11]);
             for (int32_t i = 0; i < p.n_axes && i < 3; i++) p.sections[i] = (int32_t)PyLong_AsLong(PyTuple_GetItem(a[11], i));
@@ -204,8 +207,9 @@ PyObject *put(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         } else if (a[12] != Py_None) {
             return KV_EINVAL;
         }
-        if (!c.ok) return KV_EINVAL;
-        return kv_put(d->decoder, &p, c.stream(a[13]));
+        void *const stream = c.stream(a[13]);
+        if (!c.ok || PyErr_Occurred()) return KV_EINVAL;
+        return kv_put(d->decoder, &p, stream);
     });
 }
 
@@ -231,8 +235,9 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         p.mass = c.plain<float>(a[8], at::kFloat, n, d->max_blocks);
         p.mass_out = a[9] == Py_None ? const_cast<float *>(p.mass) : c.plain<float>(a[9], at::kFloat, n, d->max_blocks);
         p.mass_stride = d->max_blocks;
-        if (!c.ok || a[2] == Py_None || a[5] == Py_None) return KV_EINVAL;
-        return kv_attend(d->decoder, &p, c.stream(a[10]));
+        void *const stream = c.stream(a[10]);
+        if (!c.ok || a[2] == Py_None || a[5] == Py_None || PyErr_Occurred()) return KV_EINVAL;
+        return kv_attend(d->decoder, &p, stream);
     });
 }
 
@@ -267,8 +272,9 @@ PyObject *evict(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         p.mass_stride = d->max_blocks;
         for (int i : {1, 3, 8, 9})
             if (a[i] == Py_None) return KV_EINVAL;
-        if (!c.ok) return KV_EINVAL;
-        return kv_evict(d->decoder, &p, c.stream(a[13]));
+        void *const stream = c.stream(a[13]);
+        if (!c.ok || PyErr_Occurred()) return KV_EINVAL;
+        return kv_evict(d->decoder, &p, stream);
     });
 }
 

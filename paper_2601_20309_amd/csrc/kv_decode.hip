@@ -61,6 +61,7 @@ class OnDevice {
 };
 
 constexpr uint32_t kFewRequests = 16;
+constexpr int32_t kMostRows = 0xFFFFFF;  // of a kv_put: as many workgroups of 256 lanes as a launch can count lanes
 // Workgroups that join, over all requests.  us of the joins, with 512 / 1024 / 2048: 32 requests around 1024 tokens 7.0 /
 // 6.4 / 6.3, 128 around 500 9.2 / 8.1 / 9.2.
 constexpr uint32_t kJoinWgs = 1024;
@@ -85,8 +86,15 @@ bool rows_ok(const kv_rows &r) { return r.row >= 0 && r.head >= 0; }
 // 16-bit elements: rows begin on multiples of 16 bytes
 bool rows_aligned(const kv_rows &r) { return (uintptr_t)r.data % 16 == 0 && r.row % 8 == 0 && r.head % 8 == 0; }
 
-// rows that are written must not be one and the same
-bool apart(const kv_rows &r, int32_t n, int32_t heads) { return (n < 2 || r.row > 0) && (heads < 2 || r.head > 0); }
+// rows that are written lie apart, token by token or head by head
+bool apart(const kv_rows &r, int32_t n, int32_t heads, int32_t dim)
+{
+    const auto spans = [](int64_t outer, int64_t inner, int32_t n_outer, int32_t n_inner, int32_t dim) {
+        const __int128 span = (__int128)inner * (n_inner - 1) + dim;
+        return (n_inner < 2 || inner >= dim) && (n_outer < 2 || outer >= span);
+    };
+    return n <= 0 || spans(r.row, r.head, n, heads, dim) || spans(r.head, r.row, heads, n, dim);
+}
 
 uint8_t *plane(const kv_decoder *d, int32_t layer, int which)
 {
@@ -141,6 +149,8 @@ int kv_decoder_create(kv_decoder **out, const kv_config *cfg, const kv_decoder_c
     if (tokens > 0x7FFFFFC0 || dc->max_seqs > 65535 || (tokens / dkv::kTile + 1) * dc->max_seqs > 0x7FFFFFFF) return KV_EUNSUP;
     const uint64_t token_bytes = (uint64_t)cfg->n_kv_heads * (uint64_t)cfg->head_dim * (uint64_t)cfg->elem_bytes;
     const uint64_t cells = (uint64_t)cfg->block_size * (cfg->hbm_layout == KV_HBM_BLOCK_FIRST ? 2ull * cfg->n_layers : 1ull);
+    // granules of a block, over all query heads, are counted in 31 bits
+    if (dc->weigh && (uint64_t)cfg->block_size * (uint64_t)dc->n_heads > 0x7FFFFFFFull) return KV_EUNSUP;
     if (token_bytes >> 31 || cells >> 31 || cells * (uint64_t)cfg->n_hbm_blocks >= 0xFFFFFFFFull) return KV_EUNSUP;
     int ndev = 0;
     if (hipGetDeviceCount(&ndev) != hipSuccess || ndev <= 0) {
@@ -222,7 +232,6 @@ int kv_put(kv_decoder *d, const kv_put_args *a, void *stream)
     if (a->table_stride < d->dc.max_blocks && a->n_seqs > 1) return KV_EINVAL;
     if (!rows_ok(a->k) || !rows_ok(a->v) || !rows_ok(a->q) || !rows_ok(a->q_out)) return KV_EINVAL;
     if ((a->q.data == nullptr) != (a->q_out.data == nullptr)) return KV_EINVAL;
-    if (a->q_out.data && !apart(a->q_out, a->n_rows, d->dc.n_heads)) return KV_EINVAL;
     int32_t pairs = 0;
     if (a->inv_freq) {
         if (a->rot_dim <= 0 || a->rot_dim > d->cfg.head_dim || a->n_axes < 1 || a->n_axes > 3) return KV_EINVAL;
@@ -232,10 +241,12 @@ int kv_put(kv_decoder *d, const kv_put_args *a, void *stream)
             pairs += a->sections[i];
         }
         if (2 * pairs != a->rot_dim) return KV_EINVAL;
-        if (a->positions && a->n_axes > 1 && a->position_stride < a->n_rows) return KV_EINVAL;
+        if (a->positions && a->n_axes > 1 && a->position_stride != 0 && a->position_stride < a->n_rows) return KV_EINVAL;
         if (a->rot_dim % 8 != 0) return KV_EUNSUP;
     }
     if (!rows_aligned(a->k) || !rows_aligned(a->v) || !rows_aligned(a->q) || !rows_aligned(a->q_out)) return KV_EUNSUP;
+    if (a->q_out.data && !apart(a->q_out, a->n_rows, d->dc.n_heads, d->cfg.head_dim)) return KV_EINVAL;
+    if (a->n_rows > kMostRows) return KV_EUNSUP;
     if (!rows_here) return KV_OK;
     OnDevice on(d->device);
     if (!on.ok()) return KV_EHIP;
@@ -311,9 +322,9 @@ int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
     if (!rows_ok(a->q) || !rows_ok(a->out)) return KV_EINVAL;
     if (a->n_seqs > 1 && (a->table_stride < d->dc.max_blocks || (a->mass_out && a->mass_stride < d->dc.max_blocks))) return KV_EINVAL;
     if (a->mass && !a->mass_out) return KV_EINVAL;
-    if (!apart(a->out, a->n_seqs, d->dc.n_heads)) return KV_EINVAL;
     if (a->mass_out && !d->dc.weigh) return KV_EUNSUP;
     if (!rows_aligned(a->q) || !rows_aligned(a->out)) return KV_EUNSUP;
+    if (!apart(a->out, a->n_seqs, d->dc.n_heads, d->cfg.head_dim)) return KV_EINVAL;
     if (a->n_seqs == 0) return KV_OK;
     OnDevice on(d->device);
     if (!on.ok()) return KV_EHIP;

@@ -4,7 +4,8 @@ eviction of the blocks that attention has weighed least.
 
 Same names, rules and result codes as include/duplexkv.h.  Nothing is copied, cast
 or laid out anew on the way: a tensor of another type, shape or device than the call
-takes, or whose last dimension is not contiguous, is refused with KV_EINVAL.  A call
+takes, or whose last dimension is not contiguous, is refused with KV_EINVAL; so is one
+that asks for a gradient, outside torch.no_grad(): there are none.  A call
 goes to the current stream of the cache's device, unless it is given another
 (an integer handle); as with any torch operator, tensors that are used on another stream
 than their own must not be freed before that stream is done with them.
@@ -39,8 +40,7 @@ class Decoder:
     """Owns one kv_decoder handle.  `cfg` and `cache_ptr` are the Engine's; the cache must
     outlive the decoder.  Calls have to be ordered one after the other (one stream, or
     streams that the caller orders) and come from one host thread at a time: steps that overlap
-    in time take a decoder each.  weigh=False: without the memory that kv_attend's mass takes.
-    There are no gradients."""
+    in time take a decoder each.  weigh=False: without the memory that kv_attend's mass takes."""
 
     def __init__(self, cfg: B.kv_config, cache_ptr: int, n_heads: int, max_seqs: int, max_blocks: int,
                  x_type: int = B.KV_BF16, kv_type: Optional[int] = None, k_scale: float = 1.0, v_scale: float = 1.0,
@@ -61,7 +61,7 @@ class Decoder:
                starts: Optional[torch.Tensor] = None, rope: Optional[Rope] = None,
                positions: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> int:
         """k, v [row, kv_head, dim] (and q, q_out [row, head, dim]): the last starts[s + 1] - starts[s] tokens
-        of each request s, or the last one of each.  positions: int32 [axis, row]."""
+        of each request s, or the last one of each.  positions: int32 [axis, row] (expanded along the axes: the same for each)."""
         if rope is None:
             return _T.put(self._spec, layer, k, v, table, lens, q, q_out, starts, None, False, (), positions, stream)
         return _T.put(self._spec, layer, k, v, table, lens, q, q_out, starts, rope.inv_freq, rope.interleaved, rope.sections,

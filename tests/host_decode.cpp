@@ -145,6 +145,7 @@ void creation()
     CHECK(of(shape(1, 1, 64, 16, 2, 4), 1025) == KV_EUNSUP && of(shape(1, 1, 64, 16, 2, 4), 1024) == KV_OK, "query heads");
     CHECK(of(shape(1, 1, 8, 16, 2, 0x10000000)) == KV_EUNSUP && of(shape(1, 1, 8, 16, 2, 0xFFFFFFF)) == KV_OK, "rows");
     CHECK(of(shape(0, 1, 8, 16, 2, 4)) == KV_EINVAL, "layers");
+    CHECK(of(shape(1, 1, 8, 0x200000, 2, 4), 1024) == KV_EUNSUP && of(shape(1, 1, 8, 0x100000, 2, 4), 1024) == KV_OK, "granules of a block");
     CHECK(create(&d, sh, ok, (void *)0x100008) == KV_EUNSUP, "alignment");
     device_memory = false;
     CHECK(create(&d, sh, ok) == KV_EINVAL && d == nullptr, "host memory");
@@ -214,6 +215,14 @@ void refusals()
     EINVALS(put, a.n_axes = 4);
     EINVALS(put, a.n_axes = 2; a.sections[0] = a.sections[1] = 16);                                     // two axes want positions
     EINVALS(put, a.n_axes = 2; a.sections[0] = a.sections[1] = 16; a.positions = (int32_t *)16; a.position_stride = 2);
+    EINVALS(put, a.n_axes = 2; a.sections[0] = a.sections[1] = 16; a.positions = (int32_t *)16; a.position_stride = -3);
+    // rows that are written into one another: neither token by token nor head by head
+    EINVALS(put, a.q_out.row = 248);
+    EINVALS(put, a.q_out.head = 56);
+    EINVALS(attend, a.out.row = 128);
+    EINVALS(attend, a.out = rows(64, 184));
+    EINVALS(attend, a.out = rows(0x4000000000000000, 56));
+    EUNSUPS(put, a.n_rows = 0x1000000; a.starts = (int32_t *)16);
     EUNSUPS(put, a.rot_dim = 12; a.sections[0] = 6);
     EUNSUPS(put, a.k.data = (void *)0x2004);
     EUNSUPS(put, a.v.row = 132);
@@ -230,6 +239,12 @@ void refusals()
     EINVALS(evict, a.n_evicted = nullptr);
     EINVALS(evict, a.evicted_at = nullptr);
     CHECK(launches.empty(), "something refused was launched");
+    CHECK(attend([](auto &a) { a.out = rows(64, 192); }) == KV_OK && put([](auto &a) { a.q_out = rows(64, 192); }) == KV_OK, "head by head");
+    CHECK(attend([](auto &a) { a.n_seqs = 1; a.out = rows(0, 64); }) == KV_OK, "one row");
+    CHECK(attend([](auto &a) { a.q = rows(0, 0); }) == KV_OK && put([](auto &a) { a.k = a.v = a.q = rows(0, 0); }) == KV_OK, "read several times");
+    CHECK(put([](auto &a) { a.n_axes = 2; a.sections[0] = a.sections[1] = 16; a.positions = (int32_t *)16; }) == KV_OK, "one axis' positions");
+    CHECK(put([](auto &a) { a.n_rows = 0xFFFFFF; a.starts = (int32_t *)16; }) == KV_OK && launches.back().b.x <= 256, "rows");
+    launches.clear();
     // nothing to do is done without a launch, whatever the pointers
     CHECK(attend([](auto &a) { a.n_seqs = 0; a.table = nullptr; }) == KV_OK && evict([](auto &a) { a.n_seqs = 0; a.mass = nullptr; }) == KV_OK, "none");
     CHECK(put([](auto &a) { a.n_rows = 0; a.starts = (int32_t *)16; a.k.data = nullptr; }) == KV_OK && launches.empty(), "none");

@@ -536,6 +536,36 @@ def test_refusals_change_nothing():
     assert torch.equal(c.cache, before) and (out == 3.0).all() and torch.equal(t.cpu(), c.table) and torch.equal(n.cpu(), c.lens)
 
 
+def test_calls_that_raise_do_nothing():
+    """What is no tensor, number or stream at all raises, before anything is launched."""
+    c = Case(2, 2, 64, lens=(40, 20), seed=40)
+    q, t, n = c.queries().cuda(), c.table.cuda(), c.lens.cuda()
+    out, k, before = torch.full_like(q, 3.0), torch.ones((2, 2, 64), dtype=c.x, device="cuda"), c.cache.clone()
+    mass = torch.zeros((2, c.max_blocks), device="cuda")
+    ids, count = torch.full((2, 3), 9, dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    ev = dict(budget=1, n_first=0, n_last=1, evicted_ids=ids, evicted_at=ids.clone(), n_evicted=count)
+    for stream in (torch.cuda.current_stream(), "0"):
+        for call in (lambda s: c.dec.kv_attend(1, q, t, n, out, stream=s), lambda s: c.dec.kv_put(1, k, k, t, n, stream=s),
+                     lambda s: c.dec.kv_evict(t, n, mass, stream=s, **ev)):
+            with pytest.raises(TypeError):
+                call(stream)
+    with pytest.raises(TypeError):
+        c.dec.kv_attend(1, q, t, n, out, scale="1")
+    with pytest.raises(TypeError):
+        c.dec.kv_attend(1.0, q, t, n, out)
+    gone = D.Decoder(c.cfg, c.cache.data_ptr(), 4, max_seqs=2, max_blocks=c.max_blocks)
+    assert gone.kv_decoder_destroy() == 0 and gone.kv_decoder_destroy() == 0
+    with pytest.raises(ValueError):
+        gone.kv_attend(1, q, t, n, out)
+    # a gradient is asked for, and there is none
+    asks = q.clone().requires_grad_()
+    assert c.dec.kv_attend(1, asks, t, n, out) == B.KV_EINVAL
+    torch.cuda.synchronize()
+    assert (out == 3.0).all() and torch.equal(c.cache, before) and (ids == 9).all() and torch.equal(t.cpu(), c.table)
+    with torch.no_grad():
+        assert c.dec.kv_attend(1, asks, t, n, out) == 0
+
+
 def test_decoders_that_cannot_be():
     def rc_of(shape, n_heads=4, ptr=None, elem=2, **kw):
         cache = torch.empty(2 * shape.n_layers * shape.n_hbm_blocks * shape.block_size * shape.n_kv_heads * shape.head_dim + 8,
@@ -706,6 +736,77 @@ def test_decode_command_runs_on_a_small_cache():
     got = X.decode("small8b", n_heads=32, n_run=6, n_rotate=2, rotate_tokens=160, budget=6, steps=3, longest=300)
     assert got["finite"] and got["evicted"] > 0 and len(got["rows"]) == 4 and got["rotated"]["gbs"] > 0
     assert got["rows"][3]["gib"] < got["rows"][0]["gib"]
+
+
+def test_pages_that_several_entries_name():
+    """A prefix that requests share, and one page twice in a row of the table: read as often as it is named."""
+    c = Case(2, 4, 128, lens=(90, 75, 64), seed=41)
+    table = c.table.clone()
+    table[1, :3] = table[0, :3]
+    table[2, 1] = table[2, 3] = table[2, 0]
+    c.check_attend(c.queries(), table=table)
+
+
+def test_put_of_broadcast_rows_and_positions():
+    """One row of k, v and q for all tokens, and the same positions along every axis."""
+    c = Case(2, 2, 64, lens=(20, 33, 5), seed=42)
+    other = Case(2, 2, 64, lens=(20, 33, 5), seed=42)
+    rope = rope_of(64, (16, 8, 8))
+    one = [torch.randn((1, h, 64), generator=c.g).to(c.x).cuda() for h in (2, 2, 4)]
+    k, v, q = (x.expand(3, -1, -1) for x in one)
+    pos = torch.tensor([[7, 70000, 3]], dtype=torch.int32, device="cuda")
+    outs = [torch.empty((3, 4, 64), dtype=c.x, device="cuda") for _ in range(2)]
+    t, n = c.table.cuda(), c.lens.cuda()
+    assert c.dec.kv_put(1, k, v, t, n, q=q, q_out=outs[0], rope=rope, positions=pos.expand(3, 3)) == 0
+    assert other.dec.kv_put(1, k.contiguous(), v.contiguous(), t, n, q=q.contiguous(), q_out=outs[1], rope=rope,
+                            positions=pos.expand(3, 3).contiguous()) == 0
+    assert torch.equal(outs[0], outs[1]) and torch.equal(c.cache, other.cache)
+    assert c.dec.kv_put(1, k, v, t, n, q=q, q_out=outs[0][:1].expand(3, 4, 64)) == B.KV_EINVAL
+
+
+def test_two_recorded_calls_share_a_decoder():
+    """Graphs of one decoder, replayed in turn on one stream, between eager calls through it."""
+    c = Case(4, 4, 128, lens=(3000, 300, 17, 0), seed=43)
+    t, n = c.table.cuda(), c.lens.cuda()
+    few = torch.tensor([100, 2990, 0, 64], dtype=torch.int32).clamp(max=c.max_blocks * 16).cuda()
+    q = [c.queries().cuda() for _ in range(2)]
+    outs, masses = [torch.empty_like(x) for x in q], [torch.zeros((4, c.max_blocks), device="cuda") for _ in q]
+    call = lambda i, out, mass: c.dec.kv_attend(i, q[i], t, (n, few)[i], out, mass_out=mass)    # noqa: E731
+    want = []
+    for i in range(2):
+        o, m = torch.empty_like(q[i]), torch.zeros_like(masses[i])
+        assert call(i, o, m) == 0
+        want.append((o, m))
+    graphs = []
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            assert call(i, outs[i], masses[i]) == 0
+        graphs.append(g)
+    for turn in range(5):
+        for i in (0, 1, 1, 0)[turn % 2:]:
+            outs[i].fill_(float("nan"))
+            masses[i].fill_(float("nan"))
+            graphs[i].replay()
+            o, m = torch.empty_like(q[1 - i]), torch.empty_like(masses[i])
+            assert call(1 - i, o, m) == 0
+            torch.cuda.synchronize()
+            assert torch.equal(outs[i], want[i][0]) and torch.equal(masses[i], want[i][1])
+            assert torch.equal(o, want[1 - i][0]) and torch.equal(m, want[1 - i][1])
+
+
+def test_evict_with_many_of_one_weight_and_close_ones():
+    """Rows on both sides of where entries are compared instead of counted: many that begin alike, few, all equal."""
+    for b in (300, 512, 513, 2048, 2049):
+        table, lens, mass = evict_inputs(6, b, 16, seed=b, lens=(b * 16,) * 6)
+        close = torch.rand((b,), generator=torch.Generator().manual_seed(b))
+        mass[0] = 1.0 + close * 2.0 ** -12                  # all in one first digit
+        mass[1] = 0.25
+        mass[2] = torch.where(close < 0.5, 1.0, 1.0 + 2.0 ** -23)
+        mass[3] = torch.where(close < 0.02, 1.0, 4.0 + close)
+        mass[4] = close * 1e-38
+        for budget in (1, b // 3, b - 3):
+            check_evict(table, lens, mass, 16, budget, 1, 1, b)
 
 
 def test_q_is_its_own_output_and_broadcast_queries():
