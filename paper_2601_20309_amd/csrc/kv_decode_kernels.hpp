@@ -232,15 +232,14 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
     using T = Step<DP>;
     constexpr int KJ = T::KJ, VW = T::VW, NV = T::NV, ACC = T::ACC;
     constexpr uint32_t WAVES = T::WAVES;
-    // Of a key a lane takes 8 dimensions for each step of 32: in 16 bits dimensions 32 j + 8 kq on, 64 bytes
-    // of a row at once; in 8 bits, where rows are whole, those of its quarter of the row, 16 at once (q is
-    // brought in the same order).
-    constexpr bool RUNS = FP8 && WHOLE;
-    constexpr int KL = RUNS ? KJ / 2 : KJ;
-    // Rows of 128 bytes and less in 8 bits leave room for two tiles of values: they are asked for ahead, too.
-    constexpr bool AHEAD = FP8 && DP <= 128;
-    typedef typename Raw<FP8 && !RUNS ? 8 : 16>::type kraw;
-    auto k_dim = [](int j, uint32_t kq) { return RUNS ? kq * (DP / 4) + (uint32_t)j * 8u : (uint32_t)j * 32u + kq * 8u; };
+    // Of a key a lane takes 16 bytes at once: in 16 bits the 8 dimensions of a step of 32, 32 j + 8 kq on; in 8 bits
+    // 16 dimensions, 64 l + 16 kq on, of which 8 go into each of two steps (q is brought in the same order).
+    constexpr int KL = FP8 ? KJ / 2 : KJ;
+    // In 8 bits there is room for two tiles of values: they are asked for a tile ahead, like the keys.  us without / with:
+    // 128 requests around 600 tokens, 8 heads of 128, 39.4 / 37.4; 4 of 32768 tokens, 8 heads of 128 48.4 / 50.4, of 192
+    // 102 / 85, 4 heads of 256 51.4 / 55.2; in 16 bits, 32 requests around 1000, 8 heads of 128, 35.6 / 39.7.
+    constexpr bool AHEAD = FP8 && !(WHOLE && DP == 256);
+    auto k_dim = [](int j, uint32_t kq) { return FP8 ? (uint32_t)(j / 2) * 64u + kq * 16u + (uint32_t)(j & 1) * 8u : (uint32_t)j * 32u + kq * 8u; };
     typedef typename Raw<(FP8 ? 1 : 2) * VW>::type vraw;
     __shared__ f32x4 joined[WAVES][ACC][64];
     __shared__ f32x4 ml[WAVES][16];
@@ -271,8 +270,8 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
     const uint8_t *const vb = p.v + (uint64_t)kv_head * p.head_bytes + (WHOLE ? n * VW * elem : 0u);
     // (Where rows are not whole, found anew for every row: kept, they are what does not fit the registers.)
     auto k_off = [&](int l, uint32_t kq) {
-        const uint32_t d = (uint32_t)l * 32u + kq * 8u;
-        return RUNS ? (uint32_t)l * 16u : WHOLE ? (uint32_t)l * 32u * elem : min(d, p.dim - 8u) * elem;
+        constexpr uint32_t step = FP8 ? 64u : 32u, each = FP8 ? 16u : 8u;
+        return WHOLE ? (uint32_t)l * step * elem : min((uint32_t)l * step + kq * each, p.dim - each) * elem;
     };
     auto v_off = [&](int c, uint32_t n) {
         const uint32_t d = (uint32_t)c * 128u + n * VW;
@@ -311,13 +310,20 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
     };
     Part now = {s, t, 0u, 0u, 0u}, next = part_at(s, t, at);
     w32x4 qf[KJ];
-    kraw kr[2][KL];
-    auto load_keys = [&](kraw(&to)[KL], uint32_t cell) {
+    w32x4 kr[2][KL];
+    auto load_keys = [&](w32x4(&to)[KL], uint32_t cell) {
         const uint64_t off = (uint64_t)(cell == kNoCell ? 0u : cell) * p.token_bytes;
         uint32_t k = kq;
         if constexpr (!WHOLE) asm volatile("" : "+v"(k));
+        if constexpr (FP8 && !WHOLE && DP == 64) {
+            if (p.dim < 16u) {  // a row of 8 bytes, and nothing behind the last one
+                const w32x2 x = *reinterpret_cast<const w32x2 *>(kb + off);
+                to[0] = w32x4{0u, 0u, x[0], x[1]};
+                return;
+            }
+        }
 #pragma unroll
-        for (int l = 0; l < KL; l++) to[l] = *reinterpret_cast<const kraw *>(kb + off + k_off(l, k));
+        for (int l = 0; l < KL; l++) to[l] = *reinterpret_cast<const w32x4 *>(kb + off + k_off(l, k));
     };
     uint32_t cell[2], page[2];
     // The lane's 8 tokens of the step whose cells are `cell`, and their values.
@@ -374,19 +380,22 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
                 // scores: token x head
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
-                    kraw(&key)[KL] = kr[h];
+                    w32x4(&key)[KL] = kr[h];
                     if constexpr (!WHOLE) {
                         // dimensions that are not there meet zeros of q: they must not be NaN
 #pragma unroll
-                        for (int j = 0; j < KJ; j++)
-                            if ((uint32_t)j * 32u + kq * 8u >= p.dim) clear(key[j]);
+                        for (int l = 0; l < KL; l++) {
+                            const uint32_t d = k_dim(FP8 ? 2 * l : l, kq);
+                            if (d >= p.dim) clear(key[l]);
+                            else if (FP8 && d + 16u > p.dim) key[l] = w32x4{key[l][2], key[l][3], 0u, 0u};  // 8 are there: the last 16 were read
+                        }
                     }
                     sc[h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int j = 0; j < KJ; j++) {
                         w32x4 a;
                         if constexpr (FP8) {
-                            const uint32_t lo = RUNS ? key[j / 2][2 * (j & 1)] : key[j][0], hi = RUNS ? key[j / 2][2 * (j & 1) + 1] : key[j][1];
+                            const uint32_t lo = key[j / 2][2 * (j & 1)], hi = key[j / 2][2 * (j & 1) + 1];
                             a = w32x4{X::template from_fp8<false>(lo), X::template from_fp8<true>(lo), X::template from_fp8<false>(hi),
                                       X::template from_fp8<true>(hi)};
                         } else {
