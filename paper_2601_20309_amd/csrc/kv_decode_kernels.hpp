@@ -15,7 +15,8 @@ typedef uint32_t w32x2 __attribute__((ext_vector_type(2)));
 struct Bf16 {
     typedef __bf16 x8 __attribute__((ext_vector_type(8)));
     typedef __bf16 x2 __attribute__((ext_vector_type(2)));
-    // Weights are exp2(score - reference): the reference is at most kSlack below the largest score.
+    // Weights are exp2(score - reference): the reference is at most kSlack + kBias below the largest score, so that it
+    // and all sums change scale only when a score is 2^kSlack times above what was met before.
     static constexpr float kBias = 0.0f, kSlack = 8.0f;
     static __device__ __forceinline__ f32x4 mma(w32x4 a, w32x4 b, f32x4 c)
     {
@@ -61,28 +62,6 @@ struct Fp16 {
     static constexpr uint32_t kOnes = 0x3C003C00u;
 };
 
-// ---- attention of one new token --------------------------------------------------------------
-//
-// scores s_t = q.k_t, weights w_t = exp2(c s_t - m), out = sum w_t v_t / sum w_t with a running
-// reference m.  Every key and value is read once, so HBM bounds it: a matrix instruction per
-// 16 x 16 x 32 products does what the vector units could not beside the loads.
-//
-// Work is cut into tiles of 32 tokens of one request.  The tiles of all requests, one behind
-// the other, are dealt to `groups` equal ranges, whatever the requests' lengths; a range
-// belongs to one workgroup (or several that share the KV heads).  (Where no request can be longer than a few
-// steps of a workgroup's waves, a range is a request, by_request: a second launch would take longer than they do.)  A wave has one KV head and up
-// to 16 of its query heads (a unit); where there are fewer units than waves, several
-// waves take turns at the tiles of a range and join in LDS.  A request that lies in one
-// range is finished there; others leave sum, reference and unnormalised output per range, and
-// kv_join_kernel joins them.
-//
-// No operand passes through LDS.  The products are taken transposed, tokens x heads and
-// dimensions x heads, so that the weights come out where the second product wants
-// them: lane (n, kq) = (lane % 16, lane / 16) holds of head n the tokens kq * 4 + r and
-// 16 + kq * 4 + r (r < 4), which are the eight its operand takes if the values are
-// brought in the same order (the order of a contraction is free).  For the values it loads
-// 8 dimensions of each of those eight tokens, 16 lanes a row, whole rows of 256 bytes, and puts
-// the pairs of tokens that a dimension's operand is made of together with byte permutes.
 // Quotients of whole numbers below 2^31 by a divisor that the host knows: with 2^(bits - 1) < divisor <= 2^bits and
 // magic = ceil(2^(31 + bits) / divisor), x / divisor = x * magic >> (31 + bits).
 struct Divide {
@@ -99,6 +78,40 @@ struct Divide {
         return magic ? (uint32_t)((uint64_t)x * magic >> 32) >> shift : x;
     }
 };
+
+// ---- attention of one new token --------------------------------------------------------------
+//
+// scores s_t = q.k_t, weights w_t = exp2(c s_t - m), out = sum w_t v_t / sum w_t with a running
+// reference m.  Every key and value is read once, so HBM bounds it: a matrix instruction per
+// 16 x 16 x 32 products does what the vector units could not beside the loads.
+//
+// Work is cut into tiles of 32 tokens of one request.  The tiles of all requests, one behind the other, are dealt
+// to `groups` equal ranges, whatever the requests' lengths; a range belongs to one workgroup (or several that share
+// the KV heads).  A wave has one KV head and up to 16 of its query heads (a unit); where there are fewer units than
+// waves, several waves take turns at the tiles of a range and join in LDS.  A request that lies in one range is
+// finished there; others leave sum, reference and unnormalised output per range, and kv_join_kernel joins them.
+// Where no request can be longer than a few steps of a workgroup's waves, a range is a request (by_request), and
+// the second launch, which would take longer than they do, is not made.
+//
+// No operand passes through LDS.  The products are taken transposed, tokens x heads and
+// dimensions x heads, so that the weights come out where the second product wants
+// them: lane (n, kq) = (lane % 16, lane / 16) holds of head n the tokens kq * 4 + r and
+// 16 + kq * 4 + r (r < 4), which are the eight its operand takes if the values are
+// brought in the same order (the order of a contraction is free).  For the values it loads
+// 8 dimensions of each of those eight tokens, 16 lanes a row, whole rows of 256 bytes, and puts
+// the pairs of tokens that a dimension's operand is made of together with byte permutes.
+//
+// Scores, references, weights and both sums are held in 32 bits.  Weights are rounded to the 16-bit type only as
+// the second product's operand: that product takes two operands of one type, and the values have 16 bits or fewer.
+//
+// Keys are read with plain loads (a row's 128-byte lines are met by several loads of a wave, which find them in the
+// CU's cache), values past the caches: 16 lanes take a row at once.  us of this kernel as it is / with keys past the
+// caches too / with values through them: 32 requests around 1000 tokens, 32 query heads over 8 of 128, bf16 35.6 /
+// 38.1 / 40.9; 4 of 32768 tokens, 64 over 8 of 128, 88.8 / 88.9 / 95.0; 4 of 32768, 8 heads of 96, 77.0 / 87.9 / 76.3;
+// 8-bit, 128 around 600, 37.4 / 39.2 / 41.6.
+//
+// The 4 requests of 32768 tokens are 537 MB: 6.1 TB/s, of them some 5 us until all keys are under way and 6.4 TB/s from
+// then on.  Counters: each byte of the cache fetched once, no LDS bank conflicts.
 
 struct AttendParams {
     const uint8_t *k, *v;      // the layer's planes
@@ -207,7 +220,8 @@ struct Step {
     static constexpr int VW = DP == 64 ? 4 : 8;     // dimensions of a row that a lane loads at once,
     static constexpr int NV = DP == 64 ? 1 : DP / 128;  // and how often
     static constexpr int ACC = VW * NV;
-    // Waves of a workgroup, one or two per SIMD: rows of 256 dimensions need more than half of its registers.
+    // Waves of a workgroup, one or two per SIMD: rows of 256 dimensions need more than half of its registers.  us with
+    // four / eight: 4 requests of 32768 tokens, 4 heads of 256, 92 / 171.
     static constexpr uint32_t WAVES = DP == 256 ? 4 : 8;
 };
 
@@ -602,7 +616,9 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
 constexpr uint32_t kMaxGroups = 256;    // ranges of a call
 constexpr uint32_t kMassBlocks = 32;    // blocks of a workgroup that adds up weights
 
-// Joins what several ranges left of one request: out = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i.
+// Joins what several ranges left of one request: out = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i.  Bound by the
+// launch itself: behind a kernel that has filled the caches one that returns at once takes 4.7 us, this one 5.4 (4
+// requests in 65 ranges each, 8.5 MB of parts), 6.5 (one request in 256), 7.8 with the weights of 32 requests' blocks.
 struct Joined {
     float top, sum, own;  // reference, sum of rounded weights, sum of weights
     f32x4 all[4];
