@@ -105,7 +105,7 @@ struct Divide {
 // the second product's operand: that product takes two operands of one type, and the values have 16 bits or fewer.
 //
 // Keys are read with plain loads (a row's 128-byte lines are met by several loads of a wave, which find them in the
-// CU's cache), values past the caches: 16 lanes take a row at once.  us of this kernel as it is / with keys past the
+// CU's cache), whole values past the caches: 16 lanes take a row at once.  us of this kernel as it is / with keys past the
 // caches too / with values through them: 32 requests around 1000 tokens, 32 query heads over 8 of 128, bf16 35.6 /
 // 38.1 / 40.9; 4 of 32768 tokens, 64 over 8 of 128, 88.8 / 88.9 / 95.0; 4 of 32768, 8 heads of 96, 77.0 / 87.9 / 76.3;
 // 8-bit, 128 around 600, 37.4 / 39.2 / 41.6.
@@ -255,6 +255,10 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
     constexpr bool AHEAD = FP8 && !(WHOLE && DP == 256);
     auto k_dim = [](int j, uint32_t kq) { return FP8 ? (uint32_t)(j / 2) * 64u + kq * 16u + (uint32_t)(j & 1) * 8u : (uint32_t)j * 32u + kq * 8u; };
     typedef typename Raw<(FP8 ? 1 : 2) * VW>::type vraw;
+    // Values go past the caches, except short rows that share 128-byte lines with other heads' all along.  us past /
+    // through them: 4 requests of 32768 tokens, 8-bit, 8 heads of 40 30.8 / 26.2, of 80 46.7 / 45.0, of 64 28.9 / 32.2;
+    // 16-bit, 4 heads of 192 78.3 / 83.0, 8 of 96 76.0 / 77.2.
+    constexpr bool PAST = WHOLE || (!FP8 && DP > 64);
     __shared__ f32x4 joined[WAVES][ACC][64];
     __shared__ f32x4 ml[WAVES][16];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -356,7 +360,11 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
         if constexpr (!WHOLE) asm volatile("" : "+v"(v));
 #pragma unroll
         for (int r = 0; r < 8; r++)
-            to[r][c] = __builtin_nontemporal_load(reinterpret_cast<const vraw *>(vb + (uint64_t)vcell[r] * p.token_bytes + v_off(c, v)));
+        {
+            const vraw *const from = reinterpret_cast<const vraw *>(vb + (uint64_t)vcell[r] * p.token_bytes + v_off(c, v));
+            if constexpr (PAST) to[r][c] = __builtin_nontemporal_load(from);
+            else to[r][c] = *from;
+        }
     };
     vraw next_vr[8][NV];
     uint32_t next_present = 0;
