@@ -377,17 +377,24 @@ int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
     // parts.  More requests: a wave each, so that ranges meet fewer of their ends.  us, by eight / by four: 4 requests of
     // 32768 tokens (64 query heads) 93.2 / 90.7, one of 8192 17.7 / 16.7; 32 around 1024 43.4 / 45.6.
     Workgroup w(d->units, p.n_seqs <= kFewRequests ? d->waves / 2 : d->waves, d->waves);
-    // Where no request can be longer than two steps of its waves, each is a range, and nothing is left to join: with
+    // Where no request can be longer than three steps of its waves, each is a range, and nothing is left to join: with
     // fewer units, and so more waves for each, to a workgroup, as long as two workgroups per compute unit take all requests,
     // and no second launch is needed for block weights anyway.  us, split and joined / a range each: 3 requests of up to
-    // 100 tokens 9.6 / 5.9; 32 of 192 15.2 / 10.6, of 512 21.1 / 15.7; 128 of 256 31.0 / 27.6; with weights 16 of up to
-    // 512 13.0 / 15.2.
+    // 100 tokens 9.6 / 5.9; 32 of 192 15.2 / 10.6, of 512 21.1 / 15.7; 128 of 256 31.0 / 27.6; 3 of 600, three steps, 15.3 /
+    // 12.3; 4 of 1000, four steps, 14.0 / 17.6; with weights 16 of up to 512 13.0 / 15.2.
+    // More waves for each, up to one a tile, as long as a compute unit has one workgroup: us with as few / as many, 32 requests
+    // of 64 tokens 10.5 / 8.4, of 192 10.7 / 9.3, 2 of 256 10.2 / 8.3; with two workgroups a compute unit 64 of 256 14.8 / 19.3.
     for (uint32_t most = d->waves; most > 0 && !p.by_request; most /= 2) {
         const Workgroup x(d->units, most, d->waves);
-        if (tiles > 2u * x.subs) continue;
+        if (tiles > 3u * x.subs) continue;
         if (most < d->waves && (p.n_seqs * x.per_range > 2u * (uint32_t)d->n_cus || p.granules)) continue;
         w = x;
         p.by_request = 1u;
+        for (uint32_t fewer = most / 2; fewer > 0 && w.subs < tiles; fewer /= 2) {
+            const Workgroup y(d->units, fewer, d->waves);
+            if (p.n_seqs * y.per_range > (uint32_t)d->n_cus) break;
+            w = y;
+        }
     }
     p.wgs_per_group = w.per_range;
     p.units_per_wg = w.units;

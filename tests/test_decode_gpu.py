@@ -812,7 +812,7 @@ def test_evict_with_many_of_one_weight_and_close_ones():
 def test_q_is_its_own_output_and_broadcast_queries():
     c = Case(4, 3, 128, lens=(700, 33, 0, 5), seed=31)
     q = c.queries()
-    want, _, _ = c.check_attend(q)
+    want, _, _ = c.check_attend(q, mass=False, lse=False)      # the same call: with weights the split is another
     mine = q.cuda()
     assert c.dec.kv_attend(c.layer, mine, c.table.cuda(), c.lens.cuda(), mine) == 0
     assert torch.equal(mine, want)
