@@ -382,11 +382,14 @@ int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
     // and no second launch is needed for block weights anyway.  us, split and joined / a range each: 3 requests of up to
     // 100 tokens 9.6 / 5.9; 32 of 192 15.2 / 10.6, of 512 21.1 / 15.7; 128 of 256 31.0 / 27.6; 3 of 600, three steps, 15.3 /
     // 12.3; 4 of 1000, four steps, 14.0 / 17.6; with weights 16 of up to 512 13.0 / 15.2.
+    // Where one range each fills the chip, up to six steps: 300 of up to 128 tokens 25.7 / 24.2, of 8-bit and up to 160 24.3 /
+    // 21.1; 1000 of up to 128 65.8 / 61.9; 512 of up to 192 42.9 / 42.0, 300 31.2 / 31.6.
     // More waves for each, up to one a tile, as long as a compute unit has one workgroup: us with as few / as many, 32 requests
     // of 64 tokens 10.5 / 8.4, of 192 10.7 / 9.3, 2 of 256 10.2 / 8.3; with two workgroups a compute unit 64 of 256 14.8 / 19.3.
     for (uint32_t most = d->waves; most > 0 && !p.by_request; most /= 2) {
         const Workgroup x(d->units, most, d->waves);
-        if (tiles > 3u * x.subs) continue;
+        const bool full = !p.granules && most == d->waves && p.n_seqs * x.per_range >= (uint32_t)d->n_cus;
+        if (tiles > (full ? 6u : 3u) * x.subs) continue;
         if (most < d->waves && (p.n_seqs * x.per_range > 2u * (uint32_t)d->n_cus || p.granules)) continue;
         w = x;
         p.by_request = 1u;

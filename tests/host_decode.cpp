@@ -277,7 +277,7 @@ void attend_launches()
                             CHECK((uint64_t)x.units_per_wg * x.wgs_per_group >= x.units && x.units_per_wg * (x.wgs_per_group - 1) < x.units, "every unit once");
                             CHECK(launches[0].g.x == x.groups * x.wgs_per_group, "grid");
                             if (x.by_request) {
-                                CHECK(x.groups == (uint32_t)n && tiles <= 3 * x.subs && x.joins == 0, "a range per request");
+                                CHECK(x.groups == (uint32_t)n && tiles <= (a.mass_out ? 3 : 6) * x.subs && x.joins == 0, "a range per request");
                             } else {
                                 CHECK(x.groups >= 1 && x.groups <= dkv::kMaxGroups && x.groups * x.wgs_per_group <= 256 + x.wgs_per_group, "ranges");
                                 CHECK(x.groups <= d->max_groups && x.joins >= 1, "memory for ranges");

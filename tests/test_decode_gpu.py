@@ -738,6 +738,20 @@ def test_decode_command_runs_on_a_small_cache():
     assert got["rows"][3]["gib"] < got["rows"][0]["gib"]
 
 
+@pytest.mark.parametrize("types", ALL_TYPES, ids="-".join)
+@pytest.mark.parametrize("n,longest,heads,group,dim,p", [
+    (300, 192, 8, 2, 128, 16), (40, 64, 8, 4, 64, 16), (3, 600, 4, 4, 128, 16), (5, 300, 2, 3, 40, 5), (2, 256, 8, 4, 256, 16),
+    (70, 130, 3, 3, 96, 16), (1, 33, 16, 2, 128, 8), (9, 1200, 2, 4, 64, 16)])
+def test_short_tables_without_weights(n, longest, heads, group, dim, p, types):
+    """A range per request with as many waves each as there is room for, one launch: lengths 0 to the longest."""
+    lens = [longest] + np.random.default_rng(n).integers(0, longest + 1, n - 1).tolist()
+    if n > 2:
+        lens[1] = 0
+    c = Case(heads, group, dim, p, lens=lens, types=types, seed=n, k_scale=0.02 if types[1] == "fp8" else 1.0)
+    c.check_attend(c.queries(), mass=False)
+    c.check_attend(c.queries(), mass=False, lse=False)
+
+
 def test_pages_that_several_entries_name():
     """A prefix that requests share, and one page twice in a row of the table: read as often as it is named."""
     c = Case(2, 4, 128, lens=(90, 75, 64), seed=41)
