@@ -370,6 +370,8 @@ int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
     p.granule_bits = (uint32_t)__builtin_ctz(d->granule);
     p.by_block = dkv::Divide::by(p.block_size);
     p.max_granules = d->max_granules;
+    // few numbers a block: four lanes for it, so that a workgroup has more blocks
+    p.mass_bits = p.block_size / p.granule * p.n_heads <= 16u ? 2u : 4u;
     p.qk_scale = (float)((double)a->scale * 1.4426950408889634074 * (double)d->dc.k_scale);
     p.v_scale = d->dc.v_scale;
     const uint32_t tiles = (p.max_tokens + dkv::kTile - 1) / dkv::kTile;
@@ -404,7 +406,7 @@ int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
     p.subs = w.subs;
     // no more ranges than there is memory for, and than there can be turns in this call
     p.groups = p.by_request ? p.n_seqs
-                            : (uint32_t)std::min<uint64_t>(std::min(d->max_groups, ranges(d, w)), ((uint64_t)p.n_seqs * tiles + w.subs - 1) / w.subs);
+                            : (uint32_t)std::min<uint64_t>(std::min(d->max_groups, ranges(d, w)), (uint64_t)p.n_seqs * tiles);
     hipStream_t s = (hipStream_t)stream;
     const dim3 g(p.groups * p.wgs_per_group), b(64 * p.units_per_wg * p.subs);
     int dp;
@@ -418,7 +420,8 @@ int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
     DECTRY(hipGetLastError());
     const uint32_t lines = (p.units * p.part_vecs / 4u + 7u) / 8u;
     if (!p.by_request) p.joins = std::min(lines, std::max(1u, kJoinWgs / p.n_seqs));
-    const dim3 gj(p.joins + (p.granules ? (p.max_blocks + dkv::kMassBlocks - 1u) / dkv::kMassBlocks : 0u), p.n_seqs);
+    const uint32_t mass_blocks = dkv::mass_blocks(p.mass_bits);
+    const dim3 gj(p.joins + (p.granules ? (p.max_blocks + mass_blocks - 1u) / mass_blocks : 0u), p.n_seqs);
     if (gj.x == 0u) return KV_OK;
     if (d->dc.x_type == KV_FP16) hipLaunchKernelGGL(dkv::kv_join_kernel<dkv::Fp16>, gj, dim3(256), 0, s, p);
     else hipLaunchKernelGGL(dkv::kv_join_kernel<dkv::Bf16>, gj, dim3(256), 0, s, p);

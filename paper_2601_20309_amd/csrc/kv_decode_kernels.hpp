@@ -139,6 +139,7 @@ struct AttendParams {
     Divide by_items, by_rows, by_head_tiles;  // by part_vecs / 4, part_rows, head_tiles
     uint32_t granule, granule_bits, max_granules;
     uint32_t joins;            // workgroups that join, per request
+    uint32_t mass_bits;        // log2 of the lanes that add up a block's weights
     uint32_t by_request;       // a range is a request: nothing to join
     float qk_scale;            // to base 2
     float v_scale;
@@ -189,7 +190,9 @@ struct Deal {
             if (asked >= base && asked - base < 64u) before = total + (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), (int)(asked - base));
             total += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
         }
-        per = max((total + p.groups - 1u) / p.groups, p.subs);  // at least a tile for each wave
+        // (As few as one: a range of a tile for each of its waves meets the ends of several short requests one after the
+        // other.  50 requests around 75 tokens, one KV head, us: 22.9 with at least a tile a wave, 14.5 so.)
+        per = max((total + p.groups - 1u) / p.groups, 1u);
     }
     __device__ __forceinline__ uint32_t tokens_of(uint32_t s) const { return (uint32_t)__builtin_amdgcn_readlane((int)tokens, (int)s); }
     // The request that tile `at` is one of, and which of its tiles.
@@ -622,7 +625,6 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
 }
 
 constexpr uint32_t kMaxGroups = 256;    // ranges of a call
-constexpr uint32_t kMassBlocks = 32;    // blocks of a workgroup that adds up weights
 
 // Joins what several ranges left of one request: out = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i.  Bound by the
 // launch itself: behind a kernel that has filled the caches one that returns at once takes 4.7 us, this one 5.4 (4
@@ -735,14 +737,17 @@ __device__ __forceinline__ void join(const AttendParams &p, uint32_t s, uint32_t
     }
 }
 
-// What each block received: 16 lanes a block add up 2^(granule - lse) over its granules and
-// all query heads, in a fixed order.  The heads' lse are joined once more here, for 32 blocks
-// at a time, so that this need not wait for the workgroups that join.
+// Blocks of a workgroup that adds up weights, two for the same lanes.
+__host__ __device__ __forceinline__ uint32_t mass_blocks(uint32_t mass_bits) { return 512u >> mass_bits; }
+
+// What each block received: 4 or 16 lanes a block add up 2^(granule - lse) over its granules and all query heads, in
+// a fixed order (20 requests of 65381 tokens, 4 heads, blocks of 8: 11.4 us with 4 lanes, 26.7 with 16).  The heads' lse are joined once more here, for all blocks of a workgroup at a time, so that this need not
+// wait for the workgroups that join.
 __device__ __forceinline__ void add_mass(const AttendParams &p, uint32_t s, uint32_t first_block, uint32_t tokens, uint32_t g0, uint32_t g1)
 {
     __shared__ float lse[1024];
     __shared__ float2 some[256];
-    const uint32_t tid = threadIdx.x, part = tid & 15u;
+    const uint32_t tid = threadIdx.x, lanes = 1u << p.mass_bits, part = tid & (lanes - 1u), apart = 256u >> p.mass_bits;
     // the first granules of a lane are under way while the heads' lse are found
     constexpr uint32_t kAhead = 4;
     const uint32_t per_block = p.block_size >> p.granule_bits, n_gran = (tokens + p.granule - 1u) >> p.granule_bits;
@@ -751,11 +756,11 @@ __device__ __forceinline__ void add_mass(const AttendParams &p, uint32_t s, uint
     float ahead[2][kAhead];
 #pragma unroll
     for (int k = 0; k < 2; k++) {
-        const uint32_t j = first_block + 16u * (uint32_t)k + (tid >> 4), f = min(j * per_block, n_gran), l = min(f + per_block, n_gran);
+        const uint32_t j = first_block + apart * (uint32_t)k + (tid >> p.mass_bits), f = min(j * per_block, n_gran), l = min(f + per_block, n_gran);
         from[k] = p.granules + ((uint64_t)s * p.max_granules + f) * p.n_heads;
         n[k] = (l - f) * p.n_heads;
 #pragma unroll
-        for (uint32_t i = 0; i < kAhead; i++) ahead[k][i] = part + 16u * i < n[k] ? from[k][part + 16u * i] : 0.f;
+        for (uint32_t i = 0; i < kAhead; i++) ahead[k][i] = part + lanes * i < n[k] ? from[k][part + lanes * i] : 0.f;
     }
     if (g0 == g1) {
         for (uint32_t h = tid; h < p.n_heads; h += 256u) lse[h] = tokens ? p.lse2[(uint64_t)s * p.n_heads + h] : 0.f;
@@ -785,20 +790,19 @@ __device__ __forceinline__ void add_mass(const AttendParams &p, uint32_t s, uint
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < 2; k++) {
-        const uint32_t j = first_block + 16u * (uint32_t)k + (tid >> 4);
+        const uint32_t j = first_block + apart * (uint32_t)k + (tid >> p.mass_bits);
         float sum = 0.f;
         uint32_t h = part % p.n_heads;
         auto add = [&](float granule) {
             sum += lse[h] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(granule - lse[h]);
-            h = (h + 16u) % p.n_heads;
+            h = (h + lanes) % p.n_heads;
         };
 #pragma unroll
         for (uint32_t i = 0; i < kAhead; i++)
-            if (part + 16u * i < n[k]) add(ahead[k][i]);
+            if (part + lanes * i < n[k]) add(ahead[k][i]);
 #pragma unroll 4
-        for (uint32_t i = part + 16u * kAhead; i < n[k]; i += 16u) add(from[k][i]);
-#pragma unroll
-        for (int d = 8; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+        for (uint32_t i = part + lanes * kAhead; i < n[k]; i += lanes) add(from[k][i]);
+        for (uint32_t d = lanes / 2u; d > 0u; d >>= 1) sum += __shfl_xor(sum, (int)d, 64);
         if (part == 0u && j < p.max_blocks) {
             const int64_t at = (int64_t)s * p.mass_stride + j;
             p.mass_out[at] = (p.mass ? p.mass[at] : 0.f) + sum;
@@ -816,7 +820,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(const AttendParams p)
     const Deal deal(p, lane, s);
     const uint32_t first = deal.before;
     const uint32_t g0 = p.by_request ? 0u : first / deal.per, g1 = p.by_request ? 0u : n_tiles ? (first + n_tiles - 1u) / deal.per : g0;
-    if (blockIdx.x >= p.joins) add_mass(p, s, (blockIdx.x - p.joins) * kMassBlocks, tokens, g0, g1);
+    if (blockIdx.x >= p.joins) add_mass(p, s, (blockIdx.x - p.joins) * mass_blocks(p.mass_bits), tokens, g0, g1);
     else if (!n_tiles || g0 != g1) join<X>(p, s, blockIdx.x, p.joins, n_tiles ? g1 - g0 + 1u : 0u, g0);
 }
 

@@ -291,7 +291,7 @@ void attend_launches()
                             CHECK((const char *)(x.granules + (uint64_t)n * x.max_granules * x.n_heads) <= end, "granules end");
                             CHECK(p % x.granule == 0 && 16 % x.granule == 0 && x.granule == 1u << x.granule_bits, "granule");
                             CHECK((uint64_t)x.max_granules * x.granule == (uint64_t)blocks * p, "granules");
-                            CHECK(launches[1].g.y == (uint32_t)n && launches[1].g.x == x.joins + (blocks + 31u) / 32u, "join grid");
+                            CHECK(launches[1].g.y == (uint32_t)n && launches[1].g.x == x.joins + (blocks + dkv::mass_blocks(x.mass_bits) - 1) / dkv::mass_blocks(x.mass_bits), "join grid");
                             kv_decoder_destroy(d);
                         }
                     }
