@@ -370,9 +370,13 @@ int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
     p.granule_bits = (uint32_t)__builtin_ctz(d->granule);
     p.by_block = dkv::Divide::by(p.block_size);
     p.max_granules = d->max_granules;
-    // Few numbers a block: four lanes for it, so that a workgroup has more blocks.  us of the second launch, four / 16 lanes: 63
-    // requests of 1203 blocks of 20 numbers 7.9 / 13.7, 32 of 512 of 32 7.9 / 8.2, 2 of 710 of 24 10.6 / 9.7.
-    p.mass_bits = p.block_size / p.granule * p.n_heads <= 32u ? 2u : 4u;
+    // Few numbers a block: four lanes for it, so that a workgroup has more blocks; up to 64, where there are more workgroups
+    // than the chip holds at once, eight.  us of the second launch, four / 16 lanes: 63 requests of 1203 blocks of 20
+    // numbers 7.9 / 13.7, 32 of 512 of 32 7.9 / 8.2, 2 of 710 of 24 10.6 / 9.7; eight / 16: 118 of 1594 of 40 16.3 / 25.0, 37 of
+    // 340 of 45 6.4 / 6.1.
+    const uint32_t numbers = p.block_size / p.granule * p.n_heads;
+    const uint64_t mass_wgs = (uint64_t)p.n_seqs * p.max_blocks / dkv::mass_blocks(4u);
+    p.mass_bits = numbers <= 32u ? 2u : numbers <= 64u && mass_wgs > 8ull * (uint32_t)d->n_cus ? 3u : 4u;
     p.qk_scale = (float)((double)a->scale * 1.4426950408889634074 * (double)d->dc.k_scale);
     p.v_scale = d->dc.v_scale;
     const uint32_t tiles = (p.max_tokens + dkv::kTile - 1) / dkv::kTile;
@@ -463,6 +467,7 @@ int kv_evict(kv_decoder *d, const kv_evict_args *a, void *stream)
     hipStream_t s = (hipStream_t)stream;
     if (p.max_blocks <= 512u) hipLaunchKernelGGL((dkv::kv_evict_kernel<512, 1, 11>), g, dim3(512), 0, s, p);
     else if (p.max_blocks <= 2048u) hipLaunchKernelGGL((dkv::kv_evict_kernel<1024, 2, 11>), g, dim3(1024), 0, s, p);
+    else if (p.max_blocks <= 4096u) hipLaunchKernelGGL((dkv::kv_evict_kernel<1024, 4, 11>), g, dim3(1024), 0, s, p);
     else hipLaunchKernelGGL((dkv::kv_evict_kernel<1024, 8, 11>), g, dim3(1024), 0, s, p);
     DECTRY(hipGetLastError());
     return KV_OK;

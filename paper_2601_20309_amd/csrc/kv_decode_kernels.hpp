@@ -740,9 +740,10 @@ __device__ __forceinline__ void join(const AttendParams &p, uint32_t s, uint32_t
 // Blocks of a workgroup that adds up weights, two for the same lanes.
 __host__ __device__ __forceinline__ uint32_t mass_blocks(uint32_t mass_bits) { return 512u >> mass_bits; }
 
-// What each block received: 4 or 16 lanes a block add up 2^(granule - lse) over its granules and all query heads, in
-// a fixed order (20 requests of 65381 tokens, 4 heads, blocks of 8: 11.4 us with 4 lanes, 26.7 with 16).  The heads' lse are joined once more here, for all blocks of a workgroup at a time, so that this need not
-// wait for the workgroups that join.
+// What each block received: 4, 8 or 16 lanes a block add up 2^(granule - lse) over its granules and all query heads, in
+// a fixed order (20 requests of 65381 tokens, 4 heads, blocks of 8: 11.4 us with 4 lanes, 26.7 with 16).  The heads'
+// lse are joined once more here, for all blocks of a workgroup at a time, so that this need not wait for the
+// workgroups that join.
 __device__ __forceinline__ void add_mass(const AttendParams &p, uint32_t s, uint32_t first_block, uint32_t tokens, uint32_t g0, uint32_t g1)
 {
     __shared__ float lse[1024];
@@ -1008,8 +1009,8 @@ __host__ __device__ __forceinline__ uint32_t weight_key(float x)
 //
 // Bound by its own chain of barriers, not by memory: a row of 512 is 4 KB.  Measured, rows of random weights, a
 // quarter kept: 64 rows of 512 in 4.3 us (5.1 with counts alone; 5.4 with 256 threads of two entries and 8-bit
-// digits), 64 of 2048 entries 6.2 (6.8; 8.9), 8 of 8192 entries 11.8; there the comparison costs 1.3 us more than
-// it saves.
+// digits), 64 of 2048 entries 6.2 (6.8; 8.9), 64 of 4096 8.9 (11.4 with eight entries a thread), 8 of 8192 entries 11.8; from four
+// entries a thread on the comparison costs 1.3 us more than it saves.
 template <uint32_t THREADS, uint32_t EACH, uint32_t DIGIT>
 __global__ __launch_bounds__(THREADS) void kv_evict_kernel(const EvictParams p)
 {

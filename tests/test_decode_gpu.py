@@ -752,6 +752,14 @@ def test_short_tables_without_weights(n, longest, heads, group, dim, p, types):
     c.check_attend(c.queries(), mass=False, lse=False)
 
 
+@pytest.mark.parametrize("p,heads,group,n,longest", [(5, 1, 8, 45, 8000), (5, 1, 4, 9, 700), (16, 1, 24, 3, 5000), (7, 2, 3, 40, 11000), (3, 1, 30, 5, 90)])
+def test_weights_of_many_blocks(p, heads, group, n, longest):
+    """Few and many numbers a block, few and many blocks: long tables of which requests fill little, but one."""
+    lens = [longest // 8] + np.random.default_rng(p).integers(0, 400, n - 1).tolist()
+    c = Case(heads, group, 40, p, lens=lens, max_blocks=-(-longest // p), seed=p + n)
+    c.check_attend(c.queries())
+
+
 def test_pages_that_several_entries_name():
     """A prefix that requests share, and one page twice in a row of the table: read as often as it is named."""
     c = Case(2, 4, 128, lens=(90, 75, 64), seed=41)
@@ -811,7 +819,7 @@ def test_two_recorded_calls_share_a_decoder():
 
 def test_evict_with_many_of_one_weight_and_close_ones():
     """Rows on both sides of where entries are compared instead of counted: many that begin alike, few, all equal."""
-    for b in (300, 512, 513, 2048, 2049):
+    for b in (300, 512, 513, 2048, 2049, 4096, 4097):
         table, lens, mass = evict_inputs(6, b, 16, seed=b, lens=(b * 16,) * 6)
         close = torch.rand((b,), generator=torch.Generator().manual_seed(b))
         mass[0] = 1.0 + close * 2.0 ** -12                  # all in one first digit
