@@ -10,6 +10,7 @@ namespace dkv {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t w32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t w32x2 __attribute__((ext_vector_type(2)));
+typedef w32x4 w32x4_by8 __attribute__((aligned(8)));  // where rows of 8-bit values begin on multiples of 8 bytes
 
 // The 16-bit types of q, k, v and the outputs.
 struct Bf16 {
@@ -344,7 +345,10 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
             }
         }
 #pragma unroll
-        for (int l = 0; l < KL; l++) to[l] = *reinterpret_cast<const w32x4 *>(kb + off + k_off(l, k));
+        for (int l = 0; l < KL; l++) {
+            if constexpr (FP8 && !WHOLE) to[l] = *reinterpret_cast<const w32x4_by8 *>(kb + off + k_off(l, k));
+            else to[l] = *reinterpret_cast<const w32x4 *>(kb + off + k_off(l, k));
+        }
     };
     uint32_t cell[2], page[2];
     // The lane's 8 tokens of the step whose cells are `cell`, and their values.
