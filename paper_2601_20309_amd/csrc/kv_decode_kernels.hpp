@@ -792,15 +792,17 @@ __device__ __forceinline__ void add_mass(const AttendParams &p, uint32_t s, uint
             }
         }
     }
+    const uint32_t part_head = part % p.n_heads, step = lanes % p.n_heads;  // heads of a lane's numbers
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < 2; k++) {
         const uint32_t j = first_block + apart * (uint32_t)k + (tid >> p.mass_bits);
         float sum = 0.f;
-        uint32_t h = part % p.n_heads;
+        uint32_t h = part_head;
         auto add = [&](float granule) {
             sum += lse[h] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(granule - lse[h]);
-            h = (h + lanes) % p.n_heads;
+            h += step;
+            h = h < p.n_heads ? h : h - p.n_heads;
         };
 #pragma unroll
         for (uint32_t i = 0; i < kAhead; i++)
