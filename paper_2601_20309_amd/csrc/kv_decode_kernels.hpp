@@ -1008,7 +1008,7 @@ __host__ __device__ __forceinline__ uint32_t weight_key(float x)
 
 // One workgroup per request.  A thread holds EACH entries, THREADS apart, of those that are looked at together; a
 // row of no more than EACH x THREADS is read once.  The key of the last block to go is found digit by digit, counted
-// in LDS, by three of 11 bits and less: the first has 8 steps per power of two, so that few lanes of many meet in
+// in LDS, by three of 11 bits and less: the first has 4 steps per power of two, so that few lanes of many meet in
 // one count.  Where as a rule few enough entries then begin with it, they are compared with one another instead of
 // counted twice more.  Then the row is closed up: a block moves down by the number of those before it that went.
 // All that is written lies before all that is read later, so a row may be its own output.
