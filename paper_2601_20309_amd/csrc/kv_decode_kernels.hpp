@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace dkv {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -35,15 +37,23 @@ struct Bf16 {
     {
         return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
     }
-    static constexpr uint32_t kOnes = 0x3F803F80u;
+    // Two weights as two numbers of 8 digits each: the upper one cut off, the lower the nearest to what that leaves, together
+    // within 2^-15.  The lower one gets 2^-20 of the weight on top, so that it is never 0 beside one: 0 times a value
+    // of infinity is NaN.
+    static __device__ __forceinline__ void split(float a, float b, uint32_t &upper, uint32_t &lower)
+    {
+        const uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
+        upper = __builtin_amdgcn_perm(y, x, 0x07060302u);
+        lower = pack(__builtin_fmaf(a, 1.0f + 0x1p-20f, -hi(x)), __builtin_fmaf(b, 1.0f + 0x1p-20f, -hi(y)));
+    }
 };
 
 struct Fp16 {
     typedef _Float16 x8 __attribute__((ext_vector_type(8)));
     typedef _Float16 x2 __attribute__((ext_vector_type(2)));
-    // fp16 has normal numbers from 2^-14 to 2^15: the largest weights lie between 2^8 and 2^15,
-    // which leaves 22 powers of two below them before a weight loses digits.
-    static constexpr float kBias = 8.0f, kSlack = 7.0f;
+    // fp16 has numbers from 2^-24 to 2^15: the largest weights lie between 2^12 and 2^15, so that its
+    // smallest number is 2^-36 of them and less.
+    static constexpr float kBias = 12.0f, kSlack = 3.0f;
     static __device__ __forceinline__ f32x4 mma(w32x4 a, w32x4 b, f32x4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
@@ -61,6 +71,13 @@ struct Fp16 {
         return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HI));
     }
     static constexpr uint32_t kOnes = 0x3C003C00u;
+    // As above, of 11 digits each, within 2^-21; each at least the smallest number there is, 2^-24.
+    static __device__ __forceinline__ void split(float a, float b, uint32_t &upper, uint32_t &lower)
+    {
+        const auto cut = __builtin_amdgcn_cvt_pkrtz(fmaxf(a, 0x1p-24f), fmaxf(b, 0x1p-24f));
+        upper = __builtin_bit_cast(uint32_t, cut);
+        lower = pack(fmaxf(a - (float)cut[0], 0x1p-24f), fmaxf(b - (float)cut[1], 0x1p-24f));
+    }
 };
 
 // Quotients of whole numbers below 2^31 by a divisor that the host knows: with 2^(bits - 1) < divisor <= 2^bits and
@@ -102,8 +119,13 @@ struct Divide {
 // 8 dimensions of each of those eight tokens, 16 lanes a row, whole rows of 256 bytes, and puts
 // the pairs of tokens that a dimension's operand is made of together with byte permutes.
 //
-// Scores, references, weights and both sums are held in 32 bits.  Weights are rounded to the 16-bit type only as
-// the second product's operand: that product takes two operands of one type, and the values have 16 bits or fewer.
+// Scores, references, weights and both sums are held in 32 bits.  The second product takes two operands of one type, and
+// the values have 16 bits or fewer.  So a weight meets 16-bit values as the sum of two such numbers, in two products: the
+// result is as far from 64 bits as its own rounding.  Beside outputs in bf16 8-bit values are taken as fp16, which holds them
+// exactly, and one fp16 number is enough for a weight.  Root of the mean square of the relative error, 1e-4, a number
+// of the output's type / so: bf16, 3 requests of 100 tokens 16.8 / 15.6, 32 around 1000 17.0 / 16.5; fp16 1.62 / 1.53; bf16 beside
+// 8-bit values 16.8 / 16.5.  us: 5.6 / 5.7; 35.3 / 35.7; 4 requests of 32768 tokens 87.7 / 88.1; fp16, 37 to 1700 13.6 / 13.9, 119 to 1100
+// and one head of 128 17.3 / 18.0; 8-bit, 128 around 600 38.1 / 38.4 (two numbers 39.0).
 //
 // Keys are read with plain loads (a row's 128-byte lines are met by several loads of a wave, which find them in the
 // CU's cache), whole values past the caches: 16 lanes take a row at once.  us of this kernel as it is / with keys past the
@@ -123,7 +145,7 @@ struct AttendParams {
     // What ranges leave of requests that go on in others, unnormalised and as it lies in a wave's registers:
     // [groups * 2][units][sum i][kq][part_rows], a vector of the dimensions i + (kq * 4 + r) * (8, or 4 up to 64 dimensions)
     f32x4 *part;
-    f32x4 *part_ml;            // [groups * 2][n_heads]: reference, sum of rounded weights, sum of weights, its log2 + reference
+    f32x4 *part_ml;            // [groups * 2][n_heads]: reference, sum of weights as they met the values, as they were, its log2 + reference
     float *lse2;               // [n_seqs][n_heads], base 2; written where granules is
     float *granules;           // nullptr, or [n_seqs][max_granules][n_heads]: log2 of the weight of `granule` tokens
     const float *mass;
@@ -263,6 +285,9 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
     // through them: 4 requests of 32768 tokens, 8-bit, 8 heads of 40 30.8 / 26.2, of 80 46.7 / 45.0, of 64 28.9 / 32.2;
     // 16-bit, 4 heads of 192 78.3 / 83.0, 8 of 96 76.0 / 77.2.
     constexpr bool PAST = WHOLE || (!FP8 && DP > 64);
+    // The type of the second product, and whether a weight is two numbers of it.
+    using Y = std::conditional_t<FP8, Fp16, X>;
+    constexpr bool SPLIT = !FP8 || std::is_same_v<X, Fp16>;
     __shared__ f32x4 joined[WAVES][ACC][64];
     __shared__ f32x4 ml[WAVES][16];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -471,14 +496,14 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
             }
 #pragma unroll
             for (int r = 0; r < 8; r++) top = fmaxf(top, w[r]);
-            if (__any(top > ref + X::kBias + X::kSlack)) {
+            if (__any(top > ref + Y::kBias + Y::kSlack)) {
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const float higher = fmaxf(ref, top - X::kBias), shrink = __builtin_amdgcn_exp2f(ref - higher);
+                const float higher = fmaxf(ref, top - Y::kBias), shrink = __builtin_amdgcn_exp2f(ref - higher);
                 ref = higher;
 #pragma unroll
                 for (int i = 0; i < ACC; i++) acc[i] *= shrink;
-                sum *= shrink;
+                if constexpr (!SPLIT) sum *= shrink;
                 own *= shrink;
             }
 #pragma unroll
@@ -486,10 +511,22 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
                 w[r] = __builtin_amdgcn_exp2f(w[r] - ref);
                 own += w[r];
             }
-            const w32x4 pw = {X::pack(w[0], w[1]), X::pack(w[2], w[3]), X::pack(w[4], w[5]), X::pack(w[6], w[7])};
-            // out is divided by the sum of the weights that it is made of, the rounded ones (rows of
-            // ones beside the values); lse and the blocks' weights go by the sum of those that they were.
-            sum = X::mma(w32x4{X::kOnes, X::kOnes, X::kOnes, X::kOnes}, pw, sum);
+            w32x4 pw, pl;  // of two numbers the lower one
+#pragma unroll
+            for (int r = 0; r < 4; r++) {
+                uint32_t upper, lower = 0u;
+                if constexpr (SPLIT) Y::split(w[2 * r], w[2 * r + 1], upper, lower);
+                else upper = Y::pack(w[2 * r], w[2 * r + 1]);
+                pw[r] = upper;
+                pl[r] = lower;
+            }
+            // Weights of one number: out is divided by the sum of the rounded ones, which it is made of (rows of ones beside
+            // the values); lse and the blocks' weights go by the sum of those that they were.
+            if constexpr (!SPLIT) sum = Y::mma(w32x4{Y::kOnes, Y::kOnes, Y::kOnes, Y::kOnes}, pw, sum);
+            auto add_values = [&](f32x4 &to, w32x4 values) {
+                if constexpr (SPLIT) to = Y::mma(values, pl, to);
+                to = Y::mma(values, pw, to);
+            };
 #pragma unroll
             for (int c = 0; c < NV; c++) {
                 if (gaps) {  // a weight of 0 does not make up for NaN
@@ -500,8 +537,8 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
                 // of token r: dimensions 2i and 2i + 1
                 auto pair = [&](int r, int i) {
                     const vraw &v = vr[r][c];
-                    if constexpr (FP8 && VW == 8) return i & 1 ? X::template from_fp8<true>(v[i / 2]) : X::template from_fp8<false>(v[i / 2]);
-                    else if constexpr (FP8) return i & 1 ? X::template from_fp8<true>(v) : X::template from_fp8<false>(v);
+                    if constexpr (FP8 && VW == 8) return i & 1 ? Y::template from_fp8<true>(v[i / 2]) : Y::template from_fp8<false>(v[i / 2]);
+                    else if constexpr (FP8) return i & 1 ? Y::template from_fp8<true>(v) : Y::template from_fp8<false>(v);
                     else return v[i];
                 };
 #pragma unroll
@@ -513,8 +550,8 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
                         even[k] = __builtin_amdgcn_perm(b, a, 0x05040100u);
                         odd[k] = __builtin_amdgcn_perm(b, a, 0x07060302u);
                     }
-                    acc[c * VW + 2 * i] = X::mma(even, pw, acc[c * VW + 2 * i]);
-                    acc[c * VW + 2 * i + 1] = X::mma(odd, pw, acc[c * VW + 2 * i + 1]);
+                    add_values(acc[c * VW + 2 * i], even);
+                    add_values(acc[c * VW + 2 * i + 1], odd);
                 }
             }
             if (p.granules) {
@@ -542,6 +579,7 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
         if (now.here) {
             own += __shfl_xor(own, 16, 64);
             own += __shfl_xor(own, 32, 64);
+            if constexpr (SPLIT) sum[0] = own;
             const bool whole = now.here == tiles_of(now.tokens);
             const uint32_t slot = group * 2u + (now.first > 0u ? 0u : 1u);
             f32x4 *const part = p.part + ((uint64_t)slot * p.units + unit) * p.part_vecs;
@@ -634,7 +672,7 @@ constexpr uint32_t kMaxGroups = 256;    // ranges of a call
 // launch itself: behind a kernel that has filled the caches one that returns at once takes 4.7 us, this one 5.4 (4
 // requests in 65 ranges each, 8.5 MB of parts), 6.5 (one request in 256), 7.8 with the weights of 32 requests' blocks.
 struct Joined {
-    float top, sum, own;  // reference, sum of rounded weights, sum of weights
+    float top, sum, own;  // reference, sum of weights as they met the values, as they were
     f32x4 all[4];
     __device__ __forceinline__ void none()
     {
