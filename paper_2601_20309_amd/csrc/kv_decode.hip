@@ -287,8 +287,8 @@ int kv_put(kv_decoder *d, const kv_put_args *a, void *stream)
     p.interleaved = a->interleaved ? 1u : 0u;
     p.section0 = a->inv_freq ? (uint32_t)a->sections[0] : 0u;
     p.section01 = p.section0 + (a->inv_freq && a->n_axes > 1 ? (uint32_t)a->sections[1] : 0u);
-    p.k_inv = 1.f / d->dc.k_scale;
-    p.v_inv = 1.f / d->dc.v_scale;
+    p.k_scale = dkv::Scale::of(d->dc.k_scale);
+    p.v_scale = dkv::Scale::of(d->dc.v_scale);
     // 8 dimensions a step, or 4 where the halves of pairs are no multiple of 8 apart
     const bool eights = p.interleaved || p.rot % 16u == 0;
     const uint32_t n = eights ? 8u : 4u;
