@@ -552,7 +552,8 @@ typedef struct {
     int32_t interleaved;   /* pairs are (2i, 2i + 1); else (i, i + rot_dim / 2) */
     int32_t n_axes;        /* 1 to 3 */
     int32_t sections[3];   /* pairs of each axis, one axis after the other: sum rot_dim / 2 */
-    const int32_t *positions; /* [n_axes][position_stride]: of each row; NULL (1 axis): its place in the request */
+    const int32_t *positions; /* [n_axes][position_stride]: of each row; NULL (1 axis): its place in the request, as lens and
+                                 starts have it: wrong once blocks have left (kv_evict), whose tokens still came before */
     int64_t position_stride;  /* n_rows and more, or 0: all axes have the first one's */
 } kv_put_args;
 
@@ -622,7 +623,9 @@ typedef struct {
  * of equal ones the lower entry; NaN weighs most.  Its table and mass rows close up in
  * their order, its length falls by block_size per block.  Rows have max_blocks entries;
  * behind the blocks that stay, table_out holds -1 and mass_out 0.  Keys keep the rotary
- * positions that they were put with.  Only tables change: the caller copies the blocks out
+ * positions that they were put with, so from then on tokens of such a request have to be put with
+ * `positions` that go on from there: places in the shortened request lie before or on those of
+ * keys that stayed.  Only tables change: the caller copies the blocks out
  * (kv_swap_out) if they are to be had again, and gives them back (kv_table_drop).
  * KV_EINVAL, KV_E2BIG as for kv_put.
  */

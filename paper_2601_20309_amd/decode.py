@@ -61,7 +61,8 @@ class Decoder:
                starts: Optional[torch.Tensor] = None, rope: Optional[Rope] = None,
                positions: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> int:
         """k, v [row, kv_head, dim] (and q, q_out [row, head, dim]): the last starts[s + 1] - starts[s] tokens
-        of each request s, or the last one of each.  positions: int32 [axis, row] (expanded along the axes: the same for each)."""
+        of each request s, or the last one of each.  positions: int32 [axis, row] (expanded along the axes: the same for each);
+        without them a row stands at its place in the request, which it does no more once kv_evict has shortened that."""
         if rope is None:
             return _T.put(self._spec, layer, k, v, table, lens, q, q_out, starts, None, False, (), positions, stream)
         return _T.put(self._spec, layer, k, v, table, lens, q, q_out, starts, rope.inv_freq, rope.interleaved, rope.sections,
@@ -79,7 +80,8 @@ class Decoder:
                  table_out: Optional[torch.Tensor] = None, lens_out: Optional[torch.Tensor] = None,
                  mass_out: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> int:
         """table int32 and mass float32 [request, max_blocks], lens int32 [request]; evicted_ids and
-        evicted_at int32 [request, most to leave]; outputs that are not given: in place."""
+        evicted_at int32 [request, most to leave]; outputs that are not given: in place.  Later tokens of a request that
+        gave up blocks need kv_put's positions: the keys that stay keep theirs."""
         return _T.evict(self._spec, table, lens, mass, budget, n_first, n_last, evicted_ids, evicted_at, n_evicted, table_out,
                         lens_out, mass_out, stream)
 
