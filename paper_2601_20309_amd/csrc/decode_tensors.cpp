@@ -5,6 +5,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/core/grad_mode.h>
+#include <c10/core/AutogradState.h>
 #include <c10/hip/HIPStream.h>
 #include <hip/hip_runtime_api.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -42,11 +43,18 @@ struct Call {
         }
         const at::Tensor *t = &THPVariable_Unpack(o);
         if (!t->defined() || !t->is_cuda() || t->layout() != at::kStrided || t->device().index() != device || t->is_neg() ||
-            (t->requires_grad() && at::GradMode::is_enabled())) {
+            !t->has_storage() || differentiated(*t)) {
             ok = false;
             return nullptr;
         }
         return t;
+    }
+
+    // A gradient is asked for, backward or forward (torch.no_grad() leaves the latter).
+    static bool differentiated(const at::Tensor &t)
+    {
+        return (t.requires_grad() && at::GradMode::is_enabled()) ||
+               (c10::AutogradState::get_tls_state().get_fw_grad_mode() && t._fw_grad(0).defined());
     }
 
     // [row, head, dim] of the 16-bit type, the last dimension contiguous
