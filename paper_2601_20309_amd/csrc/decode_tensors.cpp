@@ -13,6 +13,7 @@
 #include <algorithm>
 #include <cstring>
 #include <exception>
+#include <initializer_list>
 #include <new>
 
 #include "../../include/duplexkv.h"
@@ -119,6 +120,15 @@ struct Call {
         return v;
     }
 
+    // What a call has written has another version, so that a backward pass that saved it says so.  (Inference tensors
+    // have no versions.)
+    static int written(int rc, std::initializer_list<PyObject *> outputs)
+    {
+        for (PyObject *o : outputs)
+            if (rc == KV_OK && o != Py_None && !THPVariable_Unpack(o).is_inference()) THPVariable_Unpack(o).unsafeGetTensorImpl()->bump_version();
+        return rc;
+    }
+
     // None: the current stream of the decoder's device
     void *stream(PyObject *o)
     {
@@ -217,7 +227,7 @@ PyObject *put(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         }
         void *const stream = c.stream(a[13]);
         if (!c.ok || PyErr_Occurred()) return KV_EINVAL;
-        return kv_put(d->decoder, &p, stream);
+        return c.written(kv_put(d->decoder, &p, stream), {a[7]});
     });
 }
 
@@ -245,7 +255,7 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         p.mass_stride = d->max_blocks;
         void *const stream = c.stream(a[10]);
         if (!c.ok || a[2] == Py_None || a[5] == Py_None || PyErr_Occurred()) return KV_EINVAL;
-        return kv_attend(d->decoder, &p, stream);
+        return c.written(kv_attend(d->decoder, &p, stream), {a[5], a[7], a[9] == Py_None ? a[8] : a[9]});
     });
 }
 
@@ -282,7 +292,8 @@ PyObject *evict(PyObject *, PyObject *const *a, Py_ssize_t n_args)
             if (a[i] == Py_None) return KV_EINVAL;
         void *const stream = c.stream(a[13]);
         if (!c.ok || PyErr_Occurred()) return KV_EINVAL;
-        return kv_evict(d->decoder, &p, stream);
+        return c.written(kv_evict(d->decoder, &p, stream), {a[7], a[8], a[9], a[10] == Py_None ? a[1] : a[10],
+                                                            a[11] == Py_None ? a[2] : a[11], a[12] == Py_None ? a[3] : a[12]});
     });
 }
 

@@ -7,7 +7,8 @@ or laid out anew on the way: a tensor of another type, shape or device than the 
 takes, or whose last dimension is not contiguous, is refused with KV_EINVAL; so is one
 that asks for a gradient, outside torch.no_grad(), that carries a tangent of forward-mode
 differentiation, or that stands for others inside torch.func's transforms: there are no
-gradients.  A call goes to the current stream of the cache's device, unless it is given another
+gradients.  What a call writes counts as changed in place, as by torch's own operators (the
+cache does not: it is known by its address alone).  A call goes to the current stream of the cache's device, unless it is given another
 (an integer handle); as with any torch operator, tensors that are used on another stream
 than their own must not be freed before that stream is done with them.
 """

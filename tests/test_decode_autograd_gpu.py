@@ -76,3 +76,45 @@ def test_transforms_are_refused():
     torch.func.vmap(f)(q.expand(3, -1, -1, -1))
     torch.cuda.synchronize()
     assert codes == [B.KV_EINVAL] * 3 and torch.equal(calls.t["out"], before)
+
+
+def test_what_is_written_has_another_version():
+    """Outputs count as changed in place, inputs do not; a call that is refused changes nothing."""
+    calls = Calls()
+    t, versions = calls.t, lambda: {k: x._version for k, x in calls.t.items()}     # noqa: E731
+    for call, outputs in ((calls.attend, {"out", "lse", "mass_out"}), (calls.put, {"q_out"}),
+                          (calls.evict, {"ids", "at", "count", "table_out", "lens_out", "weights_out"})):
+        before = versions()
+        assert call() == B.KV_OK
+        assert {k for k, n in versions().items() if n != before[k]} == outputs
+    # in place
+    before = versions()
+    assert calls.attend(mass_out=None, out=t["q"]) == B.KV_OK and calls.put(q_out=t["q_in"]) == B.KV_OK
+    assert calls.evict(table_out=None, lens_out=None, weights_out=None) == B.KV_OK
+    assert {k for k, n in versions().items() if n != before[k]} == {"lse", "mass", "q", "q_in", "ids", "at", "count", "table", "lens", "weights"}
+    before = versions()
+    assert calls.attend(lens=t["lens"].long()) == B.KV_EINVAL and calls.evict(table=t["table"].long()) == B.KV_EINVAL
+    assert calls.put(q_out=None) == B.KV_EINVAL and versions() == before
+
+
+def test_a_backward_pass_sees_that_what_it_saved_was_overwritten():
+    """The same out for one layer after the other: a product that saved the first one's cannot go backward."""
+    calls = Calls()
+    w = torch.ones((), device="cuda", requires_grad=True)
+    assert calls.attend() == B.KV_OK
+    y = (w * calls.t["out"].float()).sum() + (w * calls.t["lse"]).sum()
+    y.backward()                                # nothing has been overwritten
+    y = (w * calls.t["lse"]).sum()
+    assert calls.attend() == B.KV_OK
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+
+
+def test_inference_tensors_are_written():
+    calls = Calls()
+    with torch.inference_mode():
+        out = torch.zeros_like(calls.t["out"])
+        assert calls.attend(out=out) == B.KV_OK
+    again = torch.zeros_like(out)
+    assert calls.attend(out=again) == B.KV_OK and torch.equal(out, again)
+    assert calls.attend(out=out) == B.KV_OK and torch.equal(out, again)
