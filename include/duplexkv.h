@@ -593,8 +593,8 @@ typedef struct {
  * weights that the tokens of block j got, summed over the query heads (n_heads in all,
  * per request), j below the request's blocks; behind these it is mass[s][j].  The result
  * is the same, bit for bit, whenever the same call runs with the same lens.
- * out may be q itself.  KV_EINVAL, KV_EUNSUP, KV_E2BIG as for kv_put; KV_EUNSUP for mass_out
- * without `weigh`.
+ * out may be q itself.  KV_EINVAL, KV_EUNSUP, KV_E2BIG as for kv_put; KV_EINVAL for a scale that is no
+ * number or, times k_scale and log2(e), too large for a float; KV_EUNSUP for mass_out without `weigh`.
  */
 int kv_attend(kv_decoder *decoder, const kv_attend_args *args, void *stream);
 

@@ -316,7 +316,9 @@ int kv_put(kv_decoder *d, const kv_put_args *a, void *stream)
 
 int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
 {
-    if (!d || !a || a->layer < 0 || a->layer >= d->cfg.n_layers || a->n_seqs < 0 || !std::isfinite(a->scale)) return KV_EINVAL;
+    if (!d || !a || a->layer < 0 || a->layer >= d->cfg.n_layers || a->n_seqs < 0) return KV_EINVAL;
+    const float qk_scale = (float)((double)a->scale * 1.4426950408889634074 * (double)d->dc.k_scale);
+    if (!std::isfinite(qk_scale)) return KV_EINVAL;
     if (a->n_seqs > d->dc.max_seqs) return KV_E2BIG;
     if (a->n_seqs > 0 && (!a->table || !a->lens || !a->q.data || !a->out.data)) return KV_EINVAL;
     if (!rows_ok(a->q) || !rows_ok(a->out)) return KV_EINVAL;
@@ -377,7 +379,7 @@ int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
     const uint32_t numbers = p.block_size / p.granule * p.n_heads;
     const uint64_t mass_wgs = (uint64_t)p.n_seqs * p.max_blocks / dkv::mass_blocks(4u);
     p.mass_bits = numbers <= 32u ? 2u : numbers <= 64u && mass_wgs > 8ull * (uint32_t)d->n_cus ? 3u : 4u;
-    p.qk_scale = (float)((double)a->scale * 1.4426950408889634074 * (double)d->dc.k_scale);
+    p.qk_scale = qk_scale;
     p.v_scale = d->dc.v_scale;
     const uint32_t tiles = (p.max_tokens + dkv::kTile - 1) / dkv::kTile;
     // Up to 16 requests: half as many units, and two waves each, to a workgroup, so that ranges are longer and leave half as many
