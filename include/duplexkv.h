@@ -516,7 +516,7 @@ typedef struct {
  * 256 or no multiple of 8, more than 1024 query heads, a cache that is not
  * aligned to 16 bytes or of 2^32 and more token rows per KV plane, more than 65535
  * requests, 2^31 and more tokens in a table row, tiles of 32 tokens in all or, with
- * `weigh`, tokens of a block times query heads.  KV_ENOMEM, KV_EHIP.
+ * `weigh`, tokens of a block times query heads, and more than 2^28 blocks.  KV_ENOMEM, KV_EHIP.
  */
 int kv_decoder_create(kv_decoder **decoder, const kv_config *cfg, const kv_decoder_config *dc, void *hbm_cache);
 

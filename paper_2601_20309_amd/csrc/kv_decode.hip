@@ -149,8 +149,8 @@ int kv_decoder_create(kv_decoder **out, const kv_config *cfg, const kv_decoder_c
     if (tokens > 0x7FFFFFC0 || dc->max_seqs > 65535 || (tokens / dkv::kTile + 1) * dc->max_seqs > 0x7FFFFFFF) return KV_EUNSUP;
     const uint64_t token_bytes = (uint64_t)cfg->n_kv_heads * (uint64_t)cfg->head_dim * (uint64_t)cfg->elem_bytes;
     const uint64_t cells = (uint64_t)cfg->block_size * (cfg->hbm_layout == KV_HBM_BLOCK_FIRST ? 2ull * cfg->n_layers : 1ull);
-    // granules of a block, over all query heads, are counted in 31 bits
-    if (dc->weigh && (uint64_t)cfg->block_size * (uint64_t)dc->n_heads > 0x7FFFFFFFull) return KV_EUNSUP;
+    // granules of a block, over all query heads, are counted in 31 bits, and the lanes that add them up in 32
+    if (dc->weigh && ((uint64_t)cfg->block_size * (uint64_t)dc->n_heads > 0x7FFFFFFFull || dc->max_blocks > (1 << 28))) return KV_EUNSUP;
     if (token_bytes >> 31 || cells >> 31 || cells * (uint64_t)cfg->n_hbm_blocks >= 0xFFFFFFFFull) return KV_EUNSUP;
     int ndev = 0;
     if (hipGetDeviceCount(&ndev) != hipSuccess || ndev <= 0) {

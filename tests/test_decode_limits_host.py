@@ -19,7 +19,7 @@ def limits(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("what", ["scales"])
+@pytest.mark.parametrize("what", ["scales", "grids"])
 def test_limits(limits, what):
     run = subprocess.run([limits, what], capture_output=True, text=True, timeout=300)
     assert run.returncode == 0, run.stdout[-1000:] + run.stderr[-3000:]
