@@ -71,12 +71,14 @@ struct Fp16 {
         return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HI));
     }
     static constexpr uint32_t kOnes = 0x3C003C00u;
-    // As above, of 11 digits each, within 2^-21; each at least the smallest number there is, 2^-24.
+    // As above, of 11 digits each, within 2^-21; each at least the smallest number there is, 2^-24, if there is a weight (no
+    // weight that is one is below 2^-126).
     static __device__ __forceinline__ void split(float a, float b, uint32_t &upper, uint32_t &lower)
     {
-        const auto cut = __builtin_amdgcn_cvt_pkrtz(fmaxf(a, 0x1p-24f), fmaxf(b, 0x1p-24f));
+        const float u = fminf(a * 0x1p102f, 0x1p-24f), v = fminf(b * 0x1p102f, 0x1p-24f);
+        const auto cut = __builtin_amdgcn_cvt_pkrtz(fmaxf(a, u), fmaxf(b, v));
         upper = __builtin_bit_cast(uint32_t, cut);
-        lower = pack(fmaxf(a - (float)cut[0], 0x1p-24f), fmaxf(b - (float)cut[1], 0x1p-24f));
+        lower = pack(fmaxf(a - (float)cut[0], u), fmaxf(b - (float)cut[1], v));
     }
 };
 
@@ -124,7 +126,7 @@ struct Divide {
 // result is as far from 64 bits as its own rounding.  Beside outputs in bf16 8-bit values are taken as fp16, which holds them
 // exactly, and one fp16 number is enough for a weight.  Root of the mean square of the relative error, 1e-4, a number
 // of the output's type / so: bf16, 3 requests of 100 tokens 16.8 / 15.6, 32 around 1000 17.0 / 16.5; fp16 1.62 / 1.53; bf16 beside
-// 8-bit values 16.8 / 16.5.  us: 5.6 / 5.7; 35.3 / 35.7; 4 requests of 32768 tokens 87.7 / 88.1; fp16, 37 to 1700 13.6 / 13.9, 119 to 1100
+// 8-bit values 16.8 / 16.5.  us: 5.6 / 5.7; 35.3 / 35.7; 4 requests of 32768 tokens 87.7 / 88.1; fp16, 37 to 1700 13.9 / 14.5, 119 to 1100
 // and one head of 128 17.3 / 18.0; 8-bit, 128 around 600 38.1 / 38.4 (two numbers 39.0).
 //
 // Keys are read with plain loads (a row's 128-byte lines are met by several loads of a wave, which find them in the

@@ -67,3 +67,23 @@ def test_a_value_of_infinity_stays_one(types, n, p, below):
     rest = torch.ones(64, dtype=torch.bool, device="cuda")
     rest[[5, 6, 9, 11]] = False
     assert torch.equal(got[..., rest], want[..., rest])
+
+
+@pytest.mark.parametrize("types", [("bf16", "bf16"), ("fp16", "fp16")], ids="-".join)
+@pytest.mark.parametrize("n", [40, 9000])
+def test_scores_of_minus_infinity_weigh_nothing(types, n):
+    """Not even beside the largest values there are, and many of them."""
+    c = Case(1, 2, 64, lens=(n,), types=types, seed=n)
+    k, v = c.plane(0), c.plane(1)
+    q = (c.queries().abs() + 0.25).cuda()
+    table, lens = c.table.cuda(), c.lens.cuda()
+    some = torch.tensor([t for t in range(n) if t % 3], device="cuda")
+    page, row = table[0, some // 16].long(), some % 16
+    k[page, row] = 0.0
+    k[page, row, :, 0] = float("-inf")
+    want, got = torch.empty_like(q), torch.empty_like(q)
+    v[page, row] = 0.0
+    assert c.dec.kv_attend(c.layer, q, table, lens, want) == 0 and torch.isfinite(want).all()
+    v[page, row] = torch.finfo(c.x).max
+    assert c.dec.kv_attend(c.layer, q, table, lens, got) == 0
+    assert torch.equal(got, want)
