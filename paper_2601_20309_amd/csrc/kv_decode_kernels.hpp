@@ -608,7 +608,8 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
                     own += x[o].z * scale[o];
                 }
             }
-            const float total = sum[0], inv = total == 0.f ? 0.f : p.v_scale / total;
+            // (times v_scale afterwards: v_scale / total is too small a number sooner than the result)
+            const float total = sum[0], inv = total == 0.f ? 0.f : 1.0f / total, v_scale = FP8 ? p.v_scale : 1.0f;
             if (has_row && sub == 0u && kq == 0u) {
                 const float l2 = own == 0.f ? -__builtin_inff() : ref + __builtin_amdgcn_logf(own);
                 if (!whole) p.part_ml[(uint64_t)slot * p.n_heads + head] = f32x4{ref, total, own, l2};
@@ -625,7 +626,7 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
                             const f32x4 *a = acc + c * VW;
                             uint32_t w[VW / 2];
 #pragma unroll
-                            for (int i = 0; i < VW / 2; i++) w[i] = X::pack(a[2 * i][r] * inv, a[2 * i + 1][r] * inv);
+                            for (int i = 0; i < VW / 2; i++) w[i] = X::pack(a[2 * i][r] * inv * v_scale, a[2 * i + 1][r] * inv * v_scale);
                             if (WHOLE || d < p.dim)
                                 *reinterpret_cast<typename Raw<2 * VW>::type *>(out + (uint64_t)head * p.out_head + d * 2u) =
                                     __builtin_bit_cast(typename Raw<2 * VW>::type, w);
@@ -651,7 +652,8 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
                         for (int r = 0; r < 4; r++) {
                             const uint32_t d = i0 / 8u * 128u + (kq * 4u + (uint32_t)r) * VW + i0 % 8u;
                             if (WHOLE || d < p.dim)
-                                *reinterpret_cast<uint32_t *>(out + (uint64_t)head * p.out_head + d * 2u) = X::pack(a[0][r] * inv, a[1][r] * inv);
+                                *reinterpret_cast<uint32_t *>(out + (uint64_t)head * p.out_head + d * 2u) =
+                                    X::pack(a[0][r] * inv * v_scale, a[1][r] * inv * v_scale);
                         }
                     } else if (has_row) {
                         part[(i0 * 4u + kq) * p.part_rows + n] = a[0];
@@ -765,15 +767,15 @@ __device__ __forceinline__ void join(const AttendParams &p, uint32_t s, uint32_t
             }
         }
         if (!here || c != 0u) continue;
-        const float inv = j.sum == 0.f ? 0.f : p.v_scale / j.sum;
+        const float inv = j.sum == 0.f ? 0.f : 1.0f / j.sum;
         const uint32_t vw = p.dim <= 64u ? 4u : 8u;
         uint8_t *const to = p.out + (uint64_t)s * p.out_row + (uint64_t)head * p.out_head;
 #pragma unroll
         for (int r = 0; r < 4; r++) {
             const uint32_t d = i4 / 2u * 128u + (kq * 4u + (uint32_t)r) * vw + (i4 & 1u) * 4u;
             if (d < p.dim)
-                *reinterpret_cast<w32x2 *>(to + d * 2u) = w32x2{X::pack(j.all[0][r] * inv, j.all[1][r] * inv),
-                                                                X::pack(j.all[2][r] * inv, j.all[3][r] * inv)};
+                *reinterpret_cast<w32x2 *>(to + d * 2u) = w32x2{X::pack(j.all[0][r] * inv * p.v_scale, j.all[1][r] * inv * p.v_scale),
+                                                                X::pack(j.all[2][r] * inv * p.v_scale, j.all[3][r] * inv * p.v_scale)};
         }
         if (p.lse && row_of_i4 == 0u)
             p.lse[(uint64_t)s * p.n_heads + head] =

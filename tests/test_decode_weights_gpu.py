@@ -87,3 +87,18 @@ def test_scores_of_minus_infinity_weigh_nothing(types, n):
     v[page, row] = torch.finfo(c.x).max
     assert c.dec.kv_attend(c.layer, q, table, lens, got) == 0
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("v_scale", [1e-38, 1e-30, 1e35])
+@pytest.mark.parametrize("lens", [(9000, 5), (40, 3)])
+def test_scales_near_the_ends_of_what_a_float_holds(v_scale, lens):
+    """Nothing on the way to a result that bf16 holds is too small or too large for 32 bits."""
+    types = ("bf16", "fp8")
+    c = Case(1, 2, 64, lens=lens, types=types, seed=51, k_scale=0.02, v_scale=v_scale)
+    c.plane(1).copy_(torch.randint(0, 0x7F, c.plane(1).shape, generator=c.g, dtype=torch.uint8))     # none below 0: results are no less
+    q = c.queries()
+    ref = R.attend(q.double(), c.values(0), c.values(1), c.table, c.lens, 0.125, c.n_blocks)
+    out = torch.empty(q.shape, dtype=c.x, device="cuda")
+    assert c.dec.kv_attend(c.layer, q.cuda(), c.table.cuda(), c.lens.cuda(), out) == 0
+    off, most = (out.cpu().double() - ref["out"]).abs(), bound(ref, c.lens, 64, types, c.x)
+    assert (off <= most).all(), f"off by {(off / most).max():.2f} of the bound"
