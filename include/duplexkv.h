@@ -588,7 +588,7 @@ typedef struct {
  * out = softmax(scale * q K^T) V of each request and query head over the request's
  * tokens in present pages; 0 where there are none.  Products and sums in 32 bits; what a
  * weight is as it meets V is off by at most 2^-15 of it (x_type bf16; 2^-11 with a KV_FP8 cache) or
- * 2^-21 (fp16), and 2^-35 of the largest.  A value of infinity whose weight is above 2^-100 of the largest
+ * 2^-21 (fp16), and 2^-35 of the largest.  A value of infinity whose weight is above 2^-90 of the largest
  * gives infinity.  mass_out[s][j] = mass[s][j] + the
  * weights that the tokens of block j got, summed over the query heads (n_heads in all,
  * per request), j below the request's blocks; behind these it is mass[s][j].  The result

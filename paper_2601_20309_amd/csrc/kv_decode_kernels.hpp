@@ -19,8 +19,9 @@ struct Bf16 {
     typedef __bf16 x8 __attribute__((ext_vector_type(8)));
     typedef __bf16 x2 __attribute__((ext_vector_type(2)));
     // Weights are exp2(score - reference): the reference is at most kSlack + kBias below the largest score, so that it
-    // and all sums change scale only when a score is 2^kSlack times above what was met before.
-    static constexpr float kBias = 0.0f, kSlack = 8.0f;
+    // and all sums change scale only when a score is 2^kSlack times above what was met before.  The largest weights lie between 2^-16
+    // and 2^-8 here, so that sums of the largest values that bf16 has stay within 32 bits.
+    static constexpr float kBias = -16.0f, kSlack = 8.0f;
     static __device__ __forceinline__ f32x4 mma(w32x4 a, w32x4 b, f32x4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);

@@ -102,3 +102,19 @@ def test_scales_near_the_ends_of_what_a_float_holds(v_scale, lens):
     assert c.dec.kv_attend(c.layer, q.cuda(), c.table.cuda(), c.lens.cuda(), out) == 0
     off, most = (out.cpu().double() - ref["out"]).abs(), bound(ref, c.lens, 64, types, c.x)
     assert (off <= most).all(), f"off by {(off / most).max():.2f} of the bound"
+
+
+@pytest.mark.parametrize("types", ALL_TYPES, ids="-".join)
+@pytest.mark.parametrize("lens", [(2, 40, 1), (5000, 300)])
+def test_the_largest_values_have_a_mean(types, lens):
+    """Sums over tokens stay within 32 bits where every value is the type's largest, or half of it."""
+    c = Case(2, 2, 64, lens=lens, types=types, seed=52)
+    top = 448.0 if types[1] == "fp8" else torch.finfo(c.x).max
+    for dims, value in ((slice(0, 32), top), (slice(32, 64), -top / 2)):
+        to = c.plane(1)[..., dims]
+        to.copy_(torch.full(to.shape, value).to(torch.float8_e4m3fn).view(torch.uint8) if types[1] == "fp8" else torch.full(to.shape, value))
+    for much in (0.0, 1.0):
+        q = c.queries(much).cuda()
+        out = torch.empty_like(q)
+        assert c.dec.kv_attend(c.layer, q, c.table.cuda(), c.lens.cuda(), out) == 0
+        assert (out[..., :32] == top).all() and (out[..., 32:] == -top / 2).all()
