@@ -489,7 +489,8 @@ int kv_sched_lvf(const kv_sched_params *params, const kv_sched_req *reqs, int32_
  * kv_attend's calls share the decoder's memory.  Steps that overlap in time
  * take a decoder each; any number may exist over one cache.  The caller orders
  * them against transfers, too: a block that a swap-in fills is read after
- * kv_wait() or kv_stream_wait_layer().
+ * kv_wait() or kv_stream_wait_layer().  What a call writes shares no memory with anything else
+ * that the call names, except where said.
  * ------------------------------------------------------------------------ */
 #define KV_BF16 0
 #define KV_FP16 1
@@ -559,8 +560,8 @@ typedef struct {
 
 /*
  * New tokens go into the cache, layer by layer.  With a = position[axis of pair i] *
- * inv_freq[i] (the product, its cosine and its sine as exact as float holds them, at far
- * positions too) a pair (x, y) of q and k becomes (x cos a - y sin a, y cos a + x sin a),
+ * inv_freq[i] (its cosine and its sine are off by at most 2^-22 up to angles of 2^24, 2^-20 at
+ * positions of 2^31) a pair (x, y) of q and k becomes (x cos a - y sin a, y cos a + x sin a),
  * in 32 bits, rounded once.  An 8-bit cache holds the nearest of value / scale, at most
  * 448 either way; NaN stays NaN.  Tokens whose block is no page, or that lie beyond
  * max_blocks, are left out of the cache (their q is rotated all the same).  Two tokens

@@ -76,7 +76,7 @@ struct Workgroup {
     }
 };
 
-// ranges: as many workgroups as the chip holds at once
+// ranges: a workgroup per compute unit
 uint32_t ranges(const kv_decoder *d, const Workgroup &w)
 {
     return std::max(1u, std::min(dkv::kMaxGroups, (uint32_t)d->n_cus / w.per_range));
@@ -192,7 +192,7 @@ int kv_decoder_create(kv_decoder **out, const kv_config *cfg, const kv_decoder_c
     };
     if (!on.ok() || hipDeviceGetAttribute(&d->n_cus, hipDeviceAttributeMultiprocessorCount, d->device) != hipSuccess)
         return fail(KV_EHIP);
-    // ranges: as many workgroups as the chip holds at once, no more than there can be turns
+    // ranges: a workgroup per compute unit, no more than there can be turns
     const uint64_t most_tiles = (uint64_t)dc->max_seqs * (((uint64_t)dc->max_blocks * cfg->block_size + dkv::kTile - 1) / dkv::kTile);
     d->max_groups = (uint32_t)std::min<uint64_t>(ranges(d, Workgroup(d->units, d->waves, d->waves)), most_tiles);
     const uint64_t slots = 2ull * d->max_groups;

@@ -137,7 +137,7 @@ struct Divide {
 // 8-bit, 128 around 600, 37.4 / 39.2 / 41.6.
 //
 // The 4 requests of 32768 tokens are 537 MB: 6.1 TB/s, of them some 5 us until all keys are under way and 6.4 TB/s from
-// then on.  Counters: each byte of the cache fetched once, no LDS bank conflicts.
+// then on.  Counters: 4.199 million reads of 128 bytes, 537 MB: each byte of the cache once; no LDS bank conflicts.
 
 struct AttendParams {
     const uint8_t *k, *v;      // the layer's planes

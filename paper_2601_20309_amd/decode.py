@@ -4,13 +4,16 @@ eviction of the blocks that attention has weighed least.
 
 Same names, rules and result codes as include/duplexkv.h.  Nothing is copied, cast
 or laid out anew on the way: a tensor of another type, shape or device than the call
-takes, or whose last dimension is not contiguous, is refused with KV_EINVAL; so is one
-that asks for a gradient, outside torch.no_grad(), that carries a tangent of forward-mode
-differentiation, or that stands for others inside torch.func's transforms: there are no
-gradients.  What a call writes counts as changed in place, as by torch's own operators (the
-cache does not: it is known by its address alone).  A call goes to the current stream of the cache's device, unless it is given another
-(an integer handle); as with any torch operator, tensors that are used on another stream
-than their own must not be freed before that stream is done with them.
+takes, or whose last dimension is not contiguous, is refused with KV_EINVAL.  Rows of q,
+k, v and the outputs beside them, of positions and of kv_put's and kv_attend's tables may
+lie apart; every other tensor is contiguous as a whole.  A tensor that asks for a gradient,
+outside torch.no_grad(), that carries a tangent of forward-mode differentiation, or that
+stands for others inside torch.func's transforms is refused too: there are no gradients.
+What a call writes counts as changed in place, as by torch's own operators (the cache does
+not: it is known by its address alone).  A call goes to the current stream of the cache's
+device, unless it is given another (an integer handle); as with any torch operator, tensors
+that are used on another stream than their own must not be freed before that stream is done
+with them.
 """
 from __future__ import annotations
 
