@@ -18,9 +18,9 @@ typedef w32x4 w32x4_by8 __attribute__((aligned(8)));  // where rows of 8-bit val
 struct Bf16 {
     typedef __bf16 x8 __attribute__((ext_vector_type(8)));
     typedef __bf16 x2 __attribute__((ext_vector_type(2)));
-    // Weights are exp2(score - reference): the reference is at most kSlack + kBias below the largest score, so that it
-    // and all sums change scale only when a score is 2^kSlack times above what was met before.  The largest weights lie between 2^-16
-    // and 2^-8 here, so that sums of the largest values that bf16 has stay within 32 bits.
+    // Weights are exp2(score - reference), the largest between 2^kBias and 2^(kBias + kSlack), so that the reference and
+    // all sums change scale only when a score is kSlack above what was met before.  Between 2^-16 and 2^-8 here: sums of the
+    // largest values that bf16 has stay within 32 bits.
     static constexpr float kBias = -16.0f, kSlack = 8.0f;
     static __device__ __forceinline__ f32x4 mma(w32x4 a, w32x4 b, f32x4 c)
     {
@@ -38,7 +38,7 @@ struct Bf16 {
     {
         return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
     }
-    // Two weights as two numbers of 8 digits each: the upper one cut off, the lower the nearest to what that leaves, together
+    // Each of two weights as the sum of two numbers of 8 digits, the upper cut off, the lower the nearest to what that leaves:
     // within 2^-15.  The lower one gets 2^-20 of the weight on top, so that it is never 0 beside one: 0 times a value
     // of infinity is NaN.
     static __device__ __forceinline__ void split(float a, float b, uint32_t &upper, uint32_t &lower)
@@ -132,7 +132,7 @@ struct Divide {
 //
 // Keys are read with plain loads (a row's 128-byte lines are met by several loads of a wave, which find them in the
 // CU's cache), whole values past the caches: 16 lanes take a row at once.  us of this kernel as it is / with keys past the
-// caches too / with values through them: 32 requests around 1000 tokens, 32 query heads over 8 of 128, bf16 35.6 /
+// caches too / with values through them (weights of one number each): 32 requests around 1000 tokens, 32 query heads over 8 of 128, bf16 35.6 /
 // 38.1 / 40.9; 4 of 32768 tokens, 64 over 8 of 128, 88.8 / 88.9 / 95.0; 4 of 32768, 8 heads of 96, 77.0 / 87.9 / 76.3;
 // 8-bit, 128 around 600, 37.4 / 39.2 / 41.6.
 //
