@@ -495,19 +495,25 @@ int kv_sched_lvf(const kv_sched_params *params, const kv_sched_req *reqs, int32_
 #define KV_BF16 0
 #define KV_FP16 1
 #define KV_FP8  2   /* e4m3: 448 is the largest, there is no infinity */
+#define KV_FP4  3   /* e2m1 with a power of 2 for each 32 dimensions of a head, 17 bytes for 32.  A token's row in a plane:
+                       first n_kv_heads * dim / 2 bytes of numbers, the even dimension of two in the low half (the sign above
+                       the place among 0, 0.5, 1, 1.5, 2, 3, 4, 6), then n_kv_heads * dim / 32 bytes b that stand for 2^(b - 127),
+                       255 for NaN.  elem_bytes is 1 and head_dim of kv_config dim / 32 * 17, the bytes of a head */
 
 typedef struct kv_decoder kv_decoder; /* opaque, owned by the library */
 
 typedef struct {
     int32_t n_heads;     /* query heads, a multiple of n_kv_heads: query head i reads KV head i / (n_heads / n_kv_heads) */
     int32_t x_type;      /* of q, k, v and the outputs: KV_BF16 or KV_FP16 */
-    int32_t kv_type;     /* of the cache: x_type (elem_bytes 2), or KV_FP8 (elem_bytes 1) */
+    int32_t kv_type;     /* of the cache: x_type (elem_bytes 2), KV_FP8 or KV_FP4 (elem_bytes 1) */
     int32_t max_seqs;    /* most requests of a call */
     int32_t max_blocks;  /* most blocks of a request: entries of a table row */
     float k_scale;       /* what a stored 1 of K stands for (KV_FP8; else it has to be 1) */
     float v_scale;
     int32_t weigh;       /* 1: kv_attend may be asked for mass_out, which takes max_seqs * max_blocks * n_heads floats of
                             memory (as many times that as an odd block has tokens, or 4, 8 or 16 go into one) */
+    int32_t max_rows;    /* most rows of a kv_attend_rows() call; 0: none are made.  Otherwise 65536 * (64, 96, 128, 192 or 256
+                            dimensions + 2) * 4 bytes of memory: 34 MB at 128 */
 } kv_decoder_config;
 
 /*
@@ -556,6 +562,10 @@ typedef struct {
     const int32_t *positions; /* [n_axes][position_stride]: of each row; NULL (1 axis): its place in the request, as lens and
                                  starts have it: wrong once blocks have left (kv_evict), whose tokens still came before */
     int64_t position_stride;  /* n_rows and more, or 0: all axes have the first one's */
+    const float *q_norm;      /* NULL, or dim weights: each head of q becomes q / sqrt(mean(q^2) + norm_eps) * weight before it
+                                 rotates (begins on a multiple of 16 bytes; KV_EUNSUP otherwise) */
+    const float *k_norm;      /* the same for k */
+    float norm_eps;
 } kv_put_args;
 
 /*
@@ -585,6 +595,21 @@ typedef struct {
     int64_t mass_stride;
 } kv_attend_args;
 
+typedef struct {
+    int32_t layer;
+    int32_t n_seqs;
+    int32_t n_rows;        /* rows of q and out; those at and behind starts[n_seqs] are padding: not read, not written */
+    int32_t table_stride;
+    int32_t causal;        /* 1: a request's rows are its last tokens, and each sees the tokens up to and with its own; 0: all tokens */
+    float scale;           /* of the products of q and k */
+    const int32_t *table;
+    const int32_t *lens;   /* tokens of each request; causal: the rows' own included */
+    const int32_t *starts; /* n_seqs + 1: request s has rows starts[s] .. starts[s + 1] - 1; they must not fall.  NULL: one row
+                              each (n_rows == n_seqs) */
+    kv_rows q, out;
+    float *lse;            /* NULL, or [n_rows][n_heads] */
+} kv_attend_rows_args;
+
 /*
  * out = softmax(scale * q K^T) V of each request and query head over the request's
  * tokens in present pages; 0 where there are none.  Products and sums in 32 bits; what a
@@ -598,6 +623,17 @@ typedef struct {
  * number or, times k_scale and log2(e), too large for a float; KV_EUNSUP for mass_out without `weigh`.
  */
 int kv_attend(kv_decoder *decoder, const kv_attend_args *args, void *stream);
+
+/*
+ * kv_attend for several rows of every request: prompts or parts of them, drafted tokens, a decoder's rows over an
+ * encoder's states (causal 0, `lens` the encoder's).  out = softmax(scale * q K^T) V over the tokens that a row sees
+ * in present pages; 0 where there are none, and -inf in lse.  Products, references and sums in 32 bits; what a
+ * weight is as it meets V is the nearest x_type number.  What lies in rows that nothing sees, infinities and NaN among it, makes no
+ * difference; an infinite value makes what sees it infinite or, where its weight is too small for
+ * x_type, NaN.  The result is the same, bit for bit, whenever the same call runs with the same starts and lens.
+ * out may be q itself.  KV_EINVAL, KV_EUNSUP as for kv_attend; KV_E2BIG: more requests or rows than the decoder's.
+ */
+int kv_attend_rows(kv_decoder *decoder, const kv_attend_rows_args *args, void *stream);
 
 typedef struct {
     int32_t n_seqs;

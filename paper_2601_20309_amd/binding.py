@@ -31,9 +31,9 @@ EXPORTS = ["kv_seg_bytes", "kv_block_bytes", "kv_cache_bytes", "kv_pool_bytes", 
            "kv_host_pool", "kv_last_stats", "kv_probe_link", "kv_reader_start", "kv_reader_wait",
            "kv_table_create", "kv_table_destroy", "kv_table_append", "kv_table_eager", "kv_table_rotate", "kv_table_rotate_eager",
            "kv_table_finish", "kv_table_drop", "kv_table_blocks", "kv_table_get_counts", "kv_sched_vlt", "kv_sched_lvf",
-           "kv_decoder_create", "kv_decoder_destroy", "kv_put", "kv_attend", "kv_evict", "kv_strerror"]
+           "kv_decoder_create", "kv_decoder_destroy", "kv_put", "kv_attend", "kv_attend_rows", "kv_evict", "kv_strerror"]
 KV_REQ_RUNNING, KV_REQ_WAITING, KV_REQ_ROTARY = 0, 1, 2
-KV_BF16, KV_FP16, KV_FP8 = 0, 1, 2
+KV_BF16, KV_FP16, KV_FP8, KV_FP4 = 0, 1, 2, 3
 
 
 class kv_config(C.Structure):
@@ -65,7 +65,7 @@ class kv_sched_req(C.Structure):
 
 class kv_decoder_config(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_heads", "x_type", "kv_type", "max_seqs", "max_blocks")] + \
-        [("k_scale", C.c_float), ("v_scale", C.c_float), ("weigh", C.c_int32)]
+        [("k_scale", C.c_float), ("v_scale", C.c_float), ("weigh", C.c_int32), ("max_rows", C.c_int32)]
 
 
 class kv_rows(C.Structure):
@@ -76,13 +76,19 @@ class kv_put_args(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("layer", "n_seqs", "n_rows", "table_stride")] + \
         [(n, C.c_void_p) for n in ("table", "lens", "starts")] + [(n, kv_rows) for n in ("k", "v", "q", "q_out")] + \
         [("inv_freq", C.c_void_p)] + [(n, C.c_int32) for n in ("rot_dim", "interleaved", "n_axes")] + \
-        [("sections", C.c_int32 * 3), ("positions", C.c_void_p), ("position_stride", C.c_int64)]
+        [("sections", C.c_int32 * 3), ("positions", C.c_void_p), ("position_stride", C.c_int64), ("q_norm", C.c_void_p),
+         ("k_norm", C.c_void_p), ("norm_eps", C.c_float)]
 
 
 class kv_attend_args(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("layer", "n_seqs", "table_stride")] + [("scale", C.c_float)] + \
         [(n, C.c_void_p) for n in ("table", "lens")] + [(n, kv_rows) for n in ("q", "out")] + \
         [(n, C.c_void_p) for n in ("lse", "mass", "mass_out")] + [("mass_stride", C.c_int64)]
+
+
+class kv_attend_rows_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("layer", "n_seqs", "n_rows", "table_stride", "causal")] + [("scale", C.c_float)] + \
+        [(n, C.c_void_p) for n in ("table", "lens", "starts")] + [(n, kv_rows) for n in ("q", "out")] + [("lse", C.c_void_p)]
 
 
 class kv_evict_args(C.Structure):
@@ -168,7 +174,8 @@ def _load() -> C.CDLL:
     L.kv_decoder_create.argtypes = [C.POINTER(C.c_void_p), pcfg, C.POINTER(kv_decoder_config), C.c_void_p]
     L.kv_decoder_destroy.restype = C.c_int
     L.kv_decoder_destroy.argtypes = [C.c_void_p]
-    for n, args in (("kv_put", kv_put_args), ("kv_attend", kv_attend_args), ("kv_evict", kv_evict_args)):
+    for n, args in (("kv_put", kv_put_args), ("kv_attend", kv_attend_args), ("kv_attend_rows", kv_attend_rows_args),
+                    ("kv_evict", kv_evict_args)):
         getattr(L, n).restype = C.c_int
         getattr(L, n).argtypes = [C.c_void_p, C.POINTER(args), C.c_void_p]
     L.kv_strerror.restype = C.c_char_p

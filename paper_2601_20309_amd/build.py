@@ -4,18 +4,21 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
-SRCS = [os.path.join(CSRC, n) for n in ("duplexkv.hip", "kv_decode.hip", "kv_table.cpp", "kv_sched.cpp")]
+SRCS = [os.path.join(CSRC, n) for n in ("duplexkv.hip", "kv_decode.hip", "kv_rows.hip", "kv_table.cpp", "kv_sched.cpp")]
 DEPS = SRCS + [os.path.join(CSRC, "kv_kernels.hpp"), os.path.join(CSRC, "kv_engine.hpp"),
-               os.path.join(CSRC, "kv_decode_kernels.hpp"),
+               os.path.join(CSRC, "kv_decode_kernels.hpp"), os.path.join(CSRC, "kv_decoder.hpp"),
+               os.path.join(CSRC, "kv_rows.hpp"), os.path.join(CSRC, "kv_rows_kernels.hpp"),
                os.path.join(ROOT, "include", "duplexkv.h")]
 LIB = os.path.join(HERE, "libduplexkv.so")
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Wall", "-Wextra", "-Wno-unused-parameter",
     # keep the compiler from forming packed-fp32 instructions
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -37,17 +40,24 @@ def stale() -> bool:
 def build(force: bool = True, verbose: bool = False) -> str:
     if force or stale():
         hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-        cmd = [hipcc] + HIPCC_FLAGS + ["-I", os.path.join(ROOT, "include"), "-o", LIB] + SRCS
-        if verbose:
-            print(" ".join(cmd))
-        r = subprocess.run(cmd, capture_output=True, text=True)
-        err = "\n".join(l for l in r.stderr.splitlines()
-                        if "packed-fp32-ops" not in l)
-        if r.returncode != 0:
-            raise RuntimeError("hipcc failed:\n" + err)
-        if verbose and err.strip():
-            print(err, file=sys.stderr)
+        # a source at a time, all at once: those with many kernels take a minute each
+        with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(len(SRCS)) as pool:
+            objs = [os.path.join(tmp, os.path.basename(s) + ".o") for s in SRCS]
+            cmds = [[hipcc] + HIPCC_FLAGS + ["-I", os.path.join(ROOT, "include"), "-c", s, "-o", o] for s, o in zip(SRCS, objs)]
+            list(pool.map(lambda c: _hipcc(c, verbose), cmds))
+            _hipcc([hipcc, "--offload-arch=gfx950", "-fPIC", "-shared", "-o", LIB] + objs, verbose)
     return LIB
+
+
+def _hipcc(cmd, verbose):
+    if verbose:
+        print(" ".join(cmd))
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    err = "\n".join(l for l in r.stderr.splitlines() if "packed-fp32-ops" not in l)
+    if r.returncode != 0:
+        raise RuntimeError("hipcc failed:\n" + err)
+    if verbose and err.strip():
+        print(err, file=sys.stderr)
 
 
 TENSORS_SRC = os.path.join(CSRC, "decode_tensors.cpp")

@@ -186,10 +186,10 @@ PyObject *spec(PyObject *, PyObject *const *a, Py_ssize_t n)
     return capsule;
 }
 
-// put(spec, layer, k, v, table, lens, q, q_out, starts, inv_freq, interleaved, sections, positions, stream)
+// put(spec, layer, k, v, table, lens, q, q_out, starts, inv_freq, interleaved, sections, positions, q_norm, k_norm, eps, stream)
 PyObject *put(PyObject *, PyObject *const *a, Py_ssize_t n_args)
 {
-    if (!count_is(n_args, 14)) return nullptr;
+    if (!count_is(n_args, 17)) return nullptr;
     const Spec *d = spec_of(a[0]);
     if (!d) return nullptr;
     return result([&] {
@@ -225,7 +225,10 @@ PyObject *put(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         } else if (a[12] != Py_None) {
             return KV_EINVAL;
         }
-        void *const stream = c.stream(a[13]);
+        p.q_norm = c.plain<float>(a[13], at::kFloat, d->dim);
+        p.k_norm = c.plain<float>(a[14], at::kFloat, d->dim);
+        p.norm_eps = (float)PyFloat_AsDouble(a[15]);
+        void *const stream = c.stream(a[16]);
         if (!c.ok || PyErr_Occurred()) return KV_EINVAL;
         return c.written(kv_put(d->decoder, &p, stream), {a[7]});
     });
@@ -256,6 +259,34 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n_args)
         void *const stream = c.stream(a[10]);
         if (!c.ok || a[2] == Py_None || a[5] == Py_None || PyErr_Occurred()) return KV_EINVAL;
         return c.written(kv_attend(d->decoder, &p, stream), {a[5], a[7], a[9] == Py_None ? a[8] : a[9]});
+    });
+}
+
+// attend_rows(spec, layer, q, table, lens, out, starts, causal, scale, lse, stream)
+PyObject *attend_rows(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    if (!count_is(n_args, 11)) return nullptr;
+    const Spec *d = spec_of(a[0]);
+    if (!d) return nullptr;
+    return result([&] {
+        Call c(d);
+        kv_attend_rows_args p;
+        memset(&p, 0, sizeof p);
+        p.layer = (int32_t)c.number(a[1], INT32_MIN, INT32_MAX);
+        const int64_t n = c.length(a[4], 1), rows = c.length(a[2], 3);
+        p.n_seqs = (int32_t)n;
+        p.n_rows = (int32_t)rows;
+        p.q = c.rows(a[2], d->x, rows, d->n_heads, d->dim);
+        p.table = c.table(a[3], n, d->max_blocks, p.table_stride);
+        p.lens = c.plain<int32_t>(a[4], at::kInt, n);
+        p.out = c.rows(a[5], d->x, rows, d->n_heads, d->dim);
+        p.starts = c.plain<int32_t>(a[6], at::kInt, n + 1);
+        p.causal = PyObject_IsTrue(a[7]);
+        p.scale = a[8] == Py_None ? d->scale : (float)PyFloat_AsDouble(a[8]);
+        p.lse = c.plain<float>(a[9], at::kFloat, rows, d->n_heads);
+        void *const stream = c.stream(a[10]);
+        if (!c.ok || a[5] == Py_None || PyErr_Occurred()) return KV_EINVAL;
+        return c.written(kv_attend_rows(d->decoder, &p, stream), {a[5], a[9]});
     });
 }
 
@@ -300,6 +331,7 @@ PyObject *evict(PyObject *, PyObject *const *a, Py_ssize_t n_args)
 PyMethodDef methods[] = {{"spec", (PyCFunction)(void *)spec, METH_FASTCALL, nullptr},
                          {"put", (PyCFunction)(void *)put, METH_FASTCALL, nullptr},
                          {"attend", (PyCFunction)(void *)attend, METH_FASTCALL, nullptr},
+                         {"attend_rows", (PyCFunction)(void *)attend_rows, METH_FASTCALL, nullptr},
                          {"evict", (PyCFunction)(void *)evict, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 

@@ -9,56 +9,12 @@
 #include <numeric>
 #include <type_traits>
 
-#include "../../include/duplexkv.h"
-#include "kv_decode_kernels.hpp"
+#include "kv_decoder.hpp"
+#include "kv_rows.hpp"
 
-struct kv_decoder {
-    kv_config cfg;
-    kv_decoder_config dc;
-    int device = 0, n_cus = 0;
-    uint8_t *hbm = nullptr;
-    uint32_t token_bytes = 0, cells_per_block = 0;
-    uint64_t plane_bytes = 0;  // from K to V of a layer, and half the way to the next layer
-    // kv_attend: most waves of a workgroup, units (up to 16 query heads of a KV head), and the most ranges that there is memory for
-    uint32_t waves = 0, units = 0, head_tiles = 0, max_groups = 0;
-    uint32_t part_rows = 0, part_vecs = 0;
-    uint32_t granule = 0, max_granules = 0;
-    // one allocation, in this order
-    dkv::f32x4 *part = nullptr;
-    dkv::f32x4 *part_ml = nullptr;
-    float *lse2 = nullptr, *granules = nullptr;
-};
+using dkv::OnDevice, dkv::apart, dkv::plane, dkv::rows_aligned, dkv::rows_ok;
 
 namespace {
-
-#define DECTRY(call)                                                                                            \
-    do {                                                                                                        \
-        hipError_t err_ = (call);                                                                               \
-        if (err_ != hipSuccess) {                                                                               \
-            fprintf(stderr, "duplexkv: %s failed: %s (%s:%d)\n", #call, hipGetErrorString(err_), __FILE__, __LINE__); \
-            return KV_EHIP;                                                                                     \
-        }                                                                                                       \
-    } while (0)
-
-// The decoder's device is the current one for as long as this lives.
-class OnDevice {
-  public:
-    explicit OnDevice(int device)
-    {
-        if (hipGetDevice(&before_) != hipSuccess) return;
-        ok_ = before_ == device || hipSetDevice(device) == hipSuccess;
-        moved_ = ok_ && before_ != device;
-    }
-    ~OnDevice()
-    {
-        if (moved_) (void)hipSetDevice(before_);
-    }
-    bool ok() const { return ok_; }
-
-  private:
-    int before_ = 0;
-    bool ok_ = false, moved_ = false;
-};
 
 constexpr uint32_t kFewRequests = 16;
 constexpr int32_t kMostRows = 0xFFFFFF;  // of a kv_put: as many workgroups of 256 lanes as a launch can count lanes
@@ -82,29 +38,10 @@ uint32_t ranges(const kv_decoder *d, const Workgroup &w)
     return std::max(1u, std::min(dkv::kMaxGroups, (uint32_t)d->n_cus / w.per_range));
 }
 
-bool rows_ok(const kv_rows &r) { return r.row >= 0 && r.head >= 0; }
-// 16-bit elements: rows begin on multiples of 16 bytes
-bool rows_aligned(const kv_rows &r) { return (uintptr_t)r.data % 16 == 0 && r.row % 8 == 0 && r.head % 8 == 0; }
-
-// rows that are written lie apart, token by token or head by head
-bool apart(const kv_rows &r, int32_t n, int32_t heads, int32_t dim)
-{
-    const auto spans = [](int64_t outer, int64_t inner, int32_t n_outer, int32_t n_inner, int32_t dim) {
-        const __int128 span = (__int128)inner * (n_inner - 1) + dim;
-        return (n_inner < 2 || inner >= dim) && (n_outer < 2 || outer >= span);
-    };
-    return n <= 0 || spans(r.row, r.head, n, heads, dim) || spans(r.head, r.row, heads, n, dim);
-}
-
-uint8_t *plane(const kv_decoder *d, int32_t layer, int which)
-{
-    return d->hbm + (2ull * (uint64_t)layer + (uint64_t)which) * d->plane_bytes;
-}
-
 int kinds(const kv_decoder *d, int &dp)
 {
-    dp = d->cfg.head_dim <= 64 ? 64 : d->cfg.head_dim <= 128 ? 128 : 256;
-    return (d->dc.x_type == KV_FP16 ? 1 : 0) + (d->dc.kv_type == KV_FP8 ? 2 : 0);
+    dp = d->dim <= 64 ? 64 : d->dim <= 128 ? 128 : 256;
+    return (d->dc.x_type == KV_FP16 ? 1 : 0) + (d->dc.kv_type == KV_FP8 ? 2 : d->dc.kv_type == KV_FP4 ? 4 : 0);
 }
 
 template <typename X, bool FP8>
@@ -114,13 +51,25 @@ void launch_put(bool eights, uint32_t threads, hipStream_t s, const dkv::PutPara
     else hipLaunchKernelGGL((dkv::kv_put_kernel<X, FP8, 4>), dim3(p.n_rows), dim3(threads), 0, s, p);
 }
 
-template <typename X, bool FP8>
+// Normed heads, or 4 bits.
+template <typename X, int KIND>
+void launch_put_heads(hipStream_t s, const dkv::PutParams &p)
+{
+    uint32_t bits = 0;
+    while ((8u << bits) < p.dim) bits++;
+    const uint32_t heads = (p.qs ? p.n_heads : 0u) + 2u * p.n_kv_heads;
+    const uint32_t most = p.n_rows <= 1024u ? 512u : 256u, lanes = heads << bits, turns = (lanes + most - 1u) / most;
+    const uint32_t threads = ((lanes + turns - 1u) / turns + 63u) / 64u * 64u;
+    hipLaunchKernelGGL((dkv::kv_put_heads_kernel<X, KIND>), dim3(p.n_rows), dim3(threads), 0, s, p, bits);
+}
+
+template <typename X, int KIND>
 void launch_attend(int dp, dim3 g, dim3 b, hipStream_t s, const dkv::AttendParams &p)
 {
     auto go = [&](auto dims) {
         constexpr int DP = decltype(dims)::value;
-        if ((int)p.dim == DP) hipLaunchKernelGGL((dkv::kv_attend_kernel<X, FP8, DP, true>), g, b, 0, s, p);
-        else hipLaunchKernelGGL((dkv::kv_attend_kernel<X, FP8, DP, false>), g, b, 0, s, p);
+        if ((int)p.dim == DP) hipLaunchKernelGGL((dkv::kv_attend_kernel<X, KIND, DP, true>), g, b, 0, s, p);
+        else hipLaunchKernelGGL((dkv::kv_attend_kernel<X, KIND, DP, false>), g, b, 0, s, p);
     };
     if (dp == 64) go(std::integral_constant<int, 64>{});
     else if (dp == 128) go(std::integral_constant<int, 128>{});
@@ -139,11 +88,17 @@ int kv_decoder_create(kv_decoder **out, const kv_config *cfg, const kv_decoder_c
     if (!cache_bytes || !dc || !hbm_cache) return KV_EINVAL;
     if (dc->n_heads <= 0 || dc->n_heads % cfg->n_kv_heads != 0 || dc->max_seqs <= 0 || dc->max_blocks <= 0) return KV_EINVAL;
     if (dc->x_type != KV_BF16 && dc->x_type != KV_FP16) return KV_EINVAL;
-    if (dc->kv_type == KV_FP8 ? cfg->elem_bytes != 1 : dc->kv_type != dc->x_type || cfg->elem_bytes != 2) return KV_EINVAL;
+    if (dc->kv_type == KV_FP8 || dc->kv_type == KV_FP4 ? cfg->elem_bytes != 1 : dc->kv_type != dc->x_type || cfg->elem_bytes != 2)
+        return KV_EINVAL;
+    // 4 bits: 17 bytes of a row are 32 dimensions
+    const bool fp4 = dc->kv_type == KV_FP4;
+    if (fp4 && cfg->head_dim % 17 != 0) return KV_EINVAL;
+    const int64_t dim = fp4 ? (int64_t)cfg->head_dim / 17 * 32 : cfg->head_dim;
+    if (dc->max_rows < 0) return KV_EINVAL;
     for (float scale : {dc->k_scale, dc->v_scale})
         if (!(scale > 0.f) || !std::isfinite(scale) || !std::isfinite(1.f / scale) || (dc->kv_type != KV_FP8 && scale != 1.f))
             return KV_EINVAL;
-    if (cfg->head_dim > 256 || cfg->head_dim % 8 != 0 || dc->n_heads > 1024 || (uintptr_t)hbm_cache % 16 != 0) return KV_EUNSUP;
+    if (dim > 256 || dim % 8 != 0 || dc->n_heads > 1024 || (uintptr_t)hbm_cache % 16 != 0) return KV_EUNSUP;
     // tokens of a request, tiles of a call and the requests of a launch are counted in 31, 31 and 16 bits
     const int64_t tokens = (int64_t)dc->max_blocks * cfg->block_size;
     if (tokens > 0x7FFFFFC0 || dc->max_seqs > 65535 || (tokens / dkv::kTile + 1) * dc->max_seqs > 0x7FFFFFFF) return KV_EUNSUP;
@@ -152,6 +107,7 @@ int kv_decoder_create(kv_decoder **out, const kv_config *cfg, const kv_decoder_c
     // granules of a block, over all query heads, are counted in 31 bits, and the lanes that add them up in 32
     if (dc->weigh && ((uint64_t)cfg->block_size * (uint64_t)dc->n_heads > 0x7FFFFFFFull || dc->max_blocks > (1 << 28))) return KV_EUNSUP;
     if (token_bytes >> 31 || cells >> 31 || cells * (uint64_t)cfg->n_hbm_blocks >= 0xFFFFFFFFull) return KV_EUNSUP;
+    if (!dkv::rows_fit(cfg->n_kv_heads, dc->n_heads, dc->max_seqs, dc->max_rows)) return KV_EUNSUP;
     int ndev = 0;
     if (hipGetDeviceCount(&ndev) != hipSuccess || ndev <= 0) {
         (void)hipGetLastError();
@@ -174,15 +130,18 @@ int kv_decoder_create(kv_decoder **out, const kv_config *cfg, const kv_decoder_c
     d->dc = *dc;
     d->device = at.device;
     d->hbm = (uint8_t *)hbm_cache;
+    d->dim = (int32_t)dim;
+    d->head_bytes = fp4 ? (uint32_t)dim / 2u : (uint32_t)(dim * cfg->elem_bytes);
+    d->exponents = fp4 ? (uint32_t)cfg->n_kv_heads * d->head_bytes : 0u;
     d->token_bytes = (uint32_t)token_bytes;
     d->cells_per_block = (uint32_t)cells;
     d->plane_bytes = kv_seg_bytes(cfg) * (cfg->hbm_layout == KV_HBM_BLOCK_FIRST ? 1ull : (uint64_t)cfg->n_hbm_blocks);
     const uint32_t group = (uint32_t)(dc->n_heads / cfg->n_kv_heads);
-    d->waves = cfg->head_dim <= 64 ? dkv::Step<64>::WAVES : cfg->head_dim <= 128 ? dkv::Step<128>::WAVES : dkv::Step<256>::WAVES;
+    d->waves = dim <= 64 ? dkv::Step<64>::WAVES : dim <= 128 ? dkv::Step<128>::WAVES : dkv::Step<256>::WAVES;
     d->head_tiles = (group + 15) / 16;
     d->units = (uint32_t)cfg->n_kv_heads * d->head_tiles;
     d->part_rows = std::min(group, 16u);
-    d->part_vecs = (cfg->head_dim <= 64 ? 4u : cfg->head_dim <= 128 ? 8u : 16u) * 4u * d->part_rows;
+    d->part_vecs = (dim <= 64 ? 4u : dim <= 128 ? 8u : 16u) * 4u * d->part_rows;
     d->granule = cfg->block_size % 4 ? 1u : std::gcd((uint32_t)cfg->block_size, 16u);
     d->max_granules = (uint32_t)dc->max_blocks * ((uint32_t)cfg->block_size / d->granule);
     OnDevice on(d->device);
@@ -199,8 +158,9 @@ int kv_decoder_create(kv_decoder **out, const kv_config *cfg, const kv_decoder_c
     const uint64_t n_part = slots * d->units * d->part_vecs * sizeof(dkv::f32x4), n_ml = slots * (uint64_t)dc->n_heads * sizeof(dkv::f32x4),
                    n_lse = ((uint64_t)dc->max_seqs * (uint64_t)dc->n_heads * 4 + 255) / 256 * 256,
                    n_gran = dc->weigh ? (uint64_t)dc->max_seqs * d->max_granules * (uint64_t)dc->n_heads * 4 : 0;
+    const uint64_t n_rows_part = dkv::rows_part_bytes(d), n_rows_ml = dkv::rows_ml_bytes(d), n_gran16 = (n_gran + 15) / 16 * 16;
     uint8_t *mem = nullptr;
-    if (hipMalloc((void **)&mem, n_part + n_ml + n_lse + n_gran) != hipSuccess) {
+    if (hipMalloc((void **)&mem, n_part + n_ml + n_lse + n_gran16 + n_rows_part + n_rows_ml) != hipSuccess) {
         (void)hipGetLastError();
         return fail(KV_ENOMEM);
     }
@@ -208,6 +168,8 @@ int kv_decoder_create(kv_decoder **out, const kv_config *cfg, const kv_decoder_c
     d->part_ml = (dkv::f32x4 *)(mem + n_part);
     d->lse2 = (float *)(mem + n_part + n_ml);
     d->granules = (float *)(mem + n_part + n_ml + n_lse);
+    d->rows_part = (dkv::f32x4 *)(mem + n_part + n_ml + n_lse + n_gran16);
+    d->rows_ml = (float2 *)(mem + n_part + n_ml + n_lse + n_gran16 + n_rows_part);
     *out = d;
     return KV_OK;
 }
@@ -234,7 +196,7 @@ int kv_put(kv_decoder *d, const kv_put_args *a, void *stream)
     if ((a->q.data == nullptr) != (a->q_out.data == nullptr)) return KV_EINVAL;
     int32_t pairs = 0;
     if (a->inv_freq) {
-        if (a->rot_dim <= 0 || a->rot_dim > d->cfg.head_dim || a->n_axes < 1 || a->n_axes > 3) return KV_EINVAL;
+        if (a->rot_dim <= 0 || a->rot_dim > d->dim || a->n_axes < 1 || a->n_axes > 3) return KV_EINVAL;
         if (!a->positions && a->n_axes != 1) return KV_EINVAL;
         for (int i = 0; i < a->n_axes; i++) {
             if (a->sections[i] < 0 || a->sections[i] > a->rot_dim) return KV_EINVAL;
@@ -244,8 +206,11 @@ int kv_put(kv_decoder *d, const kv_put_args *a, void *stream)
         if (a->positions && a->n_axes > 1 && a->position_stride != 0 && a->position_stride < a->n_rows) return KV_EINVAL;
         if (a->rot_dim % 8 != 0) return KV_EUNSUP;
     }
+    if ((a->q_norm || a->k_norm) && !(a->norm_eps >= 0.f && std::isfinite(a->norm_eps))) return KV_EINVAL;
+    if (a->q_norm && !a->q.data) return KV_EINVAL;
+    if ((uintptr_t)a->q_norm % 16 != 0 || (uintptr_t)a->k_norm % 16 != 0) return KV_EUNSUP;
     if (!rows_aligned(a->k) || !rows_aligned(a->v) || !rows_aligned(a->q) || !rows_aligned(a->q_out)) return KV_EUNSUP;
-    if (a->q_out.data && !apart(a->q_out, a->n_rows, d->dc.n_heads, d->cfg.head_dim)) return KV_EINVAL;
+    if (a->q_out.data && !apart(a->q_out, a->n_rows, d->dc.n_heads, d->dim)) return KV_EINVAL;
     if (a->n_rows > kMostRows) return KV_EUNSUP;
     if (!rows_here) return KV_OK;
     OnDevice on(d->device);
@@ -277,9 +242,10 @@ int kv_put(kv_decoder *d, const kv_put_args *a, void *stream)
     p.n_heads = (uint32_t)d->dc.n_heads;
     p.n_kv_heads = (uint32_t)d->cfg.n_kv_heads;
     p.max_blocks = (uint32_t)d->dc.max_blocks;
-    p.dim = (uint32_t)d->cfg.head_dim;
+    p.dim = (uint32_t)d->dim;
     p.token_bytes = d->token_bytes;
-    p.head_bytes = p.dim * (uint32_t)d->cfg.elem_bytes;
+    p.head_bytes = d->head_bytes;
+    p.exponents = d->exponents;
     p.block_size = (uint32_t)d->cfg.block_size;
     p.cells_per_block = d->cells_per_block;
     p.n_blocks = (uint32_t)d->cfg.n_hbm_blocks;
@@ -287,8 +253,26 @@ int kv_put(kv_decoder *d, const kv_put_args *a, void *stream)
     p.interleaved = a->interleaved ? 1u : 0u;
     p.section0 = a->inv_freq ? (uint32_t)a->sections[0] : 0u;
     p.section01 = p.section0 + (a->inv_freq && a->n_axes > 1 ? (uint32_t)a->sections[1] : 0u);
+    p.q_norm = a->q_norm;
+    p.k_norm = a->k_norm;
+    p.eps = a->norm_eps;
     p.k_scale = dkv::Scale::of(d->dc.k_scale);
     p.v_scale = dkv::Scale::of(d->dc.v_scale);
+    hipStream_t s = (hipStream_t)stream;
+    int dp;
+    const int kind = kinds(d, dp);
+    if (a->q_norm || a->k_norm || kind >= 4) {
+        switch (kind) {
+        case 0: launch_put_heads<dkv::Bf16, dkv::kBits16>(s, p); break;
+        case 1: launch_put_heads<dkv::Fp16, dkv::kBits16>(s, p); break;
+        case 2: launch_put_heads<dkv::Bf16, dkv::kBits8>(s, p); break;
+        case 3: launch_put_heads<dkv::Fp16, dkv::kBits8>(s, p); break;
+        case 4: launch_put_heads<dkv::Bf16, dkv::kBits4>(s, p); break;
+        default: launch_put_heads<dkv::Fp16, dkv::kBits4>(s, p); break;
+        }
+        DECTRY(hipGetLastError());
+        return KV_OK;
+    }
     // 8 dimensions a step, or 4 where the halves of pairs are no multiple of 8 apart
     const bool eights = p.interleaved || p.rot % 16u == 0;
     const uint32_t n = eights ? 8u : 4u;
@@ -302,9 +286,7 @@ int kv_put(kv_decoder *d, const kv_put_args *a, void *stream)
     const uint32_t places = (p.n_heads * (p.qs ? 1u : 0u) + p.n_kv_heads) * steps + p.n_kv_heads * (p.dim / n);
     const uint32_t most = p.n_rows <= 1024u ? 512u : 256u, turns = (places + most - 1u) / most;
     const uint32_t threads = ((places + turns - 1u) / turns + 63u) / 64u * 64u;
-    hipStream_t s = (hipStream_t)stream;
-    int dp;
-    switch (kinds(d, dp)) {
+    switch (kind) {
     case 0: launch_put<dkv::Bf16, false>(eights, threads, s, p); break;
     case 1: launch_put<dkv::Fp16, false>(eights, threads, s, p); break;
     case 2: launch_put<dkv::Bf16, true>(eights, threads, s, p); break;
@@ -326,7 +308,7 @@ int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
     if (a->mass && !a->mass_out) return KV_EINVAL;
     if (a->mass_out && !d->dc.weigh) return KV_EUNSUP;
     if (!rows_aligned(a->q) || !rows_aligned(a->out)) return KV_EUNSUP;
-    if (!apart(a->out, a->n_seqs, d->dc.n_heads, d->cfg.head_dim)) return KV_EINVAL;
+    if (!apart(a->out, a->n_seqs, d->dc.n_heads, d->dim)) return KV_EINVAL;
     if (a->n_seqs == 0) return KV_OK;
     OnDevice on(d->device);
     if (!on.ok()) return KV_EHIP;
@@ -354,9 +336,10 @@ int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
     p.n_heads = (uint32_t)d->dc.n_heads;
     p.max_blocks = (uint32_t)d->dc.max_blocks;
     p.max_tokens = p.max_blocks * (uint32_t)d->cfg.block_size;
-    p.dim = (uint32_t)d->cfg.head_dim;
+    p.dim = (uint32_t)d->dim;
     p.token_bytes = d->token_bytes;
-    p.head_bytes = p.dim * (uint32_t)d->cfg.elem_bytes;
+    p.head_bytes = d->head_bytes;
+    p.exponents = d->exponents;
     p.block_size = (uint32_t)d->cfg.block_size;
     p.cells_per_block = d->cells_per_block;
     p.n_blocks = (uint32_t)d->cfg.n_hbm_blocks;
@@ -419,10 +402,12 @@ int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
     int dp;
     const int kind = kinds(d, dp);
     switch (kind) {
-    case 0: launch_attend<dkv::Bf16, false>(dp, g, b, s, p); break;
-    case 1: launch_attend<dkv::Fp16, false>(dp, g, b, s, p); break;
-    case 2: launch_attend<dkv::Bf16, true>(dp, g, b, s, p); break;
-    default: launch_attend<dkv::Fp16, true>(dp, g, b, s, p); break;
+    case 0: launch_attend<dkv::Bf16, dkv::kBits16>(dp, g, b, s, p); break;
+    case 1: launch_attend<dkv::Fp16, dkv::kBits16>(dp, g, b, s, p); break;
+    case 2: launch_attend<dkv::Bf16, dkv::kBits8>(dp, g, b, s, p); break;
+    case 3: launch_attend<dkv::Fp16, dkv::kBits8>(dp, g, b, s, p); break;
+    case 4: launch_attend<dkv::Bf16, dkv::kBits4>(dp, g, b, s, p); break;
+    default: launch_attend<dkv::Fp16, dkv::kBits4>(dp, g, b, s, p); break;
     }
     DECTRY(hipGetLastError());
     const uint32_t lines = (p.units * p.part_vecs / 4u + 7u) / 8u;

@@ -13,6 +13,15 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t w32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t w32x2 __attribute__((ext_vector_type(2)));
 typedef w32x4 w32x4_by8 __attribute__((aligned(8)));  // where rows of 8-bit values begin on multiples of 8 bytes
+// where rows of 4-bit values begin anywhere
+typedef w32x4 w32x4_any __attribute__((aligned(1)));
+typedef w32x2 w32x2_any __attribute__((aligned(1)));
+typedef uint32_t w32_any __attribute__((aligned(1)));
+typedef uint16_t w16_any __attribute__((aligned(1)));
+
+// Bits of a number in the cache.  4 bits: a sign and 0, 0.5, 1, 1.5, 2, 3, 4 or 6, times 2^(byte - 127) of its 32 dimensions
+// (byte 255: NaN).  A token has its heads' numbers first, the even dimension of two in a byte's low half, then its heads' bytes.
+enum Kind { kBits16, kBits8, kBits4 };
 
 // The 16-bit types of q, k, v and the outputs.
 struct Bf16 {
@@ -38,6 +47,16 @@ struct Bf16 {
     {
         return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
     }
+    // two 4-bit numbers of byte BYTE, times a power of 2 (its exponent alone is looked at; 255: NaN); no bits are lost
+    template <int BYTE>
+    static __device__ __forceinline__ uint32_t from_fp4(uint32_t w, float power)
+    {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, power, BYTE));
+    }
+    static constexpr int kLowPower = -126, kHighPower = 125;  // of 4-bit numbers: half of the one and 6 of the other are bf16 numbers
+    // whether either of two is infinity or NaN
+    static __device__ __forceinline__ bool odd(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
+    static constexpr float kMost = 0x1.FEp127f;
     // Each of two weights as the sum of two numbers of 8 digits, the upper cut off, the lower the nearest to what that leaves:
     // within 2^-15.  The lower one gets 2^-20 of the weight on top, so that it is never 0 beside one: 0 times a value
     // of infinity is NaN.
@@ -71,6 +90,14 @@ struct Fp16 {
     {
         return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HI));
     }
+    template <int BYTE>
+    static __device__ __forceinline__ uint32_t from_fp4(uint32_t w, float power)
+    {
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, power, BYTE));
+    }
+    static constexpr int kLowPower = -23, kHighPower = 13;
+    static __device__ __forceinline__ bool odd(uint32_t w) { return (w & 0x7C00u) == 0x7C00u || (w & 0x7C000000u) == 0x7C000000u; }
+    static constexpr float kMost = 65504.0f;
     static constexpr uint32_t kOnes = 0x3C003C00u;
     // As above, of 11 digits each, within 2^-21; each at least the smallest number there is, 2^-24, if there is a weight (no
     // weight that is one is below 2^-126).
@@ -158,6 +185,7 @@ struct AttendParams {
     int64_t table_stride;
     uint32_t n_seqs, n_heads, max_blocks, max_tokens;
     uint32_t dim, token_bytes, head_bytes;
+    uint32_t exponents;  // 4 bits: from a token's first byte to its heads' bytes
     uint32_t block_size, cells_per_block, n_blocks;  // a block begins cells_per_block rows of token_bytes behind the one before it
     Divide by_block;
     uint32_t groups, wgs_per_group, units, units_per_wg, subs, group_heads, head_tiles;
@@ -269,21 +297,24 @@ __device__ __forceinline__ void clear(uint32_t &v) { v = 0u; }
 
 // WHOLE: heads have exactly DP dimensions.  Otherwise lanes whose dimensions are not there read the row's
 // first ones, in vain.
-template <typename X, bool FP8, int DP, bool WHOLE>
+template <typename X, int KIND, int DP, bool WHOLE>
 __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const AttendParams p)
 {
     using T = Step<DP>;
+    constexpr bool FP8 = KIND == kBits8, FP4 = KIND == kBits4;
     constexpr int KJ = T::KJ, VW = T::VW, NV = T::NV, ACC = T::ACC;
     constexpr uint32_t WAVES = T::WAVES;
     // Of a key a lane takes 16 bytes at once: in 16 bits the 8 dimensions of a step of 32, 32 j + 8 kq on; in 8 bits
-    // 16 dimensions, 64 l + 16 kq on, of which 8 go into each of two steps (q is brought in the same order).
-    constexpr int KL = FP8 ? KJ / 2 : KJ;
+    // 16 dimensions, 64 l + 16 kq on, of which 8 go into each of two steps (q is brought in the same order); in 4 bits
+    // 32 dimensions, which share one power of 2, 8 of them in each of four steps (16 of a row of up to 64).
+    constexpr int KL = FP4 ? (KJ + 3) / 4 : FP8 ? KJ / 2 : KJ;
+    constexpr uint32_t K4 = DP == 64 ? 16u : 32u;  // 4 bits: dimensions of a key that a lane takes at once
     // In 8 bits there is room for two tiles of values: they are asked for a tile ahead, like the keys.  us without / with:
     // 128 requests around 600 tokens, 8 heads of 128, 39.4 / 37.4; 4 of 32768 tokens, 8 heads of 128 48.4 / 50.4, of 192
     // 102 / 85, 4 heads of 256 51.4 / 55.2; in 16 bits, 32 requests around 1000, 8 heads of 128, 35.6 / 39.7.
-    constexpr bool AHEAD = FP8 && !(WHOLE && DP == 256);
-    auto k_dim = [](int j, uint32_t kq) { return FP8 ? (uint32_t)(j / 2) * 64u + kq * 16u + (uint32_t)(j & 1) * 8u : (uint32_t)j * 32u + kq * 8u; };
-    typedef typename Raw<(FP8 ? 1 : 2) * VW>::type vraw;
+    constexpr bool AHEAD = FP4 || (FP8 && !(WHOLE && DP == 256));
+    auto k_dim = [](int j, uint32_t kq) { return FP4 ? (uint32_t)(j / 4) * 128u + kq * K4 + (uint32_t)(j & 3) * 8u : FP8 ? (uint32_t)(j / 2) * 64u + kq * 16u + (uint32_t)(j & 1) * 8u : (uint32_t)j * 32u + kq * 8u; };
+    typedef typename Raw<FP4 ? 4 : (FP8 ? 1 : 2) * VW>::type vraw;
     // Values go past the caches, except short rows that share 128-byte lines with other heads' all along.  us past /
     // through them: 4 requests of 32768 tokens, 8-bit, 8 heads of 40 30.8 / 26.2, of 80 46.7 / 45.0, of 64 28.9 / 32.2;
     // 16-bit, 4 heads of 192 78.3 / 83.0, 8 of 96 76.0 / 77.2.
@@ -309,24 +340,28 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
     const uint32_t rows = min(16u, p.group_heads - ht * 16u);      // query heads of this wave
     const uint32_t head = kv_head * p.group_heads + ht * 16u + n;  // this lane's
     const bool has_row = active && n < rows;
-    constexpr uint32_t elem = FP8 ? 1u : 2u;
+    // bytes of so many dimensions
+    auto bytes = [](uint32_t dims) { return FP4 ? dims / 2u : FP8 ? dims : dims * 2u; };
     if (at >= end) {  // a request of its own range, without a token
         for (uint32_t d = kq * 4u; has_row && sub == 0u && d < p.dim; d += 16u)
             *reinterpret_cast<w32x2 *>(p.out + (uint64_t)s * p.out_row + (uint64_t)head * p.out_head + d * 2u) = w32x2{0u, 0u};
         if (p.lse && has_row && sub == 0u && kq == 0u) p.lse[(uint64_t)s * p.n_heads + head] = -__builtin_inff();
         return;
     }
-    const uint8_t *const kb = p.k + (uint64_t)kv_head * p.head_bytes + (WHOLE ? k_dim(0, kq) * elem : 0u);
-    const uint8_t *const vb = p.v + (uint64_t)kv_head * p.head_bytes + (WHOLE ? n * VW * elem : 0u);
+    const uint8_t *const kb = p.k + (uint64_t)kv_head * p.head_bytes + (WHOLE ? bytes(k_dim(0, kq)) : 0u);
+    const uint8_t *const vb = p.v + (uint64_t)kv_head * p.head_bytes + (WHOLE ? bytes(n * VW) : 0u);
     // (Where rows are not whole, found anew for every row: kept, they are what does not fit the registers.)
     auto k_off = [&](int l, uint32_t kq) {
-        constexpr uint32_t step = FP8 ? 64u : 32u, each = FP8 ? 16u : 8u;
-        return WHOLE ? (uint32_t)l * step * elem : min((uint32_t)l * step + kq * each, p.dim - each) * elem;
+        constexpr uint32_t step = FP4 ? 128u : FP8 ? 64u : 32u, each = FP4 ? K4 : FP8 ? 16u : 8u;
+        return WHOLE ? bytes((uint32_t)l * step) : bytes(min((uint32_t)l * step + kq * each, p.dim - each));
     };
     auto v_off = [&](int c, uint32_t n) {
         const uint32_t d = (uint32_t)c * 128u + n * VW;
-        return WHOLE ? (uint32_t)c * 128u * elem : min(d, p.dim - VW) * elem;
+        return WHOLE ? bytes((uint32_t)c * 128u) : bytes(min(d, p.dim - VW));
     };
+    // 4 bits: from a token's numbers of this head to the head's powers of 2
+    const uint32_t powers = FP4 ? p.exponents + kv_head * (p.dim / 32u) - kv_head * p.head_bytes : 0u;
+    auto power = [](uint32_t byte) { return __builtin_bit_cast(float, byte << 23); };
 
     // What a step needs is asked for a step (its pages two steps) ahead, across the ends of requests,
     // too: a range goes on in the next request with its first keys under way.
@@ -361,10 +396,26 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
     Part now = {s, t, 0u, 0u, 0u}, next = part_at(s, t, at);
     w32x4 qf[KJ];
     w32x4 kr[2][KL];
-    auto load_keys = [&](w32x4(&to)[KL], uint32_t cell) {
+    uint32_t kx[2][KL];  // 4 bits: the lane's powers of 2
+    auto load_keys = [&](w32x4(&to)[KL], uint32_t (&x)[KL], uint32_t cell) {
         const uint64_t off = (uint64_t)(cell == kNoCell ? 0u : cell) * p.token_bytes;
         uint32_t k = kq;
         if constexpr (!WHOLE) asm volatile("" : "+v"(k));
+        if constexpr (FP4) {
+            const uint8_t *const row = p.k + (uint64_t)kv_head * p.head_bytes + off;
+#pragma unroll
+            for (int l = 0; l < KL; l++) {
+                const uint32_t d = WHOLE ? k_dim(4 * l, k) : min(k_dim(4 * l, k), p.dim - K4);
+                if constexpr (DP == 64) {
+                    const w32x2 y = *reinterpret_cast<const w32x2_any *>(row + d / 2u);
+                    to[l] = w32x4{y[0], y[1], 0u, 0u};
+                } else {
+                    to[l] = *reinterpret_cast<const w32x4_any *>(row + d / 2u);
+                }
+                x[l] = row[powers + d / 32u];
+            }
+            return;
+        }
         if constexpr (FP8 && !WHOLE && DP == 64) {
             if (p.dim < 16u) {  // a row of 8 bytes, and nothing behind the last one
                 const w32x2 x = *reinterpret_cast<const w32x2 *>(kb + off);
@@ -390,9 +441,21 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
             vcell[r] = c == kNoCell ? 0u : c;
         }
     };
-    auto load_values = [&](vraw(&to)[8][NV], int c) {
+    auto load_values = [&](vraw(&to)[8][NV], uint32_t (&x)[8][NV], int c) {
         uint32_t v = n;
         if constexpr (!WHOLE) asm volatile("" : "+v"(v));
+        if constexpr (FP4) {
+            const uint8_t *const rows = p.v + (uint64_t)kv_head * p.head_bytes;
+            const uint32_t d = WHOLE ? (uint32_t)c * 128u + v * VW : min((uint32_t)c * 128u + v * VW, p.dim - VW);
+#pragma unroll
+            for (int r = 0; r < 8; r++) {
+                const uint8_t *const row = rows + (uint64_t)vcell[r] * p.token_bytes;
+                if constexpr (DP == 64) to[r][c] = *reinterpret_cast<const w16_any *>(row + d / 2u);
+                else to[r][c] = *reinterpret_cast<const w32_any *>(row + d / 2u);
+                x[r][c] = row[powers + d / 32u];
+            }
+            return;
+        }
 #pragma unroll
         for (int r = 0; r < 8; r++)
         {
@@ -402,6 +465,7 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
         }
     };
     vraw next_vr[8][NV];
+    uint32_t next_vx[8][NV];  // 4 bits: powers of 2
     uint32_t next_present = 0;
     for (;;) {
         uint32_t next_page[2];
@@ -419,6 +483,7 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
         do {
             const bool have = tt < stop, last = tt + p.subs >= stop;
             vraw vr[8][NV];
+            uint32_t vx[8][NV];
             uint32_t present = 0;  // bit r: token r of the lane's 8 is there
             f32x4 sc[2];
             if (have) {
@@ -427,12 +492,15 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
 #pragma unroll
                     for (int r = 0; r < 8; r++) {
 #pragma unroll
-                        for (int c = 0; c < NV; c++) vr[r][c] = next_vr[r][c];
+                        for (int c = 0; c < NV; c++) {
+                            vr[r][c] = next_vr[r][c];
+                            if constexpr (FP4) vx[r][c] = next_vx[r][c];
+                        }
                     }
                 } else {
                     find_values(present);
 #pragma unroll
-                    for (int c = 0; c < NV; c++) load_values(vr, c);
+                    for (int c = 0; c < NV; c++) load_values(vr, vx, c);
                 }
                 // scores: token x head
 #pragma unroll
@@ -442,8 +510,11 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
                         // dimensions that are not there meet zeros of q: they must not be NaN
 #pragma unroll
                         for (int l = 0; l < KL; l++) {
-                            const uint32_t d = k_dim(FP8 ? 2 * l : l, kq);
-                            if (d >= p.dim) clear(key[l]);
+                            const uint32_t d = k_dim(FP4 ? 4 * l : FP8 ? 2 * l : l, kq);
+                            if (d >= p.dim) {
+                                clear(key[l]);
+                                if constexpr (FP4) kx[h][l] = 0u;
+                            }
                             else if (FP8 && d + 16u > p.dim) key[l] = w32x4{key[l][2], key[l][3], 0u, 0u};  // 8 are there: the last 16 were read
                         }
                     }
@@ -451,7 +522,12 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
 #pragma unroll
                     for (int j = 0; j < KJ; j++) {
                         w32x4 a;
-                        if constexpr (FP8) {
+                        if constexpr (FP4) {
+                            const uint32_t y = key[j / 4][j & 3];
+                            const float x = power(kx[h][j / 4]);
+                            a = w32x4{X::template from_fp4<0>(y, x), X::template from_fp4<1>(y, x), X::template from_fp4<2>(y, x),
+                                      X::template from_fp4<3>(y, x)};
+                        } else if constexpr (FP8) {
                             const uint32_t lo = key[j / 2][2 * (j & 1)], hi = key[j / 2][2 * (j & 1) + 1];
                             a = w32x4{X::template from_fp8<false>(lo), X::template from_fp8<true>(lo), X::template from_fp8<false>(hi),
                                       X::template from_fp8<true>(hi)};
@@ -479,11 +555,11 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
                     }
                 }
 #pragma unroll
-                for (int h = 0; h < 2; h++) load_keys(kr[h], cell[h]);
+                for (int h = 0; h < 2; h++) load_keys(kr[h], kx[h], cell[h]);
                 if constexpr (AHEAD) {
                     find_values(next_present);
 #pragma unroll
-                    for (int c = 0; c < NV; c++) load_values(next_vr, c);
+                    for (int c = 0; c < NV; c++) load_values(next_vr, next_vx, c);
                 }
 #pragma unroll
                 for (int h = 0; h < 2; h++) page[h] = page_of(part, tile + p.subs, h);
@@ -535,12 +611,21 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
                 if (gaps) {  // a weight of 0 does not make up for NaN
 #pragma unroll
                     for (int r = 0; r < 8; r++)
-                        if (!(present >> r & 1u)) clear(vr[r][c]);
+                        if (!(present >> r & 1u)) {
+                            clear(vr[r][c]);
+                            if constexpr (FP4) vx[r][c] = 0u;
+                        }
                 }
                 // of token r: dimensions 2i and 2i + 1
                 auto pair = [&](int r, int i) {
                     const vraw &v = vr[r][c];
-                    if constexpr (FP8 && VW == 8) return i & 1 ? Y::template from_fp8<true>(v[i / 2]) : Y::template from_fp8<false>(v[i / 2]);
+                    if constexpr (FP4) {
+                        const float x = power(vx[r][c]);
+                        return i == 0   ? Y::template from_fp4<0>(v, x)
+                               : i == 1 ? Y::template from_fp4<1>(v, x)
+                               : i == 2 ? Y::template from_fp4<2>(v, x)
+                                        : Y::template from_fp4<3>(v, x);
+                    } else if constexpr (FP8 && VW == 8) return i & 1 ? Y::template from_fp8<true>(v[i / 2]) : Y::template from_fp8<false>(v[i / 2]);
                     else if constexpr (FP8) return i & 1 ? Y::template from_fp8<true>(v) : Y::template from_fp8<false>(v);
                     else return v[i];
                 };
@@ -919,6 +1004,9 @@ struct PutParams {
     uint32_t n_seqs, n_rows, n_heads, n_kv_heads, max_blocks;
     uint32_t dim, token_bytes, head_bytes, block_size, cells_per_block, n_blocks;
     uint32_t rot, interleaved, section0, section01;  // pairs of the first axis, of the first two
+    uint32_t exponents;  // 4 bits: from a token's first byte to its heads' bytes
+    const float *q_norm, *k_norm;
+    float eps;
     Divide by_steps, by_vecs;  // by a rotated head's steps, and by a head's vectors
     Scale k_scale, v_scale;
 };
@@ -1055,6 +1143,154 @@ __global__ __launch_bounds__(512) void kv_put_kernel(const PutParams p)
             const Scale scale = {i < n_k ? p.k_scale.scale : p.v_scale.scale, i < n_k ? p.k_scale.inv : p.v_scale.inv};
             store_row<X, FP8>(to, d, x, scale);
             if (two) store_row<X, FP8>(to, d + pairs, y, scale);
+        }
+    }
+}
+
+// New tokens whose heads are normed first, or go into 4 bits.  A thread has 8 dimensions of a head, one behind the other,
+// and a head lies in 1 to 32 lanes of a wave (a power of 2): the sum of its squares is a sum over lanes, so is
+// the largest of 32 dimensions over four, and the other numbers of pairs come from the lanes that have them.
+//   y = x / sqrt(mean x^2 + eps) * weight, then the rotation, all in 32 bits, rounded once.
+// 4 bits: the power of 2 is the one that brings the largest of 32 dimensions to 4 and more, under 8, and numbers are the nearest
+// of those there are (6 the largest); infinity or NaN among them makes all 32 NaN.
+template <typename X, int KIND>
+__global__ __launch_bounds__(512) void kv_put_heads_kernel(const PutParams p, const uint32_t lane_bits)
+{
+    __shared__ float2 turn[128];
+    const uint32_t row = blockIdx.x, tid = threadIdx.x, lane = tid & 63u;
+    uint32_t s = row, start = row, next = row + 1u;
+    if (p.starts) {
+        s = 0;
+        for (uint32_t base = 1; base <= p.n_seqs; base += 64u)
+            s += (uint32_t)__popcll(__ballot(base + lane <= p.n_seqs && p.starts[base + lane] <= (int32_t)row));
+        if (s >= p.n_seqs || (int32_t)row < p.starts[0]) return;
+        start = (uint32_t)p.starts[s];
+        next = (uint32_t)p.starts[s + 1u];
+    }
+    const uint32_t n_q = p.qs ? p.n_heads : 0u, n_k = n_q + p.n_kv_heads, n_all = n_k + p.n_kv_heads;
+    const uint32_t lanes = 1u << lane_bits, in = tid & (lanes - 1u), d = in * 8u, at_once = blockDim.x >> lane_bits;
+    const uint32_t pairs = p.rot / 2u;
+    bool page = false;
+    uint8_t *kc = nullptr, *vc = nullptr;
+    for (uint32_t first = 0; first < n_all; first += at_once) {
+        const uint32_t i = first + (tid >> lane_bits), head = i < n_q ? i : i < n_k ? i - n_q : i - n_k;
+        const bool here = i < n_all && d < p.dim;
+        w32x4 raw;
+        clear(raw);
+        if (here) {
+            const uint8_t *const src = i < n_q ? p.qs + row * p.q_row + head * p.q_head
+                                       : i < n_k ? p.ks + row * p.k_row + head * p.k_head
+                                                 : p.vs + row * p.v_row + head * p.v_head;
+            raw = __builtin_nontemporal_load(reinterpret_cast<const w32x4 *>(src + d * 2u));
+        }
+        if (first == 0u) {
+            const int64_t token = (int64_t)p.lens[s] - (int64_t)(next - start) + (int64_t)(row - start);
+            for (uint32_t i = tid; i < pairs; i += blockDim.x) {
+                const uint32_t axis = i < p.section0 ? 0u : i < p.section01 ? 1u : 2u;
+                const double pos = p.positions ? (double)p.positions[(int64_t)axis * p.position_stride + row] : (double)token;
+                // in 64 bits: whole turns, and what is left of them; the rest as half turns
+                const double turns = pos * (double)p.inv_freq[i] * 0.15915494309189533577;
+                float sn, cs;
+                sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
+                turn[i] = float2{cs, sn};
+            }
+            page = token >= 0 && token < (int64_t)p.max_blocks * p.block_size;
+            uint32_t cell = kNoCell;
+            if (page) {
+                const uint32_t entry = (uint32_t)token / p.block_size;
+                cell = cell_in((uint32_t)p.table[(int64_t)s * p.table_stride + entry], p.n_blocks, p.cells_per_block,
+                               (uint32_t)token - entry * p.block_size);
+                page = cell != kNoCell;
+            }
+            kc = p.k + (uint64_t)cell * p.token_bytes;  // not looked at without a page
+            vc = p.v + (uint64_t)cell * p.token_bytes;
+            __syncthreads();
+        }
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            x[2 * e] = X::lo(raw[e]);
+            x[2 * e + 1] = X::hi(raw[e]);
+        }
+        // (from here to the rotation's end every lane of a wave takes part: heads that are not there hold zeros)
+        const float *const weight = i < n_q ? p.q_norm : i < n_k ? p.k_norm : nullptr;
+        if (p.q_norm || p.k_norm) {
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; e++) sum = __builtin_fmaf(x[e], x[e], sum);
+            for (uint32_t m = 1; m < lanes; m <<= 1) sum += __shfl_xor(sum, (int)m, 64);
+            if (weight && here) {
+                const float r = 1.0f / sqrtf(sum / (float)p.dim + p.eps);
+                const f32x4 w0 = *reinterpret_cast<const f32x4 *>(weight + d), w1 = *reinterpret_cast<const f32x4 *>(weight + d + 4u);
+#pragma unroll
+                for (int e = 0; e < 8; e++) x[e] *= r * (e < 4 ? w0[e & 3] : w1[e & 3]);
+            }
+        }
+        const bool turns = i < n_k;
+        if (p.interleaved) {
+            if (turns && d < p.rot) {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const float2 c = turn[(d + e) / 2u];
+                    const float u = x[e] * c.x - x[e + 1] * c.y, w = x[e + 1] * c.x + x[e] * c.y;
+                    x[e] = u;
+                    x[e + 1] = w;
+                }
+            }
+        } else if (p.rot) {
+            // four dimensions at a time: those of a thread may be of both halves
+            float other[8];
+            const uint32_t fours = pairs / 4u, base = lane & ~(lanes - 1u);
+#pragma unroll
+            for (uint32_t f = 0; f < 2; f++) {
+                const uint32_t at = in * 2u + f, from = at < fours ? at + fours : at < 2u * fours ? at - fours : at;
+                const int src = (int)(base + from / 2u);
+#pragma unroll
+                for (uint32_t e = 0; e < 4; e++) {
+                    if (fours & 1u) {
+                        const float a = __shfl(x[e], src, 64), b = __shfl(x[4 + e], src, 64);
+                        other[4 * f + e] = from & 1u ? b : a;
+                    } else {
+                        other[4 * f + e] = __shfl(x[4 * f + e], src, 64);
+                    }
+                }
+            }
+#pragma unroll
+            for (uint32_t e = 0; e < 8; e++) {
+                const uint32_t at = d + e;
+                if (!turns || at >= p.rot) continue;
+                const bool lower = at < pairs;
+                const float2 c = turn[lower ? at : at - pairs];
+                x[e] = lower ? x[e] * c.x - other[e] * c.y : x[e] * c.x + other[e] * c.y;
+            }
+        }
+        uint32_t largest = 0;
+        if constexpr (KIND == kBits4) {
+#pragma unroll
+            for (int e = 0; e < 8; e++) largest = max(largest, __builtin_bit_cast(uint32_t, x[e]) & 0x7FFFFFFFu);
+            largest = max(largest, (uint32_t)__shfl_xor((int)largest, 1, 64));
+            largest = max(largest, (uint32_t)__shfl_xor((int)largest, 2, 64));
+        }
+        if (!here || (i >= n_q && !page)) continue;
+        if (i < n_q) {
+            store_row<X, false>(p.qd + row * p.qd_row + head * p.qd_head, d, x, p.k_scale);
+            continue;
+        }
+        uint8_t *const to = i < n_k ? kc : vc;
+        if constexpr (KIND == kBits4) {
+            const bool odd = largest >= 0x7F800000u;
+            const int byte = min(max((int)(largest >> 23) - 2, X::kLowPower + 127), X::kHighPower + 127);
+            const float power = __builtin_bit_cast(float, (uint32_t)byte << 23);
+            uint32_t w = 0;
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], power, 0);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], power, 1);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], power, 2);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], power, 3);
+            *reinterpret_cast<w32_any *>(to + head * p.head_bytes + d / 2u) = odd ? 0u : w;
+            if ((in & 3u) == 0u) to[p.exponents + head * (p.dim / 32u) + d / 32u] = odd ? (uint8_t)255 : (uint8_t)byte;
+        } else {
+            const Scale scale = {i < n_k ? p.k_scale.scale : p.v_scale.scale, i < n_k ? p.k_scale.inv : p.v_scale.inv};
+            store_row<X, KIND == kBits8>(to + head * p.head_bytes, d, x, scale);
         }
     }
 }

@@ -1,0 +1,108 @@
+// Host side of attention of many rows per request (see include/duplexkv.h).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "kv_rows.hpp"
+#include "kv_rows_kernels.hpp"
+
+namespace {
+
+static_assert(dkv::kRowTile == dkv::kRowsOfTile, "memory for what splits leave");
+
+template <typename X, int KIND>
+void launch_rows(dim3 g, hipStream_t s, const dkv::RowsParams &p, uint32_t join_tiles)
+{
+    auto go = [&](auto dims) {
+        constexpr int DP = decltype(dims)::value;
+        hipLaunchKernelGGL((dkv::kv_rows_kernel<X, KIND, DP>), g, dim3(256), 0, s, p);
+        if (join_tiles)
+            hipLaunchKernelGGL((dkv::kv_rows_join_kernel<X, KIND == dkv::kBits16>), dim3(join_tiles * (DP / 32)), dim3(256), 0, s, p,
+                               (uint32_t)DP / 32u, (uint32_t)dkv::RowStep<DP>::TOKENS);
+    };
+    switch (dkv::rows_dims(p.dim)) {
+    case 64: go(std::integral_constant<int, 64>{}); break;
+    case 96: go(std::integral_constant<int, 96>{}); break;
+    case 128: go(std::integral_constant<int, 128>{}); break;
+    case 192: go(std::integral_constant<int, 192>{}); break;
+    default: go(std::integral_constant<int, 256>{}); break;
+    }
+}
+
+}  // namespace
+
+extern "C" int kv_attend_rows(kv_decoder *d, const kv_attend_rows_args *a, void *stream)
+{
+    using namespace dkv;
+    if (!d || !a || a->layer < 0 || a->layer >= d->cfg.n_layers || a->n_seqs < 0 || a->n_rows < 0) return KV_EINVAL;
+    const float qk_scale = (float)((double)a->scale * 1.4426950408889634074 * (double)d->dc.k_scale);
+    if (!std::isfinite(qk_scale)) return KV_EINVAL;
+    if (a->n_seqs > d->dc.max_seqs || a->n_rows > d->dc.max_rows) return KV_E2BIG;
+    const bool rows_here = a->n_seqs > 0 && a->n_rows > 0;
+    if (!a->starts && a->n_rows != a->n_seqs) return KV_EINVAL;
+    if (rows_here && (!a->table || !a->lens || !a->q.data || !a->out.data)) return KV_EINVAL;
+    if (a->n_seqs > 1 && a->table_stride < d->dc.max_blocks) return KV_EINVAL;
+    if (!rows_ok(a->q) || !rows_ok(a->out)) return KV_EINVAL;
+    if (!rows_aligned(a->q) || !rows_aligned(a->out)) return KV_EUNSUP;
+    if (a->out.data && !apart(a->out, a->n_rows, d->dc.n_heads, d->dim)) return KV_EINVAL;
+    if (!rows_here) return KV_OK;
+    OnDevice on(d->device);
+    if (!on.ok()) return KV_EHIP;
+    RowsParams p{};
+    p.k = plane(d, a->layer, 0);
+    p.v = plane(d, a->layer, 1);
+    p.table = a->table;
+    p.lens = a->lens;
+    p.starts = a->starts;
+    p.q = (const uint8_t *)a->q.data;
+    p.out = (uint8_t *)const_cast<void *>(a->out.data);
+    p.lse = a->lse;
+    p.part = d->rows_part;
+    p.part_ml = d->rows_ml;
+    p.q_row = 2ull * (uint64_t)a->q.row;
+    p.q_head = 2ull * (uint64_t)a->q.head;
+    p.out_row = 2ull * (uint64_t)a->out.row;
+    p.out_head = 2ull * (uint64_t)a->out.head;
+    p.table_stride = a->table_stride;
+    p.n_seqs = (uint32_t)a->n_seqs;
+    p.n_rows = (uint32_t)a->n_rows;
+    p.n_heads = (uint32_t)d->dc.n_heads;
+    p.n_kv_heads = (uint32_t)d->cfg.n_kv_heads;
+    p.max_tokens = (uint32_t)d->dc.max_blocks * (uint32_t)d->cfg.block_size;
+    p.dim = (uint32_t)d->dim;
+    p.token_bytes = d->token_bytes;
+    p.head_bytes = d->head_bytes;
+    p.exponents = d->exponents;
+    p.block_size = (uint32_t)d->cfg.block_size;
+    p.cells_per_block = d->cells_per_block;
+    p.n_blocks = (uint32_t)d->cfg.n_hbm_blocks;
+    p.group_heads = p.n_heads / p.n_kv_heads;
+    p.causal = a->causal ? 1u : 0u;
+    p.by_block = Divide::by(p.block_size);
+    p.by_group = Divide::by(p.group_heads);
+    p.negative = qk_scale < 0.f ? 1u : 0u;
+    p.qk_scale = std::max(std::fabs(qk_scale), 0x1p-126f);  // (0 times the score of what is masked, -inf, is NaN)
+    p.v_scale = d->dc.v_scale;
+    p.n_tiles = (uint32_t)row_tiles(p.n_rows, p.group_heads, p.n_seqs);
+    p.row_tile = kRowsOfTile;
+    // Few tiles of rows: the tokens are split, so that two workgroups for each compute unit have some.
+    const uint64_t each = (uint64_t)p.n_tiles * p.n_kv_heads;
+    p.least = 2u;
+    const uint32_t tokens = p.dim > 128u ? 32u : 64u, most = (p.max_tokens + tokens - 1u) / tokens;
+    p.splits = (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>(kRowSlots / each, (most + p.least - 1u) / p.least));
+    const dim3 g((uint32_t)(each * p.splits));
+    const uint32_t join_tiles = p.splits > 1u ? (uint32_t)each : 0u;
+    hipStream_t s = (hipStream_t)stream;
+    switch ((d->dc.x_type == KV_FP16 ? 1 : 0) + (d->dc.kv_type == KV_FP8 ? 2 : d->dc.kv_type == KV_FP4 ? 4 : 0)) {
+    case 0: launch_rows<Bf16, kBits16>(g, s, p, join_tiles); break;
+    case 1: launch_rows<Fp16, kBits16>(g, s, p, join_tiles); break;
+    case 2: launch_rows<Bf16, kBits8>(g, s, p, join_tiles); break;
+    case 3: launch_rows<Fp16, kBits8>(g, s, p, join_tiles); break;
+    case 4: launch_rows<Bf16, kBits4>(g, s, p, join_tiles); break;
+    default: launch_rows<Fp16, kBits4>(g, s, p, join_tiles); break;
+    }
+    DECTRY(hipGetLastError());
+    return KV_OK;
+}

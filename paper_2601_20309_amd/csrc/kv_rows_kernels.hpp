@@ -1,0 +1,471 @@
+// Device kernels of attention of many rows per request over the paged cache (gfx950, wave64).
+#pragma once
+#include "kv_decode_kernels.hpp"
+
+namespace dkv {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+
+// ---- attention of many rows -------------------------------------------------------------------
+//
+// Row i of a request's m rows sees the tokens before u_i: u_i = length - m + i + 1, or the whole length. Over those in
+// present pages: scores s_t = c q.k_t, weights w_t = 2^(s_t - reference), out = sum w_t v_t / sum w_t, one pass over the
+// tokens with a running reference.  The query heads of a KV head are rows, too: heads of a row lie one
+// behind the other, so that few rows of many heads fill a tile, and all of them share the keys that are brought.
+//
+// A workgroup has kRowTile rows of one KV head, 32 a wave, and goes over the tokens TOKENS at a time.  These go
+// through registers into LDS, two tiles in turn: in 16 bits whatever the cache holds, so that the products are the same
+// for every type of cache.  Both products are taken transposed, tokens x rows and dimensions x rows, as in kv_attend:
+// a lane has one row, its reference and its sums, and weights come out as the second product's operand.
+// Values are read from LDS transposed, four tokens of a dimension at a time.
+
+struct RowsParams {
+    const uint8_t *k, *v;
+    const int32_t *table, *lens, *starts;
+    const uint8_t *q;
+    uint8_t *out;
+    float *lse;
+    f32x4 *part;      // [tile * splits][wave][vector][lane]: sums of a split, as they lie in registers
+    float2 *part_ml;  // [tile * splits][kRowTile]: reference, sum of weights
+    uint64_t q_row, q_head, out_row, out_head;  // bytes
+    int64_t table_stride;
+    uint32_t n_seqs, n_rows, n_heads, n_kv_heads, max_tokens;
+    uint32_t dim, token_bytes, head_bytes, block_size, cells_per_block, n_blocks;
+    uint32_t exponents;  // 4 bits: from a token's first byte to its exponents
+    uint32_t group_heads, causal, splits, least;  // least: tiles of tokens of a split
+    uint32_t n_tiles, row_tile;                   // tiles of rows of a KV head, empty ones among them; rows of one
+    Divide by_block, by_group;
+    uint32_t negative;  // the scale is: keys meet -q
+    float qk_scale;     // to base 2, not negative
+    float v_scale;
+};
+
+constexpr uint32_t kRowTile = 128;
+
+// Which rows a tile has.  Request s's tiles are floor(starts[s] * group / kRowTile) + s on: as many as it needs, or
+// some more, which are empty.  So no sums over requests are needed to find one.
+struct RowTile {
+    uint32_t s, first;      // request; its rows' heads before this tile
+    int32_t start, m;       // the request's first row, and its number of rows
+    bool here;
+};
+
+__device__ __forceinline__ uint32_t first_tile(const RowsParams &p, uint32_t s)
+{
+    const int32_t start = p.starts ? p.starts[s] : (int32_t)s;
+    return (uint32_t)((uint64_t)(uint32_t)max(start, 0) * p.group_heads / kRowTile) + s;
+}
+
+__device__ __forceinline__ RowTile row_tile(const RowsParams &p, uint32_t lane, uint32_t tile)
+{
+    RowTile t;
+    // the last request whose first tile is not behind this one, 64 candidates at a time
+    uint32_t lo = 0, range = p.n_seqs;
+    while (range > 1u) {
+        const uint32_t step = (range + 63u) / 64u, at = lo + lane * step;
+        const uint64_t before = __ballot(lane * step < range && first_tile(p, at) <= tile);
+        const uint32_t n = before ? 63u - (uint32_t)__builtin_clzll(before) : 0u;
+        range = min(step, range - n * step);
+        lo += n * step;
+    }
+    t.s = __builtin_amdgcn_readfirstlane(lo);
+    const uint32_t base = first_tile(p, t.s);
+    t.start = p.starts ? p.starts[t.s] : (int32_t)t.s;
+    const int64_t next = p.starts ? p.starts[t.s + 1u] : (int64_t)t.s + 1;
+    t.m = (int32_t)min(max(next - t.start, (int64_t)0), (int64_t)p.n_rows);
+    const uint64_t first = (uint64_t)(tile - base) * kRowTile;
+    t.here = tile >= base && t.start >= 0 && first < (uint64_t)t.m * p.group_heads;
+    t.first = (uint32_t)first;
+    return t;
+}
+
+// Tokens before which row i of the request looks.
+__device__ __forceinline__ int32_t row_sees(const RowsParams &p, int32_t len, const RowTile &t, uint32_t row)
+{
+    const int64_t upto = p.causal ? (int64_t)len - t.m + (int64_t)row + 1 : (int64_t)len;
+    return (int32_t)min(max(upto, (int64_t)0), (int64_t)p.max_tokens);
+}
+
+// Tiles of tokens that a tile of rows looks at, and how many of its splits have any.
+struct Spread {
+    uint32_t tiles, per, active;
+    __device__ __forceinline__ Spread(const RowsParams &p, uint32_t upto, uint32_t tokens)
+    {
+        tiles = (upto + tokens - 1u) / tokens;
+        per = max((tiles + p.splits - 1u) / p.splits, p.least);
+        active = (tiles + per - 1u) / per;
+    }
+};
+
+template <typename X>
+__device__ __forceinline__ f32x16 mma32(w32x4 a, w32x4 b, f32x16 c)
+{
+    if constexpr (std::is_same_v<X, Fp16>)
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(typename X::x8, a), __builtin_bit_cast(typename X::x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(typename X::x8, a), __builtin_bit_cast(typename X::x8, b), c, 0, 0, 0);
+}
+
+// A mean of numbers of X that its weights' roundings have put above the largest of them is that one.
+template <typename X, bool OF_X>
+__device__ __forceinline__ float mean(float x)
+{
+    return OF_X && __builtin_fabsf(x) < __builtin_inff() ? fminf(fmaxf(x, -X::kMost), X::kMost) : x;
+}
+
+template <int DP>
+struct RowStep {
+    static constexpr int TOKENS = DP > 128 ? 32 : 64;
+    static constexpr int PITCH = DP <= 64 ? 64 : DP <= 128 ? 128 : 256;  // of a token in LDS, in numbers
+    static constexpr int CHUNKS = PITCH / 8;
+    static constexpr int NB = DP / 32, KS = DP / 16, TB = TOKENS / 32;
+    // Where 8 numbers lie: keys are read 16 bytes a lane, 32 tokens at once, values 32 dimensions of 8 tokens at once.
+    static __device__ __forceinline__ uint32_t key_at(uint32_t token, uint32_t chunk)
+    {
+        const uint32_t f = PITCH == 64 ? token >> 1 & 7u : token & 15u;
+        return (token * CHUNKS + (chunk ^ f)) * 8u;
+    }
+    static __device__ __forceinline__ uint32_t value_at(uint32_t token, uint32_t chunk)
+    {
+        const uint32_t f = PITCH == 64 ? token >> 1 & 1u : token & 3u;
+        return (token * CHUNKS + (chunk ^ f << 2)) * 8u;
+    }
+};
+
+// As much of a row of the cache as a thread takes at once, and what it becomes.
+template <typename X, int KIND>
+struct Piece;
+template <typename X>
+struct Piece<X, kBits16> {
+    static constexpr int N = 8;
+    w32x4 raw;
+    __device__ __forceinline__ void load(const uint8_t *row, uint32_t d, uint32_t) { raw = *reinterpret_cast<const w32x4 *>(row + d * 2u); }
+    __device__ __forceinline__ void none() { clear(raw); }
+    __device__ __forceinline__ w32x4 out(int) const { return raw; }
+};
+template <typename X>
+struct Piece<X, kBits8> {
+    static constexpr int N = 8;
+    w32x2 raw;
+    __device__ __forceinline__ void load(const uint8_t *row, uint32_t d, uint32_t) { raw = *reinterpret_cast<const w32x2 *>(row + d); }
+    __device__ __forceinline__ void none() { clear(raw); }
+    __device__ __forceinline__ w32x4 out(int) const
+    {
+        return w32x4{X::template from_fp8<false>(raw[0]), X::template from_fp8<true>(raw[0]), X::template from_fp8<false>(raw[1]),
+                     X::template from_fp8<true>(raw[1])};
+    }
+};
+template <typename X>
+struct Piece<X, kBits4> {
+    static constexpr int N = 32;
+    w32x4 raw;
+    uint32_t exponent;
+    __device__ __forceinline__ void load(const uint8_t *row, uint32_t d, uint32_t powers)
+    {
+        raw = *reinterpret_cast<const w32x4_any *>(row + d / 2u);
+        exponent = row[powers + d / 32u];
+    }
+    __device__ __forceinline__ void none() { clear(raw); exponent = 0u; }
+    __device__ __forceinline__ w32x4 out(int i) const
+    {
+        const float scale = __builtin_bit_cast(float, exponent << 23);
+        return w32x4{X::template from_fp4<0>(raw[i], scale), X::template from_fp4<1>(raw[i], scale), X::template from_fp4<2>(raw[i], scale),
+                     X::template from_fp4<3>(raw[i], scale)};
+    }
+};
+
+template <typename X, int KIND, int DP>
+__global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void kv_rows_kernel(const RowsParams p)
+{
+    using T = RowStep<DP>;
+    using P = Piece<X, KIND>;
+    constexpr int TOKENS = T::TOKENS, NB = T::NB, KS = T::KS, TB = T::TB;
+    constexpr uint32_t UNITS = TOKENS * DP / P::N, ROW_UNITS = DP / P::N;  // pieces of a tile, of a token
+    constexpr int EACH = (UNITS + 255) / 256;
+    __shared__ __attribute__((aligned(16))) uint16_t keys[2][TOKENS * T::PITCH];
+    __shared__ __attribute__((aligned(16))) uint16_t values[2][TOKENS * T::PITCH];
+    __shared__ uint32_t odd[2];  // a tile on the border holds values that are no numbers
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t n = lane & 31u, h = lane >> 5;
+    // KV heads first, so that those of one request's tiles meet in one die's cache; last rows, which see most, first
+    const uint32_t kv_head = blockIdx.x % p.n_kv_heads, rest = blockIdx.x / p.n_kv_heads;
+    const uint32_t split = rest % p.splits, tile = p.n_tiles - 1u - rest / p.splits;
+    const RowTile rt = row_tile(p, lane, tile);
+    if (!rt.here) return;
+    const int32_t len = p.lens[rt.s];
+    const uint32_t last_flat = min(rt.first + kRowTile, (uint32_t)rt.m * p.group_heads) - 1u;
+    const uint32_t most = (uint32_t)row_sees(p, len, rt, p.by_group.quotient(last_flat));
+    const uint32_t fewest = (uint32_t)row_sees(p, len, rt, p.by_group.quotient(rt.first));
+    const Spread spread(p, most, TOKENS);
+    if (split >= max(spread.active, 1u)) return;
+    const uint32_t begin = split * spread.per, end = min(begin + spread.per, spread.tiles);
+
+    const uint32_t flat = rt.first + wave * 32u + n, row = p.by_group.quotient(flat), head = kv_head * p.group_heads + flat - row * p.group_heads;
+    const uint32_t at_row = (uint32_t)rt.start + row;
+    const bool has_row = row < (uint32_t)rt.m && at_row < p.n_rows;
+    const uint32_t sees = has_row ? (uint32_t)row_sees(p, len, rt, row) : 0u;
+    const uint8_t *const kb = p.k + (uint64_t)kv_head * p.head_bytes;
+    const uint8_t *const vb = p.v + (uint64_t)kv_head * p.head_bytes;
+    // 4 bits: from a token's numbers of this head to the head's powers of 2
+    const uint32_t powers = KIND == kBits4 ? p.exponents + kv_head * (p.dim / 32u) - kv_head * p.head_bytes : 0u;
+    const int32_t *const pages = p.table + (int64_t)rt.s * p.table_stride;
+
+    w32x4 qf[KS];
+#pragma unroll
+    for (int j = 0; j < KS; j++) {
+        const uint32_t d = (uint32_t)j * 16u + h * 8u;
+        clear(qf[j]);
+        if (has_row && d < p.dim) qf[j] = *reinterpret_cast<const w32x4 *>(p.q + (uint64_t)at_row * p.q_row + (uint64_t)head * p.q_head + d * 2u);
+        if (p.negative) qf[j] ^= 0x80008000u;
+    }
+    // Of a tile every wave has a lane for each token: its page, then the row of the cache.
+    auto page_of = [&](uint32_t tile) {
+        const uint32_t token = tile * TOKENS + lane % TOKENS;
+        return token < most ? (uint32_t)pages[p.by_block.quotient(token)] : kNoCell;
+    };
+    auto cell_of = [&](uint32_t tile, uint32_t page) {
+        const uint32_t token = tile * TOKENS + lane % TOKENS;
+        return cell_in(page, p.n_blocks, p.cells_per_block, token - p.by_block.quotient(token) * p.block_size);
+    };
+    P kp[EACH], vp[EACH];
+    auto load = [&](uint32_t cell) {
+#pragma unroll
+        for (int i = 0; i < EACH; i++) {
+            const uint32_t u = tid + 256u * (uint32_t)i, token = u / ROW_UNITS, d = u % ROW_UNITS * P::N;
+            const uint32_t c = (uint32_t)__shfl((int)cell, (int)(token % TOKENS), 64);
+            kp[i].none();
+            vp[i].none();
+            if ((UNITS % 256u == 0u || u < UNITS) && c != kNoCell && d < p.dim) {
+                const uint64_t off = (uint64_t)c * p.token_bytes;
+                kp[i].load(kb + off, d, powers);
+                vp[i].load(vb + off, d, powers);
+            }
+        }
+    };
+    auto store = [&](uint32_t to, bool border) {
+        uint32_t bad = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; i++) {
+            const uint32_t u = tid + 256u * (uint32_t)i, token = u / ROW_UNITS, chunk = u % ROW_UNITS * (P::N / 8);
+            if (UNITS % 256u != 0u && u >= UNITS) break;
+#pragma unroll
+            for (int e = 0; e < P::N / 8; e++) {
+                *reinterpret_cast<w32x4 *>(keys[to] + T::key_at(token, chunk + e)) = kp[i].out(e);
+                const w32x4 v = vp[i].out(e);
+                *reinterpret_cast<w32x4 *>(values[to] + T::value_at(token, chunk + e)) = v;
+                if (border) {
+#pragma unroll
+                    for (int w = 0; w < 4; w++) bad |= (uint32_t)X::odd(v[w]);
+                }
+            }
+        }
+        if (bad) odd[to] = 1u;
+    };
+
+    f32x16 acc[NB];
+#pragma unroll
+    for (int b = 0; b < NB; b++)
+#pragma unroll
+        for (int i = 0; i < 16; i++) acc[b][i] = 0.f;
+    float ref = kLowest, own = 0.f;
+    uint64_t present = 0, next_present = 0;
+    auto border = [&](uint32_t tile) { return (tile + 1u) * TOKENS > fewest; };
+    if (tid < 2u) odd[tid] = 0u;
+    uint32_t page = kNoCell;
+    if (begin < end) {
+        uint32_t cell = cell_of(begin, page_of(begin));
+        next_present = __ballot(cell != kNoCell);
+        load(cell);
+        if (begin + 1u < end) page = page_of(begin + 1u);
+        __syncthreads();
+        store(begin & 1u, border(begin));
+    }
+    for (uint32_t t = begin; t < end; t++) {
+        const uint32_t buf = t & 1u;
+        present = next_present;
+        if (t + 1u < end) {
+            const uint32_t cell = cell_of(t + 1u, page);
+            next_present = __ballot(cell != kNoCell);
+            load(cell);
+            if (t + 2u < end) page = page_of(t + 2u);
+        }
+        __syncthreads();
+        const bool is_odd = border(t) && odd[buf];
+        f32x16 s[TB];
+#pragma unroll
+        for (int b = 0; b < TB; b++) {
+#pragma unroll
+            for (int i = 0; i < 16; i++) s[b][i] = 0.f;
+#pragma unroll
+            for (int j = 0; j < KS; j++) {
+                const w32x4 a = *reinterpret_cast<const w32x4 *>(keys[buf] + T::key_at((uint32_t)b * 32u + n, (uint32_t)j * 2u + h));
+                s[b] = mma32<X>(a, qf[j], s[b]);
+            }
+        }
+        // register i of block b: token b * 32 + i / 4 * 8 + h * 4 + i % 4
+        const uint64_t all = TOKENS == 64 ? ~0ull : 0xFFFFFFFFull;
+        const bool masked = border(t) || (present & all) != all;
+        const int32_t left = (int32_t)sees - (int32_t)(t * TOKENS + h * 4u);
+        const uint64_t there = present >> (h * 4u);
+        auto seen = [&](int b, int i) {
+            const int token = b * 32 + i / 4 * 8 + i % 4;
+            return token < left && (there >> token & 1u);
+        };
+        float top = -__builtin_inff();
+        if (masked) {
+#pragma unroll
+            for (int b = 0; b < TB; b++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) s[b][i] = seen(b, i) ? s[b][i] : -__builtin_inff();
+        }
+#pragma unroll
+        for (int b = 0; b < TB; b++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) top = fmaxf(top, s[b][i]);
+        top *= p.qk_scale;
+        if (__any(top > ref + X::kBias + X::kSlack)) {
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float higher = fmaxf(ref, top - X::kBias), shrink = __builtin_amdgcn_exp2f(ref - higher);
+            ref = higher;
+            own *= shrink;
+#pragma unroll
+            for (int b = 0; b < NB; b++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) acc[b][i] *= shrink;
+        }
+#pragma unroll
+        for (int b = 0; b < TB; b++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], p.qk_scale, -ref));
+        w32x4 w[2 * TB];
+#pragma unroll
+        for (int b = 0; b < TB; b++)
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                own += s[b][i];
+                if (i & 1) w[b * 2 + i / 8][i % 8 / 2] = X::pack(s[b][i - 1], s[b][i]);
+            }
+        // 16 lanes bring 4 tokens of 16 dimensions, and have 4 tokens of a dimension each
+        auto value = [&](int k, int b) {
+            const uint32_t token = (uint32_t)k * 16u + h * 4u + (lane & 15u) / 4u, d = (uint32_t)b * 32u + (lane & 16u) + (lane & 3u) * 4u;
+            w32x4 a;
+#pragma unroll
+            for (uint32_t half = 0; half < 2; half++) {
+                const uint16_t *from = values[buf] + T::value_at(token + half * 8u, d / 8u) + (d & 4u);
+                const w32x2 x = __builtin_bit_cast(w32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)from));
+                a[half * 2u] = x[0];
+                a[half * 2u + 1u] = x[1];
+            }
+            return a;
+        };
+        if (!is_odd) {
+#pragma unroll
+            for (int k = 0; k < 2 * TB; k++)
+#pragma unroll
+                for (int b = 0; b < NB; b++) acc[b] = mma32<X>(value(k, b), w[k], acc[b]);
+        } else {
+            // A weight of 0 does not make up for infinity or NaN: token by token, for the rows that see it.
+#pragma unroll
+            for (int k = 0; k < 2 * TB; k++)
+#pragma unroll
+                for (int b = 0; b < NB; b++) {
+                    const w32x4 a = value(k, b);
+#pragma unroll 1
+                    for (int one = 0; one < 16; one++) {
+                        const int place = one / 8 * 4 + one % 4;
+                        w32x4 only;
+#pragma unroll
+                        for (int e = 0; e < 4; e++)
+                            only[e] = (int)h == (one / 4 & 1) && place / 2 == e ? a[e] & (place & 1 ? 0xFFFF0000u : 0xFFFFu) : 0u;
+                        f32x16 r;
+#pragma unroll
+                        for (int i = 0; i < 16; i++) r[i] = 0.f;
+                        r = mma32<X>(only, w[k], r);
+                        const bool sees_it = t * TOKENS + (uint32_t)k * 16u + (uint32_t)one < sees;
+#pragma unroll
+                        for (int i = 0; i < 16; i++) acc[b][i] += sees_it ? r[i] : 0.f;
+                    }
+                }
+        }
+        if (is_odd) {
+            __syncthreads();
+            if (tid == 0u) odd[buf] = 0u;
+        }
+        if (t + 1u < end) store(buf ^ 1u, border(t + 1u));
+    }
+    own += __shfl_xor(own, 32, 64);
+    if (spread.active > 1u) {
+        const uint64_t slot = ((uint64_t)tile * p.splits + split) * p.n_kv_heads + kv_head;
+        f32x4 *const part = p.part + (slot * 4u + wave) * (NB * 4u) * 64u + lane;
+#pragma unroll
+        for (int b = 0; b < NB; b++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) part[(b * 4 + i) * 64] = f32x4{acc[b][4 * i], acc[b][4 * i + 1], acc[b][4 * i + 2], acc[b][4 * i + 3]};
+        if (h == 0u) p.part_ml[slot * kRowTile + wave * 32u + n] = float2{ref, own};
+        return;
+    }
+    if (!has_row) return;
+    const float inv = own == 0.f ? 0.f : 1.0f / own;
+    uint8_t *const out = p.out + (uint64_t)at_row * p.out_row + (uint64_t)head * p.out_head;
+#pragma unroll
+    for (int b = 0; b < NB; b++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const uint32_t d = (uint32_t)b * 32u + (uint32_t)i * 8u + h * 4u;
+            if (d >= p.dim) continue;
+            float o[4];
+#pragma unroll
+            for (int e = 0; e < 4; e++) o[e] = mean<X, KIND == kBits16>(acc[b][4 * i + e] * inv) * p.v_scale;
+            *reinterpret_cast<w32x2 *>(out + d * 2u) = w32x2{X::pack(o[0], o[1]), X::pack(o[2], o[3])};
+        }
+    if (p.lse && h == 0u)
+        p.lse[(uint64_t)at_row * p.n_heads + head] = own == 0.f ? -__builtin_inff() : (ref + __builtin_amdgcn_logf(own)) * 0.693147180559945309f;
+}
+
+// Joins a tile's splits: a workgroup has 32 dimensions of it.
+template <typename X, bool BITS16>
+__global__ __launch_bounds__(256) void kv_rows_join_kernel(const RowsParams p, uint32_t blocks, uint32_t tokens)
+{
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, n = lane & 31u, h = lane >> 5;
+    const uint32_t b = blockIdx.x % blocks, rest = blockIdx.x / blocks, kv_head = rest % p.n_kv_heads, tile = rest / p.n_kv_heads;
+    const RowTile rt = row_tile(p, lane, tile);
+    if (!rt.here) return;
+    const int32_t len = p.lens[rt.s];
+    const uint32_t last_flat = min(rt.first + kRowTile, (uint32_t)rt.m * p.group_heads) - 1u;
+    const Spread spread(p, (uint32_t)row_sees(p, len, rt, p.by_group.quotient(last_flat)), tokens);
+    if (spread.active <= 1u) return;
+    const uint32_t flat = rt.first + wave * 32u + n, row = p.by_group.quotient(flat), head = kv_head * p.group_heads + flat - row * p.group_heads;
+    const uint32_t at_row = (uint32_t)rt.start + row;
+    const bool has_row = row < (uint32_t)rt.m && at_row < p.n_rows;
+    float ref = kLowest, own = 0.f;
+    f32x4 all[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) all[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (uint32_t split = 0; split < spread.active; split++) {
+        const uint64_t slot = ((uint64_t)tile * p.splits + split) * p.n_kv_heads + kv_head;
+        const float2 ml = p.part_ml[slot * kRowTile + wave * 32u + n];
+        const f32x4 *const part = p.part + ((slot * 4u + wave) * (blocks * 4u) + b * 4u) * 64u + lane;
+        const float next = fmaxf(ref, ml.x), f = __builtin_amdgcn_exp2f(ref - next), g = __builtin_amdgcn_exp2f(ml.x - next);
+        ref = next;
+        own = own * f + ml.y * g;
+#pragma unroll
+        for (int i = 0; i < 4; i++) all[i] = all[i] * f + part[i * 64] * g;
+    }
+    if (!has_row) return;
+    const float inv = own == 0.f ? 0.f : 1.0f / own;
+    uint8_t *const out = p.out + (uint64_t)at_row * p.out_row + (uint64_t)head * p.out_head;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const uint32_t d = b * 32u + (uint32_t)i * 8u + h * 4u;
+        if (d >= p.dim) continue;
+        float o[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) o[e] = mean<X, BITS16>(all[i][e] * inv) * p.v_scale;
+        *reinterpret_cast<w32x2 *>(out + d * 2u) = w32x2{X::pack(o[0], o[1]), X::pack(o[2], o[3])};
+    }
+    if (p.lse && h == 0u && b == 0u)
+        p.lse[(uint64_t)at_row * p.n_heads + head] = own == 0.f ? -__builtin_inff() : (ref + __builtin_amdgcn_logf(own)) * 0.693147180559945309f;
+}
+
+}  // namespace dkv

@@ -1,6 +1,6 @@
 """The operators of a decode step over the paged cache, on torch tensors: new tokens
-into their pages (with rotary positions), attention of one new token per request,
-eviction of the blocks that attention has weighed least.
+into their pages (heads normed and with rotary positions), attention of one new token per
+request or of several rows of each, eviction of the blocks that attention has weighed least.
 
 Same names, rules and result codes as include/duplexkv.h.  Nothing is copied, cast
 or laid out anew on the way: a tensor of another type, shape or device than the call
@@ -41,37 +41,57 @@ class Rope:
         self.interleaved = bool(interleaved)
 
 
+class HeadNorm:
+    """Weights (float32 [dim], on the cache's device) by which each head of q and of k is normed before it rotates:
+    x / sqrt(mean(x^2) + eps) * weight.  None: those are left as they are."""
+
+    def __init__(self, q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor], eps: float = 1e-6):
+        for w in (q_weight, k_weight):
+            if w is not None and (w.dtype != torch.float32 or w.dim() != 1 or not w.is_contiguous() or not w.is_cuda):
+                raise ValueError("weights are contiguous float32 vectors on the GPU")
+        if not (0 <= eps < math.inf):
+            raise ValueError("eps is a number from 0 on")
+        self.q_weight, self.k_weight, self.eps = q_weight, k_weight, float(eps)
+
+
+def fp4_head_bytes(dim: int) -> int:
+    """head_dim of the kv_config (with elem_bytes 1) whose cache holds heads of `dim` dimensions in 4 bits."""
+    if dim <= 0 or dim % 32:
+        raise ValueError("heads in 4 bits have a multiple of 32 dimensions")
+    return dim // 32 * 17
+
+
 class Decoder:
     """Owns one kv_decoder handle.  `cfg` and `cache_ptr` are the Engine's; the cache must
     outlive the decoder.  Calls have to be ordered one after the other (one stream, or
     streams that the caller orders) and come from one host thread at a time: steps that overlap
-    in time take a decoder each.  weigh=False: without the memory that kv_attend's mass takes."""
+    in time take a decoder each.  weigh=False: without the memory that kv_attend's mass takes.
+    max_rows: most rows of a kv_attend_rows call."""
 
     def __init__(self, cfg: B.kv_config, cache_ptr: int, n_heads: int, max_seqs: int, max_blocks: int,
                  x_type: int = B.KV_BF16, kv_type: Optional[int] = None, k_scale: float = 1.0, v_scale: float = 1.0,
-                 weigh: bool = True):
+                 weigh: bool = True, max_rows: int = 0):
         self.cfg = cfg
         self._h = C.c_void_p()
         dc = B.kv_decoder_config(n_heads, x_type, x_type if kv_type is None else kv_type, max_seqs, max_blocks,
-                                 k_scale, v_scale, int(weigh))
+                                 k_scale, v_scale, int(weigh), max_rows)
         rc = B.lib.kv_decoder_create(C.byref(self._h), C.byref(cfg), C.byref(dc), C.c_void_p(cache_ptr or None))
         if rc != B.KV_OK:
             self._h = C.c_void_p()
             raise B.KVError(rc, "kv_decoder_create")
-        self._spec = _T.spec(self._h.value, cache_ptr, n_heads, int(cfg.n_kv_heads), int(cfg.head_dim), max_blocks, x_type,
-                             1.0 / math.sqrt(cfg.head_dim))
+        dim = int(cfg.head_dim) // 17 * 32 if dc.kv_type == B.KV_FP4 else int(cfg.head_dim)
+        self._spec = _T.spec(self._h.value, cache_ptr, n_heads, int(cfg.n_kv_heads), dim, max_blocks, x_type, 1.0 / math.sqrt(dim))
 
     def kv_put(self, layer: int, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, *,
                q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
                starts: Optional[torch.Tensor] = None, rope: Optional[Rope] = None,
-               positions: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> int:
+               positions: Optional[torch.Tensor] = None, norm: Optional[HeadNorm] = None, stream: Optional[int] = None) -> int:
         """k, v [row, kv_head, dim] (and q, q_out [row, head, dim]): the last starts[s + 1] - starts[s] tokens
         of each request s, or the last one of each.  positions: int32 [axis, row] (expanded along the axes: the same for each);
         without them a row stands at its place in the request, which it does no more once kv_evict has shortened that."""
-        if rope is None:
-            return _T.put(self._spec, layer, k, v, table, lens, q, q_out, starts, None, False, (), positions, stream)
-        return _T.put(self._spec, layer, k, v, table, lens, q, q_out, starts, rope.inv_freq, rope.interleaved, rope.sections,
-                      positions, stream)
+        turns = (None, False, ()) if rope is None else (rope.inv_freq, rope.interleaved, rope.sections)
+        norms = (None, None, 0.0) if norm is None else (norm.q_weight, norm.k_weight, norm.eps)
+        return _T.put(self._spec, layer, k, v, table, lens, q, q_out, starts, *turns, positions, *norms, stream)
 
     def kv_attend(self, layer: int, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, out: torch.Tensor, *,
                   scale: Optional[float] = None, lse: Optional[torch.Tensor] = None, mass: Optional[torch.Tensor] = None,
@@ -79,6 +99,14 @@ class Decoder:
         """q, out [request, head, dim]; lse float32 [request, head]; mass, mass_out float32
         [request, max_blocks].  With mass alone, the weights are added to it in place."""
         return _T.attend(self._spec, layer, q, table, lens, out, scale, lse, mass, mass_out, stream)
+
+    def kv_attend_rows(self, layer: int, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, out: torch.Tensor, *,
+                       starts: Optional[torch.Tensor] = None, causal: bool = True, scale: Optional[float] = None,
+                       lse: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> int:
+        """q, out [row, head, dim]; lse float32 [row, head]; starts int32 [request + 1]: each request's rows, one behind the
+        other (without it: one row each).  causal: they are its last tokens, each sees what is before it and itself; otherwise each sees
+        all of `lens`: an encoder's states, for instance."""
+        return _T.attend_rows(self._spec, layer, q, table, lens, out, starts, causal, scale, lse, stream)
 
     def kv_evict(self, table: torch.Tensor, lens: torch.Tensor, mass: torch.Tensor, *, budget: int, n_first: int, n_last: int,
                  evicted_ids: torch.Tensor, evicted_at: torch.Tensor, n_evicted: torch.Tensor,
