@@ -160,7 +160,7 @@ int kv_decoder_create(kv_decoder **out, const kv_config *cfg, const kv_decoder_c
                    n_gran = dc->weigh ? (uint64_t)dc->max_seqs * d->max_granules * (uint64_t)dc->n_heads * 4 : 0;
     const uint64_t n_rows_part = dkv::rows_part_bytes(d), n_rows_ml = dkv::rows_ml_bytes(d), n_gran16 = (n_gran + 15) / 16 * 16;
     uint8_t *mem = nullptr;
-    if (hipMalloc((void **)&mem, n_part + n_ml + n_lse + n_gran16 + n_rows_part + n_rows_ml) != hipSuccess) {
+    if (hipMalloc((void **)&mem, n_part + n_ml + n_lse + n_gran16 + n_rows_part + n_rows_ml + 16) != hipSuccess) {
         (void)hipGetLastError();
         return fail(KV_ENOMEM);
     }
@@ -170,6 +170,11 @@ int kv_decoder_create(kv_decoder **out, const kv_config *cfg, const kv_decoder_c
     d->granules = (float *)(mem + n_part + n_ml + n_lse);
     d->rows_part = (dkv::f32x4 *)(mem + n_part + n_ml + n_lse + n_gran16);
     d->rows_ml = (float2 *)(mem + n_part + n_ml + n_lse + n_gran16 + n_rows_part);
+    d->rows_zeros = mem + n_part + n_ml + n_lse + n_gran16 + n_rows_part + n_rows_ml;
+    if (dc->max_rows && (hipMemset(d->rows_zeros, 0, 16) != hipSuccess || hipDeviceSynchronize() != hipSuccess)) {
+        (void)hipFree(mem);
+        return fail(KV_EHIP);
+    }
     *out = d;
     return KV_OK;
 }

@@ -28,6 +28,7 @@ struct kv_decoder {
     // kv_attend_rows: what splits leave
     dkv::f32x4 *rows_part = nullptr;
     float2 *rows_ml = nullptr;
+    uint8_t *rows_zeros = nullptr;  // what lies in pages that are not there: 16 bytes
 };
 
 namespace dkv {

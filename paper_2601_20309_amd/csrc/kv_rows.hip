@@ -59,6 +59,7 @@ extern "C" int kv_attend_rows(kv_decoder *d, const kv_attend_rows_args *a, void 
     p.q = (const uint8_t *)a->q.data;
     p.out = (uint8_t *)const_cast<void *>(a->out.data);
     p.lse = a->lse;
+    p.zeros = d->rows_zeros;
     p.part = d->rows_part;
     p.part_ml = d->rows_ml;
     p.q_row = 2ull * (uint64_t)a->q.row;

@@ -26,6 +26,7 @@ struct RowsParams {
     const uint8_t *q;
     uint8_t *out;
     float *lse;
+    const uint8_t *zeros;  // 16 bytes
     f32x4 *part;      // [tile * splits][wave][vector][lane]: sums of a split, as they lie in registers
     float2 *part_ml;  // [tile * splits][kRowTile]: reference, sum of weights
     uint64_t q_row, q_head, out_row, out_head;  // bytes
@@ -121,16 +122,10 @@ struct RowStep {
     static constexpr int CHUNKS = PITCH / 8;
     static constexpr int NB = DP / 32, KS = DP / 16, TB = TOKENS / 32;
     // Where 8 numbers lie: keys are read 16 bytes a lane, 32 tokens at once, values 32 dimensions of 8 tokens at once.
-    static __device__ __forceinline__ uint32_t key_at(uint32_t token, uint32_t chunk)
-    {
-        const uint32_t f = PITCH == 64 ? token >> 1 & 7u : token & 15u;
-        return (token * CHUNKS + (chunk ^ f)) * 8u;
-    }
-    static __device__ __forceinline__ uint32_t value_at(uint32_t token, uint32_t chunk)
-    {
-        const uint32_t f = PITCH == 64 ? token >> 1 & 1u : token & 3u;
-        return (token * CHUNKS + (chunk ^ f << 2)) * 8u;
-    }
+    static __device__ __forceinline__ uint32_t key_turn(uint32_t token) { return PITCH == 64 ? token >> 1 & 7u : token & 15u; }
+    static __device__ __forceinline__ uint32_t value_turn(uint32_t token) { return (PITCH == 64 ? token >> 1 & 1u : token & 3u) << 2; }
+    static __device__ __forceinline__ uint32_t key_at(uint32_t token, uint32_t chunk) { return (token * CHUNKS + (chunk ^ key_turn(token))) * 8u; }
+    static __device__ __forceinline__ uint32_t value_at(uint32_t token, uint32_t chunk) { return (token * CHUNKS + (chunk ^ value_turn(token))) * 8u; }
 };
 
 // As much of a row of the cache as a thread takes at once, and what it becomes.
@@ -175,17 +170,43 @@ struct Piece<X, kBits4> {
     }
 };
 
+// 16 bytes a lane from global memory into LDS, one lane's behind the other's from `to` on.  In assembly, since beside the
+// builtin the compiler waits for all reads of LDS where some would do, as long as one of these is under way.  Whoever looks at
+// what came waits for it first (loaded_lds), and then for the other waves.
+__device__ __forceinline__ void load_lds(const uint8_t *from, uint16_t *to)
+{
+    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)to);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory", "m0");
+}
+__device__ __forceinline__ void loaded_lds() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// N products of which each reads LDS READS times: the reads are AHEAD products ahead.
+template <int N, int READS, int AHEAD>
+__device__ __forceinline__ void pipeline()
+{
+    constexpr int kMma = 0x008, kRead = 0x100;
+    __builtin_amdgcn_sched_group_barrier(kRead, READS * AHEAD, 0);
+#pragma unroll
+    for (int i = 0; i < N - AHEAD; i++) {
+        __builtin_amdgcn_sched_group_barrier(kMma, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kRead, READS, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(kMma, AHEAD, 0);
+}
+
 template <typename X, int KIND, int DP>
 __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void kv_rows_kernel(const RowsParams p)
 {
     using T = RowStep<DP>;
     using P = Piece<X, KIND>;
     constexpr int TOKENS = T::TOKENS, NB = T::NB, KS = T::KS, TB = T::TB;
+    constexpr bool DIRECT = KIND == kBits16;
     constexpr uint32_t UNITS = TOKENS * DP / P::N, ROW_UNITS = DP / P::N;  // pieces of a tile, of a token
-    constexpr int EACH = (UNITS + 255) / 256;
-    __shared__ __attribute__((aligned(16))) uint16_t keys[2][TOKENS * T::PITCH];
-    __shared__ __attribute__((aligned(16))) uint16_t values[2][TOKENS * T::PITCH];
-    __shared__ uint32_t odd[2];  // a tile on the border holds values that are no numbers
+    constexpr int EACH = DIRECT ? 1 : (UNITS + 255) / 256;
+    // (four arrays: loads into one are then known not to touch what is read from another)
+    __shared__ __attribute__((aligned(16))) uint16_t keys0[TOKENS * T::PITCH], keys1[TOKENS * T::PITCH];
+    __shared__ __attribute__((aligned(16))) uint16_t values0[TOKENS * T::PITCH], values1[TOKENS * T::PITCH];
+    __shared__ uint32_t odd;  // a tile on the border holds values that are no numbers
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t n = lane & 31u, h = lane >> 5;
     // KV heads first, so that those of one request's tiles meet in one die's cache; last rows, which see most, first
@@ -229,38 +250,56 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void kv_rows_kernel(const Ro
         return cell_in(page, p.n_blocks, p.cells_per_block, token - p.by_block.quotient(token) * p.block_size);
     };
     P kp[EACH], vp[EACH];
-    auto load = [&](uint32_t cell) {
+    auto load = [&](auto buf, uint32_t cell) {
+        if constexpr (DIRECT) {
+            // a wave brings 512 numbers at once, whole tokens, each lane the 8 that belong where its lane's go
+            uint16_t *const keys = buf() ? keys1 : keys0, *const values = buf() ? values1 : values0;
+            // (turns of token + 4 AT_ONCE i are those of either, one with the other: they have no bit in common)
+            constexpr uint32_t AT_ONCE = 512 / T::PITCH, TURNS = TOKENS / AT_ONCE / 4;
+            uint32_t l = lane;
+            asm volatile("" : "+v"(l));  // (found anew for every tile: kept, these are what does not fit the registers)
+            const uint32_t token = wave * AT_ONCE + l / T::CHUNKS, slot = l % T::CHUNKS;
+            const uint32_t ck = slot ^ T::key_turn(token), cv = slot ^ T::value_turn(token);
 #pragma unroll
-        for (int i = 0; i < EACH; i++) {
-            const uint32_t u = tid + 256u * (uint32_t)i, token = u / ROW_UNITS, d = u % ROW_UNITS * P::N;
-            const uint32_t c = (uint32_t)__shfl((int)cell, (int)(token % TOKENS), 64);
-            kp[i].none();
-            vp[i].none();
-            if ((UNITS % 256u == 0u || u < UNITS) && c != kNoCell && d < p.dim) {
+            for (uint32_t i = 0; i < TURNS; i++) {
+                const uint32_t c = (uint32_t)__builtin_amdgcn_ds_bpermute((int)((token + i * 4u * AT_ONCE) * 4u), (int)cell);
+                const uint32_t dk = (ck ^ T::key_turn(i * 4u * AT_ONCE)) * 8u, dv = (cv ^ T::value_turn(i * 4u * AT_ONCE)) * 8u;
                 const uint64_t off = (uint64_t)c * p.token_bytes;
-                kp[i].load(kb + off, d, powers);
-                vp[i].load(vb + off, d, powers);
+                const uint8_t *k = kb + off + dk * 2u, *v = vb + off + dv * 2u;
+                if (c == kNoCell || dk >= p.dim) k = p.zeros;
+                if (c == kNoCell || dv >= p.dim) v = p.zeros;
+                load_lds(k, keys + (i * 4u + wave) * AT_ONCE * T::PITCH);
+                load_lds(v, values + (i * 4u + wave) * AT_ONCE * T::PITCH);
             }
-        }
-    };
-    auto store = [&](uint32_t to, bool border) {
-        uint32_t bad = 0;
+        } else {
 #pragma unroll
-        for (int i = 0; i < EACH; i++) {
-            const uint32_t u = tid + 256u * (uint32_t)i, token = u / ROW_UNITS, chunk = u % ROW_UNITS * (P::N / 8);
-            if (UNITS % 256u != 0u && u >= UNITS) break;
-#pragma unroll
-            for (int e = 0; e < P::N / 8; e++) {
-                *reinterpret_cast<w32x4 *>(keys[to] + T::key_at(token, chunk + e)) = kp[i].out(e);
-                const w32x4 v = vp[i].out(e);
-                *reinterpret_cast<w32x4 *>(values[to] + T::value_at(token, chunk + e)) = v;
-                if (border) {
-#pragma unroll
-                    for (int w = 0; w < 4; w++) bad |= (uint32_t)X::odd(v[w]);
+            for (int i = 0; i < EACH; i++) {
+                const uint32_t u = tid + 256u * (uint32_t)i, token = u / ROW_UNITS, d = u % ROW_UNITS * P::N;
+                const uint32_t c = (uint32_t)__shfl((int)cell, (int)(token % TOKENS), 64);
+                kp[i].none();
+                vp[i].none();
+                if ((UNITS % 256u == 0u || u < UNITS) && c != kNoCell && d < p.dim) {
+                    const uint64_t off = (uint64_t)c * p.token_bytes;
+                    kp[i].load(kb + off, d, powers);
+                    vp[i].load(vb + off, d, powers);
                 }
             }
         }
-        if (bad) odd[to] = 1u;
+    };
+    auto store = [&](auto buf) {
+        if constexpr (!DIRECT) {
+            uint16_t *const keys = buf() ? keys1 : keys0, *const values = buf() ? values1 : values0;
+#pragma unroll
+            for (int i = 0; i < EACH; i++) {
+                const uint32_t u = tid + 256u * (uint32_t)i, token = u / ROW_UNITS, chunk = u % ROW_UNITS * (P::N / 8);
+                if (UNITS % 256u != 0u && u >= UNITS) break;
+#pragma unroll
+                for (int e = 0; e < P::N / 8; e++) {
+                    *reinterpret_cast<w32x4 *>(keys + T::key_at(token, chunk + e)) = kp[i].out(e);
+                    *reinterpret_cast<w32x4 *>(values + T::value_at(token, chunk + e)) = vp[i].out(e);
+                }
+            }
+        }
     };
 
     f32x16 acc[NB];
@@ -269,56 +308,73 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void kv_rows_kernel(const Ro
 #pragma unroll
         for (int i = 0; i < 16; i++) acc[b][i] = 0.f;
     float ref = kLowest, own = 0.f;
-    uint64_t present = 0, next_present = 0;
-    auto border = [&](uint32_t tile) { return (tile + 1u) * TOKENS > fewest; };
-    if (tid < 2u) odd[tid] = 0u;
+    uint64_t next_present = 0;
     uint32_t page = kNoCell;
+    typedef std::integral_constant<int, 0> Zero;
+    typedef std::integral_constant<int, 1> One;
     if (begin < end) {
-        uint32_t cell = cell_of(begin, page_of(begin));
+        const uint32_t cell = cell_of(begin, page_of(begin));
         next_present = __ballot(cell != kNoCell);
-        load(cell);
+        load(Zero{}, cell);
         if (begin + 1u < end) page = page_of(begin + 1u);
-        __syncthreads();
-        store(begin & 1u, border(begin));
+        store(Zero{});
     }
-    for (uint32_t t = begin; t < end; t++) {
-        const uint32_t buf = t & 1u;
-        present = next_present;
+    auto step = [&](auto buf, auto other, uint32_t t) {
+        uint16_t *const keys = buf() ? keys1 : keys0, *const values = buf() ? values1 : values0;
+        const uint64_t present = next_present;
+        if constexpr (DIRECT) loaded_lds();
+        __syncthreads();
         if (t + 1u < end) {
             const uint32_t cell = cell_of(t + 1u, page);
             next_present = __ballot(cell != kNoCell);
-            load(cell);
+            load(other, cell);
             if (t + 2u < end) page = page_of(t + 2u);
         }
-        __syncthreads();
-        const bool is_odd = border(t) && odd[buf];
+        const bool border = (t + 1u) * TOKENS > fewest;
         f32x16 s[TB];
 #pragma unroll
-        for (int b = 0; b < TB; b++) {
+        for (int b = 0; b < TB; b++)
 #pragma unroll
             for (int i = 0; i < 16; i++) s[b][i] = 0.f;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int j = 0; j < KS; j++) {
-                const w32x4 a = *reinterpret_cast<const w32x4 *>(keys[buf] + T::key_at((uint32_t)b * 32u + n, (uint32_t)j * 2u + h));
+        for (int j = 0; j < KS; j++)
+#pragma unroll
+            for (int b = 0; b < TB; b++) {
+                const w32x4 a = *reinterpret_cast<const w32x4 *>(keys + T::key_at((uint32_t)b * 32u + n, (uint32_t)j * 2u + h));
                 s[b] = mma32<X>(a, qf[j], s[b]);
             }
-        }
+        pipeline<KS * TB, 1, 6>();
+        __builtin_amdgcn_sched_barrier(0);
         // register i of block b: token b * 32 + i / 4 * 8 + h * 4 + i % 4
         const uint64_t all = TOKENS == 64 ? ~0ull : 0xFFFFFFFFull;
-        const bool masked = border(t) || (present & all) != all;
-        const int32_t left = (int32_t)sees - (int32_t)(t * TOKENS + h * 4u);
-        const uint64_t there = present >> (h * 4u);
-        auto seen = [&](int b, int i) {
-            const int token = b * 32 + i / 4 * 8 + i % 4;
-            return token < left && (there >> token & 1u);
-        };
-        float top = -__builtin_inff();
-        if (masked) {
+        bool is_odd = false;
+        if (border || (present & all) != all) {
+            const int32_t left = (int32_t)sees - (int32_t)(t * TOKENS + h * 4u);
+            const uint64_t there = present >> (h * 4u);
 #pragma unroll
             for (int b = 0; b < TB; b++)
 #pragma unroll
-                for (int i = 0; i < 16; i++) s[b][i] = seen(b, i) ? s[b][i] : -__builtin_inff();
+                for (int i = 0; i < 16; i++) {
+                    const int token = b * 32 + i / 4 * 8 + i % 4;
+                    s[b][i] = token < left && (there >> token & 1u) ? s[b][i] : -__builtin_inff();
+                }
         }
+        if (border) {
+            // values that some rows of the tile do not see: are all of them numbers?
+            bool bad = false;
+            for (uint32_t u = tid; u < TOKENS * (DP / 8u); u += 256u) {
+                const uint32_t token = u / (DP / 8u), chunk = u - token * (DP / 8u);
+                const w32x4 v = *reinterpret_cast<const w32x4 *>(values + T::value_at(token, chunk));
+                bad |= X::odd(v[0]) || X::odd(v[1]) || X::odd(v[2]) || X::odd(v[3]);
+            }
+            if (tid == 0u) odd = 0u;
+            __syncthreads();
+            if (bad) odd = 1u;
+            __syncthreads();
+            is_odd = odd;
+        }
+        float top = -__builtin_inff();
 #pragma unroll
         for (int b = 0; b < TB; b++)
 #pragma unroll
@@ -334,15 +390,12 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void kv_rows_kernel(const Ro
 #pragma unroll
                 for (int i = 0; i < 16; i++) acc[b][i] *= shrink;
         }
-#pragma unroll
-        for (int b = 0; b < TB; b++)
-#pragma unroll
-            for (int i = 0; i < 16; i++) s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], p.qk_scale, -ref));
         w32x4 w[2 * TB];
 #pragma unroll
         for (int b = 0; b < TB; b++)
 #pragma unroll
             for (int i = 0; i < 16; i++) {
+                s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], p.qk_scale, -ref));
                 own += s[b][i];
                 if (i & 1) w[b * 2 + i / 8][i % 8 / 2] = X::pack(s[b][i - 1], s[b][i]);
             }
@@ -352,7 +405,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void kv_rows_kernel(const Ro
             w32x4 a;
 #pragma unroll
             for (uint32_t half = 0; half < 2; half++) {
-                const uint16_t *from = values[buf] + T::value_at(token + half * 8u, d / 8u) + (d & 4u);
+                const uint16_t *from = values + T::value_at(token + half * 8u, d / 8u) + (d & 4u);
                 const w32x2 x = __builtin_bit_cast(w32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)from));
                 a[half * 2u] = x[0];
                 a[half * 2u + 1u] = x[1];
@@ -360,10 +413,13 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void kv_rows_kernel(const Ro
             return a;
         };
         if (!is_odd) {
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int k = 0; k < 2 * TB; k++)
 #pragma unroll
                 for (int b = 0; b < NB; b++) acc[b] = mma32<X>(value(k, b), w[k], acc[b]);
+            pipeline<2 * TB * NB, 2, 6>();
+            __builtin_amdgcn_sched_barrier(0);
         } else {
             // A weight of 0 does not make up for infinity or NaN: token by token, for the rows that see it.
 #pragma unroll
@@ -388,11 +444,11 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void kv_rows_kernel(const Ro
                     }
                 }
         }
-        if (is_odd) {
-            __syncthreads();
-            if (tid == 0u) odd[buf] = 0u;
-        }
-        if (t + 1u < end) store(buf ^ 1u, border(t + 1u));
+        if (t + 1u < end) store(other);
+    };
+    for (uint32_t t = begin; t < end; t += 2u) {
+        step(Zero{}, One{}, t);
+        if (t + 1u < end) step(One{}, Zero{}, t + 1u);
     }
     own += __shfl_xor(own, 32, 64);
     if (spread.active > 1u) {

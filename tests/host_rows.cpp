@@ -64,6 +64,7 @@ hipError_t hipGetDeviceCount(int *n) { *n = 4; return hipSuccess; }
 const char *hipGetErrorString(hipError_t) { return "none"; }
 hipError_t hipGetLastError() { return hipSuccess; }
 hipError_t hipMalloc(void **p, size_t n) { allocated = n; *p = std::calloc(1, 64); return hipSuccess; }
+hipError_t hipMemset(void *, int, size_t) { return hipSuccess; }
 hipError_t hipMemGetAddressRange(hipDeviceptr_t *base, size_t *n, hipDeviceptr_t) { *base = nullptr; *n = ~(size_t)0; return hipSuccess; }
 hipError_t hipPointerGetAttributes(hipPointerAttribute_t *a, const void *)
 {
