@@ -10,17 +10,21 @@
 
 namespace {
 
-static_assert(dkv::kRowTile == dkv::kRowsOfTile, "memory for what splits leave");
-
 template <typename X, int KIND>
-void launch_rows(dim3 g, hipStream_t s, const dkv::RowsParams &p, uint32_t join_tiles)
+void launch_rows(dim3 g, hipStream_t s, const dkv::RowsParams &p)
 {
+    auto launch = [&](auto dims, auto rows) {
+        constexpr int DP = decltype(dims)::value, ROWS = decltype(rows)::value;
+        using T = dkv::RowStep<DP, ROWS>;
+        hipLaunchKernelGGL((dkv::kv_rows_kernel<X, KIND, DP, ROWS>), g, dim3(64 * T::WAVES), 0, s, p);
+        const uint64_t joins = (uint64_t)p.n_tiles * p.n_kv_heads * (ROWS / 32) * (DP / 32);
+        if (p.splits > 1u)
+            hipLaunchKernelGGL((dkv::kv_rows_join_kernel<X, KIND == dkv::kBits16>), dim3((uint32_t)((joins + 3) / 4)), dim3(256), 0, s, p,
+                               (uint32_t)DP / 32u, (uint32_t)T::TOKENS);
+    };
     auto go = [&](auto dims) {
-        constexpr int DP = decltype(dims)::value;
-        hipLaunchKernelGGL((dkv::kv_rows_kernel<X, KIND, DP>), g, dim3(256), 0, s, p);
-        if (join_tiles)
-            hipLaunchKernelGGL((dkv::kv_rows_join_kernel<X, KIND == dkv::kBits16>), dim3(join_tiles * (DP / 32)), dim3(256), 0, s, p,
-                               (uint32_t)DP / 32u, (uint32_t)dkv::RowStep<DP>::TOKENS);
+        if (p.row_bits == 5u) launch(dims, std::integral_constant<int, 32>{});
+        else launch(dims, std::integral_constant<int, 128>{});
     };
     switch (dkv::rows_dims(p.dim)) {
     case 64: go(std::integral_constant<int, 64>{}); break;
@@ -86,23 +90,25 @@ extern "C" int kv_attend_rows(kv_decoder *d, const kv_attend_rows_args *a, void 
     p.negative = qk_scale < 0.f ? 1u : 0u;
     p.qk_scale = std::max(std::fabs(qk_scale), 0x1p-126f);  // (0 times the score of what is masked, -inf, is NaN)
     p.v_scale = d->dc.v_scale;
-    p.n_tiles = (uint32_t)row_tiles(p.n_rows, p.group_heads, p.n_seqs);
-    p.row_tile = kRowsOfTile;
-    // Few tiles of rows: the tokens are split, so that two workgroups for each compute unit have some.
+    // Few rows to a request: 32 to a tile.
+    const uint64_t mean = (uint64_t)p.n_rows * p.group_heads / p.n_seqs;
+    const bool few = mean <= 48u && row_tiles(p.n_rows, p.group_heads, p.n_seqs, 5) * p.n_kv_heads <= kMostTiles;
+    p.row_bits = few ? 5u : 7u;
+    p.n_tiles = (uint32_t)row_tiles(p.n_rows, p.group_heads, p.n_seqs, (int)p.row_bits);
+    // Few tiles of rows: the tokens are split, so that every compute unit has some.
     const uint64_t each = (uint64_t)p.n_tiles * p.n_kv_heads;
-    p.least = 2u;
-    const uint32_t tokens = p.dim > 128u ? 32u : 64u, most = (p.max_tokens + tokens - 1u) / tokens;
-    p.splits = (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>(kRowSlots / each, (most + p.least - 1u) / p.least));
+    const uint32_t tokens = p.dim > 128u || p.row_bits == 5u ? 32u : 64u, most = (p.max_tokens + tokens - 1u) / tokens;
+    p.least = p.row_bits == 5u ? 16u : 2u;
+    p.splits = (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>((kRowSums >> p.row_bits) / each, (most + p.least - 1u) / p.least));
     const dim3 g((uint32_t)(each * p.splits));
-    const uint32_t join_tiles = p.splits > 1u ? (uint32_t)each : 0u;
     hipStream_t s = (hipStream_t)stream;
     switch ((d->dc.x_type == KV_FP16 ? 1 : 0) + (d->dc.kv_type == KV_FP8 ? 2 : d->dc.kv_type == KV_FP4 ? 4 : 0)) {
-    case 0: launch_rows<Bf16, kBits16>(g, s, p, join_tiles); break;
-    case 1: launch_rows<Fp16, kBits16>(g, s, p, join_tiles); break;
-    case 2: launch_rows<Bf16, kBits8>(g, s, p, join_tiles); break;
-    case 3: launch_rows<Fp16, kBits8>(g, s, p, join_tiles); break;
-    case 4: launch_rows<Bf16, kBits4>(g, s, p, join_tiles); break;
-    default: launch_rows<Fp16, kBits4>(g, s, p, join_tiles); break;
+    case 0: launch_rows<Bf16, kBits16>(g, s, p); break;
+    case 1: launch_rows<Fp16, kBits16>(g, s, p); break;
+    case 2: launch_rows<Bf16, kBits8>(g, s, p); break;
+    case 3: launch_rows<Fp16, kBits8>(g, s, p); break;
+    case 4: launch_rows<Bf16, kBits4>(g, s, p); break;
+    default: launch_rows<Fp16, kBits4>(g, s, p); break;
     }
     DECTRY(hipGetLastError());
     return KV_OK;

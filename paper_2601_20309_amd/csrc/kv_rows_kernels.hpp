@@ -14,9 +14,9 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 // tokens with a running reference.  The query heads of a KV head are rows, too: heads of a row lie one
 // behind the other, so that few rows of many heads fill a tile, and all of them share the keys that are brought.
 //
-// A workgroup has kRowTile rows of one KV head, 32 a wave, and goes over the tokens TOKENS at a time.  These go
-// through registers into LDS, two tiles in turn: in 16 bits whatever the cache holds, so that the products are the same
-// for every type of cache.  Both products are taken transposed, tokens x rows and dimensions x rows, as in kv_attend:
+// A workgroup has 128 rows of one KV head, 32 a wave, and goes over the tokens 64 at a time (32 above 128 dimensions), or, where
+// requests have few rows, 32 rows, and its waves take turns at the tokens.  These go into LDS, two tiles in
+// turn: in 16 bits whatever the cache holds, so that the products are the same for every type of cache.  Both products are taken transposed, tokens x rows and dimensions x rows, as in kv_attend:
 // a lane has one row, its reference and its sums, and weights come out as the second product's operand.
 // Values are read from LDS transposed, four tokens of a dimension at a time.
 
@@ -27,24 +27,22 @@ struct RowsParams {
     uint8_t *out;
     float *lse;
     const uint8_t *zeros;  // 16 bytes
-    f32x4 *part;      // [tile * splits][wave][vector][lane]: sums of a split, as they lie in registers
-    float2 *part_ml;  // [tile * splits][kRowTile]: reference, sum of weights
+    f32x4 *part;      // [tile * splits][32 rows][vector][lane]: sums of a split, as they lie in registers
+    float2 *part_ml;  // [tile * splits][row]: reference, sum of weights
     uint64_t q_row, q_head, out_row, out_head;  // bytes
     int64_t table_stride;
     uint32_t n_seqs, n_rows, n_heads, n_kv_heads, max_tokens;
     uint32_t dim, token_bytes, head_bytes, block_size, cells_per_block, n_blocks;
     uint32_t exponents;  // 4 bits: from a token's first byte to its exponents
     uint32_t group_heads, causal, splits, least;  // least: tiles of tokens of a split
-    uint32_t n_tiles, row_tile;                   // tiles of rows of a KV head, empty ones among them; rows of one
+    uint32_t n_tiles, row_bits;                   // tiles of rows of a KV head, empty ones among them; log2 of the rows of one
     Divide by_block, by_group;
     uint32_t negative;  // the scale is: keys meet -q
     float qk_scale;     // to base 2, not negative
     float v_scale;
 };
 
-constexpr uint32_t kRowTile = 128;
-
-// Which rows a tile has.  Request s's tiles are floor(starts[s] * group / kRowTile) + s on: as many as it needs, or
+// Which rows a tile has.  Request s's tiles are floor(starts[s] * group / rows of one) + s on: as many as it needs, or
 // some more, which are empty.  So no sums over requests are needed to find one.
 struct RowTile {
     uint32_t s, first;      // request; its rows' heads before this tile
@@ -55,7 +53,7 @@ struct RowTile {
 __device__ __forceinline__ uint32_t first_tile(const RowsParams &p, uint32_t s)
 {
     const int32_t start = p.starts ? p.starts[s] : (int32_t)s;
-    return (uint32_t)((uint64_t)(uint32_t)max(start, 0) * p.group_heads / kRowTile) + s;
+    return (uint32_t)((uint64_t)(uint32_t)max(start, 0) * p.group_heads >> p.row_bits) + s;
 }
 
 __device__ __forceinline__ RowTile row_tile(const RowsParams &p, uint32_t lane, uint32_t tile)
@@ -75,7 +73,7 @@ __device__ __forceinline__ RowTile row_tile(const RowsParams &p, uint32_t lane, 
     t.start = p.starts ? p.starts[t.s] : (int32_t)t.s;
     const int64_t next = p.starts ? p.starts[t.s + 1u] : (int64_t)t.s + 1;
     t.m = (int32_t)min(max(next - t.start, (int64_t)0), (int64_t)p.n_rows);
-    const uint64_t first = (uint64_t)(tile - base) * kRowTile;
+    const uint64_t first = (uint64_t)(tile - base) << p.row_bits;
     t.here = tile >= base && t.start >= 0 && first < (uint64_t)t.m * p.group_heads;
     t.first = (uint32_t)first;
     return t;
@@ -115,9 +113,13 @@ __device__ __forceinline__ float mean(float x)
     return OF_X && __builtin_fabsf(x) < __builtin_inff() ? fminf(fmaxf(x, -X::kMost), X::kMost) : x;
 }
 
-template <int DP>
+// ROWS 128: four waves have 32 rows each, and share tiles of tokens.  ROWS 32: all waves have the same rows, and take turns at the
+// tiles of tokens, each with LDS of its own, so that nothing waits for the others.
+template <int DP, int ROWS>
 struct RowStep {
-    static constexpr int TOKENS = DP > 128 ? 32 : 64;
+    static constexpr bool TURNS = ROWS == 32;
+    static constexpr int TOKENS = TURNS || DP > 128 ? 32 : 64;
+    static constexpr int WAVES = TURNS && DP > 128 ? 2 : 4;
     static constexpr int PITCH = DP <= 64 ? 64 : DP <= 128 ? 128 : 256;  // of a token in LDS, in numbers
     static constexpr int CHUNKS = PITCH / 8;
     static constexpr int NB = DP / 32, KS = DP / 16, TB = TOKENS / 32;
@@ -194,18 +196,20 @@ __device__ __forceinline__ void pipeline()
     __builtin_amdgcn_sched_group_barrier(kMma, AHEAD, 0);
 }
 
-template <typename X, int KIND, int DP>
-__global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void kv_rows_kernel(const RowsParams p)
+template <typename X, int KIND, int DP, int ROWS>
+__global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)) void kv_rows_kernel(const RowsParams p)
 {
-    using T = RowStep<DP>;
+    using T = RowStep<DP, ROWS>;
     using P = Piece<X, KIND>;
-    constexpr int TOKENS = T::TOKENS, NB = T::NB, KS = T::KS, TB = T::TB;
-    constexpr bool DIRECT = KIND == kBits16;
-    constexpr uint32_t UNITS = TOKENS * DP / P::N, ROW_UNITS = DP / P::N;  // pieces of a tile, of a token
-    constexpr int EACH = DIRECT ? 1 : (UNITS + 255) / 256;
-    // (four arrays: loads into one are then known not to touch what is read from another)
-    __shared__ __attribute__((aligned(16))) uint16_t keys0[TOKENS * T::PITCH], keys1[TOKENS * T::PITCH];
-    __shared__ __attribute__((aligned(16))) uint16_t values0[TOKENS * T::PITCH], values1[TOKENS * T::PITCH];
+    constexpr int TOKENS = T::TOKENS, NB = T::NB, KS = T::KS, TB = T::TB, WAVES = T::WAVES;
+    constexpr bool DIRECT = KIND == kBits16, TURNS = T::TURNS;
+    constexpr uint32_t SHARING = TURNS ? 1 : WAVES, STEP = TURNS ? WAVES : 1;  // waves of a tile of tokens; tiles of a turn
+    constexpr uint32_t UNITS = TOKENS * DP / P::N, ROW_UNITS = DP / P::N;      // pieces of a tile, of a token
+    constexpr uint32_t LANES = 64 * SHARING;
+    constexpr int EACH = DIRECT ? 1 : (UNITS + LANES - 1) / LANES;
+    constexpr uint32_t PLANE = TOKENS * T::PITCH, TILE = 2 * PLANE, ALL = 2 * TILE * (TURNS ? WAVES : 1);
+    // of each wave (or all): two tiles of keys and values; at the end sums
+    __shared__ __attribute__((aligned(16))) uint16_t lds[ALL];
     __shared__ uint32_t odd;  // a tile on the border holds values that are no numbers
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t n = lane & 31u, h = lane >> 5;
@@ -215,14 +219,15 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void kv_rows_kernel(const Ro
     const RowTile rt = row_tile(p, lane, tile);
     if (!rt.here) return;
     const int32_t len = p.lens[rt.s];
-    const uint32_t last_flat = min(rt.first + kRowTile, (uint32_t)rt.m * p.group_heads) - 1u;
+    const uint32_t last_flat = min(rt.first + ROWS, (uint32_t)rt.m * p.group_heads) - 1u;
     const uint32_t most = (uint32_t)row_sees(p, len, rt, p.by_group.quotient(last_flat));
     const uint32_t fewest = (uint32_t)row_sees(p, len, rt, p.by_group.quotient(rt.first));
     const Spread spread(p, most, TOKENS);
     if (split >= max(spread.active, 1u)) return;
-    const uint32_t begin = split * spread.per, end = min(begin + spread.per, spread.tiles);
+    const uint32_t begin = split * spread.per + (TURNS ? wave : 0u), end = min(split * spread.per + spread.per, spread.tiles);
 
-    const uint32_t flat = rt.first + wave * 32u + n, row = p.by_group.quotient(flat), head = kv_head * p.group_heads + flat - row * p.group_heads;
+    uint16_t *const tiles = lds + (TURNS ? wave * 2u * TILE : 0u);
+    const uint32_t flat = rt.first + (TURNS ? 0u : wave * 32u) + n, row = p.by_group.quotient(flat), head = kv_head * p.group_heads + flat - row * p.group_heads;
     const uint32_t at_row = (uint32_t)rt.start + row;
     const bool has_row = row < (uint32_t)rt.m && at_row < p.n_rows;
     const uint32_t sees = has_row ? (uint32_t)row_sees(p, len, rt, row) : 0u;
@@ -253,32 +258,34 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void kv_rows_kernel(const Ro
     auto load = [&](auto buf, uint32_t cell) {
         if constexpr (DIRECT) {
             // a wave brings 512 numbers at once, whole tokens, each lane the 8 that belong where its lane's go
-            uint16_t *const keys = buf() ? keys1 : keys0, *const values = buf() ? values1 : values0;
-            // (turns of token + 4 AT_ONCE i are those of either, one with the other: they have no bit in common)
-            constexpr uint32_t AT_ONCE = 512 / T::PITCH, TURNS = TOKENS / AT_ONCE / 4;
+            uint16_t *const keys = tiles + buf() * TILE, *const values = keys + PLANE;
+            // (turns of token + EVERY i are those of either, one with the other: they have no bit in common)
+            constexpr uint32_t AT_ONCE = 512 / T::PITCH, EVERY = AT_ONCE * SHARING;
             uint32_t l = lane;
             asm volatile("" : "+v"(l));  // (found anew for every tile: kept, these are what does not fit the registers)
-            const uint32_t token = wave * AT_ONCE + l / T::CHUNKS, slot = l % T::CHUNKS;
+            const uint32_t mine = TURNS ? 0u : wave * AT_ONCE, token = mine + l / T::CHUNKS, slot = l % T::CHUNKS;
             const uint32_t ck = slot ^ T::key_turn(token), cv = slot ^ T::value_turn(token);
 #pragma unroll
-            for (uint32_t i = 0; i < TURNS; i++) {
-                const uint32_t c = (uint32_t)__builtin_amdgcn_ds_bpermute((int)((token + i * 4u * AT_ONCE) * 4u), (int)cell);
-                const uint32_t dk = (ck ^ T::key_turn(i * 4u * AT_ONCE)) * 8u, dv = (cv ^ T::value_turn(i * 4u * AT_ONCE)) * 8u;
+            for (uint32_t i = 0; i < TOKENS / EVERY; i++) {
+                const uint32_t c = (uint32_t)__builtin_amdgcn_ds_bpermute((int)((token + i * EVERY) * 4u), (int)cell);
+                const uint32_t dk = (ck ^ T::key_turn(i * EVERY)) * 8u, dv = (cv ^ T::value_turn(i * EVERY)) * 8u;
                 const uint64_t off = (uint64_t)c * p.token_bytes;
                 const uint8_t *k = kb + off + dk * 2u, *v = vb + off + dv * 2u;
                 if (c == kNoCell || dk >= p.dim) k = p.zeros;
                 if (c == kNoCell || dv >= p.dim) v = p.zeros;
-                load_lds(k, keys + (i * 4u + wave) * AT_ONCE * T::PITCH);
-                load_lds(v, values + (i * 4u + wave) * AT_ONCE * T::PITCH);
+                load_lds(k, keys + (i * EVERY + mine) * T::PITCH);
+                load_lds(v, values + (i * EVERY + mine) * T::PITCH);
             }
         } else {
+            uint32_t first = tid % LANES;
+            asm volatile("" : "+v"(first));
 #pragma unroll
             for (int i = 0; i < EACH; i++) {
-                const uint32_t u = tid + 256u * (uint32_t)i, token = u / ROW_UNITS, d = u % ROW_UNITS * P::N;
+                const uint32_t u = first + LANES * (uint32_t)i, token = u / ROW_UNITS, d = u % ROW_UNITS * P::N;
                 const uint32_t c = (uint32_t)__shfl((int)cell, (int)(token % TOKENS), 64);
                 kp[i].none();
                 vp[i].none();
-                if ((UNITS % 256u == 0u || u < UNITS) && c != kNoCell && d < p.dim) {
+                if ((UNITS % LANES == 0u || u < UNITS) && c != kNoCell && d < p.dim) {
                     const uint64_t off = (uint64_t)c * p.token_bytes;
                     kp[i].load(kb + off, d, powers);
                     vp[i].load(vb + off, d, powers);
@@ -288,11 +295,13 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void kv_rows_kernel(const Ro
     };
     auto store = [&](auto buf) {
         if constexpr (!DIRECT) {
-            uint16_t *const keys = buf() ? keys1 : keys0, *const values = buf() ? values1 : values0;
+            uint16_t *const keys = tiles + buf() * TILE, *const values = keys + PLANE;
+            uint32_t first = tid % LANES;
+            asm volatile("" : "+v"(first));
 #pragma unroll
             for (int i = 0; i < EACH; i++) {
-                const uint32_t u = tid + 256u * (uint32_t)i, token = u / ROW_UNITS, chunk = u % ROW_UNITS * (P::N / 8);
-                if (UNITS % 256u != 0u && u >= UNITS) break;
+                const uint32_t u = first + LANES * (uint32_t)i, token = u / ROW_UNITS, chunk = u % ROW_UNITS * (P::N / 8);
+                if (UNITS % LANES != 0u && u >= UNITS) break;
 #pragma unroll
                 for (int e = 0; e < P::N / 8; e++) {
                     *reinterpret_cast<w32x4 *>(keys + T::key_at(token, chunk + e)) = kp[i].out(e);
@@ -316,19 +325,19 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void kv_rows_kernel(const Ro
         const uint32_t cell = cell_of(begin, page_of(begin));
         next_present = __ballot(cell != kNoCell);
         load(Zero{}, cell);
-        if (begin + 1u < end) page = page_of(begin + 1u);
+        if (begin + STEP < end) page = page_of(begin + STEP);
         store(Zero{});
     }
     auto step = [&](auto buf, auto other, uint32_t t) {
-        uint16_t *const keys = buf() ? keys1 : keys0, *const values = buf() ? values1 : values0;
+        uint16_t *const keys = tiles + buf() * TILE, *const values = keys + PLANE;
         const uint64_t present = next_present;
         if constexpr (DIRECT) loaded_lds();
-        __syncthreads();
-        if (t + 1u < end) {
-            const uint32_t cell = cell_of(t + 1u, page);
+        if constexpr (!TURNS) __syncthreads();
+        if (t + STEP < end) {
+            const uint32_t cell = cell_of(t + STEP, page);
             next_present = __ballot(cell != kNoCell);
             load(other, cell);
-            if (t + 2u < end) page = page_of(t + 2u);
+            if (t + 2u * STEP < end) page = page_of(t + 2u * STEP);
         }
         const bool border = (t + 1u) * TOKENS > fewest;
         f32x16 s[TB];
@@ -363,16 +372,20 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void kv_rows_kernel(const Ro
         if (border) {
             // values that some rows of the tile do not see: are all of them numbers?
             bool bad = false;
-            for (uint32_t u = tid; u < TOKENS * (DP / 8u); u += 256u) {
+            for (uint32_t u = tid % LANES; u < TOKENS * (DP / 8u); u += LANES) {
                 const uint32_t token = u / (DP / 8u), chunk = u - token * (DP / 8u);
                 const w32x4 v = *reinterpret_cast<const w32x4 *>(values + T::value_at(token, chunk));
                 bad |= X::odd(v[0]) || X::odd(v[1]) || X::odd(v[2]) || X::odd(v[3]);
             }
-            if (tid == 0u) odd = 0u;
-            __syncthreads();
-            if (bad) odd = 1u;
-            __syncthreads();
-            is_odd = odd;
+            if constexpr (TURNS) {
+                is_odd = __any(bad);
+            } else {
+                if (tid == 0u) odd = 0u;
+                __syncthreads();
+                if (bad) odd = 1u;
+                __syncthreads();
+                is_odd = odd;
+            }
         }
         float top = -__builtin_inff();
 #pragma unroll
@@ -444,51 +457,85 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : 2) void kv_rows_kernel(const Ro
                     }
                 }
         }
-        if (t + 1u < end) store(other);
+        if (t + STEP < end) store(other);
     };
-    for (uint32_t t = begin; t < end; t += 2u) {
+    for (uint32_t t = begin; t < end; t += 2u * STEP) {
         step(Zero{}, One{}, t);
-        if (t + 1u < end) step(One{}, Zero{}, t + 1u);
+        if (t + STEP < end) step(One{}, Zero{}, t + STEP);
     }
     own += __shfl_xor(own, 32, 64);
-    if (spread.active > 1u) {
-        const uint64_t slot = ((uint64_t)tile * p.splits + split) * p.n_kv_heads + kv_head;
-        f32x4 *const part = p.part + (slot * 4u + wave) * (NB * 4u) * 64u + lane;
-#pragma unroll
-        for (int b = 0; b < NB; b++)
-#pragma unroll
-            for (int i = 0; i < 4; i++) part[(b * 4 + i) * 64] = f32x4{acc[b][4 * i], acc[b][4 * i + 1], acc[b][4 * i + 2], acc[b][4 * i + 3]};
-        if (h == 0u) p.part_ml[slot * kRowTile + wave * 32u + n] = float2{ref, own};
-        return;
-    }
-    if (!has_row) return;
-    const float inv = own == 0.f ? 0.f : 1.0f / own;
+    constexpr uint32_t VECS = NB * 4;  // vectors of a lane: 4 dimensions each, 32 (v / 4) + 8 (v % 4) + 4 h on
+    const bool parts = spread.active > 1u;
+    const uint64_t slot = ((uint64_t)tile * p.splits + split) * p.n_kv_heads + kv_head;
+    f32x4 *const part = p.part + (slot * (ROWS / 32) + (TURNS ? 0u : wave)) * VECS * 64u + lane;
     uint8_t *const out = p.out + (uint64_t)at_row * p.out_row + (uint64_t)head * p.out_head;
-#pragma unroll
-    for (int b = 0; b < NB; b++)
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const uint32_t d = (uint32_t)b * 32u + (uint32_t)i * 8u + h * 4u;
-            if (d >= p.dim) continue;
+    auto put = [&](uint32_t v, const f32x4 &a, float inv) {
+        const uint32_t d = v / 4u * 32u + v % 4u * 8u + h * 4u;
+        if (parts) {
+            part[v * 64u] = a;
+        } else if (has_row && d < p.dim) {
             float o[4];
 #pragma unroll
-            for (int e = 0; e < 4; e++) o[e] = mean<X, KIND == kBits16>(acc[b][4 * i + e] * inv) * p.v_scale;
+            for (int e = 0; e < 4; e++) o[e] = mean<X, KIND == kBits16>(a[e] * inv) * p.v_scale;
             *reinterpret_cast<w32x2 *>(out + d * 2u) = w32x2{X::pack(o[0], o[1]), X::pack(o[2], o[3])};
         }
-    if (p.lse && h == 0u)
-        p.lse[(uint64_t)at_row * p.n_heads + head] = own == 0.f ? -__builtin_inff() : (ref + __builtin_amdgcn_logf(own)) * 0.693147180559945309f;
+    };
+    if constexpr (TURNS) {
+        // what each wave has goes into LDS, and each joins its share of the dimensions
+        f32x4 *const sums = reinterpret_cast<f32x4 *>(lds);
+        float2 *const ml = reinterpret_cast<float2 *>(sums + WAVES * VECS * 64u);
+        static_assert(ALL * 2u >= (WAVES * VECS * 64u) * 16u + WAVES * 32u * 8u, "room for the sums");
+        __syncthreads();
+#pragma unroll
+        for (uint32_t v = 0; v < VECS; v++) sums[(wave * VECS + v) * 64u + lane] = f32x4{acc[v / 4][v % 4 * 4], acc[v / 4][v % 4 * 4 + 1], acc[v / 4][v % 4 * 4 + 2], acc[v / 4][v % 4 * 4 + 3]};
+        if (h == 0u) ml[wave * 32u + n] = float2{ref, own};
+        __syncthreads();
+        float scale[WAVES];
+        float2 x[WAVES];
+#pragma unroll
+        for (uint32_t o = 0; o < WAVES; o++) {
+            x[o] = ml[o * 32u + n];
+            ref = fmaxf(ref, x[o].x);
+        }
+        own = 0.f;
+#pragma unroll
+        for (uint32_t o = 0; o < WAVES; o++) {
+            scale[o] = __builtin_amdgcn_exp2f(x[o].x - ref);
+            own += x[o].y * scale[o];
+        }
+        const float inv = own == 0.f ? 0.f : 1.0f / own;
+#pragma unroll
+        for (uint32_t i = 0; i < VECS / WAVES; i++) {
+            const uint32_t v = wave * (VECS / WAVES) + i;
+            f32x4 a = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (uint32_t o = 0; o < WAVES; o++) a += sums[(o * VECS + v) * 64u + lane] * scale[o];
+            put(v, a, inv);
+        }
+        if (wave != 0u) return;
+    } else {
+        const float inv = own == 0.f ? 0.f : 1.0f / own;
+#pragma unroll
+        for (uint32_t v = 0; v < VECS; v++) put(v, f32x4{acc[v / 4][v % 4 * 4], acc[v / 4][v % 4 * 4 + 1], acc[v / 4][v % 4 * 4 + 2], acc[v / 4][v % 4 * 4 + 3]}, inv);
+    }
+    if (h != 0u) return;
+    if (parts) p.part_ml[slot * ROWS + (TURNS ? 0u : wave * 32u) + n] = float2{ref, own};
+    else if (has_row && p.lse) p.lse[(uint64_t)at_row * p.n_heads + head] = own == 0.f ? -__builtin_inff() : (ref + __builtin_amdgcn_logf(own)) * 0.693147180559945309f;
 }
 
-// Joins a tile's splits: a workgroup has 32 dimensions of it.
+// Joins a tile's splits: a wave has 32 rows and 32 dimensions of them.
 template <typename X, bool BITS16>
 __global__ __launch_bounds__(256) void kv_rows_join_kernel(const RowsParams p, uint32_t blocks, uint32_t tokens)
 {
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, n = lane & 31u, h = lane >> 5;
-    const uint32_t b = blockIdx.x % blocks, rest = blockIdx.x / blocks, kv_head = rest % p.n_kv_heads, tile = rest / p.n_kv_heads;
+    const uint32_t lane = threadIdx.x & 63u, n = lane & 31u, h = lane >> 5;
+    const uint32_t of_tile = blocks << (p.row_bits - 5u);  // waves of a tile
+    const uint32_t at = blockIdx.x * 4u + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rest = at / of_tile, in = at - rest * of_tile;
+    const uint32_t b = in % blocks, wave = in / blocks, kv_head = rest % p.n_kv_heads, tile = rest / p.n_kv_heads;
+    if (tile >= p.n_tiles) return;
     const RowTile rt = row_tile(p, lane, tile);
     if (!rt.here) return;
     const int32_t len = p.lens[rt.s];
-    const uint32_t last_flat = min(rt.first + kRowTile, (uint32_t)rt.m * p.group_heads) - 1u;
+    const uint32_t last_flat = min(rt.first + (1u << p.row_bits), (uint32_t)rt.m * p.group_heads) - 1u;
     const Spread spread(p, (uint32_t)row_sees(p, len, rt, p.by_group.quotient(last_flat)), tokens);
     if (spread.active <= 1u) return;
     const uint32_t flat = rt.first + wave * 32u + n, row = p.by_group.quotient(flat), head = kv_head * p.group_heads + flat - row * p.group_heads;
@@ -498,15 +545,29 @@ __global__ __launch_bounds__(256) void kv_rows_join_kernel(const RowsParams p, u
     f32x4 all[4];
 #pragma unroll
     for (int i = 0; i < 4; i++) all[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (uint32_t split = 0; split < spread.active; split++) {
-        const uint64_t slot = ((uint64_t)tile * p.splits + split) * p.n_kv_heads + kv_head;
-        const float2 ml = p.part_ml[slot * kRowTile + wave * 32u + n];
-        const f32x4 *const part = p.part + ((slot * 4u + wave) * (blocks * 4u) + b * 4u) * 64u + lane;
-        const float next = fmaxf(ref, ml.x), f = __builtin_amdgcn_exp2f(ref - next), g = __builtin_amdgcn_exp2f(ml.x - next);
-        ref = next;
-        own = own * f + ml.y * g;
+    constexpr uint32_t AT_ONCE = 4;
+    for (uint32_t first = 0; first < spread.active; first += AT_ONCE) {
+        float2 ml[AT_ONCE];
+        f32x4 part[AT_ONCE][4];
 #pragma unroll
-        for (int i = 0; i < 4; i++) all[i] = all[i] * f + part[i * 64] * g;
+        for (uint32_t o = 0; o < AT_ONCE; o++) {
+            const uint32_t split = min(first + o, spread.active - 1u);
+            const uint64_t slot = ((uint64_t)tile * p.splits + split) * p.n_kv_heads + kv_head;
+            ml[o] = p.part_ml[(slot << p.row_bits) + wave * 32u + n];
+#pragma unroll
+            for (int i = 0; i < 4; i++) part[o][i] = p.part[(((slot << (p.row_bits - 5u)) + wave) * (blocks * 4u) + b * 4u + i) * 64u + lane];
+            if (first + o >= spread.active) ml[o] = float2{kLowest, 0.f};
+        }
+#pragma unroll
+        for (uint32_t o = 0; o < AT_ONCE; o++) {
+            const float next = fmaxf(ref, ml[o].x), f = __builtin_amdgcn_exp2f(ref - next);
+            const float g = first + o < spread.active ? __builtin_amdgcn_exp2f(ml[o].x - next) : 0.f;
+            ref = next;
+            own = own * f + ml[o].y * g;
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                if (first + o < spread.active) all[i] = all[i] * f + part[o][i] * g;
+        }
     }
     if (!has_row) return;
     const float inv = own == 0.f ? 0.f : 1.0f / own;

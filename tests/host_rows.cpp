@@ -184,12 +184,12 @@ void launched()
                             CHECK(x.splits >= 1 && launches.size() == (x.splits > 1 ? 2u : 1u), "launches");
                             CHECK(launches[0].g.x == x.n_tiles * x.n_kv_heads * x.splits, "grid");
                             // the last request's last tile, wherever its rows are, comes before n_tiles
-                            CHECK((uint64_t)n_rows * group / x.row_tile + n <= x.n_tiles, "tiles");
+                            CHECK((uint64_t)n_rows * group / (1u << x.row_bits) + n <= x.n_tiles, "tiles");
                             if (x.splits > 1) {
                                 const uint64_t slots = (uint64_t)x.n_tiles * x.splits * x.n_kv_heads;
-                                const uint64_t vecs = (uint64_t)x.row_tile * (dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 128 : dim <= 192 ? 192 : 256) / 4;
+                                const uint64_t vecs = (uint64_t)(1u << x.row_bits) * (dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 128 : dim <= 192 ? 192 : 256) / 4;
                                 CHECK((const char *)(x.part + slots * vecs) <= (const char *)x.part_ml, "parts end");
-                                CHECK((const char *)(x.part_ml + slots * x.row_tile) <= end, "references end");
+                                CHECK((const char *)(x.part_ml + slots * (1u << x.row_bits)) <= end, "references end");
                             }
                             kv_decoder_destroy(d);
                         }
