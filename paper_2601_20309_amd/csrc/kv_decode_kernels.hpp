@@ -56,6 +56,7 @@ struct Bf16 {
     static constexpr int kLowPower = -126, kHighPower = 125;  // of 4-bit numbers: half of the one and 6 of the other are bf16 numbers
     // whether either of two is infinity or NaN
     static __device__ __forceinline__ bool odd(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
+    static __device__ __forceinline__ bool nan(uint32_t w) { return (w & 0x7FFFu) > 0x7F80u; }  // the lower of two
     static constexpr float kMost = 0x1.FEp127f;
     // Each of two weights as the sum of two numbers of 8 digits, the upper cut off, the lower the nearest to what that leaves:
     // within 2^-15.  The lower one gets 2^-20 of the weight on top, so that it is never 0 beside one: 0 times a value
@@ -97,6 +98,7 @@ struct Fp16 {
     }
     static constexpr int kLowPower = -23, kHighPower = 13;
     static __device__ __forceinline__ bool odd(uint32_t w) { return (w & 0x7C00u) == 0x7C00u || (w & 0x7C000000u) == 0x7C000000u; }
+    static __device__ __forceinline__ bool nan(uint32_t w) { return (w & 0x7FFFu) > 0x7C00u; }
     static constexpr float kMost = 65504.0f;
     static constexpr uint32_t kOnes = 0x3C003C00u;
     // As above, of 11 digits each, within 2^-21; each at least the smallest number there is, 2^-24, if there is a weight (no

@@ -210,7 +210,9 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
     constexpr uint32_t PLANE = TOKENS * T::PITCH, TILE = 2 * PLANE, ALL = 2 * TILE * (TURNS ? WAVES : 1);
     // of each wave (or all): two tiles of keys and values; at the end sums
     __shared__ __attribute__((aligned(16))) uint16_t lds[ALL];
-    __shared__ uint32_t odd;  // a tile on the border holds values that are no numbers
+    // of each row and dimension: whether it sees infinities or NaN that were taken out, of either sign
+    __shared__ uint32_t marks[ROWS * NB * 2];
+    __shared__ uint32_t any;
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t n = lane & 31u, h = lane >> 5;
     // KV heads first, so that those of one request's tiles meet in one die's cache; last rows, which see most, first
@@ -237,6 +239,9 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
     const uint32_t powers = KIND == kBits4 ? p.exponents + kv_head * (p.dim / 32u) - kv_head * p.head_bytes : 0u;
     const int32_t *const pages = p.table + (int64_t)rt.s * p.table_stride;
 
+    for (uint32_t i = tid; i < ROWS * NB * 2; i += 64u * WAVES) marks[i] = 0u;
+    if (tid == 0u) any = 0u;
+    if constexpr (TURNS) __syncthreads();  // (otherwise: the one of the first tile)
     w32x4 qf[KS];
 #pragma unroll
     for (int j = 0; j < KS; j++) {
@@ -265,14 +270,20 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
             asm volatile("" : "+v"(l));  // (found anew for every tile: kept, these are what does not fit the registers)
             const uint32_t mine = TURNS ? 0u : wave * AT_ONCE, token = mine + l / T::CHUNKS, slot = l % T::CHUNKS;
             const uint32_t ck = slot ^ T::key_turn(token), cv = slot ^ T::value_turn(token);
+            const uint64_t off = (uint64_t)cell * p.token_bytes;
+            const bool whole = p.dim == T::PITCH && !__any(cell == kNoCell);
 #pragma unroll
             for (uint32_t i = 0; i < TOKENS / EVERY; i++) {
-                const uint32_t c = (uint32_t)__builtin_amdgcn_ds_bpermute((int)((token + i * EVERY) * 4u), (int)cell);
+                const int from = (int)((token + i * EVERY) * 4u);
+                const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)(uint32_t)off), hi = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)(off >> 32));
+                const uint64_t at = (uint64_t)hi << 32 | lo;
                 const uint32_t dk = (ck ^ T::key_turn(i * EVERY)) * 8u, dv = (cv ^ T::value_turn(i * EVERY)) * 8u;
-                const uint64_t off = (uint64_t)c * p.token_bytes;
-                const uint8_t *k = kb + off + dk * 2u, *v = vb + off + dv * 2u;
-                if (c == kNoCell || dk >= p.dim) k = p.zeros;
-                if (c == kNoCell || dv >= p.dim) v = p.zeros;
+                const uint8_t *k = kb + dk * 2u + at, *v = vb + dv * 2u + at;
+                if (!whole) {
+                    const bool here = __builtin_amdgcn_ds_bpermute(from, (int)cell) != (int)kNoCell;
+                    if (!here || dk >= p.dim) k = p.zeros;
+                    if (!here || dv >= p.dim) v = p.zeros;
+                }
                 load_lds(k, keys + (i * EVERY + mine) * T::PITCH);
                 load_lds(v, values + (i * EVERY + mine) * T::PITCH);
             }
@@ -346,18 +357,20 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
 #pragma unroll
             for (int i = 0; i < 16; i++) s[b][i] = 0.f;
         __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int j = 0; j < KS; j++)
 #pragma unroll
             for (int b = 0; b < TB; b++) {
-                const w32x4 a = *reinterpret_cast<const w32x4 *>(keys + T::key_at((uint32_t)b * 32u + n, (uint32_t)j * 2u + h));
+                // (chunk 2 j + h of a token begins at key_at(token, h), bits of 2 j turned round)
+                const w32x4 a = *reinterpret_cast<const w32x4 *>(keys + (uint32_t)b * 32u * T::PITCH + (T::key_at(n, h) ^ (uint32_t)j * 16u));
                 s[b] = mma32<X>(a, qf[j], s[b]);
             }
         pipeline<KS * TB, 1, 6>();
+        __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
         // register i of block b: token b * 32 + i / 4 * 8 + h * 4 + i % 4
         const uint64_t all = TOKENS == 64 ? ~0ull : 0xFFFFFFFFull;
-        bool is_odd = false;
         if (border || (present & all) != all) {
             const int32_t left = (int32_t)sees - (int32_t)(t * TOKENS + h * 4u);
             const uint64_t there = present >> (h * 4u);
@@ -370,22 +383,30 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
                 }
         }
         if (border) {
-            // values that some rows of the tile do not see: are all of them numbers?
-            bool bad = false;
+            // A weight of 0 does not make up for a value of infinity or NaN.  Where not all rows see all tokens, those become 0 here, and
+            // what they make of the rows that see them is noted.
             for (uint32_t u = tid % LANES; u < TOKENS * (DP / 8u); u += LANES) {
                 const uint32_t token = u / (DP / 8u), chunk = u - token * (DP / 8u);
-                const w32x4 v = *reinterpret_cast<const w32x4 *>(values + T::value_at(token, chunk));
-                bad |= X::odd(v[0]) || X::odd(v[1]) || X::odd(v[2]) || X::odd(v[3]);
+                w32x4 *const at = reinterpret_cast<w32x4 *>(values + T::value_at(token, chunk));
+                w32x4 v = *at;
+                if (!(X::odd(v[0]) || X::odd(v[1]) || X::odd(v[2]) || X::odd(v[3]))) continue;
+                for (uint32_t e = 0; e < 8; e++) {
+                    const uint32_t word = e / 2 == 0u ? v[0] : e / 2 == 1u ? v[1] : e / 2 == 2u ? v[2] : v[3], x = e & 1u ? word >> 16 : word & 0xFFFFu;
+                    if (!X::odd(x)) continue;
+                    const bool nan = X::nan(x);
+                    reinterpret_cast<uint16_t *>(at)[e] = 0;
+                    for (uint32_t r = 0; r < ROWS; r++) {
+                        const uint32_t row = p.by_group.quotient(rt.first + r);
+                        if (row >= (uint32_t)rt.m || (uint32_t)row_sees(p, len, rt, row) <= t * TOKENS + token) continue;
+                        uint32_t *const m = marks + (r * NB + chunk / 4u) * 2u;
+                        const uint32_t bit = 1u << (chunk % 4u * 8u + e);
+                        if (nan || !(x & 0x8000u)) atomicOr(m, bit);
+                        if (nan || x & 0x8000u) atomicOr(m + 1, bit);
+                    }
+                    any = 1u;
+                }
             }
-            if constexpr (TURNS) {
-                is_odd = __any(bad);
-            } else {
-                if (tid == 0u) odd = 0u;
-                __syncthreads();
-                if (bad) odd = 1u;
-                __syncthreads();
-                is_odd = odd;
-            }
+            if constexpr (!TURNS) __syncthreads();
         }
         float top = -__builtin_inff();
 #pragma unroll
@@ -414,49 +435,28 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
             }
         // 16 lanes bring 4 tokens of 16 dimensions, and have 4 tokens of a dimension each
         auto value = [&](int k, int b) {
-            const uint32_t token = (uint32_t)k * 16u + h * 4u + (lane & 15u) / 4u, d = (uint32_t)b * 32u + (lane & 16u) + (lane & 3u) * 4u;
+            const uint32_t token = h * 4u + (lane & 15u) / 4u, d = (lane & 16u) + (lane & 3u) * 4u;
+            const uint32_t at = (T::value_at(token, d / 8u) + (d & 4u)) ^ (uint32_t)b * 32u;
             w32x4 a;
 #pragma unroll
             for (uint32_t half = 0; half < 2; half++) {
-                const uint16_t *from = values + T::value_at(token + half * 8u, d / 8u) + (d & 4u);
+                const uint16_t *from = values + ((uint32_t)k * 16u + half * 8u) * T::PITCH + at;
                 const w32x2 x = __builtin_bit_cast(w32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)from));
                 a[half * 2u] = x[0];
                 a[half * 2u + 1u] = x[1];
             }
             return a;
         };
-        if (!is_odd) {
-            __builtin_amdgcn_sched_barrier(0);
+        asm volatile("" : "+v"(own));  // (added up here, not behind the products, where all of the weights would have to be kept)
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-            for (int k = 0; k < 2 * TB; k++)
+        for (int k = 0; k < 2 * TB; k++)
 #pragma unroll
-                for (int b = 0; b < NB; b++) acc[b] = mma32<X>(value(k, b), w[k], acc[b]);
-            pipeline<2 * TB * NB, 2, 6>();
-            __builtin_amdgcn_sched_barrier(0);
-        } else {
-            // A weight of 0 does not make up for infinity or NaN: token by token, for the rows that see it.
-#pragma unroll
-            for (int k = 0; k < 2 * TB; k++)
-#pragma unroll
-                for (int b = 0; b < NB; b++) {
-                    const w32x4 a = value(k, b);
-#pragma unroll 1
-                    for (int one = 0; one < 16; one++) {
-                        const int place = one / 8 * 4 + one % 4;
-                        w32x4 only;
-#pragma unroll
-                        for (int e = 0; e < 4; e++)
-                            only[e] = (int)h == (one / 4 & 1) && place / 2 == e ? a[e] & (place & 1 ? 0xFFFF0000u : 0xFFFFu) : 0u;
-                        f32x16 r;
-#pragma unroll
-                        for (int i = 0; i < 16; i++) r[i] = 0.f;
-                        r = mma32<X>(only, w[k], r);
-                        const bool sees_it = t * TOKENS + (uint32_t)k * 16u + (uint32_t)one < sees;
-#pragma unroll
-                        for (int i = 0; i < 16; i++) acc[b][i] += sees_it ? r[i] : 0.f;
-                    }
-                }
-        }
+            for (int b = 0; b < NB; b++) acc[b] = mma32<X>(value(k, b), w[k], acc[b]);
+        pipeline<2 * TB * NB, 2, 6>();
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
         if (t + STEP < end) store(other);
     };
     for (uint32_t t = begin; t < end; t += 2u * STEP) {
@@ -469,8 +469,17 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
     const uint64_t slot = ((uint64_t)tile * p.splits + split) * p.n_kv_heads + kv_head;
     f32x4 *const part = p.part + (slot * (ROWS / 32) + (TURNS ? 0u : wave)) * VECS * 64u + lane;
     uint8_t *const out = p.out + (uint64_t)at_row * p.out_row + (uint64_t)head * p.out_head;
-    auto put = [&](uint32_t v, const f32x4 &a, float inv) {
+    auto put = [&](uint32_t v, f32x4 a, float inv) {
         const uint32_t d = v / 4u * 32u + v % 4u * 8u + h * 4u;
+        if (any) {
+            const uint32_t *const m = marks + (((TURNS ? 0u : wave * 32u) + n) * NB + v / 4u) * 2u;
+            const uint32_t up = m[0] >> (d & 31u), down = m[1] >> (d & 31u);
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                a[e] += up >> e & 1u ? __builtin_inff() : 0.f;
+                a[e] -= down >> e & 1u ? __builtin_inff() : 0.f;
+            }
+        }
         if (parts) {
             part[v * 64u] = a;
         } else if (has_row && d < p.dim) {
