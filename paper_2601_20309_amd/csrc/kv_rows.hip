@@ -23,8 +23,10 @@ void launch_rows(dim3 g, hipStream_t s, const dkv::RowsParams &p)
                                (uint32_t)DP / 32u, (uint32_t)T::TOKENS);
     };
     auto go = [&](auto dims) {
-        if (p.row_bits == 5u) launch(dims, std::integral_constant<int, 32>{});
-        else launch(dims, std::integral_constant<int, 128>{});
+        if (p.row_bits == 5u) return launch(dims, std::integral_constant<int, 32>{});
+        if constexpr (decltype(dims)::value <= dkv::kManyRowsDims)
+            if (p.row_bits == 8u) return launch(dims, std::integral_constant<int, 256>{});
+        launch(dims, std::integral_constant<int, 128>{});
     };
     switch (dkv::rows_dims(p.dim)) {
     case 64: go(std::integral_constant<int, 64>{}); break;
@@ -90,10 +92,13 @@ extern "C" int kv_attend_rows(kv_decoder *d, const kv_attend_rows_args *a, void 
     p.negative = qk_scale < 0.f ? 1u : 0u;
     p.qk_scale = std::max(std::fabs(qk_scale), 0x1p-126f);  // (0 times the score of what is masked, -inf, is NaN)
     p.v_scale = d->dc.v_scale;
-    // Few rows to a request: 32 to a tile.
+    // Few rows to a request: 32 to a tile.  Many, and enough tiles for all compute units: 256, so that half as many bytes
+    // go into LDS.  us, 128 rows / 256: 4 prompts of 2048 tokens, 32 heads over 8 of 128, 190 / 178; 1024 tokens at 31000, 64
+    // over 8, 1124 / 990; 24 requests of 180 rows of 12 heads of 64 43.9 / 50.4.
     const uint64_t mean = (uint64_t)p.n_rows * p.group_heads / p.n_seqs;
     const bool few = mean <= 48u && row_tiles(p.n_rows, p.group_heads, p.n_seqs, 5) * p.n_kv_heads <= kMostTiles;
-    p.row_bits = few ? 5u : 7u;
+    const bool many = mean >= 1024u && p.dim <= (uint32_t)kManyRowsDims && row_tiles(p.n_rows, p.group_heads, 0, 8) * p.n_kv_heads >= (uint64_t)d->n_cus;
+    p.row_bits = few ? 5u : many ? 8u : 7u;
     p.n_tiles = (uint32_t)row_tiles(p.n_rows, p.group_heads, p.n_seqs, (int)p.row_bits);
     // Few tiles of rows: the tokens are split, so that every compute unit has some.
     const uint64_t each = (uint64_t)p.n_tiles * p.n_kv_heads;

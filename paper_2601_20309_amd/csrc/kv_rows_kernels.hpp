@@ -14,7 +14,7 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 // tokens with a running reference.  The query heads of a KV head are rows, too: heads of a row lie one
 // behind the other, so that few rows of many heads fill a tile, and all of them share the keys that are brought.
 //
-// A workgroup has 128 rows of one KV head, 32 a wave, and goes over the tokens 64 at a time (32 above 128 dimensions), or, where
+// A workgroup has 128 or 256 rows of one KV head, 32 a wave, and goes over the tokens 64 at a time (32 above 128 dimensions), or, where
 // requests have few rows, 32 rows, and its waves take turns at the tokens.  These go into LDS, two tiles in
 // turn: in 16 bits whatever the cache holds, so that the products are the same for every type of cache.  Both products are taken transposed, tokens x rows and dimensions x rows, as in kv_attend:
 // a lane has one row, its reference and its sums, and weights come out as the second product's operand.
@@ -113,13 +113,14 @@ __device__ __forceinline__ float mean(float x)
     return OF_X && __builtin_fabsf(x) < __builtin_inff() ? fminf(fmaxf(x, -X::kMost), X::kMost) : x;
 }
 
-// ROWS 128: four waves have 32 rows each, and share tiles of tokens.  ROWS 32: all waves have the same rows, and take turns at the
+// ROWS 128 and 256: four or eight waves have 32 rows each, and share tiles of tokens.  ROWS 32: all waves have the same rows, and take turns at the
 // tiles of tokens, each with LDS of its own, so that nothing waits for the others.
+constexpr int kManyRowsDims = 128;  // 256 rows: eight waves have no more than 256 registers each
 template <int DP, int ROWS>
 struct RowStep {
     static constexpr bool TURNS = ROWS == 32;
     static constexpr int TOKENS = TURNS || DP > 128 ? 32 : 64;
-    static constexpr int WAVES = TURNS && DP > 128 ? 2 : 4;
+    static constexpr int WAVES = TURNS ? (DP > 128 ? 2 : 4) : ROWS / 32;
     static constexpr int PITCH = DP <= 64 ? 64 : DP <= 128 ? 128 : 256;  // of a token in LDS, in numbers
     static constexpr int CHUNKS = PITCH / 8;
     static constexpr int NB = DP / 32, KS = DP / 16, TB = TOKENS / 32;
