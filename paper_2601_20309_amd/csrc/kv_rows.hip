@@ -18,7 +18,7 @@ void launch_rows(dim3 g, hipStream_t s, const dkv::RowsParams &p)
         using T = dkv::RowStep<DP, ROWS>;
         hipLaunchKernelGGL((dkv::kv_rows_kernel<X, KIND, DP, ROWS>), g, dim3(64 * T::WAVES), 0, s, p);
         const uint64_t joins = (uint64_t)p.n_tiles * p.n_kv_heads * (ROWS / 32) * (DP / 32);
-        if (p.splits > 1u)
+        if (p.splits > 1u || p.groups)
             hipLaunchKernelGGL((dkv::kv_rows_join_kernel<X, KIND == dkv::kBits16>), dim3((uint32_t)((joins + 3) / 4)), dim3(256), 0, s, p,
                                (uint32_t)DP / 32u, (uint32_t)T::TOKENS);
     };
@@ -92,6 +92,7 @@ extern "C" int kv_attend_rows(kv_decoder *d, const kv_attend_rows_args *a, void 
     p.negative = qk_scale < 0.f ? 1u : 0u;
     p.qk_scale = std::max(std::fabs(qk_scale), 0x1p-126f);  // (0 times the score of what is masked, -inf, is NaN)
     p.v_scale = d->dc.v_scale;
+    const int kind = (d->dc.x_type == KV_FP16 ? 1 : 0) + (d->dc.kv_type == KV_FP8 ? 2 : d->dc.kv_type == KV_FP4 ? 4 : 0);
     // Few rows to a request: 32 to a tile.  Many, and enough tiles for all compute units: 256, so that half as many bytes
     // go into LDS.  us, 128 rows / 256: 4 prompts of 2048 tokens, 32 heads over 8 of 128, 190 / 178; 1024 tokens at 31000, 64
     // over 8, 1124 / 990; 24 requests of 180 rows of 12 heads of 64 43.9 / 50.4.
@@ -100,14 +101,27 @@ extern "C" int kv_attend_rows(kv_decoder *d, const kv_attend_rows_args *a, void 
     const bool many = mean >= 1024u && p.dim <= (uint32_t)kManyRowsDims && row_tiles(p.n_rows, p.group_heads, 0, 8) * p.n_kv_heads >= (uint64_t)d->n_cus;
     p.row_bits = few ? 5u : many ? 8u : 7u;
     p.n_tiles = (uint32_t)row_tiles(p.n_rows, p.group_heads, p.n_seqs, (int)p.row_bits);
-    // Few tiles of rows: the tokens are split, so that every compute unit has some.
     const uint64_t each = (uint64_t)p.n_tiles * p.n_kv_heads;
-    const uint32_t tokens = p.dim > 128u || p.row_bits == 5u ? 32u : 64u, most = (p.max_tokens + tokens - 1u) / tokens;
-    p.least = p.row_bits == 5u ? 16u : 2u;
-    p.splits = (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>((kRowSums >> p.row_bits) / each, (most + p.least - 1u) / p.least));
-    const dim3 g((uint32_t)(each * p.splits));
+    const uint32_t tokens = p.dim > 128u || few ? 32u : 64u, most = (p.max_tokens + tokens - 1u) / tokens;
+    p.splits = 1u;
+    p.least = 2u;
+    uint64_t wgs = each;
+    if (few) {
+        // Equal ranges for two workgroups a compute unit (one where their tiles fill its LDS); a workgroup for each tile where no
+        // request can be longer than four steps of its waves.
+        const uint32_t at_once = (uint32_t)d->n_cus * (kind < 2 && p.dim > 64u ? 1u : 2u);
+        if (most > 16u && (uint64_t)p.n_tiles * most <= 0x7FFFFFFFu) {
+            p.groups = (uint32_t)std::min<uint64_t>(std::max(1u, std::min(at_once, (uint32_t)kRowSums / 64u) / p.n_kv_heads), (uint64_t)p.n_tiles * most);
+            wgs = (uint64_t)p.groups * p.n_kv_heads;
+        }
+    } else {
+        // Few tiles of rows: the tokens are split, so that every compute unit has some.
+        p.splits = (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>((kRowSums >> p.row_bits) / each, (most + p.least - 1u) / p.least));
+        wgs = each * p.splits;
+    }
+    const dim3 g((uint32_t)wgs);
     hipStream_t s = (hipStream_t)stream;
-    switch ((d->dc.x_type == KV_FP16 ? 1 : 0) + (d->dc.kv_type == KV_FP8 ? 2 : d->dc.kv_type == KV_FP4 ? 4 : 0)) {
+    switch (kind) {
     case 0: launch_rows<Bf16, kBits16>(g, s, p); break;
     case 1: launch_rows<Fp16, kBits16>(g, s, p); break;
     case 2: launch_rows<Bf16, kBits8>(g, s, p); break;

@@ -27,14 +27,17 @@ struct RowsParams {
     uint8_t *out;
     float *lse;
     const uint8_t *zeros;  // 16 bytes
-    f32x4 *part;      // [tile * splits][32 rows][vector][lane]: sums of a split, as they lie in registers
-    float2 *part_ml;  // [tile * splits][row]: reference, sum of weights
+    f32x4 *part;      // [slot][32 rows][vector][lane]: sums of a part of the tokens, as they lie in registers
+    float2 *part_ml;  // [slot][row]: reference, sum of weights
     uint64_t q_row, q_head, out_row, out_head;  // bytes
     int64_t table_stride;
     uint32_t n_seqs, n_rows, n_heads, n_kv_heads, max_tokens;
     uint32_t dim, token_bytes, head_bytes, block_size, cells_per_block, n_blocks;
     uint32_t exponents;  // 4 bits: from a token's first byte to its exponents
-    uint32_t group_heads, causal, splits, least;  // least: tiles of tokens of a split
+    uint32_t group_heads, causal;
+    // Parts of the tokens: splits of a tile of rows, `least` tiles of tokens and more each, slots [tile][split][KV head]; or, of
+    // tiles of 32 rows, `groups` ranges of all (0: none), slots [range][its last request, or one that begins in it][KV head]
+    uint32_t splits, least, groups;
     uint32_t n_tiles, row_bits;                   // tiles of rows of a KV head, empty ones among them; log2 of the rows of one
     Divide by_block, by_group;
     uint32_t negative;  // the scale is: keys meet -q
@@ -94,6 +97,60 @@ struct Spread {
         tiles = (upto + tokens - 1u) / tokens;
         per = max((tiles + p.splits - 1u) / p.splits, p.least);
         active = (tiles + per - 1u) / per;
+    }
+};
+
+// Ranges: the tiles of tokens of all tiles of 32 rows, one behind the other, are dealt to p.groups equal ranges, whatever
+// requests' lengths and rows.  Every wave finds out for itself, 64 requests at a time.
+struct RowDeal {
+    uint32_t total, per, before;  // tiles of tokens; of a range; of the requests before the one asked for
+    uint32_t mine, upto;          // of request (n_seqs - 1) / 64 * 64 + lane; of its 64 up to and with it
+    // Tiles of tokens of request s, the same for each of its tiles of rows, and those in all.
+    static __device__ __forceinline__ uint32_t tokens_of(const RowsParams &p, uint32_t s, uint32_t &start, uint32_t &rows)
+    {
+        const int32_t a = p.starts ? p.starts[s] : (int32_t)s;
+        const int64_t next = p.starts ? p.starts[s + 1u] : (int64_t)s + 1;
+        start = (uint32_t)max(a, 0);
+        rows = a < 0 ? 0u : (uint32_t)min(max(next - a, (int64_t)0), (int64_t)p.n_rows);
+        return (seq_tokens(p.lens, s, p.max_tokens) + 31u) / 32u;
+    }
+    static __device__ __forceinline__ uint32_t work(const RowsParams &p, uint32_t s)
+    {
+        uint32_t start, rows;
+        if (s >= p.n_seqs) return 0u;
+        const uint32_t tokens = tokens_of(p, s, start, rows);
+        return (rows * p.group_heads + 31u) / 32u * tokens;
+    }
+    __device__ __forceinline__ RowDeal(const RowsParams &p, uint32_t lane, uint32_t asked) : total(0), per(1), before(0), mine(0), upto(0)
+    {
+        if (!p.groups) return;
+        for (uint32_t base = 0; base < p.n_seqs; base += 64u) {
+            mine = work(p, base + lane);
+            upto = wave_scan(mine);
+            if (asked >= base && asked - base < 64u) before = total + (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), (int)(asked - base));
+            total += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+        }
+        per = max((total + p.groups - 1u) / p.groups, 1u);
+    }
+    // The request that tile `at` is of, and how many of its tiles come before.
+    __device__ __forceinline__ bool find(const RowsParams &p, uint32_t lane, uint32_t at, uint32_t &s, uint32_t &t) const
+    {
+        uint32_t m = mine, u = upto, first = 0;
+        for (uint32_t base = 0; base < p.n_seqs; base += 64u) {
+            if (p.n_seqs > 64u) {
+                m = work(p, base + lane);
+                u = wave_scan(m);
+            }
+            const uint64_t beyond = __ballot(first + u > at);
+            if (beyond) {
+                const uint32_t l = (uint32_t)__builtin_ctzll(beyond);
+                s = base + l;
+                t = at - first - (uint32_t)__builtin_amdgcn_readlane((int)(u - m), (int)l);
+                return true;
+            }
+            first += (uint32_t)__builtin_amdgcn_readlane((int)u, 63);
+        }
+        return false;  // (starts that fall)
     }
 };
 
@@ -208,34 +265,33 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
     constexpr uint32_t UNITS = TOKENS * DP / P::N, ROW_UNITS = DP / P::N;      // pieces of a tile, of a token
     constexpr uint32_t LANES = 64 * SHARING;
     constexpr int EACH = DIRECT ? 1 : (UNITS + LANES - 1) / LANES;
-    constexpr uint32_t PLANE = TOKENS * T::PITCH, TILE = 2 * PLANE, ALL = 2 * TILE * (TURNS ? WAVES : 1);
-    // of each wave (or all): two tiles of keys and values; at the end sums
-    __shared__ __attribute__((aligned(16))) uint16_t lds[ALL];
+    // Numbers that go through registers are stored when the tile before them has been read: of a wave's own tiles one is enough.
+    constexpr uint32_t BUFS = TURNS && !DIRECT ? 1 : 2;
+    constexpr uint32_t PLANE = TOKENS * T::PITCH, TILE = 2 * PLANE, VECS = NB * 4;
+    // of each wave (or all): tiles of keys and values; at the end sums
+    __shared__ __attribute__((aligned(16))) uint16_t lds[BUFS * TILE * (TURNS ? WAVES : 1)];
+    __shared__ float2 ml[TURNS ? WAVES * 32 : 1];
     // of each row and dimension: whether it sees infinities or NaN that were taken out, of either sign
     __shared__ uint32_t marks[ROWS * NB * 2];
     __shared__ uint32_t any;
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t n = lane & 31u, h = lane >> 5;
-    // KV heads first, so that those of one request's tiles meet in one die's cache; last rows, which see most, first
+    // KV heads first, so that those of one request's tiles meet in one die's cache
     const uint32_t kv_head = blockIdx.x % p.n_kv_heads, rest = blockIdx.x / p.n_kv_heads;
-    const uint32_t split = rest % p.splits, tile = p.n_tiles - 1u - rest / p.splits;
-    const RowTile rt = row_tile(p, lane, tile);
-    if (!rt.here) return;
+    const uint8_t *const kb = p.k + (uint64_t)kv_head * p.head_bytes;
+    const uint8_t *const vb = p.v + (uint64_t)kv_head * p.head_bytes;
+    uint16_t *const tiles = lds + (TURNS ? wave * BUFS * TILE : 0u);
+    // Tiles of tokens `first` to `stop` of a tile of rows, a part of them or all.
+    auto run = [&](const RowTile &rt, uint32_t first_tokens, uint32_t stop, bool parts, uint64_t slot) {
     const int32_t len = p.lens[rt.s];
     const uint32_t last_flat = min(rt.first + ROWS, (uint32_t)rt.m * p.group_heads) - 1u;
     const uint32_t most = (uint32_t)row_sees(p, len, rt, p.by_group.quotient(last_flat));
     const uint32_t fewest = (uint32_t)row_sees(p, len, rt, p.by_group.quotient(rt.first));
-    const Spread spread(p, most, TOKENS);
-    if (split >= max(spread.active, 1u)) return;
-    const uint32_t begin = split * spread.per + (TURNS ? wave : 0u), end = min(split * spread.per + spread.per, spread.tiles);
-
-    uint16_t *const tiles = lds + (TURNS ? wave * 2u * TILE : 0u);
+    const uint32_t begin = first_tokens + (TURNS ? wave : 0u), end = min(stop, (most + TOKENS - 1u) / TOKENS);
     const uint32_t flat = rt.first + (TURNS ? 0u : wave * 32u) + n, row = p.by_group.quotient(flat), head = kv_head * p.group_heads + flat - row * p.group_heads;
     const uint32_t at_row = (uint32_t)rt.start + row;
     const bool has_row = row < (uint32_t)rt.m && at_row < p.n_rows;
     const uint32_t sees = has_row ? (uint32_t)row_sees(p, len, rt, row) : 0u;
-    const uint8_t *const kb = p.k + (uint64_t)kv_head * p.head_bytes;
-    const uint8_t *const vb = p.v + (uint64_t)kv_head * p.head_bytes;
     // 4 bits: from a token's numbers of this head to the head's powers of 2
     const uint32_t powers = KIND == kBits4 ? p.exponents + kv_head * (p.dim / 32u) - kv_head * p.head_bytes : 0u;
     const int32_t *const pages = p.table + (int64_t)rt.s * p.table_stride;
@@ -264,7 +320,7 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
     auto load = [&](auto buf, uint32_t cell) {
         if constexpr (DIRECT) {
             // a wave brings 512 numbers at once, whole tokens, each lane the 8 that belong where its lane's go
-            uint16_t *const keys = tiles + buf() * TILE, *const values = keys + PLANE;
+            uint16_t *const keys = tiles + (BUFS > 1 ? buf() : 0) * TILE, *const values = keys + PLANE;
             // (turns of token + EVERY i are those of either, one with the other: they have no bit in common)
             constexpr uint32_t AT_ONCE = 512 / T::PITCH, EVERY = AT_ONCE * SHARING;
             uint32_t l = lane;
@@ -307,7 +363,7 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
     };
     auto store = [&](auto buf) {
         if constexpr (!DIRECT) {
-            uint16_t *const keys = tiles + buf() * TILE, *const values = keys + PLANE;
+            uint16_t *const keys = tiles + (BUFS > 1 ? buf() : 0) * TILE, *const values = keys + PLANE;
             uint32_t first = tid % LANES;
             asm volatile("" : "+v"(first));
 #pragma unroll
@@ -341,7 +397,7 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
         store(Zero{});
     }
     auto step = [&](auto buf, auto other, uint32_t t) {
-        uint16_t *const keys = tiles + buf() * TILE, *const values = keys + PLANE;
+        uint16_t *const keys = tiles + (BUFS > 1 ? buf() : 0) * TILE, *const values = keys + PLANE;
         const uint64_t present = next_present;
         if constexpr (DIRECT) loaded_lds();
         if constexpr (!TURNS) __syncthreads();
@@ -465,9 +521,7 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
         if (t + STEP < end) step(One{}, Zero{}, t + STEP);
     }
     own += __shfl_xor(own, 32, 64);
-    constexpr uint32_t VECS = NB * 4;  // vectors of a lane: 4 dimensions each, 32 (v / 4) + 8 (v % 4) + 4 h on
-    const bool parts = spread.active > 1u;
-    const uint64_t slot = ((uint64_t)tile * p.splits + split) * p.n_kv_heads + kv_head;
+    // vector v of a lane: 4 dimensions, 32 (v / 4) + 8 (v % 4) + 4 h on
     f32x4 *const part = p.part + (slot * (ROWS / 32) + (TURNS ? 0u : wave)) * VECS * 64u + lane;
     uint8_t *const out = p.out + (uint64_t)at_row * p.out_row + (uint64_t)head * p.out_head;
     auto put = [&](uint32_t v, f32x4 a, float inv) {
@@ -493,8 +547,7 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
     if constexpr (TURNS) {
         // what each wave has goes into LDS, and each joins its share of the dimensions
         f32x4 *const sums = reinterpret_cast<f32x4 *>(lds);
-        float2 *const ml = reinterpret_cast<float2 *>(sums + WAVES * VECS * 64u);
-        static_assert(ALL * 2u >= (WAVES * VECS * 64u) * 16u + WAVES * 32u * 8u, "room for the sums");
+        static_assert(sizeof lds >= WAVES * VECS * 64u * 16u, "room for the sums");
         __syncthreads();
 #pragma unroll
         for (uint32_t v = 0; v < VECS; v++) sums[(wave * VECS + v) * 64u + lane] = f32x4{acc[v / 4][v % 4 * 4], acc[v / 4][v % 4 * 4 + 1], acc[v / 4][v % 4 * 4 + 2], acc[v / 4][v % 4 * 4 + 3]};
@@ -522,6 +575,7 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
             for (uint32_t o = 0; o < WAVES; o++) a += sums[(o * VECS + v) * 64u + lane] * scale[o];
             put(v, a, inv);
         }
+        __syncthreads();
         if (wave != 0u) return;
     } else {
         const float inv = own == 0.f ? 0.f : 1.0f / own;
@@ -531,9 +585,48 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
     if (h != 0u) return;
     if (parts) p.part_ml[slot * ROWS + (TURNS ? 0u : wave * 32u) + n] = float2{ref, own};
     else if (has_row && p.lse) p.lse[(uint64_t)at_row * p.n_heads + head] = own == 0.f ? -__builtin_inff() : (ref + __builtin_amdgcn_logf(own)) * 0.693147180559945309f;
+    };
+    RowTile rt;
+    if constexpr (TURNS) {
+        // (run() once in the code, whether the workgroup has a range or a tile)
+        const RowDeal deal(p, lane, 0u);
+        uint32_t at = p.groups ? rest * deal.per : 0u, here = 1u;
+        const uint32_t stop = p.groups ? min(at + deal.per, deal.total) : 1u;
+        for (; at < stop; at += here) {
+            uint32_t first = 0, last = ~0u;
+            uint64_t slot = 0;
+            bool parts = false;
+            if (p.groups) {
+                uint32_t t, start, rows;
+                if (!deal.find(p, lane, at, rt.s, t)) return;
+                const uint32_t tokens = RowDeal::tokens_of(p, rt.s, start, rows), tile = t / tokens;
+                first = t - tile * tokens;
+                here = min(tokens - first, stop - at);
+                last = first + here;
+                parts = here < tokens;
+                slot = (uint64_t)(rest * 2u + (first ? 0u : 1u)) * p.n_kv_heads + kv_head;
+                rt.first = tile * 32u;
+                rt.start = (int32_t)start;
+                rt.m = (int32_t)rows;
+            } else {
+                rt = row_tile(p, lane, rest);
+                if (!rt.here) return;
+            }
+            run(rt, first, last, parts, slot);
+        }
+    } else {
+        // last rows, which see most, first
+        const uint32_t split = rest % p.splits, tile = p.n_tiles - 1u - rest / p.splits;
+        rt = row_tile(p, lane, tile);
+        if (!rt.here) return;
+        const uint32_t last_flat = min(rt.first + ROWS, (uint32_t)rt.m * p.group_heads) - 1u;
+        const Spread spread(p, (uint32_t)row_sees(p, p.lens[rt.s], rt, p.by_group.quotient(last_flat)), TOKENS);
+        if (split >= max(spread.active, 1u)) return;
+        run(rt, split * spread.per, split * spread.per + spread.per, spread.active > 1u, ((uint64_t)tile * p.splits + split) * p.n_kv_heads + kv_head);
+    }
 }
 
-// Joins a tile's splits: a wave has 32 rows and 32 dimensions of them.
+// Joins the parts of a tile: a wave has 32 rows and 32 dimensions of them.
 template <typename X, bool BITS16>
 __global__ __launch_bounds__(256) void kv_rows_join_kernel(const RowsParams p, uint32_t blocks, uint32_t tokens)
 {
@@ -545,9 +638,20 @@ __global__ __launch_bounds__(256) void kv_rows_join_kernel(const RowsParams p, u
     const RowTile rt = row_tile(p, lane, tile);
     if (!rt.here) return;
     const int32_t len = p.lens[rt.s];
-    const uint32_t last_flat = min(rt.first + (1u << p.row_bits), (uint32_t)rt.m * p.group_heads) - 1u;
-    const Spread spread(p, (uint32_t)row_sees(p, len, rt, p.by_group.quotient(last_flat)), tokens);
-    if (spread.active <= 1u) return;
+    uint32_t parts, g0 = 0;
+    if (p.groups) {
+        uint32_t start, rows;
+        const uint32_t n_tokens = RowDeal::tokens_of(p, rt.s, start, rows);
+        const RowDeal deal(p, lane, rt.s);
+        const uint32_t first = deal.before + rt.first / 32u * n_tokens;
+        g0 = first / deal.per;
+        parts = n_tokens ? min((first + n_tokens - 1u) / deal.per, p.groups - 1u) - g0 + 1u : 0u;
+        if (parts == 1u) return;  // (none: no range has a request without tokens)
+    } else {
+        const uint32_t last_flat = min(rt.first + (1u << p.row_bits), (uint32_t)rt.m * p.group_heads) - 1u;
+        parts = Spread(p, (uint32_t)row_sees(p, len, rt, p.by_group.quotient(last_flat)), tokens).active;
+        if (parts <= 1u) return;
+    }
     const uint32_t flat = rt.first + wave * 32u + n, row = p.by_group.quotient(flat), head = kv_head * p.group_heads + flat - row * p.group_heads;
     const uint32_t at_row = (uint32_t)rt.start + row;
     const bool has_row = row < (uint32_t)rt.m && at_row < p.n_rows;
@@ -556,27 +660,27 @@ __global__ __launch_bounds__(256) void kv_rows_join_kernel(const RowsParams p, u
 #pragma unroll
     for (int i = 0; i < 4; i++) all[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     constexpr uint32_t AT_ONCE = 4;
-    for (uint32_t first = 0; first < spread.active; first += AT_ONCE) {
+    for (uint32_t first = 0; first < parts; first += AT_ONCE) {
         float2 ml[AT_ONCE];
         f32x4 part[AT_ONCE][4];
 #pragma unroll
         for (uint32_t o = 0; o < AT_ONCE; o++) {
-            const uint32_t split = min(first + o, spread.active - 1u);
-            const uint64_t slot = ((uint64_t)tile * p.splits + split) * p.n_kv_heads + kv_head;
+            const uint32_t i = min(first + o, parts - 1u);
+            const uint64_t slot = (p.groups ? (uint64_t)(g0 + i) * 2u + (i ? 0u : 1u) : (uint64_t)tile * p.splits + i) * p.n_kv_heads + kv_head;
             ml[o] = p.part_ml[(slot << p.row_bits) + wave * 32u + n];
 #pragma unroll
             for (int i = 0; i < 4; i++) part[o][i] = p.part[(((slot << (p.row_bits - 5u)) + wave) * (blocks * 4u) + b * 4u + i) * 64u + lane];
-            if (first + o >= spread.active) ml[o] = float2{kLowest, 0.f};
+            if (first + o >= parts) ml[o] = float2{kLowest, 0.f};
         }
 #pragma unroll
         for (uint32_t o = 0; o < AT_ONCE; o++) {
             const float next = fmaxf(ref, ml[o].x), f = __builtin_amdgcn_exp2f(ref - next);
-            const float g = first + o < spread.active ? __builtin_amdgcn_exp2f(ml[o].x - next) : 0.f;
+            const float g = first + o < parts ? __builtin_amdgcn_exp2f(ml[o].x - next) : 0.f;
             ref = next;
             own = own * f + ml[o].y * g;
 #pragma unroll
             for (int i = 0; i < 4; i++)
-                if (first + o < spread.active) all[i] = all[i] * f + part[o][i] * g;
+                if (first + o < parts) all[i] = all[i] * f + part[o][i] * g;
         }
     }
     if (!has_row) return;

@@ -181,12 +181,13 @@ void launched()
                             CHECK(kv_attend_rows(d, &a, nullptr) == KV_OK, "launch");
                             dkv::RowsParams x;
                             memcpy((void *)&x, launches[0].args.data(), sizeof x);
-                            CHECK(x.splits >= 1 && launches.size() == (x.splits > 1 ? 2u : 1u), "launches");
-                            CHECK(launches[0].g.x == x.n_tiles * x.n_kv_heads * x.splits, "grid");
+                            CHECK(x.splits >= 1 && launches.size() == (x.splits > 1 || x.groups ? 2u : 1u), "launches");
+                            CHECK(launches[0].g.x == (x.groups ? x.groups * x.n_kv_heads : x.n_tiles * x.n_kv_heads * x.splits), "grid");
+                            CHECK(!x.groups || (x.splits == 1 && x.row_bits == 5), "ranges are of tiles of 32 rows");
                             // the last request's last tile, wherever its rows are, comes before n_tiles
                             CHECK((uint64_t)n_rows * group / (1u << x.row_bits) + n <= x.n_tiles, "tiles");
-                            if (x.splits > 1) {
-                                const uint64_t slots = (uint64_t)x.n_tiles * x.splits * x.n_kv_heads;
+                            if (x.splits > 1 || x.groups) {
+                                const uint64_t slots = (x.groups ? 2ull * x.groups : (uint64_t)x.n_tiles * x.splits) * x.n_kv_heads;
                                 const uint64_t vecs = (uint64_t)(1u << x.row_bits) * (dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 128 : dim <= 192 ? 192 : 256) / 4;
                                 CHECK((const char *)(x.part + slots * vecs) <= (const char *)x.part_ml, "parts end");
                                 CHECK((const char *)(x.part_ml + slots * (1u << x.row_bits)) <= end, "references end");
