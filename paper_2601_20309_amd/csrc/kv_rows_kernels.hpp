@@ -232,11 +232,15 @@ struct Piece<X, kBits4> {
 
 // 16 bytes a lane from global memory into LDS, one lane's behind the other's from `to` on.  In assembly, since beside the
 // builtin the compiler waits for all reads of LDS where some would do, as long as one of these is under way.  Whoever looks at
-// what came waits for it first (loaded_lds), and then for the other waves.
-__device__ __forceinline__ void load_lds(const uint8_t *from, uint16_t *to)
+// what came waits for it first (loaded_lds), and then for the other waves.  (The compiler keeps nothing in m0: what needs
+// it sets it.)
+__device__ __forceinline__ void load_lds(const uint8_t *from, uint32_t to)
 {
-    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)to);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const uint16_t *p)
+{
+    return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p);
 }
 __device__ __forceinline__ void loaded_lds() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
@@ -281,6 +285,7 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
     const uint8_t *const kb = p.k + (uint64_t)kv_head * p.head_bytes;
     const uint8_t *const vb = p.v + (uint64_t)kv_head * p.head_bytes;
     uint16_t *const tiles = lds + (TURNS ? wave * BUFS * TILE : 0u);
+    const uint32_t tiles_at = lds_address(tiles + (TURNS ? 0u : wave * (512u / T::PITCH) * T::PITCH));  // where this wave's loads go
     // Tiles of tokens `first` to `stop` of a tile of rows, a part of them or all.
     auto run = [&](const RowTile &rt, uint32_t first_tokens, uint32_t stop, bool parts, uint64_t slot) {
     const int32_t len = p.lens[rt.s];
@@ -320,11 +325,12 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
     auto load = [&](auto buf, uint32_t cell) {
         if constexpr (DIRECT) {
             // a wave brings 512 numbers at once, whole tokens, each lane the 8 that belong where its lane's go
-            uint16_t *const keys = tiles + (BUFS > 1 ? buf() : 0) * TILE, *const values = keys + PLANE;
             // (turns of token + EVERY i are those of either, one with the other: they have no bit in common)
             constexpr uint32_t AT_ONCE = 512 / T::PITCH, EVERY = AT_ONCE * SHARING;
             uint32_t l = lane;
-            asm volatile("" : "+v"(l));  // (found anew for every tile: kept, these are what does not fit the registers)
+            uint32_t to = __builtin_amdgcn_readfirstlane(tiles_at);
+            asm volatile("" : "+v"(l), "+s"(to));  // (found anew for every tile: kept, these are what does not fit the registers)
+            to += buf() * TILE * 2u;
             const uint32_t mine = TURNS ? 0u : wave * AT_ONCE, token = mine + l / T::CHUNKS, slot = l % T::CHUNKS;
             const uint32_t ck = slot ^ T::key_turn(token), cv = slot ^ T::value_turn(token);
             const uint64_t off = (uint64_t)cell * p.token_bytes;
@@ -341,8 +347,8 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
                     if (!here || dk >= p.dim) k = p.zeros;
                     if (!here || dv >= p.dim) v = p.zeros;
                 }
-                load_lds(k, keys + (i * EVERY + mine) * T::PITCH);
-                load_lds(v, values + (i * EVERY + mine) * T::PITCH);
+                load_lds(k, to + i * EVERY * T::PITCH * 2u);
+                load_lds(v, to + PLANE * 2u + i * EVERY * T::PITCH * 2u);
             }
         } else {
             uint32_t first = tid % LANES;
