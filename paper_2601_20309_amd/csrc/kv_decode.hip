@@ -60,7 +60,14 @@ void launch_put_heads(hipStream_t s, const dkv::PutParams &p)
     const uint32_t heads = (p.qs ? p.n_heads : 0u) + 2u * p.n_kv_heads;
     const uint32_t most = p.n_rows <= 1024u ? 512u : 256u, lanes = heads << bits, turns = (lanes + most - 1u) / most;
     const uint32_t threads = ((lanes + turns - 1u) / turns + 63u) / 64u * 64u;
-    hipLaunchKernelGGL((dkv::kv_put_heads_kernel<X, KIND>), dim3(p.n_rows), dim3(threads), 0, s, p, bits);
+    const auto go = [&](auto whole) {
+        hipLaunchKernelGGL((dkv::kv_put_heads_kernel<X, KIND, decltype(whole)::value>), dim3(p.n_rows), dim3(threads), 0, s, p, bits);
+    };
+    const uint32_t whole = p.rot == p.dim && !p.interleaved ? p.dim / 8u : 0u;
+    if (whole == 8u) go(std::integral_constant<int, 8>{});
+    else if (whole == 16u) go(std::integral_constant<int, 16>{});
+    else if (whole == 32u) go(std::integral_constant<int, 32>{});
+    else go(std::integral_constant<int, 0>{});
 }
 
 template <typename X, int KIND>
@@ -261,6 +268,7 @@ int kv_put(kv_decoder *d, const kv_put_args *a, void *stream)
     p.q_norm = a->q_norm;
     p.k_norm = a->k_norm;
     p.eps = a->norm_eps;
+    p.inv_dim = 1.0f / (float)d->dim;
     p.k_scale = dkv::Scale::of(d->dc.k_scale);
     p.v_scale = dkv::Scale::of(d->dc.v_scale);
     hipStream_t s = (hipStream_t)stream;

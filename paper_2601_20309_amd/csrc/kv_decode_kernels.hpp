@@ -1008,7 +1008,7 @@ struct PutParams {
     uint32_t rot, interleaved, section0, section01;  // pairs of the first axis, of the first two
     uint32_t exponents;  // 4 bits: from a token's first byte to its heads' bytes
     const float *q_norm, *k_norm;
-    float eps;
+    float eps, inv_dim;
     Divide by_steps, by_vecs;  // by a rotated head's steps, and by a head's vectors
     Scale k_scale, v_scale;
 };
@@ -1149,52 +1149,89 @@ __global__ __launch_bounds__(512) void kv_put_kernel(const PutParams p)
     }
 }
 
+// What another of 16 lanes holds, by a lane pattern that needs no LDS: 0xB1 and 0x4E the lane 1 and 2 away of four, 0x141 and
+// 0x140 the one as far from the end of 8 and of 16, 0x128 the one 8 away.
+template <int CONTROL>
+__device__ __forceinline__ float lanes_of(float x)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CONTROL, 0xf, 0xf, true));
+}
+
 // New tokens whose heads are normed first, or go into 4 bits.  A thread has 8 dimensions of a head, one behind the other,
 // and a head lies in 1 to 32 lanes of a wave (a power of 2): the sum of its squares is a sum over lanes, so is
 // the largest of 32 dimensions over four, and the other numbers of pairs come from the lanes that have them.
 //   y = x / sqrt(mean x^2 + eps) * weight, then the rotation, all in 32 bits, rounded once.
 // 4 bits: the power of 2 is the one that brings the largest of 32 dimensions to 4 and more, under 8, and numbers are the nearest
 // of those there are (6 the largest); infinity or NaN among them makes all 32 NaN.
-template <typename X, int KIND>
+// WHOLE: the lanes of a head all of whose dimensions turn, halves apart, and are so many times 8; 0: any others.
+template <typename X, int KIND, int WHOLE>
 __global__ __launch_bounds__(512) void kv_put_heads_kernel(const PutParams p, const uint32_t lane_bits)
 {
     __shared__ float2 turn[128];
     const uint32_t row = blockIdx.x, tid = threadIdx.x, lane = tid & 63u;
+    const uint32_t pairs = p.rot / 2u;
+    // asked for before the row's request is known: its position, and what it is multiplied with
+    const uint32_t axis = tid < p.section0 ? 0u : tid < p.section01 ? 1u : 2u;
+    const int32_t pos0 = tid < pairs && p.positions ? p.positions[(int64_t)axis * p.position_stride + row] : 0;
+    const float freq0 = tid < pairs ? p.inv_freq[tid] : 0.f;
     uint32_t s = row, start = row, next = row + 1u;
-    if (p.starts) {
+    int32_t len;
+    if (p.starts && p.n_seqs <= 64u) {
+        // so few requests that every lane has one: their ends, and their lengths at once
+        const int32_t begin = p.starts[0], ends = lane < p.n_seqs ? p.starts[lane + 1u] : 0x7FFFFFFF, lens = lane < p.n_seqs ? p.lens[lane] : 0;
+        s = (uint32_t)__popcll(__ballot(ends <= (int32_t)row));
+        if (s >= p.n_seqs || (int32_t)row < begin) return;
+        start = (uint32_t)(s ? __builtin_amdgcn_readlane(ends, (int)s - 1) : begin);
+        next = (uint32_t)__builtin_amdgcn_readlane(ends, (int)s);
+        len = __builtin_amdgcn_readlane(lens, (int)s);
+    } else if (p.starts) {
         s = 0;
         for (uint32_t base = 1; base <= p.n_seqs; base += 64u)
             s += (uint32_t)__popcll(__ballot(base + lane <= p.n_seqs && p.starts[base + lane] <= (int32_t)row));
         if (s >= p.n_seqs || (int32_t)row < p.starts[0]) return;
         start = (uint32_t)p.starts[s];
         next = (uint32_t)p.starts[s + 1u];
+        len = p.lens[s];
+    } else {
+        len = p.lens[s];
     }
     const uint32_t n_q = p.qs ? p.n_heads : 0u, n_k = n_q + p.n_kv_heads, n_all = n_k + p.n_kv_heads;
-    const uint32_t lanes = 1u << lane_bits, in = tid & (lanes - 1u), d = in * 8u, at_once = blockDim.x >> lane_bits;
-    const uint32_t pairs = p.rot / 2u;
+    const uint32_t lanes = WHOLE ? (uint32_t)WHOLE : 1u << lane_bits, in = tid & (lanes - 1u), d = in * 8u, at_once = blockDim.x >> lane_bits;
     bool page = false;
     uint8_t *kc = nullptr, *vc = nullptr;
-    for (uint32_t first = 0; first < n_all; first += at_once) {
-        const uint32_t i = first + (tid >> lane_bits), head = i < n_q ? i : i < n_k ? i - n_q : i - n_k;
-        const bool here = i < n_all && d < p.dim;
+    const uint32_t mine = tid >> lane_bits;
+    auto load = [&](uint32_t i) {
+        const uint32_t head = i < n_q ? i : i < n_k ? i - n_q : i - n_k;
         w32x4 raw;
         clear(raw);
-        if (here) {
+        if (i < n_all && d < p.dim) {
             const uint8_t *const src = i < n_q ? p.qs + row * p.q_row + head * p.q_head
                                        : i < n_k ? p.ks + row * p.k_row + head * p.k_head
                                                  : p.vs + row * p.v_row + head * p.v_head;
             raw = __builtin_nontemporal_load(reinterpret_cast<const w32x4 *>(src + d * 2u));
         }
+        return raw;
+    };
+    w32x4 next_raw = load(mine);
+    for (uint32_t first = 0; first < n_all; first += at_once) {
+        const uint32_t i = first + mine, head = i < n_q ? i : i < n_k ? i - n_q : i - n_k;
+        const bool here = i < n_all && d < p.dim;
+        const w32x4 raw = next_raw;
+        next_raw = load(i + at_once);  // a turn ahead
         if (first == 0u) {
-            const int64_t token = (int64_t)p.lens[s] - (int64_t)(next - start) + (int64_t)(row - start);
+            const int64_t token = (int64_t)len - (int64_t)(next - start) + (int64_t)(row - start);
             for (uint32_t i = tid; i < pairs; i += blockDim.x) {
                 const uint32_t axis = i < p.section0 ? 0u : i < p.section01 ? 1u : 2u;
-                const double pos = p.positions ? (double)p.positions[(int64_t)axis * p.position_stride + row] : (double)token;
-                // in 64 bits: whole turns, and what is left of them; the rest as half turns
-                const double turns = pos * (double)p.inv_freq[i] * 0.15915494309189533577;
+                const int32_t at = i == tid || !p.positions ? pos0 : p.positions[(int64_t)axis * p.position_stride + row];
+                const double pos = p.positions ? (double)at : (double)token;
+                // in 64 bits: whole turns, and what is left of them; the sine of that in half turns
+                const double turns = pos * (double)(i == tid ? freq0 : p.inv_freq[i]) * 0.15915494309189533577;
+                const double half_turns = 2.0 * (turns - rint(turns));
                 float sn, cs;
-                sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
-                turn[i] = float2{cs, sn};
+                sincospif((float)half_turns, &sn, &cs);
+                // and by what its nearest 32-bit number is off
+                const float off = (float)(half_turns - (double)(float)half_turns) * 3.14159265f;
+                turn[i] = float2{__builtin_fmaf(-sn, off, cs), __builtin_fmaf(cs, off, sn)};
             }
             page = token >= 0 && token < (int64_t)p.max_blocks * p.block_size;
             uint32_t cell = kNoCell;
@@ -1214,32 +1251,46 @@ __global__ __launch_bounds__(512) void kv_put_heads_kernel(const PutParams p, co
             x[2 * e] = X::lo(raw[e]);
             x[2 * e + 1] = X::hi(raw[e]);
         }
-        // (from here to the rotation's end every lane of a wave takes part: heads that are not there hold zeros)
+        // (lanes of a head take part together, those behind its dimensions with zeros)
         const float *const weight = i < n_q ? p.q_norm : i < n_k ? p.k_norm : nullptr;
-        if (p.q_norm || p.k_norm) {
+        if (weight) {
             float sum = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; e++) sum = __builtin_fmaf(x[e], x[e], sum);
-            for (uint32_t m = 1; m < lanes; m <<= 1) sum += __shfl_xor(sum, (int)m, 64);
-            if (weight && here) {
-                const float r = 1.0f / sqrtf(sum / (float)p.dim + p.eps);
+            // over the head's lanes: neighbours, pairs, then each four, eight and sixteen with its mirror image
+            if (lanes > 1u) sum += lanes_of<0xB1>(sum);
+            if (lanes > 2u) sum += lanes_of<0x4E>(sum);
+            if (lanes > 4u) sum += lanes_of<0x141>(sum);
+            if (lanes > 8u) sum += lanes_of<0x140>(sum);
+            if (lanes > 16u) sum += __shfl_xor(sum, 16, 64);
+            // the root's reciprocal to its last bit, a step behind what the instruction gives
+            const float mean = __builtin_fmaf(sum, p.inv_dim, p.eps), r0 = __builtin_amdgcn_rsqf(mean);
+            const float left = __builtin_fmaf(-mean * r0, r0, 1.0f), r = left > -1.0f && left < 1.0f ? __builtin_fmaf(r0 * 0.5f, left, r0) : r0;
+            if (here) {
                 const f32x4 w0 = *reinterpret_cast<const f32x4 *>(weight + d), w1 = *reinterpret_cast<const f32x4 *>(weight + d + 4u);
 #pragma unroll
-                for (int e = 0; e < 8; e++) x[e] *= r * (e < 4 ? w0[e & 3] : w1[e & 3]);
+                for (int e = 0; e < 8; e++) x[e] = x[e] * r * (e < 4 ? w0[e & 3] : w1[e & 3]);
             }
         }
-        const bool turns = i < n_k;
-        if (p.interleaved) {
-            if (turns && d < p.rot) {
+        if (WHOLE && i < n_k) {
+            // each number of a lower half with the one half the lanes away
+            const bool lower = in < lanes / 2u;
+            const uint32_t at = d & (pairs - 1u);
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const float2 c = turn[(d + e) / 2u];
-                    const float u = x[e] * c.x - x[e + 1] * c.y, w = x[e + 1] * c.x + x[e] * c.y;
-                    x[e] = u;
-                    x[e + 1] = w;
-                }
+            for (uint32_t e = 0; e < 8; e++) {
+                const float other = WHOLE == 16 ? lanes_of<0x128>(x[e]) : __shfl_xor(x[e], WHOLE / 2, 64);
+                const float2 c = turn[at + e];
+                x[e] = __builtin_fmaf(lower ? -other : other, c.y, x[e] * c.x);
             }
-        } else if (p.rot) {
+        } else if (p.interleaved && i < n_k && d < p.rot) {
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const float2 c = turn[(d + e) / 2u];
+                const float u = x[e] * c.x - x[e + 1] * c.y, w = x[e + 1] * c.x + x[e] * c.y;
+                x[e] = u;
+                x[e + 1] = w;
+            }
+        } else if (!p.interleaved && p.rot && i < n_k) {
             // four dimensions at a time: those of a thread may be of both halves
             float other[8];
             const uint32_t fours = pairs / 4u, base = lane & ~(lanes - 1u);
@@ -1260,7 +1311,7 @@ __global__ __launch_bounds__(512) void kv_put_heads_kernel(const PutParams p, co
 #pragma unroll
             for (uint32_t e = 0; e < 8; e++) {
                 const uint32_t at = d + e;
-                if (!turns || at >= p.rot) continue;
+                if (at >= p.rot) continue;
                 const bool lower = at < pairs;
                 const float2 c = turn[lower ? at : at - pairs];
                 x[e] = lower ? x[e] * c.x - other[e] * c.y : x[e] * c.x + other[e] * c.y;
@@ -1270,8 +1321,8 @@ __global__ __launch_bounds__(512) void kv_put_heads_kernel(const PutParams p, co
         if constexpr (KIND == kBits4) {
 #pragma unroll
             for (int e = 0; e < 8; e++) largest = max(largest, __builtin_bit_cast(uint32_t, x[e]) & 0x7FFFFFFFu);
-            largest = max(largest, (uint32_t)__shfl_xor((int)largest, 1, 64));
-            largest = max(largest, (uint32_t)__shfl_xor((int)largest, 2, 64));
+            largest = max(largest, __builtin_bit_cast(uint32_t, lanes_of<0xB1>(__builtin_bit_cast(float, largest))));
+            largest = max(largest, __builtin_bit_cast(uint32_t, lanes_of<0x4E>(__builtin_bit_cast(float, largest))));
         }
         if (!here || (i >= n_q && !page)) continue;
         if (i < n_q) {
