@@ -58,7 +58,8 @@ void launch_put_heads(hipStream_t s, const dkv::PutParams &p)
     uint32_t bits = 0;
     while ((8u << bits) < p.dim) bits++;
     const uint32_t heads = (p.qs ? p.n_heads : 0u) + 2u * p.n_kv_heads;
-    const uint32_t most = p.n_rows <= 1024u ? 512u : 256u, lanes = heads << bits, turns = (lanes + most - 1u) / most;
+    // us of 768 lanes a row, by 128 / 256 / 512: 64 rows 7.1 / 5.5 / 4.8, 6853 into 4 bits 40.2 / 43.0 / 52.6.
+    const uint32_t most = p.n_rows <= 1024u ? 512u : 128u, lanes = heads << bits, turns = (lanes + most - 1u) / most;
     const uint32_t threads = ((lanes + turns - 1u) / turns + 63u) / 64u * 64u;
     const auto go = [&](auto whole) {
         hipLaunchKernelGGL((dkv::kv_put_heads_kernel<X, KIND, decltype(whole)::value>), dim3(p.n_rows), dim3(threads), 0, s, p, bits);

@@ -314,6 +314,8 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
     // In 8 bits there is room for two tiles of values: they are asked for a tile ahead, like the keys.  us without / with:
     // 128 requests around 600 tokens, 8 heads of 128, 39.4 / 37.4; 4 of 32768 tokens, 8 heads of 128 48.4 / 50.4, of 192
     // 102 / 85, 4 heads of 256 51.4 / 55.2; in 16 bits, 32 requests around 1000, 8 heads of 128, 35.6 / 39.7.
+    // In 4 bits a step has so few bytes that all of the next one's are asked for before this one's products.
+    constexpr bool EARLY = FP4;
     constexpr bool AHEAD = FP4 || (FP8 && !(WHOLE && DP == 256));
     auto k_dim = [](int j, uint32_t kq) { return FP4 ? (uint32_t)(j / 4) * 128u + kq * K4 + (uint32_t)(j & 3) * 8u : FP8 ? (uint32_t)(j / 2) * 64u + kq * 16u + (uint32_t)(j & 1) * 8u : (uint32_t)j * 32u + kq * 8u; };
     typedef typename Raw<FP4 ? 4 : (FP8 ? 1 : 2) * VW>::type vraw;
@@ -363,6 +365,7 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
     };
     // 4 bits: from a token's numbers of this head to the head's powers of 2
     const uint32_t powers = FP4 ? p.exponents + kv_head * (p.dim / 32u) - kv_head * p.head_bytes : 0u;
+    const uint8_t *const v_row = p.v + (uint64_t)kv_head * p.head_bytes;
     auto power = [](uint32_t byte) { return __builtin_bit_cast(float, byte << 23); };
 
     // What a step needs is asked for a step (its pages two steps) ahead, across the ends of requests,
@@ -434,7 +437,26 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
     uint32_t cell[2], page[2];
     // The lane's 8 tokens of the step whose cells are `cell`, and their values.
     uint32_t vcell[8];
+    uint64_t voff[8];  // 4 bits: their bytes
     auto find_values = [&](uint32_t &present) {
+        if constexpr (FP4) {
+            // (a lane has both halves' tokens n: two products here instead of eight behind the shuffles, and a bit for each token)
+            uint32_t bits[2];
+            uint64_t off[2];
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                bits[h] = (uint32_t)__ballot(cell[h] != kNoCell) & 0xFFFFu;
+                off[h] = (uint64_t)(cell[h] == kNoCell ? 0u : cell[h]) * p.token_bytes;
+            }
+            present = (bits[0] >> (kq * 4u) & 15u) | (bits[1] >> (kq * 4u) & 15u) << 4;
+#pragma unroll
+            for (int r = 0; r < 8; r++) {
+                const int from = (int)((kq * 4u + (r & 3)) * 4u);
+                const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)(uint32_t)off[r / 4]), hi = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)(off[r / 4] >> 32));
+                voff[r] = (uint64_t)hi << 32 | lo;
+            }
+            return;
+        }
         present = 0;
 #pragma unroll
         for (int r = 0; r < 8; r++) {
@@ -447,14 +469,13 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
         uint32_t v = n;
         if constexpr (!WHOLE) asm volatile("" : "+v"(v));
         if constexpr (FP4) {
-            const uint8_t *const rows = p.v + (uint64_t)kv_head * p.head_bytes;
             const uint32_t d = WHOLE ? (uint32_t)c * 128u + v * VW : min((uint32_t)c * 128u + v * VW, p.dim - VW);
 #pragma unroll
             for (int r = 0; r < 8; r++) {
-                const uint8_t *const row = rows + (uint64_t)vcell[r] * p.token_bytes;
-                if constexpr (DP == 64) to[r][c] = *reinterpret_cast<const w16_any *>(row + d / 2u);
-                else to[r][c] = *reinterpret_cast<const w32_any *>(row + d / 2u);
-                x[r][c] = row[powers + d / 32u];
+                const uint8_t *const row = v_row + d / 2u + voff[r];
+                if constexpr (DP == 64) to[r][c] = *reinterpret_cast<const w16_any *>(row);
+                else to[r][c] = *reinterpret_cast<const w32_any *>(row);
+                x[r][c] = v_row[powers + d / 32u + voff[r]];
             }
             return;
         }
@@ -468,6 +489,8 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
     };
     vraw next_vr[8][NV];
     uint32_t next_vx[8][NV];  // 4 bits: powers of 2
+    w32x4 next_kr[2][KL];
+    uint32_t next_kx[2][KL];
     uint32_t next_present = 0;
     for (;;) {
         uint32_t next_page[2];
@@ -504,6 +527,35 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
 #pragma unroll
                     for (int c = 0; c < NV; c++) load_values(vr, vx, c);
                 }
+            }
+            // the step after this one (`next`: the first of the next request)
+            const uint32_t tile = last ? next_first : tt + p.subs;
+            const bool more = tile < (last ? next_stop : stop);
+            auto read_queries = [&](uint32_t request) {
+#pragma unroll
+                for (int j = 0; j < KJ; j++) {
+                    const uint32_t d = k_dim(j, kq);
+                    qf[j] = w32x4{0u, 0u, 0u, 0u};
+                    if (has_row && (WHOLE || d < p.dim))
+                        qf[j] = *reinterpret_cast<const w32x4 *>(p.q + (uint64_t)request * p.q_row + (uint64_t)head * p.q_head + d * 2u);
+                }
+            };
+            if constexpr (EARLY) {
+                if (more) {
+                    Part part = now;
+                    if (last) part = next;
+#pragma unroll
+                    for (int h = 0; h < 2; h++) cell[h] = cell_of(tile, h, last ? next_page[h] : page[h]);
+#pragma unroll
+                    for (int h = 0; h < 2; h++) load_keys(next_kr[h], next_kx[h], cell[h]);
+                    find_values(next_present);
+#pragma unroll
+                    for (int c = 0; c < NV; c++) load_values(next_vr, next_vx, c);
+#pragma unroll
+                    for (int h = 0; h < 2; h++) page[h] = page_of(part, tile + p.subs, h);
+                }
+            }
+            if (have) {
                 // scores: token x head
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
@@ -541,21 +593,24 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
                 }
             }
             // the next step's keys, while this one's values arrive
-            const uint32_t tile = last ? next_first : tt + p.subs;
-            if (tile < (last ? next_stop : stop)) {
+            if constexpr (EARLY) {
+                if (more) {
+                    if (last) read_queries(next.s);
+#pragma unroll
+                    for (int h = 0; h < 2; h++) {
+#pragma unroll
+                        for (int l = 0; l < KL; l++) {
+                            kr[h][l] = next_kr[h][l];
+                            kx[h][l] = next_kx[h][l];
+                        }
+                    }
+                }
+            } else if (more) {
                 Part part = now;
                 if (last) part = next;
 #pragma unroll
                 for (int h = 0; h < 2; h++) cell[h] = cell_of(tile, h, last ? next_page[h] : page[h]);
-                if (last) {
-#pragma unroll
-                    for (int j = 0; j < KJ; j++) {
-                        const uint32_t d = k_dim(j, kq);
-                        qf[j] = w32x4{0u, 0u, 0u, 0u};
-                        if (has_row && (WHOLE || d < p.dim))
-                            qf[j] = *reinterpret_cast<const w32x4 *>(p.q + (uint64_t)part.s * p.q_row + (uint64_t)head * p.q_head + d * 2u);
-                    }
-                }
+                if (last) read_queries(part.s);
 #pragma unroll
                 for (int h = 0; h < 2; h++) load_keys(kr[h], kx[h], cell[h]);
                 if constexpr (AHEAD) {
