@@ -512,8 +512,7 @@ typedef struct {
     float v_scale;
     int32_t weigh;       /* 1: kv_attend may be asked for mass_out, which takes max_seqs * max_blocks * n_heads floats of
                             memory (as many times that as an odd block has tokens, or 4, 8 or 16 go into one) */
-    int32_t max_rows;    /* most rows of a kv_attend_rows() call; 0: none are made.  Otherwise 65536 * (64, 96, 128, 192 or 256
-                            dimensions + 2) * 4 bytes of memory: 34 MB at 128 */
+    int32_t max_rows;    /* most rows of a kv_attend_rows() call; 0: none are made.  Otherwise 64 MiB of memory and up to 2 more */
 } kv_decoder_config;
 
 /*

@@ -54,8 +54,8 @@ struct Bf16 {
         return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, power, BYTE));
     }
     static constexpr int kLowPower = -126, kHighPower = 125;  // of 4-bit numbers: half of the one and 6 of the other are bf16 numbers
-    // whether either of two is infinity or NaN
-    static __device__ __forceinline__ bool odd(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
+    // bits for either of two that is infinity or NaN: the carry out of an exponent of ones
+    static __device__ __forceinline__ uint32_t odd(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
     static __device__ __forceinline__ bool nan(uint32_t w) { return (w & 0x7FFFu) > 0x7F80u; }  // the lower of two
     static constexpr float kMost = 0x1.FEp127f;
     // Each of two weights as the sum of two numbers of 8 digits, the upper cut off, the lower the nearest to what that leaves:
@@ -97,7 +97,7 @@ struct Fp16 {
         return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, power, BYTE));
     }
     static constexpr int kLowPower = -23, kHighPower = 13;
-    static __device__ __forceinline__ bool odd(uint32_t w) { return (w & 0x7C00u) == 0x7C00u || (w & 0x7C000000u) == 0x7C000000u; }
+    static __device__ __forceinline__ uint32_t odd(uint32_t w) { return ((w & 0x7C007C00u) + 0x04000400u) & 0x80008000u; }
     static __device__ __forceinline__ bool nan(uint32_t w) { return (w & 0x7FFFu) > 0x7C00u; }
     static constexpr float kMost = 65504.0f;
     static constexpr uint32_t kOnes = 0x3C003C00u;

@@ -110,13 +110,16 @@ extern "C" int kv_attend_rows(kv_decoder *d, const kv_attend_rows_args *a, void 
         // Equal ranges for two workgroups a compute unit (one where their tiles fill its LDS); a workgroup for each tile where no
         // request can be longer than four steps of its waves.
         const uint32_t at_once = (uint32_t)d->n_cus * (kind < 2 && p.dim > 64u ? 1u : 2u);
-        if (most > 16u && (uint64_t)p.n_tiles * most <= 0x7FFFFFFFu) {
-            p.groups = (uint32_t)std::min<uint64_t>(std::max(1u, std::min(at_once, (uint32_t)kRowSums / 64u) / p.n_kv_heads), (uint64_t)p.n_tiles * most);
+        if (most > 16u && (uint64_t)p.n_tiles * most <= 0x7FFFFFFFu && each * (rows_dims(p.dim) / 32u) / 4u < kMostTiles) {
+            p.groups = (uint32_t)std::min<uint64_t>(std::max(1u, at_once / p.n_kv_heads), (uint64_t)p.n_tiles * most);
             wgs = (uint64_t)p.groups * p.n_kv_heads;
         }
     } else {
-        // Few tiles of rows: the tokens are split, so that every compute unit has some.
-        p.splits = (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>((kRowSums >> p.row_bits) / each, (most + p.least - 1u) / p.least));
+        // Few tiles of rows: the tokens are split, so that every compute unit has two workgroups, or one of 256 rows.  (More
+        // splits leave more to join.  us, two / four / six to a compute unit: 24 requests of 180 rows, 12 heads of 64, 42.3 / 42.2 / 48.9;
+        // 9 requests of 150 rows, 3 heads of 96 in 4 bits, 25.9 / 28.3 / 29.2.)
+        const uint64_t wanted = (uint64_t)d->n_cus * (many ? 1u : 2u);
+        p.splits = (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>(std::min(wanted, row_sums(p.dim) >> p.row_bits) / each, (most + p.least - 1u) / p.least));
         wgs = each * p.splits;
     }
     const dim3 g((uint32_t)wgs);

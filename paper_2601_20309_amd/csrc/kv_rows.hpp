@@ -6,10 +6,8 @@
 
 namespace dkv {
 
-// Rows that splits may leave, all in all: of 512 tiles of 128, two for each of the most compute units that there are, or of
-// 2048 tiles of 32.
-constexpr uint64_t kRowSums = 65536;
-
+// What splits and ranges may leave: as many rows as 64 MiB hold.
+constexpr uint64_t kRowSumsBytes = 64ull << 20;
 constexpr uint64_t kMostTiles = 0xFFFFFF;  // as many workgroups of 256 lanes as a launch can count lanes
 
 // Tiles of rows of one KV head, empty ones among them.
@@ -25,7 +23,9 @@ inline bool rows_fit(int64_t n_kv_heads, int64_t n_heads, int64_t n_seqs, int64_
 // Dimensions that the kernels are made for.
 inline uint32_t rows_dims(uint32_t dim) { return dim <= 64u ? 64u : dim <= 96u ? 96u : dim <= 128u ? 128u : dim <= 192u ? 192u : 256u; }
 
-inline uint64_t rows_part_bytes(const kv_decoder *d) { return d->dc.max_rows ? kRowSums * (uint64_t)rows_dims(d->dim) * 4u : 0u; }
-inline uint64_t rows_ml_bytes(const kv_decoder *d) { return d->dc.max_rows ? kRowSums * sizeof(float2) : 0u; }
+inline uint64_t row_sums(uint32_t dim) { return kRowSumsBytes / 4u / rows_dims(dim) / 128u * 128u; }
+
+inline uint64_t rows_part_bytes(const kv_decoder *d) { return d->dc.max_rows ? row_sums(d->dim) * rows_dims(d->dim) * 4u : 0u; }
+inline uint64_t rows_ml_bytes(const kv_decoder *d) { return d->dc.max_rows ? row_sums(d->dim) * sizeof(float2) : 0u; }
 
 }  // namespace dkv

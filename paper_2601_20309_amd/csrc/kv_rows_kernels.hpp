@@ -50,42 +50,77 @@ struct RowsParams {
 struct RowTile {
     uint32_t s, first;      // request; its rows' heads before this tile
     int32_t start, m;       // the request's first row, and its number of rows
+    int32_t len;            // its tokens
     bool here;
 };
 
-__device__ __forceinline__ uint32_t first_tile(const RowsParams &p, uint32_t s)
+// Up to 64 requests: every lane has one, so that finding one takes one round of loads.
+struct Requests {
+    int32_t start, next, len;
+    __device__ __forceinline__ Requests(const RowsParams &p, uint32_t lane) : start(0x7FFFFFFF), next(0x7FFFFFFF), len(0)
+    {
+        if (p.n_seqs > 64u || lane >= p.n_seqs) return;
+        start = p.starts ? p.starts[lane] : (int32_t)lane;
+        next = p.starts ? p.starts[lane + 1u] : (int32_t)lane + 1;
+        len = p.lens[lane];
+    }
+    // Request s's, from a lane or from memory.
+    __device__ __forceinline__ void of(const RowsParams &p, uint32_t s, int32_t &first, int32_t &last, int32_t &tokens) const
+    {
+        if (p.n_seqs <= 64u) {
+            first = __builtin_amdgcn_readlane(start, (int)s);
+            last = __builtin_amdgcn_readlane(next, (int)s);
+            tokens = __builtin_amdgcn_readlane(len, (int)s);
+        } else {
+            first = p.starts ? p.starts[s] : (int32_t)s;
+            last = p.starts ? p.starts[s + 1u] : (int32_t)s + 1;
+            tokens = p.lens[s];
+        }
+    }
+};
+
+__device__ __forceinline__ uint32_t first_tile(const RowsParams &p, uint32_t s, int32_t start)
 {
-    const int32_t start = p.starts ? p.starts[s] : (int32_t)s;
     return (uint32_t)((uint64_t)(uint32_t)max(start, 0) * p.group_heads >> p.row_bits) + s;
 }
 
-__device__ __forceinline__ RowTile row_tile(const RowsParams &p, uint32_t lane, uint32_t tile)
+__device__ __forceinline__ int32_t rows_of(const RowsParams &p, int32_t start, int32_t next)
+{
+    return start < 0 ? 0 : (int32_t)min(max((int64_t)next - start, (int64_t)0), (int64_t)p.n_rows);
+}
+
+__device__ __forceinline__ RowTile row_tile(const RowsParams &p, const Requests &requests, uint32_t lane, uint32_t tile)
 {
     RowTile t;
     // the last request whose first tile is not behind this one, 64 candidates at a time
-    uint32_t lo = 0, range = p.n_seqs;
-    while (range > 1u) {
-        const uint32_t step = (range + 63u) / 64u, at = lo + lane * step;
-        const uint64_t before = __ballot(lane * step < range && first_tile(p, at) <= tile);
-        const uint32_t n = before ? 63u - (uint32_t)__builtin_clzll(before) : 0u;
-        range = min(step, range - n * step);
-        lo += n * step;
+    uint32_t lo = 0;
+    if (p.n_seqs <= 64u) {
+        const uint64_t before = __ballot(lane < p.n_seqs && first_tile(p, lane, requests.start) <= tile);
+        lo = before ? 63u - (uint32_t)__builtin_clzll(before) : 0u;
+    } else {
+        for (uint32_t range = p.n_seqs; range > 1u;) {
+            const uint32_t step = (range + 63u) / 64u, at = lo + lane * step;
+            const uint64_t before = __ballot(lane * step < range && first_tile(p, at, p.starts ? p.starts[at] : (int32_t)at) <= tile);
+            const uint32_t n = before ? 63u - (uint32_t)__builtin_clzll(before) : 0u;
+            range = min(step, range - n * step);
+            lo += n * step;
+        }
     }
     t.s = __builtin_amdgcn_readfirstlane(lo);
-    const uint32_t base = first_tile(p, t.s);
-    t.start = p.starts ? p.starts[t.s] : (int32_t)t.s;
-    const int64_t next = p.starts ? p.starts[t.s + 1u] : (int64_t)t.s + 1;
-    t.m = (int32_t)min(max(next - t.start, (int64_t)0), (int64_t)p.n_rows);
+    int32_t next;
+    requests.of(p, t.s, t.start, next, t.len);
+    t.m = rows_of(p, t.start, next);
+    const uint32_t base = first_tile(p, t.s, t.start);
     const uint64_t first = (uint64_t)(tile - base) << p.row_bits;
-    t.here = tile >= base && t.start >= 0 && first < (uint64_t)t.m * p.group_heads;
+    t.here = tile >= base && first < (uint64_t)t.m * p.group_heads;
     t.first = (uint32_t)first;
     return t;
 }
 
 // Tokens before which row i of the request looks.
-__device__ __forceinline__ int32_t row_sees(const RowsParams &p, int32_t len, const RowTile &t, uint32_t row)
+__device__ __forceinline__ int32_t row_sees(const RowsParams &p, const RowTile &t, uint32_t row)
 {
-    const int64_t upto = p.causal ? (int64_t)len - t.m + (int64_t)row + 1 : (int64_t)len;
+    const int64_t upto = p.causal ? (int64_t)t.len - t.m + (int64_t)row + 1 : (int64_t)t.len;
     return (int32_t)min(max(upto, (int64_t)0), (int64_t)p.max_tokens);
 }
 
@@ -105,27 +140,20 @@ struct Spread {
 struct RowDeal {
     uint32_t total, per, before;  // tiles of tokens; of a range; of the requests before the one asked for
     uint32_t mine, upto;          // of request (n_seqs - 1) / 64 * 64 + lane; of its 64 up to and with it
-    // Tiles of tokens of request s, the same for each of its tiles of rows, and those in all.
-    static __device__ __forceinline__ uint32_t tokens_of(const RowsParams &p, uint32_t s, uint32_t &start, uint32_t &rows)
+    // Tiles of tokens of a request, the same for each of its tiles of rows, and those in all.
+    static __device__ __forceinline__ uint32_t tokens_of(const RowsParams &p, int32_t len) { return ((uint32_t)min(max(len, 0), (int32_t)p.max_tokens) + 31u) / 32u; }
+    static __device__ __forceinline__ uint32_t work(const RowsParams &p, const Requests &requests, uint32_t s)
     {
-        const int32_t a = p.starts ? p.starts[s] : (int32_t)s;
-        const int64_t next = p.starts ? p.starts[s + 1u] : (int64_t)s + 1;
-        start = (uint32_t)max(a, 0);
-        rows = a < 0 ? 0u : (uint32_t)min(max(next - a, (int64_t)0), (int64_t)p.n_rows);
-        return (seq_tokens(p.lens, s, p.max_tokens) + 31u) / 32u;
-    }
-    static __device__ __forceinline__ uint32_t work(const RowsParams &p, uint32_t s)
-    {
-        uint32_t start, rows;
         if (s >= p.n_seqs) return 0u;
-        const uint32_t tokens = tokens_of(p, s, start, rows);
-        return (rows * p.group_heads + 31u) / 32u * tokens;
+        int32_t start = requests.start, next = requests.next, len = requests.len;
+        if (p.n_seqs > 64u) requests.of(p, s, start, next, len);
+        return ((uint32_t)rows_of(p, start, next) * p.group_heads + 31u) / 32u * tokens_of(p, len);
     }
-    __device__ __forceinline__ RowDeal(const RowsParams &p, uint32_t lane, uint32_t asked) : total(0), per(1), before(0), mine(0), upto(0)
+    __device__ __forceinline__ RowDeal(const RowsParams &p, const Requests &requests, uint32_t lane, uint32_t asked) : total(0), per(1), before(0), mine(0), upto(0)
     {
         if (!p.groups) return;
         for (uint32_t base = 0; base < p.n_seqs; base += 64u) {
-            mine = work(p, base + lane);
+            mine = work(p, requests, base + lane);
             upto = wave_scan(mine);
             if (asked >= base && asked - base < 64u) before = total + (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), (int)(asked - base));
             total += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
@@ -133,12 +161,12 @@ struct RowDeal {
         per = max((total + p.groups - 1u) / p.groups, 1u);
     }
     // The request that tile `at` is of, and how many of its tiles come before.
-    __device__ __forceinline__ bool find(const RowsParams &p, uint32_t lane, uint32_t at, uint32_t &s, uint32_t &t) const
+    __device__ __forceinline__ bool find(const RowsParams &p, const Requests &requests, uint32_t lane, uint32_t at, uint32_t &s, uint32_t &t) const
     {
         uint32_t m = mine, u = upto, first = 0;
         for (uint32_t base = 0; base < p.n_seqs; base += 64u) {
             if (p.n_seqs > 64u) {
-                m = work(p, base + lane);
+                m = work(p, requests, base + lane);
                 u = wave_scan(m);
             }
             const uint64_t beyond = __ballot(first + u > at);
@@ -288,15 +316,14 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
     const uint32_t tiles_at = lds_address(tiles + (TURNS ? 0u : wave * (512u / T::PITCH) * T::PITCH));  // where this wave's loads go
     // Tiles of tokens `first` to `stop` of a tile of rows, a part of them or all.
     auto run = [&](const RowTile &rt, uint32_t first_tokens, uint32_t stop, bool parts, uint64_t slot) {
-    const int32_t len = p.lens[rt.s];
     const uint32_t last_flat = min(rt.first + ROWS, (uint32_t)rt.m * p.group_heads) - 1u;
-    const uint32_t most = (uint32_t)row_sees(p, len, rt, p.by_group.quotient(last_flat));
-    const uint32_t fewest = (uint32_t)row_sees(p, len, rt, p.by_group.quotient(rt.first));
+    const uint32_t most = (uint32_t)row_sees(p, rt, p.by_group.quotient(last_flat));
+    const uint32_t fewest = (uint32_t)row_sees(p, rt, p.by_group.quotient(rt.first));
     const uint32_t begin = first_tokens + (TURNS ? wave : 0u), end = min(stop, (most + TOKENS - 1u) / TOKENS);
     const uint32_t flat = rt.first + (TURNS ? 0u : wave * 32u) + n, row = p.by_group.quotient(flat), head = kv_head * p.group_heads + flat - row * p.group_heads;
     const uint32_t at_row = (uint32_t)rt.start + row;
     const bool has_row = row < (uint32_t)rt.m && at_row < p.n_rows;
-    const uint32_t sees = has_row ? (uint32_t)row_sees(p, len, rt, row) : 0u;
+    const uint32_t sees = has_row ? (uint32_t)row_sees(p, rt, row) : 0u;
     // 4 bits: from a token's numbers of this head to the head's powers of 2
     const uint32_t powers = KIND == kBits4 ? p.exponents + kv_head * (p.dim / 32u) - kv_head * p.head_bytes : 0u;
     const int32_t *const pages = p.table + (int64_t)rt.s * p.table_stride;
@@ -452,7 +479,7 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
                 const uint32_t token = u / (DP / 8u), chunk = u - token * (DP / 8u);
                 w32x4 *const at = reinterpret_cast<w32x4 *>(values + T::value_at(token, chunk));
                 w32x4 v = *at;
-                if (!(X::odd(v[0]) || X::odd(v[1]) || X::odd(v[2]) || X::odd(v[3]))) continue;
+                if (!(X::odd(v[0]) | X::odd(v[1]) | X::odd(v[2]) | X::odd(v[3]))) continue;
                 for (uint32_t e = 0; e < 8; e++) {
                     const uint32_t word = e / 2 == 0u ? v[0] : e / 2 == 1u ? v[1] : e / 2 == 2u ? v[2] : v[3], x = e & 1u ? word >> 16 : word & 0xFFFFu;
                     if (!X::odd(x)) continue;
@@ -460,7 +487,7 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
                     reinterpret_cast<uint16_t *>(at)[e] = 0;
                     for (uint32_t r = 0; r < ROWS; r++) {
                         const uint32_t row = p.by_group.quotient(rt.first + r);
-                        if (row >= (uint32_t)rt.m || (uint32_t)row_sees(p, len, rt, row) <= t * TOKENS + token) continue;
+                        if (row >= (uint32_t)rt.m || (uint32_t)row_sees(p, rt, row) <= t * TOKENS + token) continue;
                         uint32_t *const m = marks + (r * NB + chunk / 4u) * 2u;
                         const uint32_t bit = 1u << (chunk % 4u * 8u + e);
                         if (nan || !(x & 0x8000u)) atomicOr(m, bit);
@@ -592,10 +619,11 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
     if (parts) p.part_ml[slot * ROWS + (TURNS ? 0u : wave * 32u) + n] = float2{ref, own};
     else if (has_row && p.lse) p.lse[(uint64_t)at_row * p.n_heads + head] = own == 0.f ? -__builtin_inff() : (ref + __builtin_amdgcn_logf(own)) * 0.693147180559945309f;
     };
+    const Requests requests(p, lane);
     RowTile rt;
     if constexpr (TURNS) {
         // (run() once in the code, whether the workgroup has a range or a tile)
-        const RowDeal deal(p, lane, 0u);
+        const RowDeal deal(p, requests, lane, 0u);
         uint32_t at = p.groups ? rest * deal.per : 0u, here = 1u;
         const uint32_t stop = p.groups ? min(at + deal.per, deal.total) : 1u;
         for (; at < stop; at += here) {
@@ -603,19 +631,20 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
             uint64_t slot = 0;
             bool parts = false;
             if (p.groups) {
-                uint32_t t, start, rows;
-                if (!deal.find(p, lane, at, rt.s, t)) return;
-                const uint32_t tokens = RowDeal::tokens_of(p, rt.s, start, rows), tile = t / tokens;
+                uint32_t t;
+                int32_t next;
+                if (!deal.find(p, requests, lane, at, rt.s, t)) return;
+                requests.of(p, rt.s, rt.start, next, rt.len);
+                rt.m = rows_of(p, rt.start, next);
+                const uint32_t tokens = RowDeal::tokens_of(p, rt.len), tile = t / tokens;
                 first = t - tile * tokens;
                 here = min(tokens - first, stop - at);
                 last = first + here;
                 parts = here < tokens;
                 slot = (uint64_t)(rest * 2u + (first ? 0u : 1u)) * p.n_kv_heads + kv_head;
                 rt.first = tile * 32u;
-                rt.start = (int32_t)start;
-                rt.m = (int32_t)rows;
             } else {
-                rt = row_tile(p, lane, rest);
+                rt = row_tile(p, requests, lane, rest);
                 if (!rt.here) return;
             }
             run(rt, first, last, parts, slot);
@@ -623,10 +652,10 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
     } else {
         // last rows, which see most, first
         const uint32_t split = rest % p.splits, tile = p.n_tiles - 1u - rest / p.splits;
-        rt = row_tile(p, lane, tile);
+        rt = row_tile(p, requests, lane, tile);
         if (!rt.here) return;
         const uint32_t last_flat = min(rt.first + ROWS, (uint32_t)rt.m * p.group_heads) - 1u;
-        const Spread spread(p, (uint32_t)row_sees(p, p.lens[rt.s], rt, p.by_group.quotient(last_flat)), TOKENS);
+        const Spread spread(p, (uint32_t)row_sees(p, rt, p.by_group.quotient(last_flat)), TOKENS);
         if (split >= max(spread.active, 1u)) return;
         run(rt, split * spread.per, split * spread.per + spread.per, spread.active > 1u, ((uint64_t)tile * p.splits + split) * p.n_kv_heads + kv_head);
     }
@@ -641,21 +670,20 @@ __global__ __launch_bounds__(256) void kv_rows_join_kernel(const RowsParams p, u
     const uint32_t at = blockIdx.x * 4u + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rest = at / of_tile, in = at - rest * of_tile;
     const uint32_t b = in % blocks, wave = in / blocks, kv_head = rest % p.n_kv_heads, tile = rest / p.n_kv_heads;
     if (tile >= p.n_tiles) return;
-    const RowTile rt = row_tile(p, lane, tile);
+    const Requests requests(p, lane);
+    const RowTile rt = row_tile(p, requests, lane, tile);
     if (!rt.here) return;
-    const int32_t len = p.lens[rt.s];
     uint32_t parts, g0 = 0;
     if (p.groups) {
-        uint32_t start, rows;
-        const uint32_t n_tokens = RowDeal::tokens_of(p, rt.s, start, rows);
-        const RowDeal deal(p, lane, rt.s);
+        const uint32_t n_tokens = RowDeal::tokens_of(p, rt.len);
+        const RowDeal deal(p, requests, lane, rt.s);
         const uint32_t first = deal.before + rt.first / 32u * n_tokens;
         g0 = first / deal.per;
         parts = n_tokens ? min((first + n_tokens - 1u) / deal.per, p.groups - 1u) - g0 + 1u : 0u;
         if (parts == 1u) return;  // (none: no range has a request without tokens)
     } else {
         const uint32_t last_flat = min(rt.first + (1u << p.row_bits), (uint32_t)rt.m * p.group_heads) - 1u;
-        parts = Spread(p, (uint32_t)row_sees(p, len, rt, p.by_group.quotient(last_flat)), tokens).active;
+        parts = Spread(p, (uint32_t)row_sees(p, rt, p.by_group.quotient(last_flat)), tokens).active;
         if (parts <= 1u) return;
     }
     const uint32_t flat = rt.first + wave * 32u + n, row = p.by_group.quotient(flat), head = kv_head * p.group_heads + flat - row * p.group_heads;
