@@ -272,12 +272,11 @@ __device__ __forceinline__ uint32_t lds_address(const uint16_t *p)
 }
 __device__ __forceinline__ void loaded_lds() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-// N products of which each reads LDS READS times: the reads are AHEAD products ahead.
+// N products of which each reads LDS READS times: the reads are AHEAD products ahead, those of the first ones done.
 template <int N, int READS, int AHEAD>
 __device__ __forceinline__ void pipeline()
 {
     constexpr int kMma = 0x008, kRead = 0x100;
-    __builtin_amdgcn_sched_group_barrier(kRead, READS * AHEAD, 0);
 #pragma unroll
     for (int i = 0; i < N - AHEAD; i++) {
         __builtin_amdgcn_sched_group_barrier(kMma, 1, 0);
@@ -296,6 +295,7 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
     constexpr uint32_t SHARING = TURNS ? 1 : WAVES, STEP = TURNS ? WAVES : 1;  // waves of a tile of tokens; tiles of a turn
     constexpr uint32_t UNITS = TOKENS * DP / P::N, ROW_UNITS = DP / P::N;      // pieces of a tile, of a token
     constexpr uint32_t LANES = 64 * SHARING;
+    constexpr int READY = KS * TB < 6 ? KS * TB : 6;  // operands that are ready before the first product
     constexpr int EACH = DIRECT ? 1 : (UNITS + LANES - 1) / LANES;
     // Numbers that go through registers are stored when the tile before them has been read: of a wave's own tiles one is enough.
     constexpr uint32_t BUFS = TURNS && !DIRECT ? 1 : 2;
@@ -434,6 +434,14 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
         const uint64_t present = next_present;
         if constexpr (DIRECT) loaded_lds();
         if constexpr (!TURNS) __syncthreads();
+        // The first operands of either product are asked for before what comes between: the next tile's places, the weights.
+        // (chunk 2 j + h of a token begins at key_at(token, h), bits of 2 j turned round)
+        auto key = [&](int i) {
+            return *reinterpret_cast<const w32x4 *>(keys + (uint32_t)(i % TB) * 32u * T::PITCH + (T::key_at(n, h) ^ (uint32_t)(i / TB) * 16u));
+        };
+        w32x4 ready[READY];
+#pragma unroll
+        for (int i = 0; i < READY; i++) ready[i] = key(i);
         if (t + STEP < end) {
             const uint32_t cell = cell_of(t + STEP, page);
             next_present = __ballot(cell != kNoCell);
@@ -449,14 +457,8 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int j = 0; j < KS; j++)
-#pragma unroll
-            for (int b = 0; b < TB; b++) {
-                // (chunk 2 j + h of a token begins at key_at(token, h), bits of 2 j turned round)
-                const w32x4 a = *reinterpret_cast<const w32x4 *>(keys + (uint32_t)b * 32u * T::PITCH + (T::key_at(n, h) ^ (uint32_t)j * 16u));
-                s[b] = mma32<X>(a, qf[j], s[b]);
-            }
-        pipeline<KS * TB, 1, 6>();
+        for (int i = 0; i < KS * TB; i++) s[i % TB] = mma32<X>(i < READY ? ready[i] : key(i), qf[i / TB], s[i % TB]);
+        pipeline<KS * TB, 1, READY>();
         __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
         // register i of block b: token b * 32 + i / 4 * 8 + h * 4 + i % 4
@@ -498,6 +500,25 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
             }
             if constexpr (!TURNS) __syncthreads();
         }
+        // 16 lanes bring 4 tokens of 16 dimensions, and have 4 tokens of a dimension each
+        auto value = [&](int i) {
+            const int k = i / NB, b = i % NB;
+            const uint32_t token = h * 4u + (lane & 15u) / 4u, d = (lane & 16u) + (lane & 3u) * 4u;
+            const uint32_t at = (T::value_at(token, d / 8u) + (d & 4u)) ^ (uint32_t)b * 32u;
+            w32x4 a;
+#pragma unroll
+            for (uint32_t half = 0; half < 2; half++) {
+                const uint16_t *from = values + ((uint32_t)k * 16u + half * 8u) * T::PITCH + at;
+                const w32x2 x = __builtin_bit_cast(w32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)from));
+                a[half * 2u] = x[0];
+                a[half * 2u + 1u] = x[1];
+            }
+            return a;
+        };
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < READY; i++) ready[i] = value(i);
+        __builtin_amdgcn_sched_barrier(0);
         float top = -__builtin_inff();
 #pragma unroll
         for (int b = 0; b < TB; b++)
@@ -523,28 +544,12 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
                 own += s[b][i];
                 if (i & 1) w[b * 2 + i / 8][i % 8 / 2] = X::pack(s[b][i - 1], s[b][i]);
             }
-        // 16 lanes bring 4 tokens of 16 dimensions, and have 4 tokens of a dimension each
-        auto value = [&](int k, int b) {
-            const uint32_t token = h * 4u + (lane & 15u) / 4u, d = (lane & 16u) + (lane & 3u) * 4u;
-            const uint32_t at = (T::value_at(token, d / 8u) + (d & 4u)) ^ (uint32_t)b * 32u;
-            w32x4 a;
-#pragma unroll
-            for (uint32_t half = 0; half < 2; half++) {
-                const uint16_t *from = values + ((uint32_t)k * 16u + half * 8u) * T::PITCH + at;
-                const w32x2 x = __builtin_bit_cast(w32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)from));
-                a[half * 2u] = x[0];
-                a[half * 2u + 1u] = x[1];
-            }
-            return a;
-        };
         asm volatile("" : "+v"(own));  // (added up here, not behind the products, where all of the weights would have to be kept)
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int k = 0; k < 2 * TB; k++)
-#pragma unroll
-            for (int b = 0; b < NB; b++) acc[b] = mma32<X>(value(k, b), w[k], acc[b]);
-        pipeline<2 * TB * NB, 2, 6>();
+        for (int i = 0; i < 2 * TB * NB; i++) acc[i % NB] = mma32<X>(i < READY ? ready[i] : value(i), w[i / NB], acc[i % NB]);
+        pipeline<2 * TB * NB, 2, READY>();
         __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
         if (t + STEP < end) store(other);
