@@ -19,7 +19,7 @@ void launch_rows(dim3 g, hipStream_t s, const dkv::RowsParams &p)
         hipLaunchKernelGGL((dkv::kv_rows_kernel<X, KIND, DP, ROWS>), g, dim3(64 * T::WAVES), 0, s, p);
         const uint64_t joins = (uint64_t)p.n_tiles * p.n_kv_heads * (ROWS / 32) * (DP / 32);
         if (p.splits > 1u || p.groups)
-            hipLaunchKernelGGL((dkv::kv_rows_join_kernel<X, KIND == dkv::kBits16>), dim3((uint32_t)((joins + 3) / 4)), dim3(256), 0, s, p,
+            hipLaunchKernelGGL((dkv::kv_rows_join_kernel<X, KIND == dkv::kBits16>), dim3((uint32_t)joins), dim3(256), 0, s, p,
                                (uint32_t)DP / 32u, (uint32_t)T::TOKENS);
     };
     auto go = [&](auto dims) {
@@ -108,9 +108,12 @@ extern "C" int kv_attend_rows(kv_decoder *d, const kv_attend_rows_args *a, void 
     uint64_t wgs = each;
     if (few) {
         // Equal ranges for two workgroups a compute unit (one where their tiles fill its LDS); a workgroup for each tile where no
-        // request can be longer than four steps of its waves.
+        // request can be longer than four steps of its waves.  A range is two steps at least, so that one long request leaves no
+        // more parts than can be joined in a few rounds (us, 3 rows of 4 heads of 96 over 15900 tokens in 4 bits, by one tile / 4 /
+        // 8 / 16: 183 / 18.4 / 16.1 / 17.0).
         const uint32_t at_once = (uint32_t)d->n_cus * (kind < 2 && p.dim > 64u ? 1u : 2u);
-        if (most > 16u && (uint64_t)p.n_tiles * most <= 0x7FFFFFFFu && each * (rows_dims(p.dim) / 32u) / 4u < kMostTiles) {
+        if (most > 16u && (uint64_t)p.n_tiles * most <= 0x7FFFFFFFu && each * (rows_dims(p.dim) / 32u) <= kMostTiles) {
+            p.least = 8u;
             p.groups = (uint32_t)std::min<uint64_t>(std::max(1u, at_once / p.n_kv_heads), (uint64_t)p.n_tiles * most);
             wgs = (uint64_t)p.groups * p.n_kv_heads;
         }

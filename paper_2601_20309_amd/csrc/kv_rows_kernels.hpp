@@ -35,7 +35,7 @@ struct RowsParams {
     uint32_t dim, token_bytes, head_bytes, block_size, cells_per_block, n_blocks;
     uint32_t exponents;  // 4 bits: from a token's first byte to its exponents
     uint32_t group_heads, causal;
-    // Parts of the tokens: splits of a tile of rows, `least` tiles of tokens and more each, slots [tile][split][KV head]; or, of
+    // Parts of the tokens, `least` tiles of tokens and more each: splits of a tile of rows, slots [tile][split][KV head]; or, of
     // tiles of 32 rows, `groups` ranges of all (0: none), slots [range][its last request, or one that begins in it][KV head]
     uint32_t splits, least, groups;
     uint32_t n_tiles, row_bits;                   // tiles of rows of a KV head, empty ones among them; log2 of the rows of one
@@ -158,7 +158,7 @@ struct RowDeal {
             if (asked >= base && asked - base < 64u) before = total + (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), (int)(asked - base));
             total += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
         }
-        per = max((total + p.groups - 1u) / p.groups, 1u);
+        per = max((total + p.groups - 1u) / p.groups, p.least);
     }
     // The request that tile `at` is of, and how many of its tiles come before.
     __device__ __forceinline__ bool find(const RowsParams &p, const Requests &requests, uint32_t lane, uint32_t at, uint32_t &s, uint32_t &t) const
@@ -286,7 +286,7 @@ __device__ __forceinline__ void pipeline()
 }
 
 template <typename X, int KIND, int DP, int ROWS>
-__global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)) void kv_rows_kernel(const RowsParams p)
+__global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), 2) void kv_rows_kernel(const RowsParams p)
 {
     using T = RowStep<DP, ROWS>;
     using P = Piece<X, KIND>;
@@ -666,15 +666,16 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (DP > 128 ? 1 : 2)
     }
 }
 
-// Joins the parts of a tile: a wave has 32 rows and 32 dimensions of them.
+// Joins the parts of a tile: a workgroup has 32 rows and 32 dimensions of them, its waves every fourth part each, four at a time.
 template <typename X, bool BITS16>
 __global__ __launch_bounds__(256) void kv_rows_join_kernel(const RowsParams p, uint32_t blocks, uint32_t tokens)
 {
-    const uint32_t lane = threadIdx.x & 63u, n = lane & 31u, h = lane >> 5;
-    const uint32_t of_tile = blocks << (p.row_bits - 5u);  // waves of a tile
-    const uint32_t at = blockIdx.x * 4u + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rest = at / of_tile, in = at - rest * of_tile;
+    __shared__ f32x4 sums[4][4][64];
+    __shared__ float2 refs[4][64];
+    const uint32_t lane = threadIdx.x & 63u, n = lane & 31u, h = lane >> 5, quarter = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t of_tile = blocks << (p.row_bits - 5u);  // workgroups of a tile
+    const uint32_t rest = blockIdx.x / of_tile, in = blockIdx.x - rest * of_tile;
     const uint32_t b = in % blocks, wave = in / blocks, kv_head = rest % p.n_kv_heads, tile = rest / p.n_kv_heads;
-    if (tile >= p.n_tiles) return;
     const Requests requests(p, lane);
     const RowTile rt = row_tile(p, requests, lane, tile);
     if (!rt.here) return;
@@ -699,28 +700,36 @@ __global__ __launch_bounds__(256) void kv_rows_join_kernel(const RowsParams p, u
 #pragma unroll
     for (int i = 0; i < 4; i++) all[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     constexpr uint32_t AT_ONCE = 4;
-    for (uint32_t first = 0; first < parts; first += AT_ONCE) {
+    auto add = [&](const float2 &ml, const f32x4 (&part)[4]) {
+        const float next = fmaxf(ref, ml.x), f = __builtin_amdgcn_exp2f(ref - next), g = __builtin_amdgcn_exp2f(ml.x - next);
+        ref = next;
+        own = own * f + ml.y * g;
+#pragma unroll
+        for (int i = 0; i < 4; i++) all[i] = all[i] * f + part[i] * g;
+    };
+    for (uint32_t first = quarter; first < parts; first += 4u * AT_ONCE) {
         float2 ml[AT_ONCE];
         f32x4 part[AT_ONCE][4];
 #pragma unroll
         for (uint32_t o = 0; o < AT_ONCE; o++) {
-            const uint32_t i = min(first + o, parts - 1u);
+            const uint32_t i = min(first + 4u * o, parts - 1u);
             const uint64_t slot = (p.groups ? (uint64_t)(g0 + i) * 2u + (i ? 0u : 1u) : (uint64_t)tile * p.splits + i) * p.n_kv_heads + kv_head;
             ml[o] = p.part_ml[(slot << p.row_bits) + wave * 32u + n];
 #pragma unroll
-            for (int i = 0; i < 4; i++) part[o][i] = p.part[(((slot << (p.row_bits - 5u)) + wave) * (blocks * 4u) + b * 4u + i) * 64u + lane];
-            if (first + o >= parts) ml[o] = float2{kLowest, 0.f};
+            for (int j = 0; j < 4; j++) part[o][j] = p.part[(((slot << (p.row_bits - 5u)) + wave) * (blocks * 4u) + b * 4u + j) * 64u + lane];
         }
 #pragma unroll
-        for (uint32_t o = 0; o < AT_ONCE; o++) {
-            const float next = fmaxf(ref, ml[o].x), f = __builtin_amdgcn_exp2f(ref - next);
-            const float g = first + o < parts ? __builtin_amdgcn_exp2f(ml[o].x - next) : 0.f;
-            ref = next;
-            own = own * f + ml[o].y * g;
+        for (uint32_t o = 0; o < AT_ONCE; o++)
+            if (first + 4u * o < parts) add(ml[o], part[o]);
+    }
+    refs[quarter][lane] = float2{ref, own};
 #pragma unroll
-            for (int i = 0; i < 4; i++)
-                if (first + o < parts) all[i] = all[i] * f + part[o][i] * g;
-        }
+    for (int i = 0; i < 4; i++) sums[quarter][i][lane] = all[i];
+    __syncthreads();
+    if (quarter) return;
+    for (uint32_t o = 1; o < min(parts, 4u); o++) {
+        const f32x4 part[4] = {sums[o][0][lane], sums[o][1][lane], sums[o][2][lane], sums[o][3][lane]};
+        add(refs[o][lane], part);
     }
     if (!has_row) return;
     const float inv = own == 0.f ? 0.f : 1.0f / own;
