@@ -98,7 +98,8 @@ extern "C" int kv_attend_rows(kv_decoder *d, const kv_attend_rows_args *a, void 
     // over 8, 1124 / 990; 24 requests of 180 rows of 12 heads of 64 43.9 / 50.4.
     const uint64_t mean = (uint64_t)p.n_rows * p.group_heads / p.n_seqs;
     const bool few = mean <= 48u && row_tiles(p.n_rows, p.group_heads, p.n_seqs, 5) * p.n_kv_heads <= kMostTiles;
-    const bool many = mean >= 1024u && p.dim <= (uint32_t)kManyRowsDims && row_tiles(p.n_rows, p.group_heads, 0, 8) * p.n_kv_heads >= (uint64_t)d->n_cus;
+    const bool many = mean >= 1024u && p.dim <= (uint32_t)kManyRowsDims && row_tiles(p.n_rows, p.group_heads, 0, 8) * p.n_kv_heads >= (uint64_t)d->n_cus &&
+                      row_tiles(p.n_rows, p.group_heads, p.n_seqs, 8) * p.n_kv_heads <= kMostTiles / 2;
     p.row_bits = few ? 5u : many ? 8u : 7u;
     p.n_tiles = (uint32_t)row_tiles(p.n_rows, p.group_heads, p.n_seqs, (int)p.row_bits);
     const uint64_t each = (uint64_t)p.n_tiles * p.n_kv_heads;

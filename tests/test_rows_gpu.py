@@ -219,6 +219,18 @@ def test_odd_values_of_later_tokens(bad, dim, x):
     assert torch.isfinite(out[:20]).all()
 
 
+def test_rows_that_see_nothing_behind_odd_values():
+    """What one call notes of infinities is nothing to the next one's tiles without a token."""
+    c = Case((300, 40), (300, 40), 4, 2, 64, seed=22)
+    q = c.queries()
+    c.plane(1)[:] = float("inf")
+    for _ in range(3):
+        out, _ = c.check(q, lse=False)
+        assert torch.isinf(out).all()
+        none, lse = c.check(q, lens=torch.tensor([0, 0], dtype=torch.int32))
+        assert (none == 0).all() and torch.isinf(lse).all()
+
+
 @pytest.mark.parametrize("x", ["bf16", "fp16"])
 def test_the_mean_of_the_largest_values_is_no_infinity(x):
     c = Case((3, 130), (400, 130), 1, 2, 64, types=(x, x), seed=13)
