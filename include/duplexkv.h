@@ -462,9 +462,11 @@ int kv_sched_lvf(const kv_sched_params *params, const kv_sched_req *reqs, int32_
 /* ------------------------------------------------------------------------
  * The operators of a decode step over the paged cache: what writes it, what
  * reads it and what says which of its blocks are worth keeping.
- *   kv_put     new tokens: q and k get their rotary positions, k and v go into
- *              their pages, rounded to the cache's type
+ *   kv_put     new tokens: q and k are normed head by head, if wanted, and get their rotary
+ *              positions, k and v go into their pages, rounded to the cache's type
  *   kv_attend  attention of one new token per request over the pages it holds
+ *   kv_attend_rows  attention of several rows of every request: prompts, drafted tokens,
+ *              a decoder's rows over an encoder's states
  *   kv_evict   the blocks that attention has weighed least leave a request
  * A decoder is the handle they are called through: a cache (kv_config gives its
  * shape and layout; host pool, path and launch fields are not looked at), the
@@ -486,7 +488,7 @@ int kv_sched_lvf(const kv_sched_params *params, const kv_sched_req *reqs, int32_
  *
  * Calls through one decoder have to be ordered one after the other (the same
  * stream, or streams the caller orders), replays of recorded ones included:
- * kv_attend's calls share the decoder's memory.  Steps that overlap in time
+ * kv_attend's calls, and kv_attend_rows', share the decoder's memory.  Steps that overlap in time
  * take a decoder each; any number may exist over one cache.  The caller orders
  * them against transfers, too: a block that a swap-in fills is read after
  * kv_wait() or kv_stream_wait_layer().  What a call writes shares no memory with anything else
@@ -518,11 +520,13 @@ typedef struct {
 /*
  * hbm_cache: device pointer, kv_cache_bytes(cfg) bytes, owned by the caller; it
  * must outlive the decoder.  KV_EINVAL: bad configuration, types that do not fit
- * elem_bytes, scales that are not finite and above 0.  KV_EUNSUP: head_dim above
+ * elem_bytes, KV_FP4 with a head_dim that is no multiple of 17, scales that are not finite and above 0.  KV_EUNSUP: head_dim above
  * 256 or no multiple of 8, more than 1024 query heads, a cache that is not
  * aligned to 16 bytes or of 2^32 and more token rows per KV plane, more than 65535
  * requests, 2^31 and more tokens in a table row, tiles of 32 tokens in all or, with
- * `weigh`, tokens of a block times query heads, and more than 2^28 blocks.  KV_ENOMEM, KV_EHIP.
+ * `weigh`, tokens of a block times query heads, and more than 2^28 blocks; max_rows times query heads of a KV head
+ * above 2^31 - 256, or in tiles of 128 with max_seqs more, times KV heads, 2^24 and more.  (Dimensions of KV_FP4: those that its
+ * numbers have.)  KV_ENOMEM, KV_EHIP.
  */
 int kv_decoder_create(kv_decoder **decoder, const kv_config *cfg, const kv_decoder_config *dc, void *hbm_cache);
 
@@ -571,8 +575,12 @@ typedef struct {
  * New tokens go into the cache, layer by layer.  With a = position[axis of pair i] *
  * inv_freq[i] (its cosine and its sine are off by at most 2^-22 up to angles of 2^24, 2^-20 at
  * positions of 2^31) a pair (x, y) of q and k becomes (x cos a - y sin a, y cos a + x sin a),
- * in 32 bits, rounded once.  An 8-bit cache holds the nearest of value / scale, at most
- * 448 either way; NaN stays NaN.  Tokens whose block is no page, or that lie beyond
+ * in 32 bits, rounded once.  Norms are taken in 32 bits before that (where the sum of a head's
+ * squares is too large for a float, what is left of it is 0).  An 8-bit cache holds the nearest of value / scale, at most
+ * 448 either way; NaN stays NaN.  A 4-bit cache has for each 32 dimensions the power of 2 that brings the largest to 4 and more, under 8,
+ * from 2^-126 to 2^125 (x_type fp16: from 2^-23 to 2^13, so that numbers times powers are fp16 numbers; who writes
+ * such a cache otherwise stays within these), and the nearest numbers, of two as near the one at an even place, 6 for what is above; infinity or
+ * NaN among the 32 makes them all NaN.  Tokens whose block is no page, or that lie beyond
  * max_blocks, are left out of the cache (their q is rotated all the same).  Two tokens
  * that name one row of one page leave either's values there.
  * KV_EINVAL: NULL or negative, a layer, axis or section that does not fit.  KV_E2BIG:
@@ -605,14 +613,14 @@ typedef struct {
     const int32_t *lens;   /* tokens of each request; causal: the rows' own included */
     const int32_t *starts; /* n_seqs + 1: request s has rows starts[s] .. starts[s + 1] - 1; they must not fall.  NULL: one row
                               each (n_rows == n_seqs) */
-    kv_rows q, out;
+    kv_rows q, out;        /* out is written */
     float *lse;            /* NULL, or [n_rows][n_heads] */
 } kv_attend_rows_args;
 
 /*
  * out = softmax(scale * q K^T) V of each request and query head over the request's
  * tokens in present pages; 0 where there are none.  Products and sums in 32 bits; what a
- * weight is as it meets V is off by at most 2^-15 of it (x_type bf16; 2^-11 with a KV_FP8 cache) or
+ * weight is as it meets V is off by at most 2^-15 of it (x_type bf16, with a KV_FP4 cache too; 2^-11 with a KV_FP8 cache) or
  * 2^-21 (fp16), and 2^-35 of the largest.  A value of infinity whose weight is above 2^-90 of the largest
  * gives infinity.  mass_out[s][j] = mass[s][j] + the
  * weights that the tokens of block j got, summed over the query heads (n_heads in all,
@@ -629,7 +637,7 @@ int kv_attend(kv_decoder *decoder, const kv_attend_args *args, void *stream);
  * in present pages; 0 where there are none, and -inf in lse.  Products, references and sums in 32 bits; what a
  * weight is as it meets V is the nearest x_type number.  What lies in rows that nothing sees, infinities and NaN among it, makes no
  * difference; an infinite value makes what sees it infinite or, where its weight is too small for
- * x_type, NaN.  The result is the same, bit for bit, whenever the same call runs with the same starts and lens.
+ * x_type, NaN.  (Row i of a request's m is at place lens - m + i, whatever max_blocks is: places below 0 see nothing.)  The result is the same, bit for bit, whenever the same call runs with the same starts and lens.
  * out may be q itself.  KV_EINVAL, KV_EUNSUP as for kv_attend; KV_E2BIG: more requests or rows than the decoder's.
  */
 int kv_attend_rows(kv_decoder *decoder, const kv_attend_rows_args *args, void *stream);
