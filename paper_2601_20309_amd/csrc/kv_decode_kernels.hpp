@@ -314,7 +314,10 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
     // In 8 bits there is room for two tiles of values: they are asked for a tile ahead, like the keys.  us without / with:
     // 128 requests around 600 tokens, 8 heads of 128, 39.4 / 37.4; 4 of 32768 tokens, 8 heads of 128 48.4 / 50.4, of 192
     // 102 / 85, 4 heads of 256 51.4 / 55.2; in 16 bits, 32 requests around 1000, 8 heads of 128, 35.6 / 39.7.
-    // In 4 bits a step has so few bytes that all of the next one's are asked for before this one's products.
+    // In 4 bits a step has so few bytes that all of the next one's are asked for before this one's products.  What bounds it then are
+    // vector instructions: some 300 for 32 tokens of 128 dimensions, 64 of them conversions, 36 for pairs of tokens.  us, both launches: 4
+    // requests of 32768 tokens, 8 heads of 128 (143 MB) 53.3, with places multiplied before the shuffles 51.3 (2.8 TB/s), with all pages in
+    // the caches 39.3; 128 around 600 (95 MB) 51.
     constexpr bool EARLY = FP4;
     constexpr bool AHEAD = FP4 || (FP8 && !(WHOLE && DP == 256));
     auto k_dim = [](int j, uint32_t kq) { return FP4 ? (uint32_t)(j / 4) * 128u + kq * K4 + (uint32_t)(j & 3) * 8u : FP8 ? (uint32_t)(j / 2) * 64u + kq * 16u + (uint32_t)(j & 1) * 8u : (uint32_t)j * 32u + kq * 8u; };
@@ -1216,6 +1219,9 @@ __device__ __forceinline__ float lanes_of(float x)
 // and a head lies in 1 to 32 lanes of a wave (a power of 2): the sum of its squares is a sum over lanes, so is
 // the largest of 32 dimensions over four, and the other numbers of pairs come from the lanes that have them.
 //   y = x / sqrt(mean x^2 + eps) * weight, then the rotation, all in 32 bits, rounded once.
+// Bound by vector instructions and by how many rows are under way: 6853 rows of 32 + 8 + 8 heads of 128 into 4 bits (148 MB), us: with sums by
+// shuffles through LDS 53.5, over lanes 51, without a choice for each dimension 45, with the row's request in one round of loads 43, of 128 threads
+// 39 (3.8 TB/s); 64 rows into 16 bits 4.6.
 // 4 bits: the power of 2 is the one that brings the largest of 32 dimensions to 4 and more, under 8, and numbers are the nearest
 // of those there are (6 the largest); infinity or NaN among them makes all 32 NaN.
 // WHOLE: the lanes of a head all of whose dimensions turn, halves apart, and are so many times 8; 0: any others.

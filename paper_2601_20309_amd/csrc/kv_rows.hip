@@ -18,9 +18,13 @@ void launch_rows(dim3 g, hipStream_t s, const dkv::RowsParams &p)
         using T = dkv::RowStep<DP, ROWS>;
         hipLaunchKernelGGL((dkv::kv_rows_kernel<X, KIND, DP, ROWS>), g, dim3(64 * T::WAVES), 0, s, p);
         const uint64_t joins = (uint64_t)p.n_tiles * p.n_kv_heads * (ROWS / 32) * (DP / 32);
-        if (p.splits > 1u || p.groups)
-            hipLaunchKernelGGL((dkv::kv_rows_join_kernel<X, KIND == dkv::kBits16>), dim3((uint32_t)joins), dim3(256), 0, s, p,
+        const auto join = [&](auto wide) {
+            constexpr bool WIDE = decltype(wide)::value;
+            hipLaunchKernelGGL((dkv::kv_rows_join_kernel<X, KIND == dkv::kBits16, WIDE>), dim3((uint32_t)(WIDE ? joins : (joins + 3) / 4)), dim3(256), 0, s, p,
                                (uint32_t)DP / 32u, (uint32_t)T::TOKENS);
+        };
+        if (p.groups || p.splits > 8u) join(std::true_type{});
+        else if (p.splits > 1u) join(std::false_type{});
     };
     auto go = [&](auto dims) {
         if (p.row_bits == 5u) return launch(dims, std::integral_constant<int, 32>{});

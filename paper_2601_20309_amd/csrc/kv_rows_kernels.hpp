@@ -677,16 +677,21 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), 2) void kv_rows_ke
     }
 }
 
-// Joins the parts of a tile: a workgroup has 32 rows and 32 dimensions of them, its waves every fourth part each, four at a time.
-template <typename X, bool BITS16>
+// Joins the parts of a tile: a wave has 32 rows and 32 dimensions of them, and four parts at a time.  WIDE: so has a workgroup, and its
+// waves every fourth part each.  (us, wide / not: 9 requests of 150 rows in four splits 7.8 / 6.0; 16 requests of up to 8005 tokens, 5 rows
+// of 40 heads over 8, in 64 ranges a KV head 5.6 / 7.2.)
+template <typename X, bool BITS16, bool WIDE>
 __global__ __launch_bounds__(256) void kv_rows_join_kernel(const RowsParams p, uint32_t blocks, uint32_t tokens)
 {
-    __shared__ f32x4 sums[4][4][64];
-    __shared__ float2 refs[4][64];
-    const uint32_t lane = threadIdx.x & 63u, n = lane & 31u, h = lane >> 5, quarter = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t of_tile = blocks << (p.row_bits - 5u);  // workgroups of a tile
-    const uint32_t rest = blockIdx.x / of_tile, in = blockIdx.x - rest * of_tile;
+    constexpr uint32_t WAVES = WIDE ? 4 : 1;
+    __shared__ f32x4 sums[WAVES][4][64];
+    __shared__ float2 refs[WAVES][64];
+    const uint32_t lane = threadIdx.x & 63u, n = lane & 31u, h = lane >> 5, own_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t quarter = WIDE ? own_wave : 0u, item = WIDE ? blockIdx.x : blockIdx.x * 4u + own_wave;
+    const uint32_t of_tile = blocks << (p.row_bits - 5u);  // items of a tile
+    const uint32_t rest = item / of_tile, in = item - rest * of_tile;
     const uint32_t b = in % blocks, wave = in / blocks, kv_head = rest % p.n_kv_heads, tile = rest / p.n_kv_heads;
+    if (tile >= p.n_tiles) return;
     const Requests requests(p, lane);
     const RowTile rt = row_tile(p, requests, lane, tile);
     if (!rt.here) return;
@@ -718,12 +723,12 @@ __global__ __launch_bounds__(256) void kv_rows_join_kernel(const RowsParams p, u
 #pragma unroll
         for (int i = 0; i < 4; i++) all[i] = all[i] * f + part[i] * g;
     };
-    for (uint32_t first = quarter; first < parts; first += 4u * AT_ONCE) {
+    for (uint32_t first = quarter; first < parts; first += WAVES * AT_ONCE) {
         float2 ml[AT_ONCE];
         f32x4 part[AT_ONCE][4];
 #pragma unroll
         for (uint32_t o = 0; o < AT_ONCE; o++) {
-            const uint32_t i = min(first + 4u * o, parts - 1u);
+            const uint32_t i = min(first + WAVES * o, parts - 1u);
             const uint64_t slot = (p.groups ? (uint64_t)(g0 + i) * 2u + (i ? 0u : 1u) : (uint64_t)tile * p.splits + i) * p.n_kv_heads + kv_head;
             ml[o] = p.part_ml[(slot << p.row_bits) + wave * 32u + n];
 #pragma unroll
@@ -731,16 +736,18 @@ __global__ __launch_bounds__(256) void kv_rows_join_kernel(const RowsParams p, u
         }
 #pragma unroll
         for (uint32_t o = 0; o < AT_ONCE; o++)
-            if (first + 4u * o < parts) add(ml[o], part[o]);
+            if (first + WAVES * o < parts) add(ml[o], part[o]);
     }
-    refs[quarter][lane] = float2{ref, own};
+    if constexpr (WIDE) {
+        refs[quarter][lane] = float2{ref, own};
 #pragma unroll
-    for (int i = 0; i < 4; i++) sums[quarter][i][lane] = all[i];
-    __syncthreads();
-    if (quarter) return;
-    for (uint32_t o = 1; o < min(parts, 4u); o++) {
-        const f32x4 part[4] = {sums[o][0][lane], sums[o][1][lane], sums[o][2][lane], sums[o][3][lane]};
-        add(refs[o][lane], part);
+        for (int i = 0; i < 4; i++) sums[quarter][i][lane] = all[i];
+        __syncthreads();
+        if (quarter) return;
+        for (uint32_t o = 1; o < min(parts, 4u); o++) {
+            const f32x4 part[4] = {sums[o][0][lane], sums[o][1][lane], sums[o][2][lane], sums[o][3][lane]};
+            add(refs[o][lane], part);
+        }
     }
     if (!has_row) return;
     const float inv = own == 0.f ? 0.f : 1.0f / own;
