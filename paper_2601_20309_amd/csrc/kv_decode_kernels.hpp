@@ -187,7 +187,6 @@ struct AttendParams {
     int64_t table_stride;
     uint32_t n_seqs, n_heads, max_blocks, max_tokens;
     uint32_t dim, token_bytes, head_bytes;
-    uint32_t exponents;  // 4 bits: from a token's first byte to its heads' bytes
     uint32_t block_size, cells_per_block, n_blocks;  // a block begins cells_per_block rows of token_bytes behind the one before it
     Divide by_block;
     uint32_t groups, wgs_per_group, units, units_per_wg, subs, group_heads, head_tiles;
@@ -199,6 +198,7 @@ struct AttendParams {
     uint32_t by_request;       // a range is a request: nothing to join
     float qk_scale;            // to base 2
     float v_scale;
+    uint32_t exponents;        // 4 bits: from a token's first byte to its heads' bytes
 };
 
 constexpr uint32_t kTile = 32;
@@ -514,52 +514,8 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
             uint32_t vx[8][NV];
             uint32_t present = 0;  // bit r: token r of the lane's 8 is there
             f32x4 sc[2];
-            if (have) {
-                if constexpr (AHEAD) {
-                    present = next_present;
-#pragma unroll
-                    for (int r = 0; r < 8; r++) {
-#pragma unroll
-                        for (int c = 0; c < NV; c++) {
-                            vr[r][c] = next_vr[r][c];
-                            if constexpr (FP4) vx[r][c] = next_vx[r][c];
-                        }
-                    }
-                } else {
-                    find_values(present);
-#pragma unroll
-                    for (int c = 0; c < NV; c++) load_values(vr, vx, c);
-                }
-            }
-            // the step after this one (`next`: the first of the next request)
-            const uint32_t tile = last ? next_first : tt + p.subs;
-            const bool more = tile < (last ? next_stop : stop);
-            auto read_queries = [&](uint32_t request) {
-#pragma unroll
-                for (int j = 0; j < KJ; j++) {
-                    const uint32_t d = k_dim(j, kq);
-                    qf[j] = w32x4{0u, 0u, 0u, 0u};
-                    if (has_row && (WHOLE || d < p.dim))
-                        qf[j] = *reinterpret_cast<const w32x4 *>(p.q + (uint64_t)request * p.q_row + (uint64_t)head * p.q_head + d * 2u);
-                }
-            };
-            if constexpr (EARLY) {
-                if (more) {
-                    Part part = now;
-                    if (last) part = next;
-#pragma unroll
-                    for (int h = 0; h < 2; h++) cell[h] = cell_of(tile, h, last ? next_page[h] : page[h]);
-#pragma unroll
-                    for (int h = 0; h < 2; h++) load_keys(next_kr[h], next_kx[h], cell[h]);
-                    find_values(next_present);
-#pragma unroll
-                    for (int c = 0; c < NV; c++) load_values(next_vr, next_vx, c);
-#pragma unroll
-                    for (int h = 0; h < 2; h++) page[h] = page_of(part, tile + p.subs, h);
-                }
-            }
-            if (have) {
-                // scores: token x head
+            // scores: token x head
+            auto take_scores = [&] {
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
                     w32x4(&key)[KL] = kr[h];
@@ -594,6 +550,52 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
                         sc[h] = X::mma(a, qf[j], sc[h]);
                     }
                 }
+            };
+            if (have) {
+                if constexpr (AHEAD) {
+                    present = next_present;
+#pragma unroll
+                    for (int r = 0; r < 8; r++) {
+#pragma unroll
+                        for (int c = 0; c < NV; c++) {
+                            vr[r][c] = next_vr[r][c];
+                            if constexpr (FP4) vx[r][c] = next_vx[r][c];
+                        }
+                    }
+                } else {
+                    find_values(present);
+#pragma unroll
+                    for (int c = 0; c < NV; c++) load_values(vr, vx, c);
+                }
+                if constexpr (!EARLY) take_scores();
+            }
+            // the step after this one (`next`: the first of the next request)
+            const uint32_t tile = last ? next_first : tt + p.subs;
+            const bool more = tile < (last ? next_stop : stop);
+            auto read_queries = [&](uint32_t request) {
+#pragma unroll
+                for (int j = 0; j < KJ; j++) {
+                    const uint32_t d = k_dim(j, kq);
+                    qf[j] = w32x4{0u, 0u, 0u, 0u};
+                    if (has_row && (WHOLE || d < p.dim))
+                        qf[j] = *reinterpret_cast<const w32x4 *>(p.q + (uint64_t)request * p.q_row + (uint64_t)head * p.q_head + d * 2u);
+                }
+            };
+            if constexpr (EARLY) {
+                if (more) {
+                    Part part = now;
+                    if (last) part = next;
+#pragma unroll
+                    for (int h = 0; h < 2; h++) cell[h] = cell_of(tile, h, last ? next_page[h] : page[h]);
+#pragma unroll
+                    for (int h = 0; h < 2; h++) load_keys(next_kr[h], next_kx[h], cell[h]);
+                    find_values(next_present);
+#pragma unroll
+                    for (int c = 0; c < NV; c++) load_values(next_vr, next_vx, c);
+#pragma unroll
+                    for (int h = 0; h < 2; h++) page[h] = page_of(part, tile + p.subs, h);
+                }
+                if (have) take_scores();
             }
             // the next step's keys, while this one's values arrive
             if constexpr (EARLY) {
@@ -1064,11 +1066,12 @@ struct PutParams {
     uint32_t n_seqs, n_rows, n_heads, n_kv_heads, max_blocks;
     uint32_t dim, token_bytes, head_bytes, block_size, cells_per_block, n_blocks;
     uint32_t rot, interleaved, section0, section01;  // pairs of the first axis, of the first two
-    uint32_t exponents;  // 4 bits: from a token's first byte to its heads' bytes
-    const float *q_norm, *k_norm;
-    float eps, inv_dim;
     Divide by_steps, by_vecs;  // by a rotated head's steps, and by a head's vectors
     Scale k_scale, v_scale;
+    // normed heads, 4 bits
+    const float *q_norm, *k_norm;
+    float eps, inv_dim;
+    uint32_t exponents;  // from a token's first byte to its heads' bytes
 };
 
 // The nearest e4m3 values of four numbers up to 448.  (The conversion has no bounds of its own: beyond, it gives NaN.)
