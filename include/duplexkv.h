@@ -576,7 +576,7 @@ typedef struct {
  * inv_freq[i] (its cosine and its sine are off by at most 2^-22 up to angles of 2^24, 2^-20 at
  * positions of 2^31) a pair (x, y) of q and k becomes (x cos a - y sin a, y cos a + x sin a),
  * in 32 bits, rounded once.  Norms are taken in 32 bits before that (where the sum of a head's
- * squares is too large for a float, what is left of it is 0).  An 8-bit cache holds the nearest of value / scale, at most
+ * squares is too large for a float, what is left of it is 0; none is too small).  An 8-bit cache holds the nearest of value / scale, at most
  * 448 either way; NaN stays NaN.  A 4-bit cache has for each 32 dimensions the power of 2 that brings the largest to 4 and more, under 8,
  * from 2^-126 to 2^125 (x_type fp16: from 2^-23 to 2^13, so that numbers times powers are fp16 numbers; who writes
  * such a cache otherwise stays within these), and the nearest numbers, of two as near the one at an even place, 6 for what is above; infinity or

@@ -1318,17 +1318,28 @@ __global__ __launch_bounds__(512) void kv_put_heads_kernel(const PutParams p, co
         // (lanes of a head take part together, those behind its dimensions with zeros)
         const float *const weight = i < n_q ? p.q_norm : i < n_k ? p.k_norm : nullptr;
         if (weight) {
-            float sum = 0.f;
+            // Small heads and next to no eps: again, of 2^76 times as much.  (The squares of numbers as small as 2^-64 are no normal
+            // numbers, of which the root's instruction makes infinity.)
+            float mean, eps = p.eps;
+            for (bool again = p.eps < 0x1p-90f;; again = false) {
+                float sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; e++) sum = __builtin_fmaf(x[e], x[e], sum);
-            // over the head's lanes: neighbours, pairs, then each four, eight and sixteen with its mirror image
-            if (lanes > 1u) sum += lanes_of<0xB1>(sum);
-            if (lanes > 2u) sum += lanes_of<0x4E>(sum);
-            if (lanes > 4u) sum += lanes_of<0x141>(sum);
-            if (lanes > 8u) sum += lanes_of<0x140>(sum);
-            if (lanes > 16u) sum += __shfl_xor(sum, 16, 64);
+                for (int e = 0; e < 8; e++) sum = __builtin_fmaf(x[e], x[e], sum);
+                // over the head's lanes: neighbours, pairs, then each four, eight and sixteen with its mirror image
+                if (lanes > 1u) sum += lanes_of<0xB1>(sum);
+                if (lanes > 2u) sum += lanes_of<0x4E>(sum);
+                if (lanes > 4u) sum += lanes_of<0x141>(sum);
+                if (lanes > 8u) sum += lanes_of<0x140>(sum);
+                if (lanes > 16u) sum += __shfl_xor(sum, 16, 64);
+                mean = __builtin_fmaf(sum, p.inv_dim, eps);
+                if (!again || !__any(mean < 0x1p-90f)) break;
+                const float up = mean < 0x1p-90f ? 0x1p76f : 1.0f;
+                eps = eps * up * up;
+#pragma unroll
+                for (int e = 0; e < 8; e++) x[e] *= up;
+            }
             // the root's reciprocal to its last bit, a step behind what the instruction gives
-            const float mean = __builtin_fmaf(sum, p.inv_dim, p.eps), r0 = __builtin_amdgcn_rsqf(mean);
+            const float r0 = __builtin_amdgcn_rsqf(mean);
             const float left = __builtin_fmaf(-mean * r0, r0, 1.0f), r = left > -1.0f && left < 1.0f ? __builtin_fmaf(r0 * 0.5f, left, r0) : r0;
             if (here) {
                 const f32x4 w0 = *reinterpret_cast<const f32x4 *>(weight + d), w1 = *reinterpret_cast<const f32x4 *>(weight + d + 4u);
