@@ -270,12 +270,15 @@ struct Piece<X, kBits4> {
 
 // 16 bytes a lane from global memory into LDS, one lane's behind the other's from `to` on.  In assembly, since beside the
 // builtin the compiler waits for all reads of LDS where some would do, as long as one of these is under way.  Whoever looks at
-// what came waits for it first (loaded_lds), and then for the other waves.  (The compiler keeps nothing in m0: what needs
-// it sets it.)
+// what came waits for it first (loaded_lds), and then for the other waves.  (m0 is a register that the compiler sets where it
+// needs it, and would warn that nobody else's value in it is kept: none is.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_lds(const uint8_t *from, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 __device__ __forceinline__ uint32_t lds_address(const uint16_t *p)
 {
     return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p);
