@@ -96,6 +96,7 @@ extern "C" int kv_attend_rows(kv_decoder *d, const kv_attend_rows_args *a, void 
     p.negative = qk_scale < 0.f ? 1u : 0u;
     p.qk_scale = std::max(std::fabs(qk_scale), 0x1p-126f);  // (0 times the score of what is masked, -inf, is NaN)
     p.v_scale = d->dc.v_scale;
+    p.bias = bf16_bias(p.max_tokens);
     const int kind = (d->dc.x_type == KV_FP16 ? 1 : 0) + (d->dc.kv_type == KV_FP8 ? 2 : d->dc.kv_type == KV_FP4 ? 4 : 0);
     // Few rows to a request: 32 to a tile.  Many, and enough tiles for all compute units: 256, so that half as many bytes
     // go into LDS.  us, 128 rows / 256: 4 prompts of 2048 tokens, 32 heads over 8 of 128, 190 / 178; 1024 tokens at 31000, 64

@@ -53,7 +53,28 @@ struct RowsParams {
     uint32_t negative;  // the scale is: keys meet -q
     float qk_scale;     // to base 2, not negative
     float v_scale;
+    float bias;         // beside bf16: of Weights
 };
+
+// Weights are exp2(score - reference), the largest between 2^bias and 2^(bias + slack).  Beside fp16 they are Fp16's.  Beside
+// bf16 the products of as many as there may be tokens with its largest value add up to less than 2^127: between 2^-16 and 2^-13 in a
+// decoder of 4096 tokens, half of that in one of twice as many.
+struct Weights {
+    float bias, slack;
+};
+constexpr float kBf16Slack = 3.0f;
+inline float bf16_bias(uint32_t max_tokens)
+{
+    int bits = 12;
+    while (bits < 31 && 1u << bits < max_tokens) bits++;
+    return -(float)(bits + 1) - kBf16Slack;
+}
+template <typename X>
+__device__ __forceinline__ Weights weights(const RowsParams &p)
+{
+    if constexpr (std::is_same_v<X, Fp16>) return {X::kBias, X::kSlack};
+    else return {p.bias, kBf16Slack};
+}
 
 // Which rows a tile has.  Request s's tiles are floor(starts[s] * group / rows of one) + s on: as many as it needs, or
 // some more, which are empty.  So no sums over requests are needed to find one.
@@ -430,6 +451,7 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), 2) void kv_rows_ke
     for (int b = 0; b < NB; b++)
 #pragma unroll
         for (int i = 0; i < 16; i++) acc[b][i] = 0.f;
+    const Weights largest = weights<X>(p);
     float ref = kLowest, own = 0.f;
     uint64_t next_present = 0;
     uint32_t page = kNoCell;
@@ -538,9 +560,9 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), 2) void kv_rows_ke
 #pragma unroll
             for (int i = 0; i < 16; i++) top = fmaxf(top, s[b][i]);
         top *= p.qk_scale;
-        if (__any(top > ref + X::kBias + X::kSlack)) {
+        if (__any(top > ref + (largest.bias + largest.slack))) {
             top = fmaxf(top, __shfl_xor(top, 32, 64));
-            const float higher = fmaxf(ref, top - X::kBias), shrink = __builtin_amdgcn_exp2f(ref - higher);
+            const float higher = fmaxf(ref, top - largest.bias), shrink = __builtin_amdgcn_exp2f(ref - higher);
             ref = higher;
             own *= shrink;
 #pragma unroll
