@@ -28,9 +28,10 @@ struct Bf16 {
     typedef __bf16 x8 __attribute__((ext_vector_type(8)));
     typedef __bf16 x2 __attribute__((ext_vector_type(2)));
     // Weights are exp2(score - reference), the largest between 2^kBias and 2^(kBias + kSlack), so that the reference and
-    // all sums change scale only when a score is kSlack above what was met before.  Between 2^-16 and 2^-8 here: sums of the
-    // largest values that bf16 has stay within 32 bits.
+    // all sums change scale only when a score is kSlack above what was met before.  Between 2^-16 and 2^-8 here, and 2^-kShare
+    // of that as they meet the values: the largest that bf16 has, of up to 2^28 tokens, add up to less than 2^128.
     static constexpr float kBias = -16.0f, kSlack = 8.0f;
+    static constexpr int kShare = 20;
     static __device__ __forceinline__ f32x4 mma(w32x4 a, w32x4 b, f32x4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
@@ -59,13 +60,19 @@ struct Bf16 {
     static __device__ __forceinline__ bool nan(uint32_t w) { return (w & 0x7FFFu) > 0x7F80u; }  // the lower of two
     static constexpr float kMost = 0x1.FEp127f;
     // Each of two weights as the sum of two numbers of 8 digits, the upper cut off, the lower the nearest to what that leaves:
-    // within 2^-15.  The lower one gets 2^-20 of the weight on top, so that it is never 0 beside one: 0 times a value
-    // of infinity is NaN.
+    // within 2^-15, times 2^-kShare.  The lower one gets 2^-20 of the weight on top, and the least normal number if that is less, so
+    // that it is never 0 beside one: 0 times a value of infinity is NaN.
     static __device__ __forceinline__ void split(float a, float b, uint32_t &upper, uint32_t &lower)
     {
+        typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+        constexpr u16x2 share = {kShare << 7, kShare << 7}, least = {0x80, 0x80};
+        constexpr float part = 1.0f / (float)(1 << kShare);
         const uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
-        upper = __builtin_amdgcn_perm(y, x, 0x07060302u);
-        lower = pack(__builtin_fmaf(a, 1.0f + 0x1p-20f, -hi(x)), __builtin_fmaf(b, 1.0f + 0x1p-20f, -hi(y)));
+        // (exponents, down to 0; a weight of NaN becomes a number here, but their sum stays NaN)
+        const u16x2 up = __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, __builtin_amdgcn_perm(y, x, 0x07060302u)), share);
+        upper = __builtin_bit_cast(uint32_t, up);
+        const u16x2 low = __builtin_bit_cast(u16x2, pack(__builtin_fmaf(a, part * (1.0f + 0x1p-20f), -lo(upper)), __builtin_fmaf(b, part * (1.0f + 0x1p-20f), -hi(upper))));
+        lower = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(low, __builtin_elementwise_min(up, least)));
     }
 };
 
@@ -75,6 +82,7 @@ struct Fp16 {
     // fp16 has numbers from 2^-24 to 2^15: the largest weights lie between 2^12 and 2^15, so that its
     // smallest number is 2^-36 of them and less.
     static constexpr float kBias = 12.0f, kSlack = 3.0f;
+    static constexpr int kShare = 0;
     static __device__ __forceinline__ f32x4 mma(w32x4 a, w32x4 b, f32x4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
@@ -109,6 +117,31 @@ struct Fp16 {
         const auto cut = __builtin_amdgcn_cvt_pkrtz(fmaxf(a, u), fmaxf(b, v));
         upper = __builtin_bit_cast(uint32_t, cut);
         lower = pack(fmaxf(a - (float)cut[0], u), fmaxf(b - (float)cut[1], v));
+    }
+};
+
+// Weights are exp2(score - reference), the largest between 2^bias and 2^(bias + slack).  Fp16 and Bf16 say what they are in
+// kv_attend.  Beside 4 bits, and in kv_attend_rows, the products of as many as there may be tokens with bf16's largest value add up to less
+// than 2^127: between 2^-16 and 2^-13 in a decoder of 4096 tokens, half of that in one of twice as many.
+struct Weights {
+    float bias, slack;
+};
+constexpr float kBf16Slack = 3.0f;
+inline float bf16_bias(uint32_t max_tokens)
+{
+    int bits = 12;
+    while (bits < 31 && 1u << bits < max_tokens) bits++;
+    return -(float)(bits + 1) - kBf16Slack;
+}
+
+// bf16 beside 4 bits, where there is no infinity: weights meet the values as they are, and Weights says how large they get.
+struct Bf16Of4 : Bf16 {
+    static constexpr int kShare = 0;
+    static __device__ __forceinline__ void split(float a, float b, uint32_t &upper, uint32_t &lower)
+    {
+        const uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
+        upper = __builtin_amdgcn_perm(y, x, 0x07060302u);
+        lower = pack(a - hi(x), b - hi(y));
     }
 };
 
@@ -199,6 +232,7 @@ struct AttendParams {
     float qk_scale;            // to base 2
     float v_scale;
     uint32_t exponents;        // 4 bits: from a token's first byte to its heads' bytes
+    float bias;                // 4 bits beside bf16: of Weights
 };
 
 constexpr uint32_t kTile = 32;
@@ -327,8 +361,9 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
     // 16-bit, 4 heads of 192 78.3 / 83.0, 8 of 96 76.0 / 77.2.
     constexpr bool PAST = WHOLE || (!FP8 && DP > 64);
     // The type of the second product, and whether a weight is two numbers of it.
-    using Y = std::conditional_t<FP8, Fp16, X>;
+    using Y = std::conditional_t<FP8, Fp16, std::conditional_t<FP4 && std::is_same_v<X, Bf16>, Bf16Of4, X>>;
     constexpr bool SPLIT = !FP8 || std::is_same_v<X, Fp16>;
+    const Weights largest = std::is_same_v<Y, Bf16Of4> ? Weights{p.bias, kBf16Slack} : Weights{Y::kBias, Y::kSlack};
     __shared__ f32x4 joined[WAVES][ACC][64];
     __shared__ f32x4 ml[WAVES][16];
     const uint32_t lane = threadIdx.x & 63u, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -637,10 +672,10 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
             }
 #pragma unroll
             for (int r = 0; r < 8; r++) top = fmaxf(top, w[r]);
-            if (__any(top > ref + Y::kBias + Y::kSlack)) {
+            if (__any(top > ref + largest.bias + largest.slack)) {
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const float higher = fmaxf(ref, top - Y::kBias), shrink = __builtin_amdgcn_exp2f(ref - higher);
+                const float higher = fmaxf(ref, top - largest.bias), shrink = __builtin_amdgcn_exp2f(ref - higher);
                 ref = higher;
 #pragma unroll
                 for (int i = 0; i < ACC; i++) acc[i] *= shrink;
@@ -729,7 +764,7 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
         if (now.here) {
             own += __shfl_xor(own, 16, 64);
             own += __shfl_xor(own, 32, 64);
-            if constexpr (SPLIT) sum[0] = own;
+            if constexpr (SPLIT) sum[0] = own * (1.0f / (float)(1 << Y::kShare));  // as they met the values
             const bool whole = now.here == tiles_of(now.tokens);
             const uint32_t slot = group * 2u + (now.first > 0u ? 0u : 1u);
             f32x4 *const part = p.part + ((uint64_t)slot * p.units + unit) * p.part_vecs;

@@ -56,19 +56,6 @@ struct RowsParams {
     float bias;         // beside bf16: of Weights
 };
 
-// Weights are exp2(score - reference), the largest between 2^bias and 2^(bias + slack).  Beside fp16 they are Fp16's.  Beside
-// bf16 the products of as many as there may be tokens with its largest value add up to less than 2^127: between 2^-16 and 2^-13 in a
-// decoder of 4096 tokens, half of that in one of twice as many.
-struct Weights {
-    float bias, slack;
-};
-constexpr float kBf16Slack = 3.0f;
-inline float bf16_bias(uint32_t max_tokens)
-{
-    int bits = 12;
-    while (bits < 31 && 1u << bits < max_tokens) bits++;
-    return -(float)(bits + 1) - kBf16Slack;
-}
 template <typename X>
 __device__ __forceinline__ Weights weights(const RowsParams &p)
 {

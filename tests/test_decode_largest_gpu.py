@@ -58,7 +58,7 @@ def are_means(out, top):
 
 
 @pytest.mark.parametrize("types", ALL, ids="-".join)
-@pytest.mark.parametrize("call", ["rows of 32", "rows of 128", "rows of 256"])
+@pytest.mark.parametrize("call", ["one", "rows of 32", "rows of 128", "rows of 256"])
 @pytest.mark.parametrize("score", [5.1875, 2.0, 40.0])
 def test_scores_rise_behind_the_first_tokens(types, call, score):
     """All requests have the same pages: the first 256 tokens have scores of 0 and the others higher ones (7.5, 2.9 and 58 to base 2).  So many
@@ -82,7 +82,7 @@ def test_scores_rise_behind_the_first_tokens(types, call, score):
 
 
 @pytest.mark.parametrize("types", ALL, ids="-".join)
-@pytest.mark.parametrize("call,new", [("rows", 1), ("rows", 64), ("rows", 300)])
+@pytest.mark.parametrize("call,new", [("one", 1), ("rows", 1), ("rows", 64), ("rows", 300)])
 def test_more_tokens_than_a_small_weight_makes_up_for(types, call, new):
     """300 000 tokens with the same score, of one page that a request has again and again."""
     heads, group, dim, n = 2, 4, 64, 300_000
