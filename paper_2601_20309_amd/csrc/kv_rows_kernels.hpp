@@ -20,8 +20,8 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 // transposed, tokens x rows and dimensions x rows, as in kv_attend: a lane has one row, its reference and its sums, and
 // weights come out as the second product's operand.  Values are read from LDS transposed, four tokens of a dimension at a time.
 //
-// Scores, references and both sums are held in 32 bits.  A weight meets the values as the nearest number of X (here products bound
-// the time, and two numbers for a weight would make it half as many again); out is divided by the sum of the weights as they were,
+// Scores, references and both sums are held in 32 bits.  A weight meets the values as the nearest number of their type: X, fp16 beside 8
+// bits (here products bound the time, and two numbers for a weight would make it half as many again); out is divided by the sum of the weights as they were,
 // so that lse has 32 bits.  Errors against 64 bits, root of the mean square, 1e-4: bf16 19, of the outputs' own rounding 17; fp16 2.2, 2.1.
 //
 // What bounds it: LDS.  Of 64 tokens a wave reads 32 KB for 32 products of 32 x 32 x 16, and a CU's eight waves that much each.  1024
@@ -310,7 +310,9 @@ template <typename X, int KIND, int DP, int ROWS>
 __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), 2) void kv_rows_kernel(const RowsParams p)
 {
     using T = RowStep<DP, ROWS>;
-    using P = Piece<X, KIND>;
+    // The type of the second product: beside 8 bits fp16, which holds the values exactly, and of a weight as much as one number can.
+    using Y = std::conditional_t<KIND == kBits8, Fp16, X>;
+    using P = Piece<X, KIND>;  // of keys
     constexpr int TOKENS = T::TOKENS, NB = T::NB, KS = T::KS, TB = T::TB, WAVES = T::WAVES;
     constexpr bool DIRECT = KIND == kBits16, TURNS = T::TURNS;
     constexpr uint32_t SHARING = TURNS ? 1 : WAVES, STEP = TURNS ? WAVES : 1;  // waves of a tile of tokens; tiles of a turn
@@ -369,7 +371,8 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), 2) void kv_rows_ke
         const uint32_t token = tile * TOKENS + lane % TOKENS;
         return cell_in(page, p.n_blocks, p.cells_per_block, token - p.by_block.quotient(token) * p.block_size);
     };
-    P kp[EACH], vp[EACH];
+    P kp[EACH];
+    Piece<Y, KIND> vp[EACH];
     auto load = [&](auto buf, uint32_t cell) {
         if constexpr (DIRECT) {
             // a wave brings 512 numbers at once, whole tokens, each lane the 8 that belong where its lane's go
@@ -438,7 +441,7 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), 2) void kv_rows_ke
     for (int b = 0; b < NB; b++)
 #pragma unroll
         for (int i = 0; i < 16; i++) acc[b][i] = 0.f;
-    const Weights largest = weights<X>(p);
+    const Weights largest = weights<Y>(p);
     float ref = kLowest, own = 0.f;
     uint64_t next_present = 0;
     uint32_t page = kNoCell;
@@ -503,11 +506,11 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), 2) void kv_rows_ke
                 const uint32_t token = u / (DP / 8u), chunk = u - token * (DP / 8u);
                 w32x4 *const at = reinterpret_cast<w32x4 *>(values + T::value_at(token, chunk));
                 w32x4 v = *at;
-                if (!(X::odd(v[0]) | X::odd(v[1]) | X::odd(v[2]) | X::odd(v[3]))) continue;
+                if (!(Y::odd(v[0]) | Y::odd(v[1]) | Y::odd(v[2]) | Y::odd(v[3]))) continue;
                 for (uint32_t e = 0; e < 8; e++) {
                     const uint32_t word = e / 2 == 0u ? v[0] : e / 2 == 1u ? v[1] : e / 2 == 2u ? v[2] : v[3], x = e & 1u ? word >> 16 : word & 0xFFFFu;
-                    if (!X::odd(x)) continue;
-                    const bool nan = X::nan(x);
+                    if (!Y::odd(x)) continue;
+                    const bool nan = Y::nan(x);
                     reinterpret_cast<uint16_t *>(at)[e] = 0;
                     for (uint32_t r = 0; r < ROWS; r++) {
                         const uint32_t row = p.by_group.quotient(rt.first + r);
@@ -564,13 +567,13 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), 2) void kv_rows_ke
             for (int i = 0; i < 16; i++) {
                 s[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][i], p.qk_scale, -ref));
                 own += s[b][i];
-                if (i & 1) w[b * 2 + i / 8][i % 8 / 2] = X::pack(s[b][i - 1], s[b][i]);
+                if (i & 1) w[b * 2 + i / 8][i % 8 / 2] = Y::pack(s[b][i - 1], s[b][i]);
             }
         asm volatile("" : "+v"(own));  // (added up here, not behind the products, where all of the weights would have to be kept)
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int i = 0; i < 2 * TB * NB; i++) acc[i % NB] = mma32<X>(i < READY ? ready[i] : value(i), w[i / NB], acc[i % NB]);
+        for (int i = 0; i < 2 * TB * NB; i++) acc[i % NB] = mma32<Y>(i < READY ? ready[i] : value(i), w[i / NB], acc[i % NB]);
         pipeline<2 * TB * NB, 2, READY>();
         __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
