@@ -50,3 +50,35 @@ def test_scales_near_the_ends_of_what_a_float_holds(v_scale, new, lens):
     assert c.dec.kv_attend_rows(c.layer, q.cuda(), c.table.cuda(), c.lens.cuda(), out, starts=c.starts.cuda()) == B.KV_OK
     off, most = (out.cpu().double() - ref["out"]).abs(), bound(ref, 64, c.x, 2.0 ** -11)
     assert (off <= most).all(), f"off by {(off / most).max():.2f} of the bound"
+
+
+@pytest.mark.parametrize("x,below", [("bf16", 0), ("bf16", 28), ("bf16", 60), ("fp16", 0), ("fp16", 12), ("fp16", 24)])
+@pytest.mark.parametrize("new,n,heads,group", [(3, 20, 1, 2), (3, 9000, 1, 2), (130, 300, 1, 2), (130, 5000, 1, 2), (1300, 1700, 32, 2)])
+def test_a_value_of_infinity_stays_one(x, below, new, n, heads, group):
+    """Under weights of 2^-86 (bf16) and 2^-34 (fp16) of the largest, and under one that a 16-bit number holds exactly, in a tile that all rows
+    see and in the last one; both signs together are NaN; other dimensions do not see it, and neither do rows before it."""
+    c = Case((new,), (n,), heads, group, 64, types=(x, x), seed=n + below)
+    k, v = c.plane(0), c.plane(1)
+    at = lambda t: (int(c.table[0, t // c.p]), t % c.p)  # noqa: E731
+    k.fill_(0.0)
+    for t in range(0, n, 3):
+        k[at(t)] = -below / 64              # scores of -below beside scores of 0
+    q, table, lens, starts = torch.ones((new, heads * group, 64), dtype=c.x).cuda(), c.table.cuda(), c.lens.cuda(), c.starts.cuda()
+    want, got = torch.empty_like(q), torch.empty_like(q)
+    call = lambda out: c.dec.kv_attend_rows(c.layer, q, table, lens, out, starts=starts, scale=1.0)  # noqa: E731
+    assert call(want) == B.KV_OK and torch.isfinite(want).all()
+    first, last, heavy = (n - new) // 2 // 3 * 3, (n - 2) // 3 * 3, 7
+    v[at(first)][..., 5] = float("inf")
+    v[at(first)][..., 6] = float("-inf")
+    v[at(heavy)][..., 9] = float("-inf")
+    v[at(first)][..., 11] = float("inf")
+    v[at(heavy)][..., 11] = float("-inf")
+    v[at(last)][..., 13] = float("-inf")
+    assert call(got) == B.KV_OK
+    assert torch.isposinf(got[..., 5]).all() and torch.isneginf(got[..., 6]).all() and torch.isneginf(got[..., 9]).all()
+    assert got[..., 11].isnan().all()
+    before = last - (n - new)               # rows that do not see the last one
+    assert torch.isneginf(got[before:, :, 13]).all() and torch.equal(got[:before, :, 13], want[:before, :, 13])
+    rest = torch.ones(64, dtype=torch.bool, device="cuda")
+    rest[[5, 6, 9, 11, 13]] = False
+    assert torch.equal(got[..., rest], want[..., rest])
