@@ -22,8 +22,6 @@ HIPCC_FLAGS = [
     "-Wall", "-Wextra", "-Wno-unused-parameter",
     # keep the compiler from forming packed-fp32 instructions
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-    # (kernels whose LDS leaves room for fewer waves than their registers are bounded for)
-    "-Wno-pass-failed",
     # The tile draws of the move kernel are one atomic per wave whose result is
     # wanted a whole step later.  The compiler's atomic optimizer would rewrite
     # each into "one lane adds for all active lanes, then broadcast", and the

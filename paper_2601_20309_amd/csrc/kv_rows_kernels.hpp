@@ -306,8 +306,23 @@ __device__ __forceinline__ void pipeline()
     __builtin_amdgcn_sched_group_barrier(kMma, AHEAD, 0);
 }
 
+// What a workgroup keeps in LDS, and the waves of a SIMD that leaves room for: no more than two, which have 256 registers each.
+template <int KIND, int DP, int ROWS>
+struct RowLds {
+    using T = RowStep<DP, ROWS>;
+    // Numbers that go through registers are stored when the tile before them has been read: of a wave's own tiles one is enough.
+    static constexpr uint32_t BUFS = T::TURNS && KIND != kBits16 ? 1 : 2;
+    static constexpr uint32_t PLANE = T::TOKENS * T::PITCH, TILE = 2 * PLANE;
+    static constexpr uint32_t NUMBERS = BUFS * TILE * (T::TURNS ? T::WAVES : 1), SUMS = T::TURNS ? T::WAVES * 32 : 1, MARKS = ROWS * T::NB * 2;
+    static constexpr uint32_t BYTES = NUMBERS * 2 + SUMS * 8 + MARKS * 4 + 4;
+    static constexpr int AT_ONCE = (int)(160 * 1024 / BYTES) * T::WAVES / 4;
+    // Above 192 dimensions what passes through registers has one wave to a SIMD, too.  (us, one / two with scratch memory, prompts as at
+    // READY: 8 bits 146 / 172, 4 bits 147 / 148; in 16 bits 131 / 120, without.)
+    static constexpr int WAVES_OF_SIMD = AT_ONCE < 2 || (DP > 192 && KIND != kBits16) ? 1 : 2;
+};
+
 template <typename X, int KIND, int DP, int ROWS>
-__global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), 2) void kv_rows_kernel(const RowsParams p)
+__global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), (RowLds<KIND, DP, ROWS>::WAVES_OF_SIMD)) void kv_rows_kernel(const RowsParams p)
 {
     using T = RowStep<DP, ROWS>;
     // The type of the second product: beside 8 bits fp16, which holds the values exactly, and of a weight as much as one number can.
@@ -318,16 +333,17 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), 2) void kv_rows_ke
     constexpr uint32_t SHARING = TURNS ? 1 : WAVES, STEP = TURNS ? WAVES : 1;  // waves of a tile of tokens; tiles of a turn
     constexpr uint32_t UNITS = TOKENS * DP / P::N, ROW_UNITS = DP / P::N;      // pieces of a tile, of a token
     constexpr uint32_t LANES = 64 * SHARING;
-    constexpr int READY = KS * TB < 6 ? KS * TB : 6;  // operands that are ready before the first product
+    // Operands that are ready before the first product: of 256 dimensions no more than the registers hold.  (us, two / six, which then wait in
+    // scratch memory, two prompts of 2048 tokens, 16 heads over 4 of 256: 120 / 135.)
+    constexpr int READY = DP > 192 ? 2 : KS * TB < 6 ? KS * TB : 6;
     constexpr int EACH = DIRECT ? 1 : (UNITS + LANES - 1) / LANES;
-    // Numbers that go through registers are stored when the tile before them has been read: of a wave's own tiles one is enough.
-    constexpr uint32_t BUFS = TURNS && !DIRECT ? 1 : 2;
-    constexpr uint32_t PLANE = TOKENS * T::PITCH, TILE = 2 * PLANE, VECS = NB * 4;
+    using L = RowLds<KIND, DP, ROWS>;
+    constexpr uint32_t BUFS = L::BUFS, PLANE = L::PLANE, TILE = L::TILE, VECS = NB * 4;
     // of each wave (or all): tiles of keys and values; at the end sums
-    __shared__ __attribute__((aligned(16))) uint16_t lds[BUFS * TILE * (TURNS ? WAVES : 1)];
-    __shared__ float2 ml[TURNS ? WAVES * 32 : 1];
+    __shared__ __attribute__((aligned(16))) uint16_t lds[L::NUMBERS];
+    __shared__ float2 ml[L::SUMS];
     // of each row and dimension: whether it sees infinities or NaN that were taken out, of either sign
-    __shared__ uint32_t marks[ROWS * NB * 2];
+    __shared__ uint32_t marks[L::MARKS];
     __shared__ uint32_t any;
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t n = lane & 31u, h = lane >> 5;
@@ -354,10 +370,12 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), 2) void kv_rows_ke
     for (uint32_t i = tid; i < ROWS * NB * 2; i += 64u * WAVES) marks[i] = 0u;
     if (tid == 0u) any = 0u;
     if constexpr (TURNS) __syncthreads();  // (otherwise: the one of the first tile)
+    uint32_t half = h;
+    asm volatile("" : "+v"(half));  // (what goes by it is found anew for every tile of rows: kept, it does not fit the registers)
     w32x4 qf[KS];
 #pragma unroll
     for (int j = 0; j < KS; j++) {
-        const uint32_t d = (uint32_t)j * 16u + h * 8u;
+        const uint32_t d = (uint32_t)j * 16u + half * 8u;
         clear(qf[j]);
         if (has_row && d < p.dim) qf[j] = *reinterpret_cast<const w32x4 *>(p.q + (uint64_t)at_row * p.q_row + (uint64_t)head * p.q_head + d * 2u);
         if (p.negative) qf[j] ^= 0x80008000u;
@@ -588,7 +606,7 @@ __global__ __launch_bounds__((64 * RowStep<DP, ROWS>::WAVES), 2) void kv_rows_ke
     f32x4 *const part = p.part + (slot * (ROWS / 32) + (TURNS ? 0u : wave)) * VECS * 64u + lane;
     uint8_t *const out = p.out + (uint64_t)at_row * p.out_row + (uint64_t)head * p.out_head;
     auto put = [&](uint32_t v, f32x4 a, float inv) {
-        const uint32_t d = v / 4u * 32u + v % 4u * 8u + h * 4u;
+        const uint32_t d = v / 4u * 32u + v % 4u * 8u + half * 4u;
         // (without a tile of tokens there was no barrier behind the one who cleared these, and nothing to note)
         if ((TURNS || begin < end) && any) {
             const uint32_t *const m = marks + (((TURNS ? 0u : wave * 32u) + n) * NB + v / 4u) * 2u;

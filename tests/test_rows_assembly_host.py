@@ -31,3 +31,13 @@ def test_m0_is_the_direct_loads_alone(tmp_path):
     assert not [line for line in said if "warning" in line and "unused" not in line]
     ours = "".join(re.findall(r";;?#ASMSTART(.*?);;?#ASMEND", text, re.S))
     assert len(re.findall(r"\bm0\b", ours)) == len(re.findall(r"\bm0\b", text)) > 0
+
+
+def test_no_kernel_keeps_what_it_needs_in_scratch_memory(tmp_path):
+    """Heads of 256 dimensions, which take most registers; and no bound that the compiler cannot keep."""
+    kernels = [f"kv_rows_kernel<{x}, {kind}, 256, {rows}>" for x, kind in (("Bf16", "kBits16"), ("Bf16", "kBits8"), ("Fp16", "kBits4")) for rows in (32, 128)]
+    kernels += ["kv_rows_kernel<Fp16, kBits16, 128, 32>", "kv_rows_kernel<Bf16, kBits8, 192, 32>"]
+    text, said = compiled(tmp_path, kernels)
+    sizes = [int(n) for n in re.findall(r"\.private_segment_fixed_size:\s*(\d+)", text)]
+    assert sizes == [0] * len(kernels)
+    assert not [line for line in said if "warning" in line and "unused" not in line], said
