@@ -514,7 +514,8 @@ typedef struct {
     float v_scale;
     int32_t weigh;       /* 1: kv_attend may be asked for mass_out, which takes max_seqs * max_blocks * n_heads floats of
                             memory (as many times that as an odd block has tokens, or 4, 8 or 16 go into one) */
-    int32_t max_rows;    /* most rows of a kv_attend_rows() call; 0: none are made.  Otherwise 64 MiB of memory and up to 2 more */
+    int32_t max_rows;    /* most rows of a kv_attend_rows() call; 0: none are made.  Otherwise 16 MiB of memory for heads of up
+                            to 64 dimensions, 24 to 96, 32 to 128, 48 to 192, 64 above, and half a MiB */
 } kv_decoder_config;
 
 /*

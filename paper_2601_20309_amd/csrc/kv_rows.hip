@@ -128,7 +128,7 @@ extern "C" int kv_attend_rows(kv_decoder *d, const kv_attend_rows_args *a, void 
         // splits leave more to join.  us, two / four / six to a compute unit: 24 requests of 180 rows, 12 heads of 64, 42.3 / 42.2 / 48.9;
         // 9 requests of 150 rows, 3 heads of 96 in 4 bits, 25.9 / 28.3 / 29.2.)
         const uint64_t wanted = (uint64_t)d->n_cus * (many ? 1u : 2u);
-        p.splits = (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>(std::min(wanted, row_sums(p.dim) >> p.row_bits) / each, (most + p.least - 1u) / p.least));
+        p.splits = (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>(wanted / each, (most + p.least - 1u) / p.least));
         wgs = each * p.splits;
     }
     const dim3 g((uint32_t)wgs);

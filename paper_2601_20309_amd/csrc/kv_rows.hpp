@@ -6,8 +6,6 @@
 
 namespace dkv {
 
-// What splits and ranges may leave: as many rows as 64 MiB hold.
-constexpr uint64_t kRowSumsBytes = 64ull << 20;
 constexpr uint64_t kMostTiles = 0xFFFFFF;  // as many workgroups of 256 lanes as a launch can count lanes
 
 // Tiles of rows of one KV head, empty ones among them.
@@ -23,9 +21,11 @@ inline bool rows_fit(int64_t n_kv_heads, int64_t n_heads, int64_t n_seqs, int64_
 // Dimensions that the kernels are made for.
 inline uint32_t rows_dims(uint32_t dim) { return dim <= 64u ? 64u : dim <= 96u ? 96u : dim <= 128u ? 128u : dim <= 192u ? 192u : 256u; }
 
-inline uint64_t row_sums(uint32_t dim) { return kRowSumsBytes / 4u / rows_dims(dim) / 128u * 128u; }
+// Rows that splits and ranges may leave sums of: splits of two workgroups to a compute unit, of 128 rows (or one, of 256), or two parts of 32
+// rows of every range, as many ranges, and one of each KV head at least.
+inline uint64_t row_sums(const kv_decoder *d) { return std::max(256ull * (uint64_t)d->n_cus, 64ull * (uint64_t)d->cfg.n_kv_heads); }
 
-inline uint64_t rows_part_bytes(const kv_decoder *d) { return d->dc.max_rows ? row_sums(d->dim) * rows_dims(d->dim) * 4u : 0u; }
-inline uint64_t rows_ml_bytes(const kv_decoder *d) { return d->dc.max_rows ? row_sums(d->dim) * sizeof(float2) : 0u; }
+inline uint64_t rows_part_bytes(const kv_decoder *d) { return d->dc.max_rows ? row_sums(d) * rows_dims((uint32_t)d->dim) * 4u : 0u; }
+inline uint64_t rows_ml_bytes(const kv_decoder *d) { return d->dc.max_rows ? row_sums(d) * sizeof(float2) : 0u; }
 
 }  // namespace dkv
