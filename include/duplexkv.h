@@ -639,6 +639,7 @@ int kv_attend(kv_decoder *decoder, const kv_attend_args *args, void *stream);
  * weight is as it meets V is the nearest x_type number (fp16 beside a KV_FP8 cache, 2^-11 of it at most).  What lies in rows that nothing sees, infinities and NaN among it, makes no
  * difference.  A value of infinity makes what sees it infinite where its weight is above 2^-90 (x_type bf16) or 2^-36 (fp16) of the
  * largest, and infinite or NaN where it is below, as its place in a tile has it.  (Row i of a request's m is at place lens - m + i, whatever max_blocks is: places below 0 see nothing.)  The result is the same, bit for bit, whenever the same call runs with the same starts and lens.
+ * A long chunk beside many requests of one row is faster as two calls, kv_attend() for the latter.
  * out may be q itself.  KV_EINVAL, KV_EUNSUP as for kv_attend; KV_E2BIG: more requests or rows than the decoder's.
  */
 int kv_attend_rows(kv_decoder *decoder, const kv_attend_rows_args *args, void *stream);

@@ -185,7 +185,7 @@ struct Divide {
 // the pairs of tokens that a dimension's operand is made of together with byte permutes.
 //
 // Scores, references, weights and both sums are held in 32 bits.  The second product takes two operands of one type, and
-// the values have 16 bits or fewer.  So a weight meets 16-bit values as the sum of two such numbers, in two products: the
+// the values have 16 bits or fewer.  So a weight meets 16-bit (and 4-bit) values as the sum of two such numbers, in two products: the
 // result is as far from 64 bits as its own rounding.  Beside outputs in bf16 8-bit values are taken as fp16, which holds them
 // exactly, and one fp16 number is enough for a weight.  Root of the mean square of the relative error, 1e-4, a number
 // of the output's type / so: bf16, 3 requests of 100 tokens 16.8 / 15.6, 32 around 1000 17.0 / 16.5; fp16 1.62 / 1.53; bf16 beside
@@ -348,10 +348,11 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
     // In 8 bits there is room for two tiles of values: they are asked for a tile ahead, like the keys.  us without / with:
     // 128 requests around 600 tokens, 8 heads of 128, 39.4 / 37.4; 4 of 32768 tokens, 8 heads of 128 48.4 / 50.4, of 192
     // 102 / 85, 4 heads of 256 51.4 / 55.2; in 16 bits, 32 requests around 1000, 8 heads of 128, 35.6 / 39.7.
-    // In 4 bits a step has so few bytes that all of the next one's are asked for before this one's products.  What bounds it then are
-    // vector instructions: some 300 for 32 tokens of 128 dimensions, 64 of them conversions, 36 for pairs of tokens.  us, both launches: 4
-    // requests of 32768 tokens, 8 heads of 128 (143 MB) 53.3, with places multiplied before the shuffles 51.3 (2.8 TB/s), with all pages in
-    // the caches 39.3; 128 around 600 (95 MB) 51.
+    // In 4 bits a step has so few bytes that all of the next one's are asked for before this one's products.  Half of what it takes
+    // then are vector instructions, some 360 for 32 tokens of 128 dimensions, 64 of them conversions, 36 for pairs of tokens: they are
+    // busy 53 % of a SIMD's cycles; and its two waves wait 43 % of theirs for memory, a step of little ahead, or for shuffles.  us, both
+    // launches: 4 requests of 32768 tokens, 8 heads of 128 (143 MB) 53.3, with places multiplied before the shuffles 51 (2.8 TB/s), with all
+    // pages in the caches 39; 128 around 600 (95 MB) 51.
     constexpr bool EARLY = FP4;
     constexpr bool AHEAD = FP4 || (FP8 && !(WHOLE && DP == 256));
     auto k_dim = [](int j, uint32_t kq) { return FP4 ? (uint32_t)(j / 4) * 128u + kq * K4 + (uint32_t)(j & 3) * 8u : FP8 ? (uint32_t)(j / 2) * 64u + kq * 16u + (uint32_t)(j & 1) * 8u : (uint32_t)j * 32u + kq * 8u; };

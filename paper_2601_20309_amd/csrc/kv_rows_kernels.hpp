@@ -22,12 +22,14 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 //
 // Scores, references and both sums are held in 32 bits.  A weight meets the values as the nearest number of their type: X, fp16 beside 8
 // bits (here products bound the time, and two numbers for a weight would make it half as many again); out is divided by the sum of the weights as they were,
-// so that lse has 32 bits.  Errors against 64 bits, root of the mean square, 1e-4: bf16 19, of the outputs' own rounding 17; fp16 2.2, 2.1.
+// so that lse has 32 bits.  Errors against 64 bits, root of the mean square, 1e-4, of 300 to 5000
+// tokens / of the outputs' own rounding: bf16 22 / 16.6, fp16 2.7 / 2.05, bf16 beside 8 bits 16.7 / 16.6 (a bf16 number for a weight 22).
 //
 // What bounds it: LDS.  Of 64 tokens a wave reads 32 KB for 32 products of 32 x 32 x 16, and a CU's eight waves that much each.  1024
-// rows of 64 heads over 8 of 128 at 31000 tokens, us: as it is 1050, without loads 854, without reads of LDS 932, without exponentials
-// 988, the products alone 524 (128 rows to a workgroup).  Two waves' halves of a step in alternation, with a barrier
-// between them, were no faster (1012 / 945), nor were 64 rows a wave and one wave to a SIMD (1227 / 1050), which halve the reads.
+// rows of 64 heads over 8 of 128 at 31000 tokens take 925 us (1110 TFLOP/s), of 256 rows to a workgroup.  What that is made of, of 128 rows to
+// one, which took 1050: without loads 854, without reads of LDS 932, without exponentials 988, the products alone 524.  Beside
+// 945 two waves' halves of a step in alternation, with a barrier between them, took 1012; beside 1050 64 rows a wave and one wave to a SIMD,
+// which halve the reads, 1227.
 // 16-bit rows go from memory into LDS directly: 4 prompts of 2048 tokens 489 us through registers, 194 so.
 
 struct RowsParams {
