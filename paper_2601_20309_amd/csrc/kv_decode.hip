@@ -351,6 +351,7 @@ int kv_attend(kv_decoder *d, const kv_attend_args *a, void *stream)
     p.max_blocks = (uint32_t)d->dc.max_blocks;
     p.max_tokens = p.max_blocks * (uint32_t)d->cfg.block_size;
     p.bias = dkv::bf16_bias(p.max_tokens);
+    p.share = dkv::Share::of(p.max_tokens);
     p.dim = (uint32_t)d->dim;
     p.token_bytes = d->token_bytes;
     p.head_bytes = d->head_bytes;

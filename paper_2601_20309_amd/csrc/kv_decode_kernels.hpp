@@ -23,15 +23,28 @@ typedef uint16_t w16_any __attribute__((aligned(1)));
 // (byte 255: NaN).  A token has its heads' numbers first, the even dimension of two in a byte's low half, then its heads' bytes.
 enum Kind { kBits16, kBits8, kBits4 };
 
+// What of a weight of up to 2^-8 meets a bf16 value: a power of 2, and it again where two bf16 numbers have their exponents.  As many as
+// there may be tokens, of the largest value each, add up to less than 2^128 (of up to 2^28 tokens: no less than 2^-20, which leaves a
+// weight of 2^-90 of the largest a number); and no less than that takes, since products of small values are lost below 2^-149.
+struct Share {
+    float part;
+    uint32_t exponents;
+    static Share of(uint32_t max_tokens)
+    {
+        uint32_t bits = 0;
+        while (bits < 20u && max_tokens >> 7 > 1u << bits) bits++;
+        return Share{1.0f / (float)(1u << bits), bits << 7 | bits << 23};
+    }
+};
+
 // The 16-bit types of q, k, v and the outputs.
 struct Bf16 {
     typedef __bf16 x8 __attribute__((ext_vector_type(8)));
     typedef __bf16 x2 __attribute__((ext_vector_type(2)));
     // Weights are exp2(score - reference), the largest between 2^kBias and 2^(kBias + kSlack), so that the reference and
-    // all sums change scale only when a score is kSlack above what was met before.  Between 2^-16 and 2^-8 here, and 2^-kShare
-    // of that as they meet the values: the largest that bf16 has, of up to 2^28 tokens, add up to less than 2^128.
+    // all sums change scale only when a score is kSlack above what was met before.  Between 2^-16 and 2^-8 here, and a Share of
+    // that as they meet the values.
     static constexpr float kBias = -16.0f, kSlack = 8.0f;
-    static constexpr int kShare = 20;
     static __device__ __forceinline__ f32x4 mma(w32x4 a, w32x4 b, f32x4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
@@ -60,18 +73,18 @@ struct Bf16 {
     static __device__ __forceinline__ bool nan(uint32_t w) { return (w & 0x7FFFu) > 0x7F80u; }  // the lower of two
     static constexpr float kMost = 0x1.FEp127f;
     // Each of two weights as the sum of two numbers of 8 digits, the upper cut off, the lower the nearest to what that leaves:
-    // within 2^-15, times 2^-kShare.  The lower one gets 2^-20 of the weight on top, and the least normal number if that is less, so
+    // within 2^-15, times the share.  The lower one gets 2^-20 of the weight on top, and the least normal number if that is less, so
     // that it is never 0 beside one: 0 times a value of infinity is NaN.
-    static __device__ __forceinline__ void split(float a, float b, uint32_t &upper, uint32_t &lower)
+    static __device__ __forceinline__ void split(float a, float b, const Share &share, uint32_t &upper, uint32_t &lower)
     {
         typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-        constexpr u16x2 share = {kShare << 7, kShare << 7}, least = {0x80, 0x80};
-        constexpr float part = 1.0f / (float)(1 << kShare);
+        constexpr u16x2 least = {0x80, 0x80};
+        const float part = share.part * (1.0f + 0x1p-20f);
         const uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
         // (exponents, down to 0; a weight of NaN becomes a number here, but their sum stays NaN)
-        const u16x2 up = __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, __builtin_amdgcn_perm(y, x, 0x07060302u)), share);
+        const u16x2 up = __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, __builtin_amdgcn_perm(y, x, 0x07060302u)), __builtin_bit_cast(u16x2, share.exponents));
         upper = __builtin_bit_cast(uint32_t, up);
-        const u16x2 low = __builtin_bit_cast(u16x2, pack(__builtin_fmaf(a, part * (1.0f + 0x1p-20f), -lo(upper)), __builtin_fmaf(b, part * (1.0f + 0x1p-20f), -hi(upper))));
+        const u16x2 low = __builtin_bit_cast(u16x2, pack(__builtin_fmaf(a, part, -lo(upper)), __builtin_fmaf(b, part, -hi(upper))));
         lower = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(low, __builtin_elementwise_min(up, least)));
     }
 };
@@ -82,7 +95,6 @@ struct Fp16 {
     // fp16 has numbers from 2^-24 to 2^15: the largest weights lie between 2^12 and 2^15, so that its
     // smallest number is 2^-36 of them and less.
     static constexpr float kBias = 12.0f, kSlack = 3.0f;
-    static constexpr int kShare = 0;
     static __device__ __forceinline__ f32x4 mma(w32x4 a, w32x4 b, f32x4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
@@ -111,7 +123,7 @@ struct Fp16 {
     static constexpr uint32_t kOnes = 0x3C003C00u;
     // As above, of 11 digits each, within 2^-21; each at least the smallest number there is, 2^-24, if there is a weight (no
     // weight that is one is below 2^-126).
-    static __device__ __forceinline__ void split(float a, float b, uint32_t &upper, uint32_t &lower)
+    static __device__ __forceinline__ void split(float a, float b, const Share &, uint32_t &upper, uint32_t &lower)
     {
         const float u = fminf(a * 0x1p102f, 0x1p-24f), v = fminf(b * 0x1p102f, 0x1p-24f);
         const auto cut = __builtin_amdgcn_cvt_pkrtz(fmaxf(a, u), fmaxf(b, v));
@@ -136,8 +148,7 @@ inline float bf16_bias(uint32_t max_tokens)
 
 // bf16 beside 4 bits, where there is no infinity: weights meet the values as they are, and Weights says how large they get.
 struct Bf16Of4 : Bf16 {
-    static constexpr int kShare = 0;
-    static __device__ __forceinline__ void split(float a, float b, uint32_t &upper, uint32_t &lower)
+    static __device__ __forceinline__ void split(float a, float b, const Share &, uint32_t &upper, uint32_t &lower)
     {
         const uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
         upper = __builtin_amdgcn_perm(y, x, 0x07060302u);
@@ -233,6 +244,7 @@ struct AttendParams {
     float v_scale;
     uint32_t exponents;        // 4 bits: from a token's first byte to its heads' bytes
     float bias;                // 4 bits beside bf16: of Weights
+    Share share;               // 16 bits, bf16
 };
 
 constexpr uint32_t kTile = 32;
@@ -692,7 +704,7 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
 #pragma unroll
             for (int r = 0; r < 4; r++) {
                 uint32_t upper, lower = 0u;
-                if constexpr (SPLIT) Y::split(w[2 * r], w[2 * r + 1], upper, lower);
+                if constexpr (SPLIT) Y::split(w[2 * r], w[2 * r + 1], p.share, upper, lower);
                 else upper = Y::pack(w[2 * r], w[2 * r + 1]);
                 pw[r] = upper;
                 pl[r] = lower;
@@ -765,7 +777,7 @@ __global__ __launch_bounds__(64 * Step<DP>::WAVES) void kv_attend_kernel(const A
         if (now.here) {
             own += __shfl_xor(own, 16, 64);
             own += __shfl_xor(own, 32, 64);
-            if constexpr (SPLIT) sum[0] = own * (1.0f / (float)(1 << Y::kShare));  // as they met the values
+            if constexpr (SPLIT) sum[0] = std::is_same_v<Y, Bf16> ? own * p.share.part : own;  // as they met the values
             const bool whole = now.here == tiles_of(now.tokens);
             const uint32_t slot = group * 2u + (now.first > 0u ? 0u : 1u);
             f32x4 *const part = p.part + ((uint64_t)slot * p.units + unit) * p.part_vecs;

@@ -21,6 +21,9 @@ void largest_weights()
     for (uint32_t tokens : {1u, 16u, 4095u, 4096u, 4097u, 8192u, 70001u, 1u << 20, (1u << 28) + 1u, 0x7FFFFFC0u}) {
         const double most = std::exp2((double)dkv::bf16_bias(tokens) + (double)dkv::kBf16Slack);
         CHECK(most * tokens <= 0.5 && most * std::max(tokens, 4096u) > 0.25, "%u tokens: weights up to %g", tokens, most);
+        const dkv::Share share = dkv::Share::of(tokens);
+        CHECK(0x1p-8 * share.part * std::min(tokens, 1u << 28) <= 1.0 && (share.part == 1.0f || 0x1p-8 * share.part * tokens > 0.25), "%u tokens: %g of weights", tokens, (double)share.part);
+        CHECK(share.exponents == (uint32_t)-std::ilogb(share.part) * 0x800080u && share.part >= 0x1p-20f, "%u tokens", tokens);
     }
 }
 

@@ -6,6 +6,9 @@ import torch
 from paper_2601_20309_amd import binding as B
 from paper_2601_20309_amd import decode as D
 from paper_2601_20309_amd import workloads as W
+from tests import rows_reference as R
+from tests.test_rows_gpu import Case
+from tests.test_rows_weights_gpu import bound
 
 pytestmark = pytest.mark.gpu
 
@@ -99,3 +102,25 @@ def test_more_tokens_than_a_small_weight_makes_up_for(types, call, new):
         starts = torch.tensor([0, new], dtype=torch.int32, device="cuda")
         assert dec.kv_attend_rows(0, q, table, lens, out, starts=starts, scale=1.0) == B.KV_OK
     are_means(out, top)
+
+
+@pytest.mark.parametrize("call", ["one", "rows"])
+@pytest.mark.parametrize("n", [40, 100, 5000])
+@pytest.mark.parametrize("power", [-60, -100, -110, -115])
+def test_small_values_are_not_lost(call, n, power):
+    """Room for the largest values is no more than they take: those near the other end of bf16 are as exact as others.  A sum in 32 bits is
+    off by 2^-150 for each of its steps of 16 tokens (and 64 in the joins), beside weights that add up to 2^-16 and more, times the share
+    that meets the values, 2^-6 in a decoder of 5000 tokens."""
+    c = Case((1,), (n,), 2, 4, 64, seed=n)
+    c.plane(1).mul_(2.0 ** power)
+    q = c.queries()
+    ref = R.rows(q, c.values(0), c.values(1), c.table, c.lens, c.starts, 0.125, True, c.n_blocks)
+    out = torch.empty(q.shape, dtype=c.x, device="cuda")
+    if call == "one":
+        assert c.dec.kv_attend(c.layer, q.cuda(), c.table.cuda(), c.lens.cuda(), out, scale=0.125) == B.KV_OK
+    else:
+        assert c.dec.kv_attend_rows(c.layer, q.cuda(), c.table.cuda(), c.lens.cuda(), out, starts=c.starts.cuda(), scale=0.125) == B.KV_OK
+    most = bound(ref, 64, c.x, 2.0 ** -15 if call == "one" else 2.0 ** -8) - 2.0 ** -36 * n * ref["top"][..., None]
+    most = most + (n / 16 + 64) * 2.0 ** -150 * 2.0 ** 16 * (2.0 ** 6 if n > 128 else 1.0)
+    off = (out.cpu().double() - ref["out"]).abs()
+    assert (off <= most).all(), f"off by {(off / most).max():.2f} of the bound"
